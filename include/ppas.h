@@ -312,6 +312,71 @@ ppas_status ppas_attention_step_noalloc(const void *q, const void *k_cache, cons
                                         int32_t n_kv_heads, int32_t head_dim, float scale, void *out,
                                         int32_t out_is_fp32, int32_t *d_err_flag, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Rotary positions and KV append in one pass (device).  For every new token t
+ * at position d_positions[t], with phi_i = d_positions[t] * d_inv_freq[i],
+ * c_i = factor cos phi_i, s_i = factor sin phi_i, i < rotary_dim / 2, each
+ * query and key head x becomes
+ *   half layout        (interleaved == 0): (x[i], x[i + rotary_dim/2])
+ *   interleaved layout (interleaved != 0): (x[2i], x[2i + 1])
+ *   pair (a, b) -> (a c_i - b s_i, b c_i + a s_i),
+ * and dims from rotary_dim on are unchanged.  The rotated queries go to q_out,
+ * the rotated keys and the values to the token's slot of the paged cache, as
+ * ppas_kv_append stores them.  Arithmetic in fp32, rounded once to bf16; the
+ * phase is reduced modulo one turn in 64-bit fixed point, so its error does
+ * not grow with the position.
+ *   q, k, v        : device bf16, head h of token t at x + t * x_stride +
+ *                    h * head_dim (strides in elements, heads contiguous), so
+ *                    the three may be columns of one fused projection
+ *   d_positions    : device int32 [n_tokens] (any value, negative ones too)
+ *   d_slot_mapping : device int32 [n_tokens], slot = block*16 + offset; a
+ *                    negative slot skips that token's key and value (its
+ *                    queries are still rotated)
+ *   d_inv_freq     : device fp32 [rotary_dim / 2], finite (NULL when
+ *                    rotary_dim == 0); ppas_rope_frequencies makes them
+ *   q_out          : device bf16 [n_tokens, n_q_heads, head_dim], contiguous;
+ *                    q itself when its rows are contiguous, else it must not
+ *                    overlap the inputs
+ *   k_cache,v_cache: device bf16 [num_blocks, n_kv_heads, 16, head_dim],
+ *                    16-byte aligned
+ *   d_err_flag     : device int32 or NULL; PPAS_DEVERR_BAD_INDEX is written
+ *                    when a slot is >= num_blocks*16 (key and value skipped)
+ * head_dim: a multiple of 8, at most 512; rotary_dim: even, 0 .. head_dim;
+ * n_q_heads may be 0 (keys and values alone).  Rows whose addresses and strides
+ * are multiples of 16 bytes with rotary_dim a multiple of 16 move 16 bytes at
+ * a time, others a pair at a time.  n_tokens == 0 is a no-op.  One launch,
+ * with programmatic stream serialization as ppas_kv_append.
+ * ------------------------------------------------------------------------- */
+ppas_status ppas_rope_append(const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                             int64_t v_stride, const int32_t *d_positions, const int32_t *d_slot_mapping,
+                             int32_t n_tokens, const float *d_inv_freq, int32_t rotary_dim, int32_t interleaved,
+                             float factor, void *q_out, void *k_cache, void *v_cache, int32_t num_blocks,
+                             int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t *d_err_flag,
+                             void *stream);
+
+/* Inverse frequencies f_i = base^(-2i / rotary_dim), i < rotary_dim / 2, and
+ * the factor on cosine and sine, scaled by `scale` >= 1 for contexts longer
+ * than a model was trained on (original_len tokens); host only, in double,
+ * rounded once:
+ *   PLAIN  f_i
+ *   LINEAR f_i / scale (positions interpolated)
+ *   BASE   base * scale^(rotary_dim / (rotary_dim - 2)) in place of base
+ *   BANDS  by the turns n_i = original_len f_i / 2 pi that pair i makes over
+ *          the original window: f_i where n_i >= high, f_i / scale where
+ *          n_i <= low, in between linear in n_i
+ *   RAMP   the same ends (turns high and low), in between linear in the index
+ *          i, from floor of the index with `high` turns to the ceiling of the
+ *          one with `low`; factor = 0.1 ln(scale) + 1 (elsewhere 1)
+ * h_inv_freq: HOST float [rotary_dim / 2]; h_factor: HOST float.  scale is
+ * ignored by PLAIN; original_len, low < high by all but BANDS and RAMP. */
+#define PPAS_ROPE_PLAIN 0
+#define PPAS_ROPE_LINEAR 1
+#define PPAS_ROPE_BASE 2
+#define PPAS_ROPE_BANDS 3
+#define PPAS_ROPE_RAMP 4
+ppas_status ppas_rope_frequencies(int32_t kind, int32_t rotary_dim, double base, double scale, int32_t original_len,
+                                  double low, double high, float *h_inv_freq, float *h_factor);
+
 /* Failure-path check (device).  Launches one thread that waits, with a
  * limit of limit_us microseconds (1 .. 2,000,000), on a barrier nothing
  * arrives on -- the same bounded wait every kernel of this library uses --

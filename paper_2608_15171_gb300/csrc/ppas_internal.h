@@ -333,6 +333,21 @@ cudaError_t launch_gateup_few(const CUtensorMap &tm_x, const CUtensorMap &tm_w, 
                               cudaStream_t st);
 cudaError_t launch_gateup_pack(const void *w, void *wp, int hidden, int inter, cudaStream_t st);
 
+// ------------------------------------------------------------------ rotary positions + append
+struct RopeParams {
+    const __nv_bfloat16 *q, *k, *v;       // [n_tokens] rows of heads, strides in elements
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *positions, *slots;
+    const float *inv_freq;                // [rotary_dim / 2]
+    __nv_bfloat16 *q_out, *k_cache, *v_cache;
+    int32_t *err;
+    float factor;
+    int32_t n_tokens, num_blocks, n_q_heads, n_kv_heads, head_dim, rotary_dim, interleaved;
+    // a warp's task: `iters` passes of 32 lanes over a token's head rows
+    int32_t iters, tasks_per_token, n_tasks;
+};
+cudaError_t launch_rope_append(RopeParams p, cudaStream_t st);
+
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its
 // own global accesses after it with grid_dep_wait()

@@ -70,7 +70,29 @@ static PyObject *py_kv_append(PyObject *self, PyObject *args) {
     return PyLong_FromLong((long)st);
 }
 
+/* rope_append(q, k, v, q_stride, k_stride, v_stride, d_positions,
+ *             d_slot_mapping, n_tokens, d_inv_freq, rotary_dim, interleaved,
+ *             factor, q_out, k_cache, v_cache, num_blocks, n_q_heads,
+ *             n_kv_heads, head_dim, d_err_flag, stream) -> ppas_status */
+static PyObject *py_rope_append(PyObject *self, PyObject *args) {
+    unsigned long long q, k, v, pos, slots, freq, qo, kc, vc, err, stream;
+    long long qs, ks, vs;
+    int n_tokens, rotary, inter, num_blocks, hq, hk, d;
+    float factor;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KKKLLLKKiKiifKKKiiiiKK", &q, &k, &v, &qs, &ks, &vs, &pos, &slots, &n_tokens, &freq,
+                          &rotary, &inter, &factor, &qo, &kc, &vc, &num_blocks, &hq, &hk, &d, &err, &stream))
+        return NULL;
+    const ppas_status st = ppas_rope_append(
+        (const void *)(uintptr_t)q, (const void *)(uintptr_t)k, (const void *)(uintptr_t)v, qs, ks, vs,
+        (const int32_t *)(uintptr_t)pos, (const int32_t *)(uintptr_t)slots, n_tokens, (const float *)(uintptr_t)freq,
+        rotary, inter, factor, (void *)(uintptr_t)qo, (void *)(uintptr_t)kc, (void *)(uintptr_t)vc, num_blocks, hq, hk,
+        d, (int32_t *)(uintptr_t)err, (void *)(uintptr_t)stream);
+    return PyLong_FromLong((long)st);
+}
+
 static PyMethodDef methods[] = {
+    {"rope_append", py_rope_append, METH_VARARGS, "ppas_rope_append (see include/ppas.h)"},
     {"attention_step", py_attention_step, METH_VARARGS, "ppas_attention_step (see include/ppas.h)"},
     {"kv_append", py_kv_append, METH_VARARGS, "ppas_kv_append (see include/ppas.h)"},
     {NULL, NULL, 0, NULL},

@@ -44,7 +44,8 @@ EXPORTED = ("ppas_sched_create", "ppas_sched_destroy", "ppas_sched_free_blocks",
             "ppas_kv_append", "ppas_attention_workspace_size", "ppas_attention_step",
             "ppas_status_string", "ppas_abi_version", "ppas_attention_step_noalloc",
             "ppas_debug_wait_timeout", "ppas_attention_kernel_count", "ppas_gateup_pack",
-            "ppas_gateup_swiglu")
+            "ppas_gateup_swiglu", "ppas_rope_append", "ppas_rope_frequencies")
+PPAS_ROPE_PLAIN, PPAS_ROPE_LINEAR, PPAS_ROPE_BASE, PPAS_ROPE_BANDS, PPAS_ROPE_RAMP = 0, 1, 2, 3, 4
 PPAS_NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024
 
 
@@ -92,6 +93,14 @@ _lib.ppas_gateup_pack.restype = _c.c_int32
 _lib.ppas_gateup_swiglu.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32,
                                     _c.c_void_p, _c.c_void_p]
 _lib.ppas_gateup_swiglu.restype = _c.c_int32
+_lib.ppas_rope_append.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                  _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_int32, _c.c_int32,
+                                  _c.c_float, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32,
+                                  _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_void_p]
+_lib.ppas_rope_append.restype = _c.c_int32
+_lib.ppas_rope_frequencies.argtypes = [_c.c_int32, _c.c_int32, _c.c_double, _c.c_double, _c.c_int32, _c.c_double,
+                                       _c.c_double, _c.c_void_p, _c.c_void_p]
+_lib.ppas_rope_frequencies.restype = _c.c_int32
 _lib.ppas_attention_step.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p,
                                      _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32,
                                      _c.c_float, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_size_t,
@@ -277,6 +286,28 @@ def ppas_attention_step_noalloc(q, k_cache, v_cache, num_blocks: int, d_block_ta
                                             float(scale), _ptr(out), 1 if out_is_fp32 else 0, _ptr(d_err_flag),
                                             _stream(stream)),
            "ppas_attention_step_noalloc")
+
+
+def ppas_rope_frequencies(kind: int, rotary_dim: int, base: float, scale: float = 1.0, original_len: int = 0,
+                          low: float = 1.0, high: float = 4.0):
+    """(inverse frequencies as a float32 array, factor on cosine and sine)."""
+    f = np.empty(max(int(rotary_dim) // 2, 1), np.float32)
+    factor = ctypes.c_float()
+    _check(_lib.ppas_rope_frequencies(int(kind), int(rotary_dim), float(base), float(scale), int(original_len),
+                                      float(low), float(high), f.ctypes.data, ctypes.addressof(factor)),
+           "ppas_rope_frequencies")
+    return f, float(factor.value)
+
+
+def ppas_rope_append(q, k, v, q_stride: int, k_stride: int, v_stride: int, d_positions, d_slot_mapping,
+                     n_tokens: int, d_inv_freq, rotary_dim: int, interleaved: bool, factor: float, q_out, k_cache,
+                     v_cache, num_blocks: int, n_q_heads: int, n_kv_heads: int, head_dim: int, d_err_flag=None,
+                     stream=None) -> None:
+    call = _lib.ppas_rope_append if _fast is None else _fast.rope_append
+    _check(call(_ptr(q), _ptr(k), _ptr(v), int(q_stride), int(k_stride), int(v_stride), _ptr(d_positions),
+                _ptr(d_slot_mapping), int(n_tokens), _ptr(d_inv_freq), int(rotary_dim), 1 if interleaved else 0,
+                float(factor), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), int(num_blocks), int(n_q_heads),
+                int(n_kv_heads), int(head_dim), _ptr(d_err_flag), _stream(stream)), "ppas_rope_append")
 
 
 def ppas_debug_wait_timeout(d_err_flag, limit_us: int, stream=None) -> None:
