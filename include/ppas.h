@@ -377,6 +377,41 @@ ppas_status ppas_rope_append(const void *q, const void *k, const void *v, int64_
 ppas_status ppas_rope_frequencies(int32_t kind, int32_t rotary_dim, double base, double scale, int32_t original_len,
                                   double low, double high, float *h_inv_freq, float *h_factor);
 
+/* ---------------------------------------------------------------------------
+ * Next tokens from logits (device): temperature, top-k, top-p and min-p, with
+ * one given uniform number a row.  For a row x with maximum M:
+ *   z_i = (x_i - M) * (1 / temperature),  W_i = floor(exp(z_i) * 2^40)
+ * (z and exp in fp32, the weights W whole numbers: sums of them are exact, so
+ * a row's token depends neither on the batch nor on the order of additions).
+ * Tokens are ordered by x descending, index ascending; kept are the first n,
+ * n the least of
+ *   top_k                               (off where <= 0 or >= vocab),
+ *   the fewest whose weights reach top_p times the weights of the top_k
+ *                                       (off where >= 1; at least one token),
+ *   the tokens with z_i >= ln(min_p)    (off where <= 0; at least one token),
+ * and with S their weight the token is the first, in that order, whose running
+ * weight exceeds uniform * S; d_logprobs receives its
+ * log-probability among the kept tokens, z - ln(S 2^-40).
+ *   logits        : device fp32, or bf16 (logits_are_bf16 != 0), row r at
+ *                   logits + r * row_stride elements, any alignment
+ *   d_temperature : device fp32 [n_rows], finite, or NULL (1); <= 0 takes the
+ *                   largest logit, the lowest index of several, logprob 0
+ *   d_top_k       : device int32 [n_rows] or NULL (off)
+ *   d_top_p, d_min_p : device fp32 [n_rows] or NULL (off)
+ *   d_uniform     : device fp32 [n_rows] in [0, 1)
+ *   d_tokens      : device int32 [n_rows]
+ *   d_logprobs    : device fp32 [n_rows] or NULL
+ * A logit of -inf (a banned token) or NaN is never drawn; +inf shares the row
+ * with the other +inf.  A row with nothing else gives token -1, logprob -inf.
+ * vocab at most 262144, else PPAS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op.
+ * One launch (of thread-block clusters, up to 8 CTAs a row), with programmatic
+ * stream serialization; no workspace.
+ * ------------------------------------------------------------------------- */
+ppas_status ppas_sample_tokens(const void *logits, int32_t logits_are_bf16, int64_t row_stride, int32_t n_rows,
+                               int32_t vocab, const float *d_temperature, const int32_t *d_top_k,
+                               const float *d_top_p, const float *d_min_p, const float *d_uniform,
+                               int32_t *d_tokens, float *d_logprobs, int32_t *d_err_flag, void *stream);
+
 /* Failure-path check (device).  Launches one thread that waits, with a
  * limit of limit_us microseconds (1 .. 2,000,000), on a barrier nothing
  * arrives on -- the same bounded wait every kernel of this library uses --

@@ -348,6 +348,22 @@ struct RopeParams {
 };
 cudaError_t launch_rope_append(RopeParams p, cudaStream_t st);
 
+// ------------------------------------------------------------------ sampling
+constexpr int kSMaxVocab = 1 << 18;
+struct SampleParams {
+    const void *logits;  // fp32 or bf16, row r at logits + r * row_stride
+    int64_t row_stride;
+    const float *temperature;  // per row; NULL: 1
+    const int32_t *top_k;      // NULL: off
+    const float *top_p, *min_p, *uniform;
+    int32_t *tokens;
+    float *logprobs;  // or NULL
+    int32_t *err;
+    int32_t vocab;
+    int32_t chunk;  // logits of a row in each CTA of its cluster, a multiple of 8
+};
+cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_t st);
+
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its
 // own global accesses after it with grid_dep_wait()

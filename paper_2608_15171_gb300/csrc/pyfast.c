@@ -91,7 +91,27 @@ static PyObject *py_rope_append(PyObject *self, PyObject *args) {
     return PyLong_FromLong((long)st);
 }
 
+/* sample_tokens(logits, logits_are_bf16, row_stride, n_rows, vocab,
+ *               d_temperature, d_top_k, d_top_p, d_min_p, d_uniform, d_tokens,
+ *               d_logprobs, d_err_flag, stream) -> ppas_status */
+static PyObject *py_sample_tokens(PyObject *self, PyObject *args) {
+    unsigned long long x, t, k, p, m, u, tok, lp, err, stream;
+    long long stride;
+    int bf16, n_rows, vocab;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KiLiiKKKKKKKKK", &x, &bf16, &stride, &n_rows, &vocab, &t, &k, &p, &m, &u, &tok, &lp,
+                          &err, &stream))
+        return NULL;
+    const ppas_status st = ppas_sample_tokens(
+        (const void *)(uintptr_t)x, bf16, stride, n_rows, vocab, (const float *)(uintptr_t)t,
+        (const int32_t *)(uintptr_t)k, (const float *)(uintptr_t)p, (const float *)(uintptr_t)m,
+        (const float *)(uintptr_t)u, (int32_t *)(uintptr_t)tok, (float *)(uintptr_t)lp, (int32_t *)(uintptr_t)err,
+        (void *)(uintptr_t)stream);
+    return PyLong_FromLong((long)st);
+}
+
 static PyMethodDef methods[] = {
+    {"sample_tokens", py_sample_tokens, METH_VARARGS, "ppas_sample_tokens (see include/ppas.h)"},
     {"rope_append", py_rope_append, METH_VARARGS, "ppas_rope_append (see include/ppas.h)"},
     {"attention_step", py_attention_step, METH_VARARGS, "ppas_attention_step (see include/ppas.h)"},
     {"kv_append", py_kv_append, METH_VARARGS, "ppas_kv_append (see include/ppas.h)"},

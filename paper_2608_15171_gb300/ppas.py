@@ -44,7 +44,7 @@ EXPORTED = ("ppas_sched_create", "ppas_sched_destroy", "ppas_sched_free_blocks",
             "ppas_kv_append", "ppas_attention_workspace_size", "ppas_attention_step",
             "ppas_status_string", "ppas_abi_version", "ppas_attention_step_noalloc",
             "ppas_debug_wait_timeout", "ppas_attention_kernel_count", "ppas_gateup_pack",
-            "ppas_gateup_swiglu", "ppas_rope_append", "ppas_rope_frequencies")
+            "ppas_gateup_swiglu", "ppas_rope_append", "ppas_rope_frequencies", "ppas_sample_tokens")
 PPAS_ROPE_PLAIN, PPAS_ROPE_LINEAR, PPAS_ROPE_BASE, PPAS_ROPE_BANDS, PPAS_ROPE_RAMP = 0, 1, 2, 3, 4
 PPAS_NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024
 
@@ -101,6 +101,10 @@ _lib.ppas_rope_append.restype = _c.c_int32
 _lib.ppas_rope_frequencies.argtypes = [_c.c_int32, _c.c_int32, _c.c_double, _c.c_double, _c.c_int32, _c.c_double,
                                        _c.c_double, _c.c_void_p, _c.c_void_p]
 _lib.ppas_rope_frequencies.restype = _c.c_int32
+_lib.ppas_sample_tokens.argtypes = [_c.c_void_p, _c.c_int32, _c.c_int64, _c.c_int32, _c.c_int32, _c.c_void_p,
+                                    _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p,
+                                    _c.c_void_p, _c.c_void_p]
+_lib.ppas_sample_tokens.restype = _c.c_int32
 _lib.ppas_attention_step.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p,
                                      _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32,
                                      _c.c_float, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_size_t,
@@ -308,6 +312,15 @@ def ppas_rope_append(q, k, v, q_stride: int, k_stride: int, v_stride: int, d_pos
                 _ptr(d_slot_mapping), int(n_tokens), _ptr(d_inv_freq), int(rotary_dim), 1 if interleaved else 0,
                 float(factor), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), int(num_blocks), int(n_q_heads),
                 int(n_kv_heads), int(head_dim), _ptr(d_err_flag), _stream(stream)), "ppas_rope_append")
+
+
+def ppas_sample_tokens(logits, logits_are_bf16: bool, row_stride: int, n_rows: int, vocab: int, d_temperature,
+                       d_top_k, d_top_p, d_min_p, d_uniform, d_tokens, d_logprobs=None, d_err_flag=None,
+                       stream=None) -> None:
+    call = _lib.ppas_sample_tokens if _fast is None else _fast.sample_tokens
+    _check(call(_ptr(logits), 1 if logits_are_bf16 else 0, int(row_stride), int(n_rows), int(vocab),
+                _ptr(d_temperature), _ptr(d_top_k), _ptr(d_top_p), _ptr(d_min_p), _ptr(d_uniform), _ptr(d_tokens),
+                _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens")
 
 
 def ppas_debug_wait_timeout(d_err_flag, limit_us: int, stream=None) -> None:
