@@ -378,6 +378,51 @@ ppas_status ppas_rope_frequencies(int32_t kind, int32_t rotary_dim, double base,
                                   double low, double high, float *h_inv_freq, float *h_factor);
 
 /* ---------------------------------------------------------------------------
+ * Attention of single-token rows in groups that share a prefix (device): the
+ * decode rows of several answers to one prompt, or of prompts that begin alike.
+ * The rows of group i, h_group_rows[i] of them after those of the groups
+ * before, see the same keys and values at positions 0 .. h_prefix_lens[i] - 1,
+ * each its own after them.  Per row the result is that of ppas_attention_step
+ * with q_len 1 (scale, heads, layouts as there), but a group's prefix is read
+ * once for all of its rows, and its products run on the tensor cores.
+ *   q              : device bf16 [n_rows, n_q_heads, head_dim], n_rows the sum
+ *                    of h_group_rows, 16-byte aligned
+ *   k_cache,v_cache: device bf16 [num_blocks, n_kv_heads, 16, head_dim],
+ *                    16-byte aligned
+ *   d_block_tables : device int32 [n_rows, max_blocks_per_seq]; the first
+ *                    prefix / 16 entries of a group's rows are the same blocks
+ *                    (those of its first row are read for all)
+ *   h_group_rows   : HOST int32 [n_groups], >= 1
+ *   h_prefix_lens  : HOST int32 [n_groups], multiples of 16, 0 for none
+ *   h_ctx_lens     : HOST int32 [n_rows], the row's whole context, prefix and
+ *                    own token included: >= 1 and >= its group's prefix
+ *   out            : device bf16 [n_rows, n_q_heads, head_dim], 16-byte aligned
+ *   workspace      : device scratch of at least
+ *                    ppas_shared_attention_workspace_size(...) bytes, 256-byte
+ *                    aligned, no initialisation (may be NULL when that is 0)
+ *   d_err_flag     : device int32 or NULL (see PPAS_DEVERR_*)
+ * Supported: head_dim == 128, group sizes n_q_heads / n_kv_heads and head counts
+ * as ppas_attention_step, contexts up to 65535 * 128 tokens, n_kv_heads times
+ * ceil(prefix / 65536) up to 1280; otherwise PPAS_ERR_UNSUPPORTED.
+ * n_groups == 0 is a no-op.  Block ids must lie in [0, num_blocks) for every
+ * position below the context.  Scores, sums and partial results are fp32; the
+ * weights are rounded to bf16 for the product with V, the output to bf16.
+ * Two launches (the parts, and their join) for every 512 rows, 128 groups or
+ * 1024 units of (group, kv-head, 256 query rows), with programmatic stream
+ * serialization.  Plans, and the workspace size, follow the current device's
+ * SM count; a call's plan is kept for the next calls with the same lengths.
+ * ------------------------------------------------------------------------- */
+size_t ppas_shared_attention_workspace_size(int32_t n_groups, const int32_t *h_group_rows,
+                                            const int32_t *h_prefix_lens, const int32_t *h_ctx_lens,
+                                            int32_t n_q_heads, int32_t n_kv_heads);
+ppas_status ppas_shared_attention_step(const void *q, const void *k_cache, const void *v_cache, int32_t num_blocks,
+                                       const int32_t *d_block_tables, int32_t max_blocks_per_seq, int32_t n_groups,
+                                       const int32_t *h_group_rows, const int32_t *h_prefix_lens,
+                                       const int32_t *h_ctx_lens, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, float scale, void *out, void *workspace,
+                                       size_t workspace_bytes, int32_t *d_err_flag, void *stream);
+
+/* ---------------------------------------------------------------------------
  * Next tokens from logits (device): temperature, top-k, top-p and min-p, with
  * one given uniform number a row.  For a row x with maximum M:
  *   z_i = (x_i - M) * (1 / temperature),  W_i = floor(exp(z_i) * 2^40)

@@ -165,6 +165,22 @@ bool encode_q_map(CUtensorMap *map, const void *q, int32_t total_q, int32_t n_q_
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same Q as encode_q_map, rows of single tokens: one box = the q-heads of a
+// kv-head's group of 128 / group rows, as 128 rows of 64 columns (row-major in
+// (row, head)).
+bool encode_q_group_map(CUtensorMap *map, const void *q, int32_t n_rows, int32_t n_q_heads, int32_t group) {
+    auto fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(kHeadDim), static_cast<cuuint64_t>(n_q_heads),
+                          static_cast<cuuint64_t>(n_rows)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(kRowBytes), static_cast<cuuint64_t>(kRowBytes) * n_q_heads};
+    cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(kTileQ / group)};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 DecodePlan plan_decode(int32_t n_seqs, const int32_t *q_lens, const int32_t *ctx_lens, int32_t n_q_heads,
                        int32_t n_kv_heads, int32_t num_sms, const DecodeClusterCaps &caps, bool fine_tail) {
     DecodePlan d;

@@ -426,5 +426,6 @@ cudaError_t prepare_current_device();
 // tensor maps (driver entry point fetched at run time)
 bool encode_kv_map(CUtensorMap *map, const void *cache, int32_t num_blocks, int32_t n_kv_heads);
 bool encode_q_map(CUtensorMap *map, const void *q, int32_t total_q, int32_t n_q_heads);
+bool encode_q_group_map(CUtensorMap *map, const void *q, int32_t n_rows, int32_t n_q_heads, int32_t group);
 
 }  // namespace ppas

@@ -110,7 +110,42 @@ static PyObject *py_sample_tokens(PyObject *self, PyObject *args) {
     return PyLong_FromLong((long)st);
 }
 
+/* shared_attention_step(q, k_cache, v_cache, num_blocks, d_block_tables,
+ *                       max_blocks_per_seq, group_rows, prefix_lens, ctx_lens,
+ *                       n_q_heads, n_kv_heads, head_dim, scale, out, workspace,
+ *                       workspace_bytes, d_err_flag, stream) -> ppas_status
+ * (ctx_lens as long as the sum of group_rows: the binding checks it) */
+static PyObject *py_shared_attention_step(PyObject *self, PyObject *args) {
+    unsigned long long q, k, v, tables, out, ws, ws_bytes, err, stream;
+    int num_blocks, width, hq, hk, d;
+    float scale;
+    Py_buffer gr, pl, cl;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KKKiKiy*y*y*iiifKKKKK", &q, &k, &v, &num_blocks, &tables, &width, &gr, &pl, &cl, &hq,
+                          &hk, &d, &scale, &out, &ws, &ws_bytes, &err, &stream))
+        return NULL;
+    PyObject *res = NULL;
+    if (int32_buffer(&gr, "group_rows") && int32_buffer(&pl, "prefix_lens") && int32_buffer(&cl, "ctx_lens")) {
+        if (gr.len != pl.len) {
+            PyErr_SetString(PyExc_ValueError, "group_rows and prefix_lens differ in length");
+        } else {
+            const ppas_status st = ppas_shared_attention_step(
+                (const void *)(uintptr_t)q, (const void *)(uintptr_t)k, (const void *)(uintptr_t)v, num_blocks,
+                (const int32_t *)(uintptr_t)tables, width, (int32_t)(gr.len / 4), (const int32_t *)gr.buf,
+                (const int32_t *)pl.buf, (const int32_t *)cl.buf, hq, hk, d, scale, (void *)(uintptr_t)out,
+                (void *)(uintptr_t)ws, (size_t)ws_bytes, (int32_t *)(uintptr_t)err, (void *)(uintptr_t)stream);
+            res = PyLong_FromLong((long)st);
+        }
+    }
+    PyBuffer_Release(&gr);
+    PyBuffer_Release(&pl);
+    PyBuffer_Release(&cl);
+    return res;
+}
+
 static PyMethodDef methods[] = {
+    {"shared_attention_step", py_shared_attention_step, METH_VARARGS,
+     "ppas_shared_attention_step (see include/ppas.h)"},
     {"sample_tokens", py_sample_tokens, METH_VARARGS, "ppas_sample_tokens (see include/ppas.h)"},
     {"rope_append", py_rope_append, METH_VARARGS, "ppas_rope_append (see include/ppas.h)"},
     {"attention_step", py_attention_step, METH_VARARGS, "ppas_attention_step (see include/ppas.h)"},

@@ -1,0 +1,335 @@
+// Host side of the attention over shared prefixes: the plan of its launches,
+// argument checks and the C entry points.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <exception>
+#include <stdexcept>
+
+#include "attn_shared.cuh"
+
+namespace ppas {
+
+namespace {
+
+size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+// The time of a KV tile (64 KB) in a piece and of a page (8 KB) of own keys in a
+// warp's ring, in units of a tile streamed at an SM's share of the memory
+constexpr double kTileCost = 1.0, kPageCost = 1.0 / 8;
+// pieces of a prefix at the longest
+int32_t least_pieces(int32_t prefix) {
+    return (prefix + kSharedMaxPiece * kPrefillKT - 1) / (kSharedMaxPiece * kPrefillKT);
+}
+
+constexpr double kItemCost = 0.25;  // an item besides its pages, in the same unit, over a CTA's 8 warps
+
+}  // namespace
+
+SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_t *prefix_lens,
+                       const int32_t *ctx_lens, int32_t n_q_heads, int32_t n_kv_heads, int32_t num_sms) {
+    SharedPlan plan;
+    const int32_t g = n_q_heads / n_kv_heads;
+    struct Part {
+        int32_t row0, n_rows, prefix;
+    };
+    // units of a part, and its pieces at the longest, with `tiles` Q tiles a piece
+    auto units_of = [&](const Part &pt, int32_t tiles) {
+        return n_kv_heads * ((pt.n_rows * g + kTileQ * tiles - 1) / (kTileQ * tiles));
+    };
+    auto pieces_of = [&](const Part &pt, int32_t tiles) {
+        return units_of(pt, tiles) * least_pieces(pt.prefix);
+    };
+    // A group of more rows than a launch's tables hold is several parts; rows that
+    // have their prefix to themselves read it as their own keys.
+    std::vector<Part> parts;
+    for (int32_t i = 0, row = 0; i < n_groups; row += group_rows[i++]) {
+        const int32_t tables = kSharedMaxPieces / (n_kv_heads * std::max(1, least_pieces(prefix_lens[i])));
+        const int32_t most = std::min<int64_t>(kSharedMaxRows, static_cast<int64_t>(tables) * 2 * kTileQ / g);
+        for (int32_t r = 0; r < group_rows[i]; r += most) {
+            const int32_t n = std::min(most, group_rows[i] - r);
+            parts.push_back({row + r, n, n == 1 ? 0 : prefix_lens[i]});
+        }
+    }
+    for (size_t i0 = 0; i0 < parts.size();) {
+        SharedLaunch l;
+        l.row0 = parts[i0].row0;
+        size_t i1 = i0;
+        int32_t most = 0, units[2] = {0, 0}, pieces[2] = {0, 0};  // with 1, 2 tiles a piece
+        for (; i1 < parts.size(); ++i1) {
+            const Part &pt = parts[i1];
+            if (i1 > i0 && (l.n_rows + pt.n_rows > kSharedMaxRows || i1 - i0 == kSharedMaxGroups ||
+                            units[1] + units_of(pt, 2) > kSharedMaxUnits ||
+                            pieces[1] + pieces_of(pt, 2) > kSharedMaxPieces))
+                break;
+            for (int32_t t = 1; t <= 2; ++t) {
+                units[t - 1] += units_of(pt, t);
+                pieces[t - 1] += pieces_of(pt, t);
+            }
+            if (pt.prefix > 0) most = std::max(most, pt.n_rows * g);
+            l.n_rows += pt.n_rows;
+        }
+        // two Q tiles a piece where a group fills more than one (or the tables ask for it)
+        l.tiles = most > kTileQ || units[0] > kSharedMaxUnits || pieces[0] > kSharedMaxPieces ? 2 : 1;
+        const int32_t per = kTileQ * l.tiles;
+        // ---- own keys
+        int64_t own_pages = 0;
+        double tiles = 0;
+        for (size_t i = i0; i < i1; ++i) {
+            const Part &pt = parts[i];
+            for (int32_t r = pt.row0; r < pt.row0 + pt.n_rows; ++r)
+                own_pages += static_cast<int64_t>((ctx_lens[r] - pt.prefix + kPage - 1) / kPage) * n_kv_heads;
+            tiles += static_cast<double>((pt.prefix + kPrefillKT - 1) / kPrefillKT) * n_kv_heads *
+                     ((pt.n_rows * g + per - 1) / per);
+        }
+        // the SMs in proportion to the two kinds' time
+        const double own_time = own_pages * kPageCost + static_cast<double>(l.n_rows) * n_kv_heads * kItemCost / 8;
+        int32_t own_sms = own_pages == 0 ? 0 : num_sms;
+        if (own_pages > 0 && tiles > 0)
+            own_sms = std::max(1, std::min(num_sms - 1, static_cast<int32_t>(
+                                                            num_sms * own_time / (own_time + tiles * kTileCost) + 0.5)));
+        const int64_t warps = std::max(1, own_sms) * static_cast<int64_t>(kSharedWarps);
+        l.item_pages = static_cast<int32_t>(
+            std::max<int64_t>(2, std::min<int64_t>(kSharedMaxItemPages, (own_pages + warps - 1) / warps)));
+        int64_t items = 0;
+        for (;; ++l.item_pages) {
+            items = 0;
+            int64_t longest = 0;
+            for (size_t i = i0; i < i1; ++i)
+                for (int32_t r = parts[i].row0; r < parts[i].row0 + parts[i].n_rows; ++r) {
+                    const int64_t pages = (ctx_lens[r] - parts[i].prefix + kPage - 1) / kPage;
+                    const int64_t n = (pages + l.item_pages - 1) / l.item_pages;
+                    longest = std::max(longest, n);
+                    items += n * n_kv_heads;
+                }
+            if (longest <= 0xFFFF || l.item_pages == kSharedMaxItemPages) break;
+        }
+        if (items > (1 << 27)) throw std::length_error("items");
+        l.own_ctas = static_cast<int32_t>(
+            std::min<int64_t>(own_sms, (items + kSharedWarps - 1) / kSharedWarps));
+        // ---- the prefixes' pieces: one length of piece for all, the shortest
+        // that the SMs hold in one round
+        const int32_t pre_sms = std::max(1, num_sms - own_sms);
+        int32_t len = 1, hi = kSharedMaxPiece;
+        auto pieces_at = [&](int32_t n) {
+            int64_t k = 0;
+            for (size_t i = i0; i < i1; ++i) {
+                const int64_t kt = (parts[i].prefix + kPrefillKT - 1) / kPrefillKT;
+                k += (kt + n - 1) / n * n_kv_heads * ((parts[i].n_rows * g + per - 1) / per);
+            }
+            return k;
+        };
+        while (len < hi) {
+            const int32_t mid = (len + hi) / 2;
+            if (pieces_at(mid) <= pre_sms) hi = mid;
+            else len = mid + 1;
+        }
+        int32_t first_item = 0, most_items = 0, most_pieces = 0;
+        for (size_t i = i0; i < i1; ++i) {
+            const Part &pt = parts[i];
+            const uint16_t gi = static_cast<uint16_t>(i - i0);
+            l.groups.push_back({pt.row0 - l.row0, pt.n_rows, pt.prefix});
+            for (int32_t r = pt.row0; r < pt.row0 + pt.n_rows; ++r) {
+                const int32_t own = ctx_lens[r] - pt.prefix;
+                const int32_t n = ((own + kPage - 1) / kPage + l.item_pages - 1) / l.item_pages;
+                l.rows.push_back({own, first_item, static_cast<uint16_t>(n), gi});
+                first_item += n * n_kv_heads;
+                most_items = std::max(most_items, n);
+            }
+            const int32_t kt = (pt.prefix + kPrefillKT - 1) / kPrefillKT, np = (kt + len - 1) / len;
+            for (int32_t mu = 0; mu < (pt.n_rows * g + per - 1) / per; ++mu)
+                for (int32_t h = 0; h < n_kv_heads; ++h) {
+                    l.units.push_back({gi, static_cast<uint16_t>(h), static_cast<uint16_t>(mu),
+                                       static_cast<uint16_t>(l.pieces.size()), static_cast<uint16_t>(np), 0});
+                    for (int32_t k = 0; k < np; ++k)
+                        l.pieces.push_back({gi, static_cast<uint16_t>(h), static_cast<uint16_t>(mu),
+                                            static_cast<uint16_t>(static_cast<int64_t>(kt) * k / np),
+                                            static_cast<uint16_t>(static_cast<int64_t>(kt) * (k + 1) / np), 0});
+                    most_pieces = std::max(most_pieces, np);
+                }
+        }
+        l.n_groups = static_cast<int32_t>(i1 - i0);
+        l.n_items = first_item;
+        const int32_t partials = most_pieces + most_items;
+        l.ways = partials > 32 ? 8 : partials > 16 ? 4 : partials > 8 ? 2 : 1;
+        l.pre_o_bytes = align256(l.pieces.size() * l.tiles * kTileQ * kHeadDim * sizeof(float));
+        l.pre_ml_bytes = align256(l.pieces.size() * l.tiles * kTileQ * 2 * sizeof(float));
+        l.own_o_bytes = align256(static_cast<size_t>(l.n_items) * g * kHeadDim * sizeof(float));
+        l.own_ml_bytes = align256(static_cast<size_t>(l.n_items) * g * 2 * sizeof(float));
+        plan.bytes = std::max(plan.bytes, l.total_bytes());
+        plan.launches.push_back(std::move(l));
+        i0 = i1;
+    }
+    return plan;
+}
+
+namespace {
+
+// The last few plans made on this thread (every layer of an iteration has the
+// same lengths), keyed by all that a plan depends on.
+struct CachedShared {
+    int32_t hq = 0, hk = 0, sms = 0;
+    std::vector<int32_t> rows, prefixes, ctx;
+    std::shared_ptr<const SharedPlan> plan;
+};
+constexpr int kCached = 4;
+thread_local CachedShared t_shared[kCached];
+thread_local int t_shared_next = 0;
+
+std::shared_ptr<const SharedPlan> plan_cached(int32_t n_groups, const int32_t *rows, const int32_t *prefixes,
+                                              const int32_t *ctx, int32_t n_rows, int32_t hq, int32_t hk) {
+    const int32_t sms = plan_sms();
+    for (const CachedShared &e : t_shared)
+        if (e.plan && e.hq == hq && e.hk == hk && e.sms == sms &&
+            e.rows.size() == static_cast<size_t>(n_groups) && e.ctx.size() == static_cast<size_t>(n_rows) &&
+            std::equal(rows, rows + n_groups, e.rows.begin()) &&
+            std::equal(prefixes, prefixes + n_groups, e.prefixes.begin()) && std::equal(ctx, ctx + n_rows, e.ctx.begin()))
+            return e.plan;
+    auto made = std::make_shared<const SharedPlan>(plan_shared(n_groups, rows, prefixes, ctx, hq, hk, sms));
+    CachedShared &e = t_shared[t_shared_next];
+    t_shared_next = (t_shared_next + 1) % kCached;
+    e.plan = nullptr;
+    e.hq = hq;
+    e.hk = hk;
+    e.sms = sms;
+    e.rows.assign(rows, rows + n_groups);
+    e.prefixes.assign(prefixes, prefixes + n_groups);
+    e.ctx.assign(ctx, ctx + n_rows);
+    e.plan = made;
+    return made;
+}
+
+// the lengths alone: PPAS_OK and the number of rows
+ppas_status check_lengths(int32_t n_groups, const int32_t *rows, const int32_t *prefixes, const int32_t *ctx,
+                          int32_t hq, int32_t hk, int32_t *n_rows) {
+    if (n_groups < 0 || hq < 1 || hk < 1 || (n_groups > 0 && (!rows || !prefixes || !ctx))) return PPAS_ERR_INVALID_ARG;
+    if (hq % hk != 0) return PPAS_ERR_INVALID_ARG;
+    const int32_t g = hq / hk;
+    if (g != 1 && g != 2 && g != 4 && g != 8) return PPAS_ERR_UNSUPPORTED;
+    if (hq / (g >= 2 ? 2 : 1) > 256) return PPAS_ERR_UNSUPPORTED;
+    int64_t n = 0;
+    for (int32_t i = 0; i < n_groups; ++i) {
+        if (rows[i] < 1 || prefixes[i] < 0 || prefixes[i] % kPage != 0) return PPAS_ERR_INVALID_ARG;
+        // a launch's table of pieces
+        if (static_cast<int64_t>(hk) * least_pieces(std::min(prefixes[i], 65535 * kPrefillKT)) > kSharedMaxPieces)
+            return PPAS_ERR_UNSUPPORTED;
+        if (n + rows[i] > INT32_MAX / 1024) return PPAS_ERR_UNSUPPORTED;
+        for (int32_t r = 0; r < rows[i]; ++r) {
+            const int32_t c = ctx[n + r];
+            if (c < 1 || c < prefixes[i]) return PPAS_ERR_INVALID_ARG;
+            if (c > 65535 * kPrefillKT) return PPAS_ERR_UNSUPPORTED;  // 16-bit KV tiles
+        }
+        n += rows[i];
+    }
+    *n_rows = static_cast<int32_t>(n);
+    return PPAS_OK;
+}
+
+bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+ppas_status run(const void *q, const void *k_cache, const void *v_cache, int32_t num_blocks,
+                const int32_t *d_block_tables, int32_t max_blocks_per_seq, const SharedPlan &plan, int32_t n_rows,
+                int32_t hq, int32_t hk, float scale, void *out, void *workspace, int32_t *err, cudaStream_t st) {
+    CUtensorMap tm_q, tm_k, tm_v;
+    const int32_t g = hq / hk;
+    if (!encode_kv_map(&tm_k, k_cache, num_blocks, hk) || !encode_kv_map(&tm_v, v_cache, num_blocks, hk))
+        return PPAS_ERR_CUDA;
+    static thread_local SharedParams p;  // ~24 KB each: kept off the stack
+    static thread_local SharedMergeParams m;
+    for (const SharedLaunch &l : plan.launches) {
+        const __nv_bfloat16 *const q0 = static_cast<const __nv_bfloat16 *>(q) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
+        if (!encode_q_group_map(&tm_q, q0, std::min(l.n_rows, n_rows - l.row0), hq, g)) return PPAS_ERR_CUDA;
+        uint8_t *const ws = static_cast<uint8_t *>(workspace);
+        p.q = q0;
+        p.block_tables = d_block_tables + static_cast<int64_t>(l.row0) * max_blocks_per_seq;
+        p.table_stride = max_blocks_per_seq;
+        p.num_blocks = num_blocks;
+        p.n_q_heads = hq;
+        p.n_kv_heads = hk;
+        p.group = g;
+        p.tiles = l.tiles;
+        p.n_rows = l.n_rows;
+        p.n_pieces = static_cast<int32_t>(l.pieces.size());
+        p.n_items = l.n_items;
+        p.item_pages = l.item_pages;
+        p.own_warps = l.own_ctas * kSharedWarps;
+        p.scale_log2 = scale * 1.4426950408889634f;
+        p.err = err;
+        p.pre_o = reinterpret_cast<float *>(ws);
+        p.pre_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes);
+        p.own_o = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes);
+        p.own_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes + l.own_o_bytes);
+        std::copy(l.groups.begin(), l.groups.end(), p.groups);
+        std::copy(l.rows.begin(), l.rows.end(), p.rows);
+        std::copy(l.pieces.begin(), l.pieces.end(), p.pieces);
+        if (launch_shared(tm_q, tm_k, tm_v, p, l.own_ctas, st) != cudaSuccess) return PPAS_ERR_CUDA;
+        m.out = static_cast<__nv_bfloat16 *>(out) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
+        m.pre_o = p.pre_o;
+        m.pre_ml = p.pre_ml;
+        m.own_o = p.own_o;
+        m.own_ml = p.own_ml;
+        m.n_q_heads = hq;
+        m.group = g;
+        m.tiles = l.tiles;
+        m.n_units = static_cast<int32_t>(l.units.size());
+        m.ways = l.ways;
+        std::copy(l.groups.begin(), l.groups.end(), m.groups);
+        std::copy(l.rows.begin(), l.rows.end(), m.rows);
+        std::copy(l.units.begin(), l.units.end(), m.units);
+        if (launch_shared_merge(m, st) != cudaSuccess) return PPAS_ERR_CUDA;
+    }
+    return PPAS_OK;
+}
+
+}  // namespace
+
+}  // namespace ppas
+
+using namespace ppas;
+
+extern "C" size_t ppas_shared_attention_workspace_size(int32_t n_groups, const int32_t *h_group_rows,
+                                                       const int32_t *h_prefix_lens, const int32_t *h_ctx_lens,
+                                                       int32_t n_q_heads, int32_t n_kv_heads) {
+    int32_t n_rows = 0;
+    if (check_lengths(n_groups, h_group_rows, h_prefix_lens, h_ctx_lens, n_q_heads, n_kv_heads, &n_rows) != PPAS_OK ||
+        n_groups == 0)
+        return 0;
+    try {
+        return plan_cached(n_groups, h_group_rows, h_prefix_lens, h_ctx_lens, n_rows, n_q_heads, n_kv_heads)->bytes;
+    } catch (const std::exception &) {
+        return 0;
+    }
+}
+
+extern "C" ppas_status ppas_shared_attention_step(const void *q, const void *k_cache, const void *v_cache,
+                                                  int32_t num_blocks, const int32_t *d_block_tables,
+                                                  int32_t max_blocks_per_seq, int32_t n_groups,
+                                                  const int32_t *h_group_rows, const int32_t *h_prefix_lens,
+                                                  const int32_t *h_ctx_lens, int32_t n_q_heads, int32_t n_kv_heads,
+                                                  int32_t head_dim, float scale, void *out, void *workspace,
+                                                  size_t workspace_bytes, int32_t *d_err_flag, void *stream) {
+    int32_t n_rows = 0;
+    if (head_dim < 1) return PPAS_ERR_INVALID_ARG;
+    if (head_dim != kHeadDim) return PPAS_ERR_UNSUPPORTED;
+    const ppas_status st =
+        check_lengths(n_groups, h_group_rows, h_prefix_lens, h_ctx_lens, n_q_heads, n_kv_heads, &n_rows);
+    if (st != PPAS_OK || n_groups == 0) return st;
+    if (!q || !k_cache || !v_cache || !d_block_tables || !out || num_blocks < 1 || max_blocks_per_seq < 1)
+        return PPAS_ERR_INVALID_ARG;
+    if (!on16(q) || !on16(k_cache) || !on16(v_cache) || !on16(out) || !(scale > 0.f) || !std::isfinite(scale))
+        return PPAS_ERR_INVALID_ARG;
+    for (int32_t r = 0; r < n_rows; ++r)
+        if (h_ctx_lens[r] > static_cast<int64_t>(max_blocks_per_seq) * kPage) return PPAS_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(n_rows) * n_q_heads > INT32_MAX ||
+        static_cast<int64_t>(num_blocks) * n_kv_heads * kPage > INT32_MAX)
+        return PPAS_ERR_UNSUPPORTED;
+    try {
+        const auto plan = plan_cached(n_groups, h_group_rows, h_prefix_lens, h_ctx_lens, n_rows, n_q_heads, n_kv_heads);
+        if (plan->bytes > 0 && (!workspace || workspace_bytes < plan->bytes)) return PPAS_ERR_CAPACITY;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return PPAS_ERR_INVALID_ARG;
+        return run(q, k_cache, v_cache, num_blocks, d_block_tables, max_blocks_per_seq, *plan, n_rows, n_q_heads,
+                   n_kv_heads, scale, out, workspace, d_err_flag, static_cast<cudaStream_t>(stream));
+    } catch (const std::exception &) {
+        return PPAS_ERR_CAPACITY;  // host memory
+    }
+}

@@ -44,7 +44,8 @@ EXPORTED = ("ppas_sched_create", "ppas_sched_destroy", "ppas_sched_free_blocks",
             "ppas_kv_append", "ppas_attention_workspace_size", "ppas_attention_step",
             "ppas_status_string", "ppas_abi_version", "ppas_attention_step_noalloc",
             "ppas_debug_wait_timeout", "ppas_attention_kernel_count", "ppas_gateup_pack",
-            "ppas_gateup_swiglu", "ppas_rope_append", "ppas_rope_frequencies", "ppas_sample_tokens")
+            "ppas_gateup_swiglu", "ppas_rope_append", "ppas_rope_frequencies", "ppas_sample_tokens",
+            "ppas_shared_attention_workspace_size", "ppas_shared_attention_step")
 PPAS_ROPE_PLAIN, PPAS_ROPE_LINEAR, PPAS_ROPE_BASE, PPAS_ROPE_BANDS, PPAS_ROPE_RAMP = 0, 1, 2, 3, 4
 PPAS_NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024
 
@@ -101,6 +102,14 @@ _lib.ppas_rope_append.restype = _c.c_int32
 _lib.ppas_rope_frequencies.argtypes = [_c.c_int32, _c.c_int32, _c.c_double, _c.c_double, _c.c_int32, _c.c_double,
                                        _c.c_double, _c.c_void_p, _c.c_void_p]
 _lib.ppas_rope_frequencies.restype = _c.c_int32
+_lib.ppas_shared_attention_workspace_size.argtypes = [_c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32,
+                                                      _c.c_int32]
+_lib.ppas_shared_attention_workspace_size.restype = _c.c_size_t
+_lib.ppas_shared_attention_step.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_int32,
+                                            _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32,
+                                            _c.c_int32, _c.c_int32, _c.c_float, _c.c_void_p, _c.c_void_p,
+                                            _c.c_size_t, _c.c_void_p, _c.c_void_p]
+_lib.ppas_shared_attention_step.restype = _c.c_int32
 _lib.ppas_sample_tokens.argtypes = [_c.c_void_p, _c.c_int32, _c.c_int64, _c.c_int32, _c.c_int32, _c.c_void_p,
                                     _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p,
                                     _c.c_void_p, _c.c_void_p]
@@ -314,13 +323,46 @@ def ppas_rope_append(q, k, v, q_stride: int, k_stride: int, v_stride: int, d_pos
                 int(n_kv_heads), int(head_dim), _ptr(d_err_flag), _stream(stream)), "ppas_rope_append")
 
 
+def _group_lens(ctx_lens, group_rows, prefix_lens, where: str):
+    cl, gr, pl = _i32(ctx_lens), _i32(group_rows), _i32(prefix_lens)
+    if gr.size != pl.size or cl.size != int(gr.sum()):
+        raise PpasError(PPAS_ERR_INVALID_ARG, where)
+    return cl, gr, pl
+
+
+def ppas_shared_attention_workspace_size(ctx_lens, group_rows, prefix_lens, n_q_heads: int, n_kv_heads: int) -> int:
+    cl, gr, pl = _group_lens(ctx_lens, group_rows, prefix_lens, "ppas_shared_attention_workspace_size")
+    return int(_lib.ppas_shared_attention_workspace_size(int(gr.size), _addr(gr), _addr(pl), _addr(cl),
+                                                         int(n_q_heads), int(n_kv_heads)))
+
+
+def ppas_shared_attention_step(q, k_cache, v_cache, num_blocks: int, d_block_tables, max_blocks_per_seq: int,
+                               ctx_lens, group_rows, prefix_lens, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                               scale: float, out, workspace=None, workspace_bytes: int = 0, d_err_flag=None,
+                               stream=None) -> None:
+    cl, gr, pl = _group_lens(ctx_lens, group_rows, prefix_lens, "ppas_shared_attention_step")
+    if _fast is not None:
+        _check(_fast.shared_attention_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), int(num_blocks),
+                                           _ptr(d_block_tables), int(max_blocks_per_seq), gr, pl, cl, int(n_q_heads),
+                                           int(n_kv_heads), int(head_dim), float(scale), _ptr(out), _ptr(workspace),
+                                           int(workspace_bytes), _ptr(d_err_flag), _stream(stream)),
+               "ppas_shared_attention_step")
+        return
+    _check(_lib.ppas_shared_attention_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), int(num_blocks),
+                                           _ptr(d_block_tables), int(max_blocks_per_seq), int(gr.size), _addr(gr),
+                                           _addr(pl), _addr(cl), int(n_q_heads), int(n_kv_heads), int(head_dim),
+                                           float(scale), _ptr(out), _ptr(workspace), int(workspace_bytes),
+                                           _ptr(d_err_flag), _stream(stream)), "ppas_shared_attention_step")
+
+
 def ppas_sample_tokens(logits, logits_are_bf16: bool, row_stride: int, n_rows: int, vocab: int, d_temperature,
                        d_top_k, d_top_p, d_min_p, d_uniform, d_tokens, d_logprobs=None, d_err_flag=None,
                        stream=None) -> None:
     call = _lib.ppas_sample_tokens if _fast is None else _fast.sample_tokens
     _check(call(_ptr(logits), 1 if logits_are_bf16 else 0, int(row_stride), int(n_rows), int(vocab),
                 _ptr(d_temperature), _ptr(d_top_k), _ptr(d_top_p), _ptr(d_min_p), _ptr(d_uniform), _ptr(d_tokens),
-                _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens")
+                _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens",
+            "ppas_shared_attention_workspace_size", "ppas_shared_attention_step")
 
 
 def ppas_debug_wait_timeout(d_err_flag, limit_us: int, stream=None) -> None:

@@ -1,0 +1,102 @@
+// Checks the plan of the attention over shared prefixes against what its
+// kernels index from it.  A line of input: sms hq hk n_groups, then rows and
+// prefix of each group, then the contexts; a line of output each: "ok launches
+// pieces items own_ctas tiles ways longest_piece item_pages bytes" (of the first launch) or what is wrong.
+#include <cstdio>
+#include <iostream>
+#include <set>
+#include <sstream>
+#include <string>
+
+#include "attn_shared.cuh"
+
+using namespace ppas;
+
+static std::string check(int sms, int hq, int hk, const std::vector<int> &rows, const std::vector<int> &pre,
+                         const std::vector<int> &ctx) {
+    const int g = hq / hk;
+    const SharedPlan plan = plan_shared(static_cast<int>(rows.size()), rows.data(), pre.data(), ctx.data(), hq, hk, sms);
+    std::vector<int> prefix_of;
+    for (size_t i = 0; i < rows.size(); ++i) prefix_of.insert(prefix_of.end(), rows[i], pre[i]);
+    int row = 0;
+    size_t bytes = 0;
+    for (const SharedLaunch &l : plan.launches) {
+        if (l.row0 != row) return "rows of launches";
+        if (l.rows.size() > kSharedMaxRows || static_cast<int>(l.rows.size()) != l.n_rows) return "rows table";
+        if (l.groups.size() > kSharedMaxGroups || l.groups.empty()) return "groups table";
+        if (l.units.size() > kSharedMaxUnits) return "units table";
+        if (l.pieces.size() > kSharedMaxPieces) return "pieces table";
+        if (l.tiles != 1 && l.tiles != 2) return "tiles";
+        if (l.item_pages < 1 || l.item_pages > kSharedMaxItemPages) return "item pages";
+        if (l.ways != 1 && l.ways != 2 && l.ways != 4 && l.ways != 8) return "ways";
+        int r = 0, item = 0;
+        for (size_t gi = 0; gi < l.groups.size(); ++gi) {
+            const SharedGroup &gr = l.groups[gi];
+            if (gr.row0 != r || gr.n_rows < 1 || gr.prefix % 16) return "group";
+            for (int k = 0; k < gr.n_rows; ++k, ++r) {
+                const SharedRow &sr = l.rows[r];
+                if (sr.group != gi) return "group of a row";
+                const int want = gr.prefix;
+                if (want != prefix_of[row + r] && !(gr.n_rows == 1 && want == 0)) return "prefix of a row";
+                if (sr.own != ctx[row + r] - want || sr.own < 0) return "own keys";
+                const int pages = (sr.own + 15) / 16;
+                if (sr.item0 != item) return "first item";
+                if (static_cast<int64_t>(sr.n_items) * l.item_pages < pages ||
+                    static_cast<int64_t>(sr.n_items - 1) * l.item_pages >= pages) {
+                    if (!(sr.n_items == 0 && pages == 0)) return "items cover the pages, none empty";
+                }
+                item += sr.n_items * hk;
+            }
+        }
+        if (r != l.n_rows || item != l.n_items) return "items";
+        if ((l.own_ctas > 0) != (l.n_items > 0)) return "CTAs of own keys";
+        std::set<std::vector<int>> seen;
+        size_t next = 0;
+        for (const SharedUnit &u : l.units) {
+            const SharedGroup &gr = l.groups.at(u.group);
+            if (u.kvh >= hk || u.mu * l.tiles * 128 >= gr.n_rows * g) return "unit";
+            if (!seen.insert({u.group, u.kvh, u.mu}).second) return "a unit twice";
+            if (u.n_pieces > 0 && u.piece0 != next) return "first piece";
+            const int kt = (gr.prefix + 127) / 128;
+            int at = 0;
+            for (int k = 0; k < u.n_pieces; ++k) {
+                const SharedPiece &pc = l.pieces.at(next++);
+                if (pc.group != u.group || pc.kvh != u.kvh || pc.mu != u.mu) return "piece of another unit";
+                if (pc.kt0 != at || pc.kt1 <= pc.kt0 || pc.kt1 - pc.kt0 > kSharedMaxPiece) return "piece's tiles";
+                at = pc.kt1;
+            }
+            if (at != kt) return "pieces cover the prefix";
+        }
+        if (next != l.pieces.size()) return "pieces without a unit";
+        size_t want = 0;
+        for (const SharedGroup &gr : l.groups) want += hk * ((gr.n_rows * g + 128 * l.tiles - 1) / (128 * l.tiles));
+        if (want != l.units.size()) return "units";
+        if (l.pre_o_bytes < l.pieces.size() * l.tiles * 128 * 128 * 4 || l.pre_ml_bytes < l.pieces.size() * l.tiles * 1024 ||
+            l.own_o_bytes < static_cast<size_t>(l.n_items) * g * 512 || l.own_ml_bytes < static_cast<size_t>(l.n_items) * g * 8)
+            return "workspace";
+        if (l.pre_o_bytes % 256 || l.pre_ml_bytes % 256 || l.own_o_bytes % 256 || l.own_ml_bytes % 256) return "alignment";
+        bytes = std::max(bytes, l.total_bytes());
+        row += l.n_rows;
+    }
+    if (row != static_cast<int>(ctx.size()) || bytes != plan.bytes) return "rows, bytes";
+    const SharedLaunch &l = plan.launches.front();
+    int longest = 0;
+    for (const SharedPiece &pc : l.pieces) longest = std::max(longest, pc.kt1 - pc.kt0);
+    std::ostringstream s;
+    s << "ok " << plan.launches.size() << " " << l.pieces.size() << " " << l.n_items << " " << l.own_ctas << " " << l.tiles
+      << " " << l.ways << " " << longest << " " << l.item_pages << " " << plan.bytes;
+    return s.str();
+}
+
+int main() {
+    std::string line;
+    while (std::getline(std::cin, line)) {
+        std::istringstream in(line);
+        int sms, hq, hk, n;
+        in >> sms >> hq >> hk >> n;
+        std::vector<int> rows(n), pre(n), ctx;
+        for (int i = 0; i < n; ++i) in >> rows[i] >> pre[i];
+        for (int c; in >> c;) ctx.push_back(c);
+        std::puts(check(sms, hq, hk, rows, pre, ctx).c_str());
+    }
+}
