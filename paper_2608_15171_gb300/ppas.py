@@ -361,8 +361,7 @@ def ppas_sample_tokens(logits, logits_are_bf16: bool, row_stride: int, n_rows: i
     call = _lib.ppas_sample_tokens if _fast is None else _fast.sample_tokens
     _check(call(_ptr(logits), 1 if logits_are_bf16 else 0, int(row_stride), int(n_rows), int(vocab),
                 _ptr(d_temperature), _ptr(d_top_k), _ptr(d_top_p), _ptr(d_min_p), _ptr(d_uniform), _ptr(d_tokens),
-                _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens",
-            "ppas_shared_attention_workspace_size", "ppas_shared_attention_step")
+                _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens")
 
 
 def ppas_debug_wait_timeout(d_err_flag, limit_us: int, stream=None) -> None:
