@@ -16,8 +16,8 @@
 // in the order reaches a target, and need no sort: one histogram of weights over
 // bins of z (linear, so the bins fill evenly and few additions collide), summed
 // over the cluster, gives the bin; its tokens (a few hundred) go to the first
-// CTA, which ranks them against one another.  A bin with more than that (ties,
-// flat rows) is divided again, by the bits of (x, index).
+// CTA, which sorts them.  A bin with more than that (ties, flat rows) is divided
+// again, by the bits of (x, index).
 #include <math.h>
 
 #include "ppas_device.cuh"
@@ -30,7 +30,7 @@ constexpr int kSThreads = 512;
 constexpr int kSWarps = kSThreads / 32;
 constexpr int kSBins = 1024;      // bins of z
 constexpr int kSFine = 512;       // bins of a bin's (x, index)
-constexpr int kSList = 512;       // tokens that are ranked against one another
+constexpr int kSList = 512;       // tokens that are sorted
 constexpr int kSIndexBits = 18;   // vocabularies of up to 2^18 tokens
 constexpr int kSMaxCluster = 8;
 constexpr float kSFloor = -28.f;  // z below this: W = 0 (exp(-28) 2^40 < 1)
@@ -40,12 +40,14 @@ static_assert(kSBins % (2 * kSMaxCluster) == 0 && kSFine % kSMaxCluster == 0 && 
                   kSBins == 2 * kSThreads && kSFine == kSThreads && kSList <= kSThreads,
               "the scans give each thread two bins or one");
 
-enum : uint32_t { kDone, kGatherBin, kGatherRange, kDivide };
+enum : uint32_t { kDone, kGather, kDivide };
 
 struct SCommand {
     uint32_t op, bin;
-    uint64_t lo, hi;  // range of (x, index)
-    uint32_t shift, pad;
+    uint64_t lo, hi;  // range of (x, index) in the bin
+    uint32_t shift;
+    float x_lo, x_hi;  // no token outside these belongs
+    uint32_t pad;
 };
 
 struct SShared {
@@ -53,14 +55,16 @@ struct SShared {
                                                    // behind them the first CTA's sums over the cluster
     uint64_t sum_w[kSBins];                        // first CTA: sums over the cluster, then running sums
     uint32_t sum_c[kSBins];
-    uint2 list[kSList];                            // (key, index) of a gathered bin's tokens
-    uint64_t list_w[kSList];
+    uint64_t list[kSList];                         // places (key, index) of a gathered bin's tokens
+    uint64_t sort[kSThreads];
     float2 range[kSMaxCluster];                    // (max, min finite) of each CTA
     uint64_t above[kSMaxCluster];                  // weight with z >= ln p_min, or the lowest index of the maximum
     uint64_t warp_w[kSWarps];
     uint32_t warp_c[kSWarps];
     float2 warp_range[kSWarps];
-    uint32_t n, kmin, kmax;                        // of this CTA's gathered tokens
+    uint32_t n;                                    // of this CTA's gathered tokens
+    uint32_t all_n[kSMaxCluster];                  // first CTA: every CTA's
+    uint64_t target;
     SCommand cmd;
     uint64_t base_w, base_c, got_w, got_mass;      // first CTA: sums before the bin, what a search found
     uint32_t got_bin, got_index;
@@ -96,19 +100,38 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 struct SRow {
     float top, inv_t, bin_scale;
     __device__ __forceinline__ float z(float x) const { return x == top ? 0.f : (x - top) * inv_t; }
+    // (conversions between floats and whole numbers share a slow unit with exp:
+    // here and in weight2 additions and shifts do their work)
     __device__ __forceinline__ int bin(float z_) const {
-        return min(static_cast<int>(-z_ * bin_scale), kSBins - 1);
+        return __float_as_int(fminf(-z_ * bin_scale, kSBins - 1.f) + 0x1p23f) - 0x4B000000;
+    }
+    // x of the tokens in bin b, and a little more: the bins' edges in x but for roundings
+    __device__ __forceinline__ void bin_range(int b, float &lo, float &hi) const {
+        const float t = 1.f / (inv_t * bin_scale);  // x a bin
+        const float slack = 1e-5f * (fabsf(top) + (static_cast<float>(b) + 1.f) * t) + 1e-30f;
+        lo = top - (static_cast<float>(b) + 0.5f) * t - slack;
+        hi = top - (static_cast<float>(b) - 0.5f) * t + slack;
+        if (b == kSBins - 1 || !(lo < hi)) lo = -INFINITY;
+        if (b == 0 || !(lo < hi)) hi = INFINITY;
     }
     // tokens that can be drawn or counted (a -inf is below the floor, a NaN no comparison holds for)
     __device__ __forceinline__ static bool counts(float x, float z_) { return x > -INFINITY && z_ > kSFloor; }
-    __device__ __forceinline__ static uint64_t weight(float z_) { return __float2ull_rz(expf(z_) * 0x1p40f); }
+    // floor(exp(z) 2^40), low and high half: the significand m of w = m 2^(e - 150) shifted into place
+    __device__ __forceinline__ static uint2 weight2(float z_) {
+        const uint32_t b = __float_as_uint(expf(z_));
+        const uint64_t m = static_cast<uint64_t>((b & 0x7FFFFFu) | 0x800000u) << 17;
+        const uint64_t w = m >> min(127u - (b >> 23), 63u);
+        return make_uint2(static_cast<uint32_t>(w), static_cast<uint32_t>(w >> 32));
+    }
+    __device__ __forceinline__ static uint64_t weight(float z_) {
+        const uint2 w = weight2(z_);
+        return (static_cast<uint64_t>(w.y) << 32) | w.x;
+    }
 };
 
-__device__ __forceinline__ void add_weight(uint32_t *wl, uint32_t *wh, uint64_t w) {
-    const uint32_t lo = static_cast<uint32_t>(w);
-    uint32_t hi = static_cast<uint32_t>(w >> 32);
-    if (lo) hi += atomicAdd(wl, lo) + lo < lo ? 1u : 0u;  // the carry of this addition
-    if (hi) atomicAdd(wh, hi);
+__device__ __forceinline__ void add_weight(uint32_t *wl, uint32_t *wh, uint2 w) {
+    const uint32_t carry = atomicAdd(wl, w.x) + w.x < w.x ? 1u : 0u;
+    if (w.y + carry) atomicAdd(wh, w.y + carry);
 }
 
 // inclusive sums over the CTA's threads
@@ -128,10 +151,17 @@ __device__ __forceinline__ void block_scan(SShared &s, uint64_t &w, uint32_t &c)
         s.warp_c[warp] = c;
     }
     __syncthreads();
-    for (int i = 0; i < warp; ++i) {
-        w += s.warp_w[i];
-        c += s.warp_c[i];
+    uint64_t before_w = 0;
+    uint32_t before_c = 0;
+#pragma unroll
+    for (int i = 0; i < kSWarps; ++i) {
+        const uint64_t a = s.warp_w[i];
+        const uint32_t b = s.warp_c[i];
+        before_w += i < warp ? a : 0;
+        before_c += i < warp ? b : 0;
     }
+    w += before_w;
+    c += before_c;
 }
 
 // Sums the cluster's histograms and leaves the bins' sums in the first CTA:
@@ -142,12 +172,22 @@ __device__ __forceinline__ void push_sums(SShared &s, uint32_t rank, uint32_t ct
     const int per = n / static_cast<int>(ctas);
     for (int i = threadIdx.x; i < per; i += kSThreads) {
         const int b = static_cast<int>(rank) * per + i;
+        uint32_t lo[kSMaxCluster], hi[kSMaxCluster], nc[kSMaxCluster];
+#pragma unroll
+        for (uint32_t r = 0; r < kSMaxCluster; ++r) {
+            lo[r] = hi[r] = nc[r] = 0;
+            if (r < ctas) {
+                lo[r] = ld_cluster_u32(dsmem_addr(smem_u32(&s.wl[b]), r));
+                hi[r] = ld_cluster_u32(dsmem_addr(smem_u32(&s.wh[b]), r));
+                if (counted) nc[r] = ld_cluster_u32(dsmem_addr(smem_u32(&s.cnt[b]), r));
+            }
+        }
         uint64_t w = 0;
         uint32_t c = 0;
-        for (uint32_t r = 0; r < ctas; ++r) {
-            w += static_cast<uint64_t>(ld_cluster_u32(dsmem_addr(smem_u32(&s.wl[b]), r))) +
-                 (static_cast<uint64_t>(ld_cluster_u32(dsmem_addr(smem_u32(&s.wh[b]), r))) << 32);
-            if (counted) c += ld_cluster_u32(dsmem_addr(smem_u32(&s.cnt[b]), r));
+#pragma unroll
+        for (int r = 0; r < kSMaxCluster; ++r) {
+            w += static_cast<uint64_t>(lo[r]) + (static_cast<uint64_t>(hi[r]) << 32);
+            c += nc[r];
         }
         if (kFine) {
             st_cluster_u32(dsmem_addr(smem_u32(&s.cnt[kSFine + b]), 0), c);
@@ -184,59 +224,62 @@ __device__ __forceinline__ void find_bin(SShared &s, const STarget &t) {
     __syncthreads();
 }
 
-// the first CTA's command, written into every CTA of the cluster (one thread)
+// the first CTA's command, written into every CTA of the cluster (a thread each)
 __device__ __forceinline__ void send(SShared &s, const SCommand &c, uint32_t ctas) {
-    for (uint32_t r = 0; r < ctas; ++r) {
-        const uint32_t a = dsmem_addr(smem_u32(&s.cmd), r);
-        st_cluster_u32(a + offsetof(SCommand, op), c.op);
-        st_cluster_u32(a + offsetof(SCommand, bin), c.bin);
-        st_cluster_u64(a + offsetof(SCommand, lo), c.lo);
-        st_cluster_u64(a + offsetof(SCommand, hi), c.hi);
-        st_cluster_u32(a + offsetof(SCommand, shift), c.shift);
-    }
+    if (threadIdx.x >= ctas) return;
+    const uint32_t a = dsmem_addr(smem_u32(&s.cmd), threadIdx.x);
+    st_cluster_u32(a + offsetof(SCommand, op), c.op);
+    st_cluster_u32(a + offsetof(SCommand, bin), c.bin);
+    st_cluster_u64(a + offsetof(SCommand, lo), c.lo);
+    st_cluster_u64(a + offsetof(SCommand, hi), c.hi);
+    st_cluster_u32(a + offsetof(SCommand, shift), c.shift);
+    dsmem_st_f32(a + offsetof(SCommand, x_lo), c.x_lo);
+    dsmem_st_f32(a + offsetof(SCommand, x_hi), c.x_hi);
 }
 
-// Ranks the gathered tokens (n of them, in the cluster's lists) against one
-// another: got_w (running weight up to the token found), got_mass, got_index.
-__device__ __forceinline__ void rank_list(SShared &s, const SRow &row, const STarget &t, uint32_t ctas, uint32_t n) {
+// The gathered tokens (n of them, in the cluster's lists) in order, and the one at
+// which the target is reached: got_w (running weight up to it), got_mass,
+// got_index, got_z.  A bitonic sort of one place a thread, within warps by
+// shuffles; ranking each against all of them took 6 us for 500 tokens, this 1.
+__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t, uint32_t ctas, uint32_t n) {
     const uint32_t i = threadIdx.x;
-    uint2 mine = make_uint2(0, 0);
-    uint64_t w = 0;
+    uint64_t v = ~uint64_t{0};  // behind every token
     if (i < n) {
         uint32_t at = i, r = 0;
         for (; r + 1 < ctas; ++r) {
-            const uint32_t nr = ld_cluster_u32(dsmem_addr(smem_u32(&s.n), r));
+            const uint32_t nr = s.all_n[r];
             if (at < nr) break;
             at -= nr;
         }
-        const uint64_t e = ld_cluster_u64(dsmem_addr(smem_u32(&s.list[at]), r));
-        mine = make_uint2(static_cast<uint32_t>(e), static_cast<uint32_t>(e >> 32));
-        w = SRow::weight(row.z(key_value(mine.x)));
+        v = ld_cluster_u64(dsmem_addr(smem_u32(&s.list[at]), r));
     }
-    __syncthreads();  // every entry is in registers: the first CTA's own list may be overwritten
-    if (threadIdx.x == 0) s.got_index = 0xFFFFFFFFu;
-    if (i < n) {
-        s.list[i] = mine;
-        s.list_w[i] = w;
-    }
-    __syncthreads();
-    if (i < n) {
-        uint64_t up_w = 0;  // of the tokens up to this one
-        uint32_t up_c = 0;
-        for (uint32_t j = 0; j < n; ++j) {
-            const uint2 o = s.list[j];
-            if (o.x < mine.x || (o.x == mine.x && o.y <= mine.y)) {
-                up_w += s.list_w[j];
-                ++up_c;
+    if (i == 0) s.got_index = 0xFFFFFFFFu;
+    for (uint32_t k = 2; k < 2 * n; k <<= 1) {
+        const bool up = (i & k) == 0;
+        for (uint32_t j = k >> 1; j; j >>= 1) {
+            uint64_t o;
+            if (j >= 32) {
+                s.sort[i] = v;
+                __syncthreads();
+                o = s.sort[i ^ j];
+                __syncthreads();
+            } else {
+                o = __shfl_xor_sync(0xffffffffu, v, j);
             }
+            if ((o < v) == (((i & j) == 0) == up)) v = o;
         }
-        const uint64_t at_w = s.base_w + up_w, at_c = s.base_c + up_c;
-        if (t.by_count ? at_c == t.target : (at_w - w < t.target && t.target <= at_w)) {
-            s.got_w = at_w;
-            s.got_mass = w;
-            s.got_index = mine.y;
-            s.got_z = row.z(key_value(mine.x));
-        }
+    }
+    // a sort of 2^m > n / 2 places leaves the n tokens in the first 2^m threads
+    uint64_t w = i < n ? SRow::weight(row.z(key_value(static_cast<uint32_t>(v >> kSIndexBits)))) : 0;
+    const uint64_t mass = w;
+    uint32_t c = 0;
+    block_scan(s, w, c);
+    const uint64_t at_w = s.base_w + w, at_c = s.base_c + i + 1;
+    if (i < n && (t.by_count ? at_c == t.target : (at_w - mass < t.target && t.target <= at_w))) {
+        s.got_w = at_w;
+        s.got_mass = mass;
+        s.got_index = static_cast<uint32_t>(v) & (kSMaxVocab - 1);
+        s.got_z = row.z(key_value(static_cast<uint32_t>(v >> kSIndexBits)));
     }
     __syncthreads();
 }
@@ -254,6 +297,10 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     for (int b = tid; b < kSBins; b += kSThreads) s.cnt[b] = s.wl[b] = s.wh[b] = 0;
     grid_dep_launch();
     grid_dep_wait();
+    const float temperature = p.temperature ? __ldg(p.temperature + r) : 1.f;
+    const int32_t top_k = p.top_k ? __ldg(p.top_k + r) : 0;
+    const float top_p = p.top_p ? __ldg(p.top_p + r) : 1.f, min_p = p.min_p ? __ldg(p.min_p + r) : 0.f;
+    const float uniform = __ldg(p.uniform + r);
 
     // ---- this CTA's part of the row, 16 bytes at a time between its first and last 16-byte boundary
     const int32_t i0 = min(static_cast<int32_t>(rank) * p.chunk, p.vocab);
@@ -273,6 +320,10 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         if constexpr (sizeof(T) == 4) return x;
         else return __bfloat162float(x);
     };
+    // the passes below take four values at a time, from xs on: none before the part and past it
+    const int n4 = (pad + n + 3) / 4;
+    if (tid < pad) xs[tid] = -INFINITY;
+    if (tid < 4 * n4 - pad - n) xs[pad + n + tid] = -INFINITY;
     if (tid < head) xs[pad + tid] = take(widen(src[tid]));
     if (tid < n - tail0) xs[pad + tail0 + tid] = take(widen(src[tail0 + tid]));
     const uint4 *const src4 = reinterpret_cast<const uint4 *>(src + head);
@@ -321,7 +372,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         mx = fmaxf(mx, s.range[c].x);
         mn = fminf(mn, s.range[c].y);
     }
-    const float temperature = p.temperature ? __ldg(p.temperature + r) : 1.f;
+    const float4 *const xs4 = reinterpret_cast<const float4 *>(xs);
     if (mx == -INFINITY) {  // nothing to draw
         if (rank == 0 && tid == 0) {
             p.tokens[r] = -1;
@@ -331,8 +382,14 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     }
     if (!(temperature > 0.f)) {  // the largest logit, the lowest index of several
         uint32_t first = 0xFFFFFFFFu;
-        for (int i = tid; i < n; i += kSThreads)
-            if (xs[pad + i] == mx) first = min(first, static_cast<uint32_t>(i0 + i));
+        for (int i = tid; i < n4; i += kSThreads) {
+            const float4 q = xs4[i];
+            const uint32_t at = static_cast<uint32_t>(i0 - pad + 4 * i);
+            if (q.w == mx) first = min(first, at + 3);
+            if (q.z == mx) first = min(first, at + 2);
+            if (q.y == mx) first = min(first, at + 1);
+            if (q.x == mx) first = min(first, at);
+        }
         first = __reduce_min_sync(0xffffffffu, first);
         if (lane == 0) s.warp_c[warp] = first;
         __syncthreads();
@@ -350,24 +407,54 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     }
 
     // ---- the histogram of weights over z
-    const int32_t top_k = p.top_k ? __ldg(p.top_k + r) : 0;
-    const float top_p = p.top_p ? __ldg(p.top_p + r) : 1.f, min_p = p.min_p ? __ldg(p.min_p + r) : 0.f;
     const bool by_k = top_k > 0 && top_k < p.vocab, by_m = min_p > 0.f;
     const float ln_min_p = by_m ? logf(min_p) : -INFINITY;
     SRow row;
     row.top = mx;
     row.inv_t = 1.f / temperature;
     const float lowest = fmaxf(row.z(mn), kSFloor);  // (fmaxf of a NaN is the floor)
-    row.bin_scale = lowest < 0.f ? (kSBins - 0.5f) / -lowest : 0.f;
+    row.bin_scale = lowest < 0.f ? (kSBins - 1.f) / -lowest : 0.f;
     uint64_t above = 0;
-    for (int i = tid; i < n; i += kSThreads) {
-        const float x = xs[pad + i], z = row.z(x);
-        if (!SRow::counts(x, z)) continue;
-        const uint64_t w = SRow::weight(z);
-        const int b = row.bin(z);
-        if (by_k) atomicAdd(&s.cnt[b], 1u);
-        add_weight(&s.wl[b], &s.wh[b], w);
-        if (by_m && z >= ln_min_p) above += w;
+    // (a weight of 0 adds nothing wherever it goes: no branch, so that the
+    // additions of several values are under way at once)
+    constexpr int kAtOnce = 8;
+    for (int i = tid; i < n4; i += kSThreads * (kAtOnce / 4)) {
+        float x[kAtOnce], z[kAtOnce];
+        uint2 w[kAtOnce];
+        uint32_t old[kAtOnce];
+        int b[kAtOnce];
+#pragma unroll
+        for (int v = 0; v < kAtOnce / 4; ++v) {
+            const int at = i + v * kSThreads;
+            const float4 q = at < n4 ? xs4[at] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            x[4 * v] = q.x;
+            x[4 * v + 1] = q.y;
+            x[4 * v + 2] = q.z;
+            x[4 * v + 3] = q.w;
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            z[k] = row.z(x[k]);
+            w[k] = SRow::weight2(z[k]);
+            b[k] = row.bin(z[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) old[k] = atomicAdd(&s.wl[b[k]], w[k].x);
+        if (by_k) {
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (SRow::counts(x[k], z[k])) atomicAdd(&s.cnt[b[k]], 1u);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const uint32_t hi = w[k].y + (old[k] + w[k].x < w[k].x ? 1u : 0u);  // with the carry
+            if (hi) atomicAdd(&s.wh[b[k]], hi);
+        }
+        if (by_m) {
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                above += z[k] >= ln_min_p ? (static_cast<uint64_t>(w[k].y) << 32) | w[k].x : 0;
+        }
     }
     if (by_m) {
 #pragma unroll
@@ -391,28 +478,35 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     auto next_search = [&]() {
         if (stage == kCutK && !(by_k && static_cast<uint32_t>(top_k) < s.sum_c[kSBins - 1])) stage = kCutP;
         if (stage == kCutP && !(top_p < 1.f)) stage = kDraw;
-        if (stage == kCutK) {
-            want = {true, static_cast<uint64_t>(top_k)};
-        } else if (stage == kCutP) {
-            const double goal = ceil(static_cast<double>(top_p) * static_cast<double>(sum));
-            want = {false, goal >= 1.0 ? min(sum, static_cast<uint64_t>(goal)) : 1};
-        } else {
-            if (by_m) {
-                uint64_t m = 0;
-                for (uint32_t c = 0; c < ctas; ++c) m += s.above[c];
-                sum = min(sum, max(m, uint64_t{1} << 40));
+        want.by_count = stage == kCutK;
+        if (by_m && stage == kDraw) {
+            uint64_t m = 0;
+            for (uint32_t c = 0; c < ctas; ++c) m += s.above[c];
+            sum = min(sum, max(m, uint64_t{1} << 40));
+        }
+        if (tid == 0) {  // (one warp: 64-bit floating point is slow)
+            const double all = static_cast<double>(sum);
+            if (stage == kCutK) {
+                s.target = static_cast<uint64_t>(top_k);
+            } else if (stage == kCutP) {
+                const double goal = ceil(static_cast<double>(top_p) * all);
+                s.target = goal >= 1.0 ? min(sum, static_cast<uint64_t>(goal)) : 1;
+            } else {
+                const double at = static_cast<double>(uniform) * all;
+                s.target = (at >= 1.0 ? min(sum - 1, static_cast<uint64_t>(at)) : 0) + 1;
             }
-            const double at = static_cast<double>(__ldg(p.uniform + r)) * static_cast<double>(sum);
-            want = {false, (at >= 1.0 ? min(sum - 1, static_cast<uint64_t>(at)) : 0) + 1};
         }
+        __syncthreads();
+        want.target = s.target;
         find_bin(s, want);
-        if (tid == 0) {
-            SCommand c = {};
-            c.op = s.got_bin == 0xFFFFFFFFu ? kDone : kGatherBin;
-            c.bin = s.got_bin;
-            if (c.op == kDone) report_error(p.err, PPAS_DEVERR_TIMEOUT);
-            send(s, c, ctas);
-        }
+        SCommand c = {};
+        c.op = s.got_bin == 0xFFFFFFFFu ? kDone : kGather;
+        c.bin = s.got_bin;
+        row.bin_range(static_cast<int>(c.bin), c.x_lo, c.x_hi);
+        c.lo = static_cast<uint64_t>(order_key(c.x_hi)) << kSIndexBits;
+        c.hi = (static_cast<uint64_t>(order_key(c.x_lo)) << kSIndexBits) | (kSMaxVocab - 1);
+        if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
+        send(s, c, ctas);
     };
     if (rank == 0) {
         uint64_t w0 = s.sum_w[2 * tid], w1 = s.sum_w[2 * tid + 1], w = w0 + w1;
@@ -433,40 +527,33 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         if (cmd.op == kDone) return;
         if (cmd.op == kDivide)
             for (int b = tid; b < kSFine; b += kSThreads) s.cnt[b] = s.wl[b] = s.wh[b] = 0;
-        if (tid == 0) {
-            s.n = 0;
-            s.kmin = 0xFFFFFFFFu;
-            s.kmax = 0;
-        }
+        if (tid == 0) s.n = 0;
         __syncthreads();
-        for (int i = tid; i < n + ((kSThreads - n % kSThreads) % kSThreads); i += kSThreads) {
-            const float x = i < n ? xs[pad + i] : -INFINITY;
-            const float z = row.z(x);
-            const uint32_t key = order_key(x), index = static_cast<uint32_t>(i0 + i);
-            const uint64_t place = (static_cast<uint64_t>(key) << kSIndexBits) | index;
-            bool in = i < n && SRow::counts(x, z);
-            if (cmd.op == kGatherBin) in = in && row.bin(z) == static_cast<int>(cmd.bin);
-            else in = in && cmd.lo <= place && place <= cmd.hi;
-            if (cmd.op == kDivide) {
-                if (in) {
+        for (int i = tid; i < n4; i += kSThreads) {
+            const float4 q = xs4[i];
+            const float x[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (!(x[k] >= cmd.x_lo && x[k] <= cmd.x_hi)) continue;
+                const float z = row.z(x[k]);
+                if (!SRow::counts(x[k], z)) continue;
+                const uint32_t key = order_key(x[k]);
+                const uint64_t place =
+                    (static_cast<uint64_t>(key) << kSIndexBits) | static_cast<uint32_t>(i0 - pad + 4 * i + k);
+                if (row.bin(z) != static_cast<int>(cmd.bin) || place < cmd.lo || place > cmd.hi) continue;
+                if (cmd.op == kDivide) {
                     const uint32_t b = static_cast<uint32_t>((place - cmd.lo) >> cmd.shift);
                     if (by_k) atomicAdd(&s.cnt[b], 1u);
-                    add_weight(&s.wl[b], &s.wh[b], SRow::weight(z));
+                    add_weight(&s.wl[b], &s.wh[b], SRow::weight2(z));
+                    continue;
                 }
-                continue;
+                const uint32_t at = atomicAdd(&s.n, 1u);
+                if (at < kSList) s.list[at] = place;
             }
-            const uint32_t who = __ballot_sync(0xffffffffu, in);
-            if (!who) continue;
-            const uint32_t lo = __reduce_min_sync(0xffffffffu, in ? key : 0xFFFFFFFFu);
-            const uint32_t hi = __reduce_max_sync(0xffffffffu, in ? key : 0u);
-            uint32_t at = 0;
-            if (lane == 0) {
-                at = atomicAdd(&s.n, static_cast<uint32_t>(__popc(who)));
-                atomicMin(&s.kmin, lo);
-                atomicMax(&s.kmax, hi);
-            }
-            at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
-            if (in && at < kSList) s.list[at] = make_uint2(key, index);
+        }
+        if (cmd.op != kDivide) {
+            __syncthreads();
+            if (tid == 0) st_cluster_u32(dsmem_addr(smem_u32(&s.all_n[rank]), 0), s.n);
         }
         cluster_sync_all();
         if (cmd.op == kDivide) {
@@ -474,7 +561,8 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             cluster_sync_all();
         }
         if (rank != 0) continue;
-        SCommand c = {};
+        SCommand c = cmd;
+        c.op = kDone;
         if (cmd.op == kDivide) {
             // the part of the range in which the target lies
             uint64_t w = static_cast<uint64_t>(s.wl[kSFine + tid]) + (static_cast<uint64_t>(s.wh[kSFine + tid]) << 32);
@@ -492,39 +580,27 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 s.base_c = at_c - own_c;
             }
             __syncthreads();
-            if (tid == 0) {
-                c.op = s.got_bin == 0xFFFFFFFFu ? kDone : kGatherRange;
-                c.lo = cmd.lo + (static_cast<uint64_t>(s.got_bin) << cmd.shift);
-                c.hi = min(cmd.hi, c.lo + (uint64_t{1} << cmd.shift) - 1);
-                if (c.op == kDone) report_error(p.err, PPAS_DEVERR_TIMEOUT);
-                send(s, c, ctas);
-            }
+            c.op = s.got_bin == 0xFFFFFFFFu ? kDone : kGather;
+            c.lo = cmd.lo + (static_cast<uint64_t>(s.got_bin) << cmd.shift);
+            c.hi = min(cmd.hi, c.lo + (uint64_t{1} << cmd.shift) - 1);
+            c.x_lo = key_value(static_cast<uint32_t>(c.hi >> kSIndexBits));
+            c.x_hi = key_value(static_cast<uint32_t>(c.lo >> kSIndexBits));
+            if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
+            send(s, c, ctas);
             continue;
         }
-        uint32_t total = 0, kmin = 0xFFFFFFFFu, kmax = 0;
-        for (uint32_t q = 0; q < ctas; ++q) {
-            total += ld_cluster_u32(dsmem_addr(smem_u32(&s.n), q));
-            kmin = min(kmin, ld_cluster_u32(dsmem_addr(smem_u32(&s.kmin), q)));
-            kmax = max(kmax, ld_cluster_u32(dsmem_addr(smem_u32(&s.kmax), q)));
-        }
+        uint32_t total = 0;
+        for (uint32_t q = 0; q < ctas; ++q) total += s.all_n[q];
         if (total > kSList) {
-            __syncthreads();
-            if (tid == 0) {
-                c.op = kDivide;
-                c.lo = static_cast<uint64_t>(kmin) << kSIndexBits;
-                c.hi = (static_cast<uint64_t>(kmax) << kSIndexBits) | ((1u << kSIndexBits) - 1);
-                if (cmd.op == kGatherRange) {
-                    c.lo = max(c.lo, cmd.lo);
-                    c.hi = min(c.hi, cmd.hi);
-                }
-                // at most kSFine parts of 2^shift places
-                const int bits = 64 - __clzll(static_cast<long long>(c.hi - c.lo));
-                c.shift = bits > 9 ? bits - 9 : 0;
-                send(s, c, ctas);
-            }
+            c = cmd;
+            c.op = kDivide;
+            // at most kSFine parts of 2^shift places
+            const int bits = 64 - __clzll(static_cast<long long>(c.hi - c.lo));
+            c.shift = bits > 9 ? bits - 9 : 0;
+            send(s, c, ctas);
             continue;
         }
-        rank_list(s, row, want, ctas, total);
+        search_list(s, row, want, ctas, total);
         if (s.got_index == 0xFFFFFFFFu || stage == kDraw) {
             if (tid == 0) {
                 if (s.got_index == 0xFFFFFFFFu) {
@@ -539,8 +615,8 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                                             ? log1pf(-(static_cast<float>(sum - mass) / static_cast<float>(sum)))
                                             : s.got_z - logf(static_cast<float>(sum) * 0x1p-40f);
                 }
-                send(s, c, ctas);  // kDone
             }
+            send(s, c, ctas);  // kDone
             continue;
         }
         sum = s.got_w;
@@ -551,23 +627,23 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
 static_assert(kSFine == 1 << 9, "shift of a divided range");
 
 size_t sample_smem_bytes(int32_t chunk) {
-    // up to 7 values of padding in front of the row's part
-    return (sizeof(SShared) + 15) / 16 * 16 + (static_cast<size_t>(chunk) + 8) * sizeof(float);
+    // up to 7 values of padding in front of the row's part and 3 behind it
+    return (sizeof(SShared) + 15) / 16 * 16 + (static_cast<size_t>(chunk) + 12) * sizeof(float);
 }
 
 static std::atomic<uint64_t> g_sample_smem_set[2] = {};
 
 cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_t st) {
-    constexpr int kLimit = 232448;
+    constexpr int kLimit = 232448, kHalfSm = 115712;
     const auto kernel = bf16 ? sample_kernel<__nv_bfloat16> : sample_kernel<float>;
     const cudaError_t e = ensure_smem_limit(kernel, kLimit, g_sample_smem_set[bf16]);
     if (e != cudaSuccess) return e;
     const int32_t sms = device_sm_count();
     auto chunk_of = [&](int32_t c) { return ((p.vocab + c - 1) / c + 7) / 8 * 8; };
-    // as many CTAs a row as one round of the SMs holds, at least as many as its shared memory takes
+    // CTAs small enough that two share an SM, and as many a row as one round holds
     int32_t c = 1;
-    while (c < kSMaxCluster && (sample_smem_bytes(chunk_of(c)) > static_cast<size_t>(kLimit) ||
-                                (2 * c * static_cast<int64_t>(n_rows) <= sms && chunk_of(c) > 1024)))
+    while (c < kSMaxCluster && (sample_smem_bytes(chunk_of(c)) > static_cast<size_t>(kHalfSm) ||
+                                (c * static_cast<int64_t>(n_rows) <= sms && chunk_of(c) > 1024)))
         c *= 2;
     p.chunk = chunk_of(c);
     const size_t smem = sample_smem_bytes(p.chunk);
