@@ -50,13 +50,31 @@ struct SCommand {
     uint32_t pad;
 };
 
+// what the histogram alone tells of all three searches
+enum { kCutK, kCutP, kDraw, kStages };
+struct SBinsOf {
+    int32_t lo[kStages], hi[kStages];      // the target's bin is one of these; lo > hi: no such cut
+    float x_lo[kStages], x_hi[kStages];    // no token outside these is in them
+};
+
 struct SShared {
-    uint32_t cnt[kSBins], wl[kSBins], wh[kSBins];  // this CTA's histogram; divided bins: the first kSFine, and
-                                                   // behind them the first CTA's sums over the cluster
+    // this CTA's histogram (divided bins: the first kSFine, and behind them the
+    // first CTA's sums over the cluster), later its tokens of the three searches'
+    // bins (first CTA: the cluster's)
+    union {
+        struct {
+            uint32_t cnt[kSBins], wl[kSBins], wh[kSBins];
+        };
+        uint64_t lists[kStages][kSList];
+    };
     uint64_t sum_w[kSBins];                        // first CTA: sums over the cluster, then running sums
     uint32_t sum_c[kSBins];
-    uint64_t list[kSList];                         // places (key, index) of a gathered bin's tokens
-    uint64_t sort[kSThreads];
+    union {
+        uint64_t list[kSList];                     // places (key, index) of a gathered bin's tokens
+        uint64_t sort[kSThreads];
+    };
+    SBinsOf bins;
+    uint32_t ns[kStages], at[kStages];             // tokens in the lists (first CTA: all of them), this CTA's place there
     float2 range[kSMaxCluster];                    // (max, min finite) of each CTA
     uint64_t above[kSMaxCluster];                  // weight with z >= ln p_min, or the lowest index of the maximum
     uint64_t warp_w[kSWarps];
@@ -84,6 +102,14 @@ __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
 __device__ __forceinline__ void st_cluster_u32(uint32_t a, uint32_t v) {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
+__device__ __forceinline__ uint32_t atom_cluster_add(uint32_t a, uint32_t v) {
+    uint32_t old;
+    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
+    return old;
+}
+// the cluster barrier in two halves
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait_acquire() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_cluster_u64(uint32_t a, uint64_t v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
@@ -98,12 +124,12 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 
 struct SRow {
-    float top, inv_t, bin_scale;
-    __device__ __forceinline__ float z(float x) const { return x == top ? 0.f : (x - top) * inv_t; }
+    float top, inv_t, lowest, bin_scale;  // all finite; the z of the lowest token that counts is in bin kSBins - 1
+    __device__ __forceinline__ float z(float x) const { return (x - top) * inv_t; }
     // (conversions between floats and whole numbers share a slow unit with exp:
-    // here and in weight2 additions and shifts do their work)
+    // here and in weight2 additions do most of their work)
     __device__ __forceinline__ int bin(float z_) const {
-        return __float_as_int(fminf(-z_ * bin_scale, kSBins - 1.f) + 0x1p23f) - 0x4B000000;
+        return __float_as_int(fmaf(fmaxf(z_, lowest), -bin_scale, 0x1p23f)) - 0x4B000000;
     }
     // x of the tokens in bin b, and a little more: the bins' edges in x but for roundings
     __device__ __forceinline__ void bin_range(int b, float &lo, float &hi) const {
@@ -114,14 +140,14 @@ struct SRow {
         if (b == kSBins - 1 || !(lo < hi)) lo = -INFINITY;
         if (b == 0 || !(lo < hi)) hi = INFINITY;
     }
-    // tokens that can be drawn or counted (a -inf is below the floor, a NaN no comparison holds for)
+    // tokens that can be drawn or counted (a -inf is below the floor)
     __device__ __forceinline__ static bool counts(float x, float z_) { return x > -INFINITY && z_ > kSFloor; }
-    // floor(exp(z) 2^40), low and high half: the significand m of w = m 2^(e - 150) shifted into place
+    // floor(exp(z) 2^40), low and high half, every step exact
     __device__ __forceinline__ static uint2 weight2(float z_) {
-        const uint32_t b = __float_as_uint(expf(z_));
-        const uint64_t m = static_cast<uint64_t>((b & 0x7FFFFFu) | 0x800000u) << 17;
-        const uint64_t w = m >> min(127u - (b >> 23), 63u);
-        return make_uint2(static_cast<uint32_t>(w), static_cast<uint32_t>(w >> 32));
+        const float w = expf(z_) * 256.f;
+        const float hi = __fadd_rz(w, 0x1p23f);
+        const float rest = w - (hi - 0x1p23f);
+        return make_uint2(__float2uint_rz(rest * 0x1p32f), __float_as_uint(hi) & 0x7FFFFFu);
     }
     __device__ __forceinline__ static uint64_t weight(float z_) {
         const uint2 w = weight2(z_);
@@ -224,6 +250,27 @@ __device__ __forceinline__ void find_bin(SShared &s, const STarget &t) {
     __syncthreads();
 }
 
+// the first bin whose running sum reaches the target (10 reads by one thread, lanes apart)
+template <class T>
+__device__ __forceinline__ int reach_bin(const T *sums, uint64_t target) {
+    int lo = 0, hi = kSBins - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (sums[mid] >= target) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+// running weights to reach: p of S, and the draw's (64-bit floating point is
+// slow here: by single warps)
+__device__ __forceinline__ uint64_t cut_target(float top_p, uint64_t sum) {
+    const double goal = ceil(static_cast<double>(top_p) * static_cast<double>(sum));
+    return goal >= 1.0 ? min(sum, static_cast<uint64_t>(goal)) : 1;
+}
+__device__ __forceinline__ uint64_t draw_target(float uniform, uint64_t sum) {
+    const double at = static_cast<double>(uniform) * static_cast<double>(sum);
+    return (at >= 1.0 ? min(sum - 1, static_cast<uint64_t>(at)) : 0) + 1;
+}
+
 // the first CTA's command, written into every CTA of the cluster (a thread each)
 __device__ __forceinline__ void send(SShared &s, const SCommand &c, uint32_t ctas) {
     if (threadIdx.x >= ctas) return;
@@ -237,22 +284,27 @@ __device__ __forceinline__ void send(SShared &s, const SCommand &c, uint32_t cta
     dsmem_st_f32(a + offsetof(SCommand, x_hi), c.x_hi);
 }
 
-// The gathered tokens (n of them, in the cluster's lists) in order, and the one at
-// which the target is reached: got_w (running weight up to it), got_mass,
-// got_index, got_z.  A bitonic sort of one place a thread, within warps by
-// shuffles; ranking each against all of them took 6 us for 500 tokens, this 1.
-__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t, uint32_t ctas, uint32_t n) {
-    const uint32_t i = threadIdx.x;
-    uint64_t v = ~uint64_t{0};  // behind every token
-    if (i < n) {
-        uint32_t at = i, r = 0;
-        for (; r + 1 < ctas; ++r) {
-            const uint32_t nr = s.all_n[r];
-            if (at < nr) break;
-            at -= nr;
-        }
-        v = ld_cluster_u64(dsmem_addr(smem_u32(&s.list[at]), r));
+// Entry threadIdx.x of the cluster's n gathered tokens (lists of all_n(rank)
+// tokens each, at the same place in every CTA); behind every token past them.
+template <class Count>
+__device__ __forceinline__ uint64_t list_entry(const uint64_t *list, uint32_t n, uint32_t ctas, Count all_n) {
+    if (threadIdx.x >= n) return ~uint64_t{0};
+    uint32_t at = threadIdx.x, r = 0;
+    for (; r + 1 < ctas; ++r) {
+        const uint32_t nr = all_n(r);
+        if (at < nr) break;
+        at -= nr;
     }
+    return ld_cluster_u64(dsmem_addr(smem_u32(list + at), r));
+}
+
+// The gathered tokens (n of them, one place v a thread) in order, and the one at
+// which the target is reached: got_w (running weight up to it), got_mass,
+// got_index, got_z.  A bitonic sort, within warps by shuffles; ranking each
+// against all of them took 6 us for 500 tokens, this 1.
+__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t, uint64_t v, uint32_t n) {
+    const uint32_t i = threadIdx.x;
+    __syncthreads();  // (every place is in registers: the list's room is the sort's)
     if (i == 0) s.got_index = 0xFFFFFFFFu;
     for (uint32_t k = 2; k < 2 * n; k <<= 1) {
         const bool up = (i & k) == 0;
@@ -412,8 +464,20 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     SRow row;
     row.top = mx;
     row.inv_t = 1.f / temperature;
-    const float lowest = fmaxf(row.z(mn), kSFloor);  // (fmaxf of a NaN is the floor)
-    row.bin_scale = lowest < 0.f ? (kSBins - 1.f) / -lowest : 0.f;
+    if (mx == INFINITY || row.inv_t == INFINITY) {
+        // the largest alone are left, as equals
+        for (int i = tid; i < n4; i += kSThreads) {
+            float4 *const q = reinterpret_cast<float4 *>(xs) + i;
+            *q = make_float4(q->x == mx ? 0.f : -INFINITY, q->y == mx ? 0.f : -INFINITY, q->z == mx ? 0.f : -INFINITY,
+                             q->w == mx ? 0.f : -INFINITY);
+        }
+        row.top = mn = 0.f;
+        row.inv_t = 1.f;
+        __syncthreads();
+    }
+    // (lowest * bin_scale is 1023 but for two roundings, so that no bin is past the last)
+    row.lowest = fmaxf(row.z(mn), kSFloor);
+    row.bin_scale = row.lowest < 0.f ? fminf((kSBins - 1.f) / -row.lowest, 1e30f) : 0.f;
     uint64_t above = 0;
     // (a weight of 0 adds nothing wherever it goes: no branch, so that the
     // additions of several values are under way at once)
@@ -470,34 +534,27 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     push_sums<false>(s, rank, ctas, by_k);
     cluster_sync_all();
 
-    // ---- the cuts and the draw, one search after the other (state of the first CTA)
-    enum { kCutK, kCutP, kDraw } stage = kCutK;
+    // ---- the cuts and the draw (state of the first CTA)
+    int stage = kCutK;
     STarget want = {};
     uint64_t sum = 0;  // S so far
-    // the next search that there is to do, and its first command
-    auto next_search = [&]() {
+    uint64_t m_sum = ~uint64_t{0};
+    // the search that comes next: its stage, and what it has to reach
+    auto next_target = [&]() {
         if (stage == kCutK && !(by_k && static_cast<uint32_t>(top_k) < s.sum_c[kSBins - 1])) stage = kCutP;
         if (stage == kCutP && !(top_p < 1.f)) stage = kDraw;
-        want.by_count = stage == kCutK;
-        if (by_m && stage == kDraw) {
-            uint64_t m = 0;
-            for (uint32_t c = 0; c < ctas; ++c) m += s.above[c];
-            sum = min(sum, max(m, uint64_t{1} << 40));
-        }
-        if (tid == 0) {  // (one warp: 64-bit floating point is slow)
-            const double all = static_cast<double>(sum);
-            if (stage == kCutK) {
-                s.target = static_cast<uint64_t>(top_k);
-            } else if (stage == kCutP) {
-                const double goal = ceil(static_cast<double>(top_p) * all);
-                s.target = goal >= 1.0 ? min(sum, static_cast<uint64_t>(goal)) : 1;
-            } else {
-                const double at = static_cast<double>(uniform) * all;
-                s.target = (at >= 1.0 ? min(sum - 1, static_cast<uint64_t>(at)) : 0) + 1;
-            }
+        if (stage == kDraw) sum = min(sum, m_sum);
+        if (warp == 0) {
+            const uint64_t t = stage == kCutK   ? static_cast<uint64_t>(top_k)
+                               : stage == kCutP ? cut_target(top_p, sum)
+                                                : draw_target(uniform, sum);
+            if (lane == 0) s.target = t;
         }
         __syncthreads();
-        want.target = s.target;
+        want = {stage == kCutK, s.target};
+    };
+    auto next_search = [&]() {
+        next_target();
         find_bin(s, want);
         SCommand c = {};
         c.op = s.got_bin == 0xFFFFFFFFu ? kDone : kGather;
@@ -507,6 +564,20 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         c.hi = (static_cast<uint64_t>(order_key(c.x_lo)) << kSIndexBits) | (kSMaxVocab - 1);
         if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
         send(s, c, ctas);
+    };
+    // the token that was found, by one thread
+    auto write_token = [&]() {
+        if (s.got_index == 0xFFFFFFFFu) {
+            report_error(p.err, PPAS_DEVERR_TIMEOUT);
+            return;
+        }
+        p.tokens[r] = static_cast<int32_t>(s.got_index);
+        const uint64_t mass = s.got_mass;
+        // a likely token's log from what is left of the sum, which is accurate near 0; another's
+        // from its z, which a weight of few units of 2^-40 has lost the last bits of
+        if (p.logprobs)
+            p.logprobs[r] = 2 * mass > sum ? log1pf(-(static_cast<float>(sum - mass) / static_cast<float>(sum)))
+                                           : s.got_z - logf(static_cast<float>(sum) * 0x1p-40f);
     };
     if (rank == 0) {
         uint64_t w0 = s.sum_w[2 * tid], w1 = s.sum_w[2 * tid + 1], w = w0 + w1;
@@ -518,8 +589,121 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         s.sum_c[2 * tid + 1] = c;
         __syncthreads();
         sum = s.sum_w[kSBins - 1];
-        next_search();
+        if (by_m) {
+            m_sum = 0;
+            for (uint32_t q = 0; q < ctas; ++q) m_sum += s.above[q];
+            m_sum = max(m_sum, uint64_t{1} << 40);
+        }
+        if (warp == 0) {
+            // After a cut in bin b, S lies between the running sums before and
+            // after b; the targets grow with S.  Where its ends (even and odd
+            // lanes) lead to bins b0 and b1, S itself leads to one of b0 .. b1.
+            const bool end = lane & 1;
+            uint64_t at = sum;
+            SBinsOf o;
+            auto found = [&](int j, int b) {
+                o.lo[j] = __shfl_sync(0xffffffffu, b, 0);
+                o.hi[j] = __shfl_sync(0xffffffffu, b, 1);
+                float unused;
+                row.bin_range(o.hi[j], o.x_lo[j], unused);
+                row.bin_range(o.lo[j], unused, o.x_hi[j]);
+                const uint64_t before = o.lo[j] ? s.sum_w[o.lo[j] - 1] : 0;
+                at = min(at, max(end ? s.sum_w[o.hi[j]] : before, uint64_t{1} << 40));
+            };
+#pragma unroll
+            for (int j = 0; j < kStages; ++j) {
+                o.lo[j] = 1;
+                o.hi[j] = 0;
+                o.x_lo[j] = INFINITY;
+                o.x_hi[j] = -INFINITY;
+            }
+            if (by_k && static_cast<uint32_t>(top_k) < s.sum_c[kSBins - 1])
+                found(kCutK, reach_bin(s.sum_c, static_cast<uint64_t>(top_k)));
+            if (top_p < 1.f) found(kCutP, reach_bin(s.sum_w, cut_target(top_p, at)));
+            at = min(at, m_sum);
+            found(kDraw, reach_bin(s.sum_w, draw_target(uniform, at)));
+            if (lane < ctas) {
+                const uint32_t to = dsmem_addr(smem_u32(&s.bins), lane);
+#pragma unroll
+                for (int j = 0; j < kStages; ++j) {
+                    dsmem_st_s32(to + offsetof(SBinsOf, lo) + 4 * j, o.lo[j]);
+                    dsmem_st_s32(to + offsetof(SBinsOf, hi) + 4 * j, o.hi[j]);
+                    dsmem_st_f32(to + offsetof(SBinsOf, x_lo) + 4 * j, o.x_lo[j]);
+                    dsmem_st_f32(to + offsetof(SBinsOf, x_hi) + 4 * j, o.x_hi[j]);
+                }
+            }
+        }
     }
+    if (tid < kStages) s.ns[tid] = 0;
+    cluster_sync_all();
+    // ---- one pass gathers the tokens of all three, in the first CTA
+    const SBinsOf bins = s.bins;
+    for (int i = tid; i < n4; i += kSThreads) {
+        const float4 q = xs4[i];
+        const float x[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            bool maybe = false;
+#pragma unroll
+            for (int j = 0; j < kStages; ++j) maybe = maybe || (x[k] >= bins.x_lo[j] && x[k] <= bins.x_hi[j]);
+            if (!maybe) continue;
+            const float z = row.z(x[k]);
+            if (!SRow::counts(x[k], z)) continue;
+            const int b = row.bin(z);
+#pragma unroll
+            for (int j = 0; j < kStages; ++j)
+                if (bins.lo[j] <= b && b <= bins.hi[j]) {
+                    const uint32_t at = atomicAdd(&s.ns[j], 1u);
+                    if (at < kSList)
+                        s.lists[j][at] = (static_cast<uint64_t>(order_key(x[k])) << kSIndexBits) |
+                                         static_cast<uint32_t>(i0 - pad + 4 * i + k);
+                }
+        }
+    }
+    if (rank != 0) {
+        __syncthreads();
+        if (tid < kStages) s.at[tid] = s.ns[tid] ? atom_cluster_add(dsmem_addr(smem_u32(&s.ns[tid]), 0), s.ns[tid]) : 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kStages; ++j) {
+            const uint32_t at = s.at[j] + tid;
+            if (tid < static_cast<int>(min(s.ns[j], static_cast<uint32_t>(kSList))) && at < kSList)
+                st_cluster_u64(dsmem_addr(smem_u32(&s.lists[j][at]), 0), s.lists[j][tid]);
+        }
+    }
+    cluster_sync_all();
+    uint32_t total[kStages];
+    bool enough = true;
+#pragma unroll
+    for (int j = 0; j < kStages; ++j) {
+        total[j] = ld_cluster_u32(dsmem_addr(smem_u32(&s.ns[j]), 0));
+        enough = enough && total[j] <= kSList;
+    }
+    if (enough) {
+        cluster_arrive();  // this CTA has read the first one's counts
+        if (rank == 0) {
+#pragma unroll
+            for (int j = 0; j < kStages; ++j) {
+                if (bins.lo[j] > bins.hi[j]) continue;
+                stage = j;
+                next_target();
+                if (tid == 0) {
+                    const int b = bins.lo[j];
+                    s.base_w = b ? s.sum_w[b - 1] : 0;
+                    s.base_c = b ? s.sum_c[b - 1] : 0;
+                }
+                search_list(s, row, want, tid < static_cast<int>(total[j]) ? s.lists[j][tid] : ~uint64_t{0}, total[j]);
+                if (s.got_index == 0xFFFFFFFFu) break;
+                if (j < kDraw) sum = s.got_w;
+            }
+            if (tid == 0) write_token();
+        }
+        cluster_wait_acquire();
+        return;
+    }
+    // ---- one search after the other, each bin divided while it holds too many tokens
+    stage = kCutK;
+    if (rank == 0) next_search();
     for (int step = 0; step < kSMaxCommands; ++step) {
         // (the first CTA has read every list and count when it gets here)
         cluster_sync_all();
@@ -600,22 +784,9 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             send(s, c, ctas);
             continue;
         }
-        search_list(s, row, want, ctas, total);
+        search_list(s, row, want, list_entry(s.list, total, ctas, [&](uint32_t q) { return s.all_n[q]; }), total);
         if (s.got_index == 0xFFFFFFFFu || stage == kDraw) {
-            if (tid == 0) {
-                if (s.got_index == 0xFFFFFFFFu) {
-                    report_error(p.err, PPAS_DEVERR_TIMEOUT);
-                } else {
-                    p.tokens[r] = static_cast<int32_t>(s.got_index);
-                    const uint64_t mass = s.got_mass;
-                    // a likely token's log from what is left of the sum, which is accurate near 0; another's
-                    // from its z, which a weight of few units of 2^-40 has lost the last bits of
-                    if (p.logprobs)
-                        p.logprobs[r] = 2 * mass > sum
-                                            ? log1pf(-(static_cast<float>(sum - mass) / static_cast<float>(sum)))
-                                            : s.got_z - logf(static_cast<float>(sum) * 0x1p-40f);
-                }
-            }
+            if (tid == 0) write_token();
             send(s, c, ctas);  // kDone
             continue;
         }
