@@ -20,6 +20,8 @@
 // again, by the bits of (x, index).
 #include <math.h>
 
+#include <type_traits>
+
 #include "ppas_device.cuh"
 #include "ppas_internal.h"
 
@@ -65,26 +67,33 @@ struct SShared {
         struct {
             uint32_t cnt[kSBins], wl[kSBins], wh[kSBins];
         };
-        uint64_t lists[kStages][kSList];
+        uint64_t lists[kStages][kSList];  // places (key, index)
     };
-    uint64_t sum_w[kSBins];                        // first CTA: sums over the cluster, then running sums
-    uint32_t sum_c[kSBins];
+    // first CTA: the bins' sums over the cluster, then their running sums; later the
+    // running weights of the sorted lists
     union {
-        uint64_t list[kSList];                     // places (key, index) of a gathered bin's tokens
+        struct {
+            uint64_t sum_w[kSBins];
+            uint32_t sum_c[kSBins];
+        };
+        uint64_t run[kStages][kSList];
+    };
+    union {
+        uint64_t list[kSList];             // tokens of a single search's bin
         uint64_t sort[kSThreads];
     };
     SBinsOf bins;
-    uint32_t ns[kStages], at[kStages];             // tokens in the lists (first CTA: all of them), this CTA's place there
-    float2 range[kSMaxCluster];                    // (max, min finite) of each CTA
-    uint64_t above[kSMaxCluster];                  // weight with z >= ln p_min, or the lowest index of the maximum
-    uint64_t warp_w[kSWarps];
+    uint32_t ns[kStages], at[kStages];     // tokens in the lists (first CTA: all of them), this CTA's place there
+    float2 range[kSMaxCluster];            // (max, min finite) of each CTA
+    uint64_t above[kSMaxCluster];          // weight with z >= ln p_min, or the lowest index of the maximum
+    uint64_t warp_w[kStages][kSWarps];
     uint32_t warp_c[kSWarps];
     float2 warp_range[kSWarps];
-    uint32_t n;                                    // of this CTA's gathered tokens
-    uint32_t all_n[kSMaxCluster];                  // first CTA: every CTA's
-    uint64_t target;
+    uint32_t n;                            // of this CTA's gathered tokens
+    uint32_t all_n[kSMaxCluster];          // first CTA: every CTA's
     SCommand cmd;
-    uint64_t base_w, base_c, got_w, got_mass;      // first CTA: sums before the bin, what a search found
+    uint64_t target;
+    uint64_t base_w, base_c, got_w, got_mass;  // first CTA: sums before the bin, what a search found
     uint32_t got_bin, got_index;
     float got_z;
 };
@@ -125,6 +134,7 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 
 struct SRow {
     float top, inv_t, lowest, bin_scale;  // all finite; the z of the lowest token that counts is in bin kSBins - 1
+    float width;                          // x a bin (infinite where there is one bin)
     __device__ __forceinline__ float z(float x) const { return (x - top) * inv_t; }
     // (conversions between floats and whole numbers share a slow unit with exp:
     // here and in weight2 additions do most of their work)
@@ -133,15 +143,14 @@ struct SRow {
     }
     // x of the tokens in bin b, and a little more: the bins' edges in x but for roundings
     __device__ __forceinline__ void bin_range(int b, float &lo, float &hi) const {
-        const float t = 1.f / (inv_t * bin_scale);  // x a bin
-        const float slack = 1e-5f * (fabsf(top) + (static_cast<float>(b) + 1.f) * t) + 1e-30f;
-        lo = top - (static_cast<float>(b) + 0.5f) * t - slack;
-        hi = top - (static_cast<float>(b) - 0.5f) * t + slack;
+        const float slack = 1e-5f * (fabsf(top) + (static_cast<float>(b) + 1.f) * width) + 1e-30f;
+        lo = top - (static_cast<float>(b) + 0.5f) * width - slack;
+        hi = top - (static_cast<float>(b) - 0.5f) * width + slack;
         if (b == kSBins - 1 || !(lo < hi)) lo = -INFINITY;
         if (b == 0 || !(lo < hi)) hi = INFINITY;
     }
     // tokens that can be drawn or counted (a -inf is below the floor)
-    __device__ __forceinline__ static bool counts(float x, float z_) { return x > -INFINITY && z_ > kSFloor; }
+    __device__ __forceinline__ static bool counts(float z_) { return z_ > kSFloor; }
     // floor(exp(z) 2^40), low and high half, every step exact
     __device__ __forceinline__ static uint2 weight2(float z_) {
         const float w = expf(z_) * 256.f;
@@ -173,7 +182,7 @@ __device__ __forceinline__ void block_scan(SShared &s, uint64_t &w, uint32_t &c)
         }
     }
     if (lane == 31) {
-        s.warp_w[warp] = w;
+        s.warp_w[0][warp] = w;
         s.warp_c[warp] = c;
     }
     __syncthreads();
@@ -181,7 +190,7 @@ __device__ __forceinline__ void block_scan(SShared &s, uint64_t &w, uint32_t &c)
     uint32_t before_c = 0;
 #pragma unroll
     for (int i = 0; i < kSWarps; ++i) {
-        const uint64_t a = s.warp_w[i];
+        const uint64_t a = s.warp_w[0][i];
         const uint32_t b = s.warp_c[i];
         before_w += i < warp ? a : 0;
         before_c += i < warp ? b : 0;
@@ -250,15 +259,16 @@ __device__ __forceinline__ void find_bin(SShared &s, const STarget &t) {
     __syncthreads();
 }
 
-// the first bin whose running sum reaches the target (10 reads by one thread, lanes apart)
+// The first of m <= 1024 running sums that reaches the target (the last where
+// none does), by a whole warp: 32 of them, then the ones before the first of those.
 template <class T>
-__device__ __forceinline__ int reach_bin(const T *sums, uint64_t target) {
-    int lo = 0, hi = kSBins - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (sums[mid] >= target) hi = mid; else lo = mid + 1;
-    }
-    return lo;
+__device__ __forceinline__ int reach(const T *sums, int m, uint64_t target) {
+    const int lane = threadIdx.x & 31, stride = (m + 31) / 32;
+    const uint32_t far = __ballot_sync(0xffffffffu, sums[min((lane + 1) * stride, m) - 1] >= target);
+    const int first = far ? __ffs(far) - 1 : 31;
+    const int at = min(first * stride + min(lane, stride - 1), m - 1);
+    const uint32_t near = __ballot_sync(0xffffffffu, sums[at] >= target);
+    return min(near ? first * stride + __ffs(near) - 1 : m - 1, m - 1);
 }
 // running weights to reach: p of S, and the draw's (64-bit floating point is
 // slow here: by single warps)
@@ -336,9 +346,74 @@ __device__ __forceinline__ void search_list(SShared &s, const SRow &row, const S
     __syncthreads();
 }
 
+// The same for the three lists of one pass at once (the steps of one hide the
+// latency of the others'): sorted places in s.lists, running weights in s.run.
+__device__ __forceinline__ void sort_lists(SShared &s, const SRow &row, const uint32_t (&total)[kStages]) {
+    const uint32_t i = threadIdx.x;
+    const int lane = i & 31, warp = i >> 5;
+    uint64_t v[kStages];
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < kStages; ++j) {
+        v[j] = i < total[j] ? s.lists[j][i] : ~uint64_t{0};
+        n = max(n, total[j]);
+    }
+    __syncthreads();
+    for (uint32_t k = 2; k < 2 * n; k <<= 1) {
+        const bool up = (i & k) == 0;
+        for (uint32_t d = k >> 1; d; d >>= 1) {
+            const bool low = ((i & d) == 0) == up;
+            uint64_t o[kStages];
+            if (d >= 32) {
+#pragma unroll
+                for (int j = 0; j < kStages; ++j) s.lists[j][i] = v[j];
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < kStages; ++j) o[j] = s.lists[j][i ^ d];
+                __syncthreads();
+            } else {
+#pragma unroll
+                for (int j = 0; j < kStages; ++j) o[j] = __shfl_xor_sync(0xffffffffu, v[j], d);
+            }
+#pragma unroll
+            for (int j = 0; j < kStages; ++j)
+                if ((o[j] < v[j]) == low) v[j] = o[j];
+        }
+    }
+    uint64_t w[kStages];
+#pragma unroll
+    for (int j = 0; j < kStages; ++j) {
+        s.lists[j][i] = v[j];
+        w[j] = i < total[j] ? SRow::weight(row.z(key_value(static_cast<uint32_t>(v[j] >> kSIndexBits)))) : 0;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+#pragma unroll
+        for (int j = 0; j < kStages; ++j) {
+            const uint64_t a = __shfl_up_sync(0xffffffffu, w[j], o);
+            if (lane >= o) w[j] += a;
+        }
+    }
+    if (lane == 31) {
+#pragma unroll
+        for (int j = 0; j < kStages; ++j) s.warp_w[j][warp] = w[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kStages; ++j) {
+        uint64_t before = 0;
+#pragma unroll
+        for (int q = 0; q < kSWarps; ++q) before += q < warp ? s.warp_w[j][q] : 0;
+        s.run[j][i] = w[j] + before;
+    }
+    __syncthreads();
+}
+
 }  // namespace
 
-template <class T>
+// kResident: the row's part stays in shared memory; otherwise each pass reads it
+// again, from L2 for the most part.
+template <class T, bool kResident>
 __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
     extern __shared__ __align__(16) uint8_t sample_smem[];
     SShared &s = *reinterpret_cast<SShared *>(sample_smem);
@@ -361,47 +436,80 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     constexpr int kPer = 16 / sizeof(T);
     const int pad = static_cast<int>((reinterpret_cast<uintptr_t>(src) / sizeof(T)) % kPer);
     const int head = min(n, (kPer - pad) % kPer), vecs = (n - head) / kPer, tail0 = head + vecs * kPer;
-    float mx = -INFINITY, mn = INFINITY;
-    auto take = [&](float x) {
-        x = x == x ? x + 0.f : -INFINITY;  // a NaN is no candidate; one zero
-        mx = fmaxf(mx, x);
-        if (x > -INFINITY) mn = fminf(mn, x);
-        return x;
-    };
+    const uint4 *const src4 = reinterpret_cast<const uint4 *>(src + head);
+    const int n4 = (pad + n + 3) / 4;  // resident: four values at a time, from xs on
+    const float4 *const xs4 = reinterpret_cast<const float4 *>(xs);
     auto widen = [](T x) -> float {
         if constexpr (sizeof(T) == 4) return x;
         else return __bfloat162float(x);
     };
-    // the passes below take four values at a time, from xs on: none before the part and past it
-    const int n4 = (pad + n + 3) / 4;
-    if (tid < pad) xs[tid] = -INFINITY;
-    if (tid < 4 * n4 - pad - n) xs[pad + n + tid] = -INFINITY;
-    if (tid < head) xs[pad + tid] = take(widen(src[tid]));
-    if (tid < n - tail0) xs[pad + tail0 + tid] = take(widen(src[tail0 + tid]));
-    const uint4 *const src4 = reinterpret_cast<const uint4 *>(src + head);
-    constexpr int kLoads = 4;
-    for (int v0 = tid; v0 < vecs; v0 += kLoads * kSThreads) {
-        uint4 q[kLoads];
+    // f(four values, index of the first in the row) over the part as it lies in
+    // global memory, kLoads x 16 bytes a thread under way
+    auto stream = [&](auto loads, auto &&f) {
+        constexpr int kLoads = decltype(loads)::value;
+        // what is before the first and after the last boundary, a value a thread
+        const int ends = head + n - tail0;
+        if (tid < ends) {
+            const int at = tid < head ? tid : tail0 + tid - head;
+            const float x[4] = {widen(src[at]), -INFINITY, -INFINITY, -INFINITY};
+            f(x, i0 + at);
+        }
+        for (int v0 = tid; v0 < vecs; v0 += kLoads * kSThreads) {
+            uint4 q[kLoads];
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k)
-            if (v0 + k * kSThreads < vecs) q[k] = __ldcs(src4 + v0 + k * kSThreads);
+            for (int k = 0; k < kLoads; ++k)
+                if (v0 + k * kSThreads < vecs) q[k] = __ldg(src4 + v0 + k * kSThreads);
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            if (v0 + k * kSThreads >= vecs) break;
-            float4 *dst = reinterpret_cast<float4 *>(xs + pad + head) + (v0 + k * kSThreads) * (kPer / 4);
-            const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
-            if constexpr (sizeof(T) == 4) {
-                dst[0] = make_float4(take(__uint_as_float(w[0])), take(__uint_as_float(w[1])),
-                                     take(__uint_as_float(w[2])), take(__uint_as_float(w[3])));
-            } else {
+            for (int k = 0; k < kLoads; ++k) {
+                if (v0 + k * kSThreads >= vecs) break;
+                const int at = i0 + head + (v0 + k * kSThreads) * kPer;
+                const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+                if constexpr (sizeof(T) == 4) {
+                    const float x[4] = {__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]),
+                                        __uint_as_float(w[3])};
+                    f(x, at);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    dst[e] = make_float4(take(__uint_as_float(w[2 * e] << 16)),
-                                         take(__uint_as_float(w[2 * e] & 0xFFFF0000u)),
-                                         take(__uint_as_float(w[2 * e + 1] << 16)),
-                                         take(__uint_as_float(w[2 * e + 1] & 0xFFFF0000u)));
+                    for (int e = 0; e < 2; ++e) {
+                        const float x[4] = {__uint_as_float(w[2 * e] << 16), __uint_as_float(w[2 * e] & 0xFFFF0000u),
+                                            __uint_as_float(w[2 * e + 1] << 16),
+                                            __uint_as_float(w[2 * e + 1] & 0xFFFF0000u)};
+                        f(x, at + 4 * e);
+                    }
+                }
             }
         }
+    };
+    // a pass over the part once the maximum is known
+    auto pass = [&](auto &&f) {
+        if constexpr (kResident) {
+            for (int i = tid; i < n4; i += kSThreads) {
+                const float4 q = xs4[i];
+                const float x[4] = {q.x, q.y, q.z, q.w};
+                f(x, i0 - pad + 4 * i);
+            }
+        } else {
+            stream(std::integral_constant<int, 2>{}, f);
+        }
+    };
+    float mx = -INFINITY, mn = INFINITY;
+    stream(std::integral_constant<int, 4>{}, [&](const float(&x)[4], int at) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            y[k] = fmaxf(x[k], -INFINITY);  // a NaN is no candidate
+            mx = fmaxf(mx, y[k]);
+            mn = fminf(mn, y[k] > -INFINITY ? y[k] : INFINITY);
+        }
+        if constexpr (kResident) {
+            const int to = at - i0 + pad;
+            if (at - i0 < head || at - i0 >= tail0) xs[to] = y[0];
+            else *reinterpret_cast<float4 *>(xs + to) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+    });
+    if constexpr (kResident) {
+        if (tid < pad) xs[tid] = -INFINITY;
+        if (tid < 4 * n4 - pad - n) xs[pad + n + tid] = -INFINITY;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -424,7 +532,6 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         mx = fmaxf(mx, s.range[c].x);
         mn = fminf(mn, s.range[c].y);
     }
-    const float4 *const xs4 = reinterpret_cast<const float4 *>(xs);
     if (mx == -INFINITY) {  // nothing to draw
         if (rank == 0 && tid == 0) {
             p.tokens[r] = -1;
@@ -434,14 +541,11 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     }
     if (!(temperature > 0.f)) {  // the largest logit, the lowest index of several
         uint32_t first = 0xFFFFFFFFu;
-        for (int i = tid; i < n4; i += kSThreads) {
-            const float4 q = xs4[i];
-            const uint32_t at = static_cast<uint32_t>(i0 - pad + 4 * i);
-            if (q.w == mx) first = min(first, at + 3);
-            if (q.z == mx) first = min(first, at + 2);
-            if (q.y == mx) first = min(first, at + 1);
-            if (q.x == mx) first = min(first, at);
-        }
+        pass([&](const float(&x)[4], int at) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (x[k] == mx) first = min(first, static_cast<uint32_t>(at + k));
+        });
         first = __reduce_min_sync(0xffffffffu, first);
         if (lane == 0) s.warp_c[warp] = first;
         __syncthreads();
@@ -464,69 +568,60 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     SRow row;
     row.top = mx;
     row.inv_t = 1.f / temperature;
-    if (mx == INFINITY || row.inv_t == INFINITY) {
-        // the largest alone are left, as equals
-        for (int i = tid; i < n4; i += kSThreads) {
-            float4 *const q = reinterpret_cast<float4 *>(xs) + i;
-            *q = make_float4(q->x == mx ? 0.f : -INFINITY, q->y == mx ? 0.f : -INFINITY, q->z == mx ? 0.f : -INFINITY,
-                             q->w == mx ? 0.f : -INFINITY);
-        }
+    // where z would not be a number: the largest alone are left, as equals
+    const bool odd = mx == INFINITY || row.inv_t == INFINITY;
+    if (odd) {
         row.top = mn = 0.f;
         row.inv_t = 1.f;
-        __syncthreads();
     }
+    // a logit as the passes see it: one zero, and a NaN as -inf
+    auto logit = [&](float x) {
+        if (odd) return x == mx ? 0.f : -INFINITY;
+        return fmaxf(x, -INFINITY);
+    };
     // (lowest * bin_scale is 1023 but for two roundings, so that no bin is past the last)
     row.lowest = fmaxf(row.z(mn), kSFloor);
     row.bin_scale = row.lowest < 0.f ? fminf((kSBins - 1.f) / -row.lowest, 1e30f) : 0.f;
+    row.width = 1.f / (row.inv_t * row.bin_scale);
     uint64_t above = 0;
     // (a weight of 0 adds nothing wherever it goes: no branch, so that the
     // additions of several values are under way at once)
-    constexpr int kAtOnce = 8;
-    for (int i = tid; i < n4; i += kSThreads * (kAtOnce / 4)) {
-        float x[kAtOnce], z[kAtOnce];
-        uint2 w[kAtOnce];
-        uint32_t old[kAtOnce];
-        int b[kAtOnce];
+    pass([&](const float(&x)[4], int) {
+        float z[4];
+        uint2 w[4];
+        uint32_t old[4];
+        int b[4];
 #pragma unroll
-        for (int v = 0; v < kAtOnce / 4; ++v) {
-            const int at = i + v * kSThreads;
-            const float4 q = at < n4 ? xs4[at] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            x[4 * v] = q.x;
-            x[4 * v + 1] = q.y;
-            x[4 * v + 2] = q.z;
-            x[4 * v + 3] = q.w;
-        }
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-            z[k] = row.z(x[k]);
+        for (int k = 0; k < 4; ++k) {
+            z[k] = row.z(logit(x[k]));
             w[k] = SRow::weight2(z[k]);
             b[k] = row.bin(z[k]);
         }
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) old[k] = atomicAdd(&s.wl[b[k]], w[k].x);
+        for (int k = 0; k < 4; ++k) old[k] = atomicAdd(&s.wl[b[k]], w[k].x);
         if (by_k) {
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k)
-                if (SRow::counts(x[k], z[k])) atomicAdd(&s.cnt[b[k]], 1u);
+            for (int k = 0; k < 4; ++k)
+                if (SRow::counts(z[k])) atomicAdd(&s.cnt[b[k]], 1u);
         }
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
+        for (int k = 0; k < 4; ++k) {
             const uint32_t hi = w[k].y + (old[k] + w[k].x < w[k].x ? 1u : 0u);  // with the carry
             if (hi) atomicAdd(&s.wh[b[k]], hi);
         }
         if (by_m) {
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k)
+            for (int k = 0; k < 4; ++k)
                 above += z[k] >= ln_min_p ? (static_cast<uint64_t>(w[k].y) << 32) | w[k].x : 0;
         }
-    }
+    });
     if (by_m) {
 #pragma unroll
         for (int o = 16; o; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-        if (lane == 0) s.warp_w[warp] = above;
+        if (lane == 0) s.warp_w[0][warp] = above;
         __syncthreads();
         if (tid == 0) {
-            for (int w = 1; w < kSWarps; ++w) above += s.warp_w[w];
+            for (int w = 1; w < kSWarps; ++w) above += s.warp_w[0][w];
             st_cluster_u64(dsmem_addr(smem_u32(&s.above[rank]), 0), above);
         }
     }
@@ -601,9 +696,13 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             const bool end = lane & 1;
             uint64_t at = sum;
             SBinsOf o;
-            auto found = [&](int j, int b) {
-                o.lo[j] = __shfl_sync(0xffffffffu, b, 0);
-                o.hi[j] = __shfl_sync(0xffffffffu, b, 1);
+            auto found = [&](int j, uint64_t t) {
+                if (j == kCutK) {
+                    o.lo[j] = o.hi[j] = reach(s.sum_c, kSBins, t);
+                } else {
+                    o.lo[j] = reach(s.sum_w, kSBins, __shfl_sync(0xffffffffu, t, 0));
+                    o.hi[j] = reach(s.sum_w, kSBins, __shfl_sync(0xffffffffu, t, 1));
+                }
                 float unused;
                 row.bin_range(o.hi[j], o.x_lo[j], unused);
                 row.bin_range(o.lo[j], unused, o.x_hi[j]);
@@ -618,10 +717,10 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 o.x_hi[j] = -INFINITY;
             }
             if (by_k && static_cast<uint32_t>(top_k) < s.sum_c[kSBins - 1])
-                found(kCutK, reach_bin(s.sum_c, static_cast<uint64_t>(top_k)));
-            if (top_p < 1.f) found(kCutP, reach_bin(s.sum_w, cut_target(top_p, at)));
+                found(kCutK, static_cast<uint64_t>(top_k));
+            if (top_p < 1.f) found(kCutP, cut_target(top_p, at));
             at = min(at, m_sum);
-            found(kDraw, reach_bin(s.sum_w, draw_target(uniform, at)));
+            found(kDraw, draw_target(uniform, at));
             if (lane < ctas) {
                 const uint32_t to = dsmem_addr(smem_u32(&s.bins), lane);
 #pragma unroll
@@ -638,28 +737,26 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     cluster_sync_all();
     // ---- one pass gathers the tokens of all three, in the first CTA
     const SBinsOf bins = s.bins;
-    for (int i = tid; i < n4; i += kSThreads) {
-        const float4 q = xs4[i];
-        const float x[4] = {q.x, q.y, q.z, q.w};
+    pass([&](const float(&x)[4], int first) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            bool maybe = false;
+            bool maybe = odd;
 #pragma unroll
             for (int j = 0; j < kStages; ++j) maybe = maybe || (x[k] >= bins.x_lo[j] && x[k] <= bins.x_hi[j]);
             if (!maybe) continue;
-            const float z = row.z(x[k]);
-            if (!SRow::counts(x[k], z)) continue;
+            const float y = logit(x[k]) + 0.f, z = row.z(y);
+            if (!SRow::counts(z)) continue;
             const int b = row.bin(z);
 #pragma unroll
             for (int j = 0; j < kStages; ++j)
                 if (bins.lo[j] <= b && b <= bins.hi[j]) {
                     const uint32_t at = atomicAdd(&s.ns[j], 1u);
                     if (at < kSList)
-                        s.lists[j][at] = (static_cast<uint64_t>(order_key(x[k])) << kSIndexBits) |
-                                         static_cast<uint32_t>(i0 - pad + 4 * i + k);
+                        s.lists[j][at] =
+                            (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(first + k);
                 }
         }
-    }
+    });
     if (rank != 0) {
         __syncthreads();
         if (tid < kStages) s.at[tid] = s.ns[tid] ? atom_cluster_add(dsmem_addr(smem_u32(&s.ns[tid]), 0), s.ns[tid]) : 0;
@@ -682,21 +779,25 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     if (enough) {
         cluster_arrive();  // this CTA has read the first one's counts
         if (rank == 0) {
+            uint64_t base[kStages], base_c = 0;
 #pragma unroll
-            for (int j = 0; j < kStages; ++j) {
-                if (bins.lo[j] > bins.hi[j]) continue;
-                stage = j;
-                next_target();
-                if (tid == 0) {
-                    const int b = bins.lo[j];
-                    s.base_w = b ? s.sum_w[b - 1] : 0;
-                    s.base_c = b ? s.sum_c[b - 1] : 0;
+            for (int j = 0; j < kStages; ++j) base[j] = bins.lo[j] > 0 ? s.sum_w[bins.lo[j] - 1] : 0;
+            if (bins.lo[kCutK] > 0) base_c = s.sum_c[bins.lo[kCutK] - 1];
+            sort_lists(s, row, total);
+            if (warp == 0) {
+                if (bins.lo[kCutK] <= bins.hi[kCutK]) sum = base[kCutK] + s.run[kCutK][top_k - base_c - 1];
+                if (bins.lo[kCutP] <= bins.hi[kCutP])
+                    sum = base[kCutP] + s.run[kCutP][reach(s.run[kCutP], total[kCutP], cut_target(top_p, sum) - base[kCutP])];
+                sum = min(sum, m_sum);
+                const int at = reach(s.run[kDraw], total[kDraw], draw_target(uniform, sum) - base[kDraw]);
+                if (lane == 0) {
+                    const uint64_t place = s.lists[kDraw][at];
+                    s.got_index = static_cast<uint32_t>(place) & (kSMaxVocab - 1);
+                    s.got_z = row.z(key_value(static_cast<uint32_t>(place >> kSIndexBits)));
+                    s.got_mass = s.run[kDraw][at] - (at ? s.run[kDraw][at - 1] : 0);
+                    write_token();
                 }
-                search_list(s, row, want, tid < static_cast<int>(total[j]) ? s.lists[j][tid] : ~uint64_t{0}, total[j]);
-                if (s.got_index == 0xFFFFFFFFu) break;
-                if (j < kDraw) sum = s.got_w;
             }
-            if (tid == 0) write_token();
         }
         cluster_wait_acquire();
         return;
@@ -713,17 +814,14 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             for (int b = tid; b < kSFine; b += kSThreads) s.cnt[b] = s.wl[b] = s.wh[b] = 0;
         if (tid == 0) s.n = 0;
         __syncthreads();
-        for (int i = tid; i < n4; i += kSThreads) {
-            const float4 q = xs4[i];
-            const float x[4] = {q.x, q.y, q.z, q.w};
+        pass([&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (!(x[k] >= cmd.x_lo && x[k] <= cmd.x_hi)) continue;
-                const float z = row.z(x[k]);
-                if (!SRow::counts(x[k], z)) continue;
-                const uint32_t key = order_key(x[k]);
+                if (!odd && !(x[k] >= cmd.x_lo && x[k] <= cmd.x_hi)) continue;
+                const float y = logit(x[k]) + 0.f, z = row.z(y);
+                if (!SRow::counts(z)) continue;
                 const uint64_t place =
-                    (static_cast<uint64_t>(key) << kSIndexBits) | static_cast<uint32_t>(i0 - pad + 4 * i + k);
+                    (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(first + k);
                 if (row.bin(z) != static_cast<int>(cmd.bin) || place < cmd.lo || place > cmd.hi) continue;
                 if (cmd.op == kDivide) {
                     const uint32_t b = static_cast<uint32_t>((place - cmd.lo) >> cmd.shift);
@@ -734,7 +832,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 const uint32_t at = atomicAdd(&s.n, 1u);
                 if (at < kSList) s.list[at] = place;
             }
-        }
+        });
         if (cmd.op != kDivide) {
             __syncthreads();
             if (tid == 0) st_cluster_u32(dsmem_addr(smem_u32(&s.all_n[rank]), 0), s.n);
@@ -805,20 +903,22 @@ size_t sample_smem_bytes(int32_t chunk) {
 static std::atomic<uint64_t> g_sample_smem_set[2] = {};
 
 cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_t st) {
-    constexpr int kLimit = 232448, kHalfSm = 115712;
-    const auto kernel = bf16 ? sample_kernel<__nv_bfloat16> : sample_kernel<float>;
-    const cudaError_t e = ensure_smem_limit(kernel, kLimit, g_sample_smem_set[bf16]);
-    if (e != cudaSuccess) return e;
-    const int32_t sms = device_sm_count();
+    // two CTAs share an SM
+    constexpr int kHalfSm = 115712;
+    const int64_t slots = 2 * static_cast<int64_t>(device_sm_count());
     auto chunk_of = [&](int32_t c) { return ((p.vocab + c - 1) / c + 7) / 8 * 8; };
-    // CTAs small enough that two share an SM, and as many a row as one round holds
+    // as many CTAs a row as one round holds
     int32_t c = 1;
-    while (c < kSMaxCluster && (sample_smem_bytes(chunk_of(c)) > static_cast<size_t>(kHalfSm) ||
-                                (c * static_cast<int64_t>(n_rows) <= sms && chunk_of(c) > 1024)))
-        c *= 2;
+    while (c < kSMaxCluster && 2 * c * static_cast<int64_t>(n_rows) <= slots && chunk_of(c) > 1024) c *= 2;
+    const bool resident = sample_smem_bytes(chunk_of(c)) <= static_cast<size_t>(kHalfSm);
+    const auto kernel = bf16 ? (resident ? sample_kernel<__nv_bfloat16, true> : sample_kernel<__nv_bfloat16, false>)
+                             : (resident ? sample_kernel<float, true> : sample_kernel<float, false>);
+    if (resident) {
+        const cudaError_t e = ensure_smem_limit(kernel, kHalfSm, g_sample_smem_set[bf16]);
+        if (e != cudaSuccess) return e;
+    }
     p.chunk = chunk_of(c);
-    const size_t smem = sample_smem_bytes(p.chunk);
-    if (smem > static_cast<size_t>(kLimit)) return cudaErrorInvalidValue;
+    const size_t smem = resident ? sample_smem_bytes(p.chunk) : sizeof(SShared);
     PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kSThreads), smem, st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
