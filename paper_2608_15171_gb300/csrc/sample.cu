@@ -16,8 +16,8 @@
 // in the order reaches a target, and need no sort: one histogram of weights over
 // bins of z (linear, so the bins fill evenly and few additions collide), summed
 // over the cluster, gives the bin; its tokens (a few hundred) go to the first
-// CTA, which sorts them.  A bin with more than that (ties, flat rows) is divided
-// again, by the bits of (x, index).
+// CTA, which divides them further by the bits of (x, index).  Bins with more than
+// that (ties, flat rows) are divided so by the whole cluster first.
 #include <math.h>
 
 #include <type_traits>
@@ -32,7 +32,7 @@ constexpr int kSThreads = 512;
 constexpr int kSWarps = kSThreads / 32;
 constexpr int kSBins = 1024;      // bins of z
 constexpr int kSFine = 512;       // bins of a bin's (x, index)
-constexpr int kSList = 512;       // tokens that are sorted
+constexpr int kSList = 512;       // tokens that the first CTA takes
 constexpr int kSIndexBits = 18;   // vocabularies of up to 2^18 tokens
 constexpr int kSMaxCluster = 8;
 constexpr float kSFloor = -28.f;  // z below this: W = 0 (exp(-28) 2^40 < 1)
@@ -69,24 +69,15 @@ struct SShared {
         };
         uint64_t lists[kStages][kSList];  // places (key, index)
     };
-    // first CTA: the bins' sums over the cluster, then their running sums; later the
-    // running weights of the sorted lists
-    union {
-        struct {
-            uint64_t sum_w[kSBins];
-            uint32_t sum_c[kSBins];
-        };
-        uint64_t run[kStages][kSList];
-    };
-    union {
-        uint64_t list[kSList];             // tokens of a single search's bin
-        uint64_t sort[kSThreads];
-    };
+    uint64_t sum_w[kSBins];                // first CTA: the bins' sums over the cluster, then their running sums
+    uint32_t sum_c[kSBins];
+    uint64_t list[kSList];                 // tokens of a single search's bin
+    uint32_t fine_c[kSFine], fine_l[kSFine], fine_h[kSFine];  // first CTA: the histogram of a list
     SBinsOf bins;
     uint32_t ns[kStages], at[kStages];     // tokens in the lists (first CTA: all of them), this CTA's place there
     float2 range[kSMaxCluster];            // (max, min finite) of each CTA
     uint64_t above[kSMaxCluster];          // weight with z >= ln p_min, or the lowest index of the maximum
-    uint64_t warp_w[kStages][kSWarps];
+    uint64_t warp_w[kSWarps];
     uint32_t warp_c[kSWarps];
     float2 warp_range[kSWarps];
     uint32_t n;                            // of this CTA's gathered tokens
@@ -94,7 +85,7 @@ struct SShared {
     SCommand cmd;
     uint64_t target;
     uint64_t base_w, base_c, got_w, got_mass;  // first CTA: sums before the bin, what a search found
-    uint32_t got_bin, got_index;
+    uint32_t got_bin, got_index, got_n;
     float got_z;
 };
 
@@ -132,6 +123,21 @@ __device__ __forceinline__ float key_value(uint32_t k) {
     return __uint_as_float((k >> 31) ? k : ~k & 0x7FFFFFFFu);
 }
 
+// The places of the logits of type T from x_hi down to x_lo.  (Of bf16 logits a
+// bin of z holds one value or two, of many tokens each: with the range closed
+// to them the first division tells tokens apart, and not 2^16 values that are
+// not there.)
+template <class T>
+__device__ __forceinline__ void place_range(float x_lo, float x_hi, uint64_t &lo, uint64_t &hi) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t a = __float_as_uint(x_lo), b = __float_as_uint(x_hi);
+        x_lo = __uint_as_float((a & 0xFFFF0000u) + (!(a >> 31) && (a & 0xFFFFu) ? 0x10000u : 0u));
+        x_hi = __uint_as_float((b & 0xFFFF0000u) + ((b >> 31) && (b & 0xFFFFu) ? 0x10000u : 0u));
+    }
+    lo = static_cast<uint64_t>(order_key(x_hi + 0.f)) << kSIndexBits;
+    hi = (static_cast<uint64_t>(order_key(x_lo + 0.f)) << kSIndexBits) | (kSMaxVocab - 1);
+}
+
 struct SRow {
     float top, inv_t, lowest, bin_scale;  // all finite; the z of the lowest token that counts is in bin kSBins - 1
     float width;                          // x a bin (infinite where there is one bin)
@@ -151,16 +157,12 @@ struct SRow {
     }
     // tokens that can be drawn or counted (a -inf is below the floor)
     __device__ __forceinline__ static bool counts(float z_) { return z_ > kSFloor; }
-    // floor(exp(z) 2^40), low and high half, every step exact
-    __device__ __forceinline__ static uint2 weight2(float z_) {
-        const float w = expf(z_) * 256.f;
+    // floor(e 2^40), low and high half, every step exact; e = exp(z)
+    __device__ __forceinline__ static uint2 weight2(float e) {
+        const float w = e * 256.f;
         const float hi = __fadd_rz(w, 0x1p23f);
         const float rest = w - (hi - 0x1p23f);
         return make_uint2(__float2uint_rz(rest * 0x1p32f), __float_as_uint(hi) & 0x7FFFFFu);
-    }
-    __device__ __forceinline__ static uint64_t weight(float z_) {
-        const uint2 w = weight2(z_);
-        return (static_cast<uint64_t>(w.y) << 32) | w.x;
     }
 };
 
@@ -182,7 +184,7 @@ __device__ __forceinline__ void block_scan(SShared &s, uint64_t &w, uint32_t &c)
         }
     }
     if (lane == 31) {
-        s.warp_w[0][warp] = w;
+        s.warp_w[warp] = w;
         s.warp_c[warp] = c;
     }
     __syncthreads();
@@ -190,7 +192,7 @@ __device__ __forceinline__ void block_scan(SShared &s, uint64_t &w, uint32_t &c)
     uint32_t before_c = 0;
 #pragma unroll
     for (int i = 0; i < kSWarps; ++i) {
-        const uint64_t a = s.warp_w[0][i];
+        const uint64_t a = s.warp_w[i];
         const uint32_t b = s.warp_c[i];
         before_w += i < warp ? a : 0;
         before_c += i < warp ? b : 0;
@@ -308,108 +310,68 @@ __device__ __forceinline__ uint64_t list_entry(const uint64_t *list, uint32_t n,
     return ld_cluster_u64(dsmem_addr(smem_u32(list + at), r));
 }
 
-// The gathered tokens (n of them, one place v a thread) in order, and the one at
-// which the target is reached: got_w (running weight up to it), got_mass,
-// got_index, got_z.  A bitonic sort, within warps by shuffles; ranking each
-// against all of them took 6 us for 500 tokens, this 1.
-__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t, uint64_t v, uint32_t n) {
+// Finds among n gathered tokens (one place v a thread, all within lo .. hi) the
+// one at which the target is reached, s.base_w and s.base_c being the sums before
+// them: got_w (the running weight up to it), got_mass, got_index, got_z.  Their
+// places are spread over kSFine bins, and the bin with the target again, until
+// it holds one token: mostly once or twice.  (Sorting 300 of them took 4 us,
+// bound by the shuffles; this takes 1.)
+__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t, uint64_t v, uint32_t n,
+                                            uint64_t lo, uint64_t hi) {
     const uint32_t i = threadIdx.x;
-    __syncthreads();  // (every place is in registers: the list's room is the sort's)
+    const float z = row.z(key_value(static_cast<uint32_t>(v >> kSIndexBits)));
+    const uint2 mass = SRow::weight2(expf(z));
     if (i == 0) s.got_index = 0xFFFFFFFFu;
-    for (uint32_t k = 2; k < 2 * n; k <<= 1) {
-        const bool up = (i & k) == 0;
-        for (uint32_t j = k >> 1; j; j >>= 1) {
-            uint64_t o;
-            if (j >= 32) {
-                s.sort[i] = v;
-                __syncthreads();
-                o = s.sort[i ^ j];
-                __syncthreads();
-            } else {
-                o = __shfl_xor_sync(0xffffffffu, v, j);
+    uint64_t base_w = s.base_w, base_c = s.base_c;
+    for (int level = 0; level < 8; ++level) {
+        const int bits = 64 - __clzll(static_cast<long long>(hi - lo));
+        const int shift = bits > 9 ? bits - 9 : 0;  // kSFine parts of 2^shift places
+        s.fine_c[i] = s.fine_l[i] = s.fine_h[i] = 0;
+        if (i == 0) s.got_bin = 0xFFFFFFFFu;
+        __syncthreads();
+        const bool in = i < n && lo <= v && v <= hi;
+        const uint32_t b = static_cast<uint32_t>((v - lo) >> shift);
+        if (in) {
+            atomicAdd(&s.fine_c[b], 1u);
+            add_weight(&s.fine_l[b], &s.fine_h[b], mass);
+        }
+        __syncthreads();
+        const uint64_t own_w = s.fine_l[i] + (static_cast<uint64_t>(s.fine_h[i]) << 32);
+        const uint32_t own_c = s.fine_c[i];
+        uint64_t w = own_w;
+        uint32_t c = own_c;
+        block_scan(s, w, c);
+        const uint64_t at_w = base_w + w, at_c = base_c + c;
+        if (t.by_count ? (at_c - own_c < t.target && t.target <= at_c) : (at_w - own_w < t.target && t.target <= at_w)) {
+            s.got_bin = i;
+            s.got_n = own_c;
+            s.got_w = at_w;
+            s.base_w = at_w - own_w;
+            s.base_c = at_c - own_c;
+        }
+        __syncthreads();
+        const uint32_t got = s.got_bin;
+        if (got == 0xFFFFFFFFu) return;
+        if (s.got_n == 1) {
+            if (in && b == got) {
+                s.got_mass = (static_cast<uint64_t>(mass.y) << 32) | mass.x;
+                s.got_index = static_cast<uint32_t>(v) & (kSMaxVocab - 1);
+                s.got_z = z;
             }
-            if ((o < v) == (((i & j) == 0) == up)) v = o;
+            __syncthreads();
+            return;
         }
+        base_w = s.base_w;
+        base_c = s.base_c;
+        lo += static_cast<uint64_t>(got) << shift;
+        hi = min(hi, lo + (uint64_t{1} << shift) - 1);
     }
-    // a sort of 2^m > n / 2 places leaves the n tokens in the first 2^m threads
-    uint64_t w = i < n ? SRow::weight(row.z(key_value(static_cast<uint32_t>(v >> kSIndexBits)))) : 0;
-    const uint64_t mass = w;
-    uint32_t c = 0;
-    block_scan(s, w, c);
-    const uint64_t at_w = s.base_w + w, at_c = s.base_c + i + 1;
-    if (i < n && (t.by_count ? at_c == t.target : (at_w - mass < t.target && t.target <= at_w))) {
-        s.got_w = at_w;
-        s.got_mass = mass;
-        s.got_index = static_cast<uint32_t>(v) & (kSMaxVocab - 1);
-        s.got_z = row.z(key_value(static_cast<uint32_t>(v >> kSIndexBits)));
-    }
-    __syncthreads();
-}
-
-// The same for the three lists of one pass at once (the steps of one hide the
-// latency of the others'): sorted places in s.lists, running weights in s.run.
-__device__ __forceinline__ void sort_lists(SShared &s, const SRow &row, const uint32_t (&total)[kStages]) {
-    const uint32_t i = threadIdx.x;
-    const int lane = i & 31, warp = i >> 5;
-    uint64_t v[kStages];
-    uint32_t n = 0;
-#pragma unroll
-    for (int j = 0; j < kStages; ++j) {
-        v[j] = i < total[j] ? s.lists[j][i] : ~uint64_t{0};
-        n = max(n, total[j]);
-    }
-    __syncthreads();
-    for (uint32_t k = 2; k < 2 * n; k <<= 1) {
-        const bool up = (i & k) == 0;
-        for (uint32_t d = k >> 1; d; d >>= 1) {
-            const bool low = ((i & d) == 0) == up;
-            uint64_t o[kStages];
-            if (d >= 32) {
-#pragma unroll
-                for (int j = 0; j < kStages; ++j) s.lists[j][i] = v[j];
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < kStages; ++j) o[j] = s.lists[j][i ^ d];
-                __syncthreads();
-            } else {
-#pragma unroll
-                for (int j = 0; j < kStages; ++j) o[j] = __shfl_xor_sync(0xffffffffu, v[j], d);
-            }
-#pragma unroll
-            for (int j = 0; j < kStages; ++j)
-                if ((o[j] < v[j]) == low) v[j] = o[j];
-        }
-    }
-    uint64_t w[kStages];
-#pragma unroll
-    for (int j = 0; j < kStages; ++j) {
-        s.lists[j][i] = v[j];
-        w[j] = i < total[j] ? SRow::weight(row.z(key_value(static_cast<uint32_t>(v[j] >> kSIndexBits)))) : 0;
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-#pragma unroll
-        for (int j = 0; j < kStages; ++j) {
-            const uint64_t a = __shfl_up_sync(0xffffffffu, w[j], o);
-            if (lane >= o) w[j] += a;
-        }
-    }
-    if (lane == 31) {
-#pragma unroll
-        for (int j = 0; j < kStages; ++j) s.warp_w[j][warp] = w[j];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kStages; ++j) {
-        uint64_t before = 0;
-#pragma unroll
-        for (int q = 0; q < kSWarps; ++q) before += q < warp ? s.warp_w[j][q] : 0;
-        s.run[j][i] = w[j] + before;
-    }
-    __syncthreads();
 }
 
 }  // namespace
+
+template <int n>
+using Loads = std::integral_constant<int, n>;
 
 // kResident: the row's part stays in shared memory; otherwise each pass reads it
 // again, from L2 for the most part.
@@ -481,7 +443,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         }
     };
     // a pass over the part once the maximum is known
-    auto pass = [&](auto &&f) {
+    auto pass = [&](auto loads, auto &&f) {
         if constexpr (kResident) {
             for (int i = tid; i < n4; i += kSThreads) {
                 const float4 q = xs4[i];
@@ -489,11 +451,11 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 f(x, i0 - pad + 4 * i);
             }
         } else {
-            stream(std::integral_constant<int, 2>{}, f);
+            stream(loads, f);
         }
     };
     float mx = -INFINITY, mn = INFINITY;
-    stream(std::integral_constant<int, 4>{}, [&](const float(&x)[4], int at) {
+    stream(Loads<4>{}, [&](const float(&x)[4], int at) {
         float y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -541,7 +503,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     }
     if (!(temperature > 0.f)) {  // the largest logit, the lowest index of several
         uint32_t first = 0xFFFFFFFFu;
-        pass([&](const float(&x)[4], int at) {
+        pass(Loads<4>{}, [&](const float(&x)[4], int at) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (x[k] == mx) first = min(first, static_cast<uint32_t>(at + k));
@@ -586,28 +548,43 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     uint64_t above = 0;
     // (a weight of 0 adds nothing wherever it goes: no branch, so that the
     // additions of several values are under way at once)
-    pass([&](const float(&x)[4], int) {
-        float z[4];
+    pass(Loads<2>{}, [&](const float(&x)[4], int) {
+        float z[4], e[4];
         uint2 w[4];
         uint32_t old[4];
         int b[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             z[k] = row.z(logit(x[k]));
-            w[k] = SRow::weight2(z[k]);
+            e[k] = expf(z[k]);
             b[k] = row.bin(z[k]);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) old[k] = atomicAdd(&s.wl[b[k]], w[k].x);
         if (by_k) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (SRow::counts(z[k])) atomicAdd(&s.cnt[b[k]], 1u);
         }
+        if (fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])) < 0x1p-8f) {
+            // (nearly all of them: the weight is its low half)
+            bool carry = false;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t hi = w[k].y + (old[k] + w[k].x < w[k].x ? 1u : 0u);  // with the carry
-            if (hi) atomicAdd(&s.wh[b[k]], hi);
+            for (int k = 0; k < 4; ++k) {
+                w[k] = make_uint2(__float2uint_rz(e[k] * 0x1p40f), 0);
+                old[k] = atomicAdd(&s.wl[b[k]], w[k].x);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) carry = carry || old[k] > ~w[k].x;
+            if (carry) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (old[k] > ~w[k].x) atomicAdd(&s.wh[b[k]], 1u);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                w[k] = SRow::weight2(e[k]);
+                add_weight(&s.wl[b[k]], &s.wh[b[k]], w[k]);
+            }
         }
         if (by_m) {
 #pragma unroll
@@ -618,10 +595,10 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     if (by_m) {
 #pragma unroll
         for (int o = 16; o; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-        if (lane == 0) s.warp_w[0][warp] = above;
+        if (lane == 0) s.warp_w[warp] = above;
         __syncthreads();
         if (tid == 0) {
-            for (int w = 1; w < kSWarps; ++w) above += s.warp_w[0][w];
+            for (int w = 1; w < kSWarps; ++w) above += s.warp_w[w];
             st_cluster_u64(dsmem_addr(smem_u32(&s.above[rank]), 0), above);
         }
     }
@@ -655,8 +632,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         c.op = s.got_bin == 0xFFFFFFFFu ? kDone : kGather;
         c.bin = s.got_bin;
         row.bin_range(static_cast<int>(c.bin), c.x_lo, c.x_hi);
-        c.lo = static_cast<uint64_t>(order_key(c.x_hi)) << kSIndexBits;
-        c.hi = (static_cast<uint64_t>(order_key(c.x_lo)) << kSIndexBits) | (kSMaxVocab - 1);
+        place_range<T>(c.x_lo, fminf(c.x_hi, row.top), c.lo, c.hi);
         if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
         send(s, c, ctas);
     };
@@ -737,26 +713,36 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     cluster_sync_all();
     // ---- one pass gathers the tokens of all three, in the first CTA
     const SBinsOf bins = s.bins;
-    pass([&](const float(&x)[4], int first) {
+    auto gather = [&](float x, int index) {
+        const float y = logit(x) + 0.f, z = row.z(y);
+        if (!SRow::counts(z)) return;
+        const int b = row.bin(z);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            bool maybe = odd;
+        for (int j = 0; j < kStages; ++j)
+            if (bins.lo[j] <= b && b <= bins.hi[j]) {
+                const uint32_t at = atomicAdd(&s.ns[j], 1u);
+                if (at < kSList)
+                    s.lists[j][at] = (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(index);
+            }
+    };
+    if (!odd && bins.lo[kCutK] > bins.hi[kCutK] && bins.lo[kCutP] > bins.hi[kCutP]) {
+        // (one range to compare with)
+        pass(Loads<4>{}, [&](const float(&x)[4], int first) {
 #pragma unroll
-            for (int j = 0; j < kStages; ++j) maybe = maybe || (x[k] >= bins.x_lo[j] && x[k] <= bins.x_hi[j]);
-            if (!maybe) continue;
-            const float y = logit(x[k]) + 0.f, z = row.z(y);
-            if (!SRow::counts(z)) continue;
-            const int b = row.bin(z);
+            for (int k = 0; k < 4; ++k)
+                if (x[k] >= bins.x_lo[kDraw] && x[k] <= bins.x_hi[kDraw]) gather(x[k], first + k);
+        });
+    } else {
+        pass(Loads<4>{}, [&](const float(&x)[4], int first) {
 #pragma unroll
-            for (int j = 0; j < kStages; ++j)
-                if (bins.lo[j] <= b && b <= bins.hi[j]) {
-                    const uint32_t at = atomicAdd(&s.ns[j], 1u);
-                    if (at < kSList)
-                        s.lists[j][at] =
-                            (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(first + k);
-                }
-        }
-    });
+            for (int k = 0; k < 4; ++k) {
+                bool maybe = odd;
+#pragma unroll
+                for (int j = 0; j < kStages; ++j) maybe = maybe || (x[k] >= bins.x_lo[j] && x[k] <= bins.x_hi[j]);
+                if (maybe) gather(x[k], first + k);
+            }
+        });
+    }
     if (rank != 0) {
         __syncthreads();
         if (tid < kStages) s.at[tid] = s.ns[tid] ? atom_cluster_add(dsmem_addr(smem_u32(&s.ns[tid]), 0), s.ns[tid]) : 0;
@@ -769,35 +755,29 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         }
     }
     cluster_sync_all();
-    uint32_t total[kStages];
     bool enough = true;
 #pragma unroll
-    for (int j = 0; j < kStages; ++j) {
-        total[j] = ld_cluster_u32(dsmem_addr(smem_u32(&s.ns[j]), 0));
-        enough = enough && total[j] <= kSList;
-    }
+    for (int j = 0; j < kStages; ++j) enough = ld_cluster_u32(dsmem_addr(smem_u32(&s.ns[j]), 0)) <= kSList && enough;
     if (enough) {
         cluster_arrive();  // this CTA has read the first one's counts
         if (rank == 0) {
-            uint64_t base[kStages], base_c = 0;
-#pragma unroll
-            for (int j = 0; j < kStages; ++j) base[j] = bins.lo[j] > 0 ? s.sum_w[bins.lo[j] - 1] : 0;
-            if (bins.lo[kCutK] > 0) base_c = s.sum_c[bins.lo[kCutK] - 1];
-            sort_lists(s, row, total);
-            if (warp == 0) {
-                if (bins.lo[kCutK] <= bins.hi[kCutK]) sum = base[kCutK] + s.run[kCutK][top_k - base_c - 1];
-                if (bins.lo[kCutP] <= bins.hi[kCutP])
-                    sum = base[kCutP] + s.run[kCutP][reach(s.run[kCutP], total[kCutP], cut_target(top_p, sum) - base[kCutP])];
-                sum = min(sum, m_sum);
-                const int at = reach(s.run[kDraw], total[kDraw], draw_target(uniform, sum) - base[kDraw]);
-                if (lane == 0) {
-                    const uint64_t place = s.lists[kDraw][at];
-                    s.got_index = static_cast<uint32_t>(place) & (kSMaxVocab - 1);
-                    s.got_z = row.z(key_value(static_cast<uint32_t>(place >> kSIndexBits)));
-                    s.got_mass = s.run[kDraw][at] - (at ? s.run[kDraw][at - 1] : 0);
-                    write_token();
+#pragma unroll 1
+            for (int j = 0; j < kStages; ++j) {
+                const int first = s.bins.lo[j];
+                if (first > s.bins.hi[j]) continue;
+                stage = j;
+                if (tid == 0) {
+                    s.base_w = first > 0 ? s.sum_w[first - 1] : 0;
+                    s.base_c = first > 0 ? s.sum_c[first - 1] : 0;
                 }
+                next_target();
+                uint64_t lo, hi;
+                place_range<T>(s.bins.x_lo[j], fminf(s.bins.x_hi[j], row.top), lo, hi);
+                search_list(s, row, want, s.lists[j][tid], s.ns[j], lo, hi);
+                if (s.got_index == 0xFFFFFFFFu) break;
+                if (j < kDraw) sum = s.got_w;
             }
+            if (tid == 0) write_token();
         }
         cluster_wait_acquire();
         return;
@@ -814,7 +794,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             for (int b = tid; b < kSFine; b += kSThreads) s.cnt[b] = s.wl[b] = s.wh[b] = 0;
         if (tid == 0) s.n = 0;
         __syncthreads();
-        pass([&](const float(&x)[4], int first) {
+        pass(Loads<2>{}, [&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (!odd && !(x[k] >= cmd.x_lo && x[k] <= cmd.x_hi)) continue;
@@ -826,7 +806,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 if (cmd.op == kDivide) {
                     const uint32_t b = static_cast<uint32_t>((place - cmd.lo) >> cmd.shift);
                     if (by_k) atomicAdd(&s.cnt[b], 1u);
-                    add_weight(&s.wl[b], &s.wh[b], SRow::weight2(z));
+                    add_weight(&s.wl[b], &s.wh[b], SRow::weight2(expf(z)));
                     continue;
                 }
                 const uint32_t at = atomicAdd(&s.n, 1u);
@@ -882,7 +862,8 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             send(s, c, ctas);
             continue;
         }
-        search_list(s, row, want, list_entry(s.list, total, ctas, [&](uint32_t q) { return s.all_n[q]; }), total);
+        search_list(s, row, want, list_entry(s.list, total, ctas, [&](uint32_t q) { return s.all_n[q]; }), total, cmd.lo,
+                    cmd.hi);
         if (s.got_index == 0xFFFFFFFFu || stage == kDraw) {
             if (tid == 0) write_token();
             send(s, c, ctas);  // kDone
@@ -907,9 +888,14 @@ cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_
     constexpr int kHalfSm = 115712;
     const int64_t slots = 2 * static_cast<int64_t>(device_sm_count());
     auto chunk_of = [&](int32_t c) { return ((p.vocab + c - 1) / c + 7) / 8 * 8; };
-    // as many CTAs a row as one round holds
+    // As many CTAs a row as one round holds (64 rows x 32003: 4 CTAs 20.2 us, 2 25.7,
+    // 8 27.9), and parts of at most 80 K logits: large batches in several rounds,
+    // whose passes then overlap and find more in L2 (256 x 152000: 154 us with 1
+    // CTA a row, 135 with 2 or 4, 161 with 8; 256 x 32003: 41.8, 46.0, 56.1).
     int32_t c = 1;
-    while (c < kSMaxCluster && 2 * c * static_cast<int64_t>(n_rows) <= slots && chunk_of(c) > 1024) c *= 2;
+    while (c < kSMaxCluster &&
+           ((2 * c * static_cast<int64_t>(n_rows) <= slots && chunk_of(c) > 1024) || chunk_of(c) > 80 * 1024))
+        c *= 2;
     const bool resident = sample_smem_bytes(chunk_of(c)) <= static_cast<size_t>(kHalfSm);
     const auto kernel = bf16 ? (resident ? sample_kernel<__nv_bfloat16, true> : sample_kernel<__nv_bfloat16, false>)
                              : (resident ? sample_kernel<float, true> : sample_kernel<float, false>);
