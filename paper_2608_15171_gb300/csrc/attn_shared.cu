@@ -12,8 +12,8 @@
 // kernel (attn_prefill.cu): TMA producers, a Q K^T and a P V issuer, and a softmax
 // warpgroup for each Q tile whose threads own a query row each.
 // The own keys are read by one row only: they stream through rings of single
-// warps, (row, kv-head, up to 32 pages) at a time, products by mma.sync with the
-// q-heads as 8 columns, on the CTAs after those of the pieces.
+// warps, each an equal run of their pages, products by mma.sync with the q-heads
+// as 8 columns, on the CTAs after those of the pieces.
 // Every partial goes to the workspace in fp32 and a second launch joins them.
 #include <math.h>
 
@@ -79,8 +79,9 @@ constexpr uint32_t kOwnOffBar = kSharedWarps * kOwnStages * kOwnStageBytes;
 static_assert(kOwnOffBar + kSharedWarps * kOwnStages * 8 + 1024 <= kSmemBytes, "own rings");
 
 // One piece of a prefix (all 512 threads).
+template <class P>
 __device__ __forceinline__ void prefix_cta(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
-                                           const SharedParams &p, int piece) {
+                                           const P &p, int piece) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_s = smem_u32(smem_raw);
     const uint32_t sb = (raw_s + 1023u) & ~1023u;  // 1024-aligned for the 128-byte swizzle
@@ -403,43 +404,47 @@ __device__ __forceinline__ void prefix_cta(const CUtensorMap &tm_q, const CUtens
     }
 }
 
-// An item of own keys: up to 32 pages of one (row, kv-head).
-struct OwnItem {
-    int32_t row, kvh, pages, last_valid;  // last_valid: keys of the last page
-    int32_t id;                           // lane i: the block of page i
+// A place in the line of own pages: page `page` of (row, kv-head), one of `pages`.
+struct OwnAt {
+    int32_t row, kvh, page, pages;
 };
 
-__device__ __forceinline__ OwnItem own_item(const SharedParams &p, int32_t item, int lane) {
-    OwnItem it = {};
-    if (item >= p.n_items) return it;
-    int lo = 0, hi = p.n_rows - 1;  // the last row whose items begin at or before this one
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.rows[mid].item0 <= item) lo = mid; else hi = mid - 1;
-    }
-    const SharedRow row = p.rows[lo];
-    const int local = item - row.item0;
-    const int sp = local % row.n_items;
-    const int all = (row.own + kPage - 1) / kPage, pg0 = sp * p.item_pages;
-    it.row = lo;
-    it.kvh = local / row.n_items;
-    it.pages = min(p.item_pages, all - pg0);
-    it.last_valid = min(kPage, row.own - (pg0 + it.pages - 1) * kPage);
-    const int32_t *table = p.block_tables + static_cast<int64_t>(lo) * p.table_stride +
-                           p.groups[row.group].prefix / kPage + pg0;
-    if (lane < it.pages) {
-        it.id = __ldg(table + lane);
-        if (it.id < 0 || it.id >= p.num_blocks) {
-            report_error(p.err, PPAS_DEVERR_BAD_INDEX);
-            it.id = 0;
+// the first place at or after the one given that exists (rows without own keys are left out)
+template <class P>
+__device__ __forceinline__ void own_settle(const P &p, OwnAt &a) {
+    while (a.page >= a.pages) {
+        a.page = 0;
+        if (a.pages == 0 || ++a.kvh == p.n_kv_heads) {
+            a.kvh = 0;
+            if (++a.row >= p.n_rows) {
+                a.pages = 1;  // past the end (nobody reads there)
+                return;
+            }
+            a.pages = (p.rows[a.row].own + kPage - 1) / kPage;
         }
     }
-    return it;
 }
 
-// Warp `w` of the p.own_warps that work on own keys.
-__device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const SharedParams &p,
-                                         int w) {
+// place `at` of the line
+template <class P>
+__device__ __forceinline__ OwnAt own_place(const P &p, int32_t at) {
+    int lo = 0, hi = p.n_rows - 1;  // the last row that begins at or before it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.rows[mid].page0 <= at) lo = mid; else hi = mid - 1;
+    }
+    OwnAt a;
+    a.row = lo;
+    a.pages = (p.rows[lo].own + kPage - 1) / kPage;
+    const int32_t local = at - p.rows[lo].page0;
+    a.kvh = a.pages ? local / a.pages : 0;
+    a.page = local - a.kvh * a.pages;
+    return a;
+}
+
+// Warp `w` of those that work on own keys: pages [w, w + 1) * p.warp_pages of the line.
+template <class P>
+__device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const P &p, int w) {
     using namespace decode_detail;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_s = smem_u32(smem_raw);
@@ -455,22 +460,60 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
         prefetch_tmap(&tm_k);
         prefetch_tmap(&tm_v);
     }
+    const int32_t first = w * p.warp_pages;
+    const int32_t count = min(p.warp_pages, p.own_pages - first);
+    OwnAt at = {};
+    if (count > 0) at = own_place(p, first);
     __syncwarp();
     grid_dep_wait();
+    if (count <= 0) return;
 
     const int hr = lane >> 2, c = lane & 3, g = p.group;
     const int mi = lane >> 3, ri = lane & 7;
     const float sl2 = p.scale_log2;
-    int item = w;
-    OwnItem cur = own_item(p, item, lane), nxt = own_item(p, item + p.own_warps, lane);
-    int issued = 0, consumed = 0;  // pages of this warp
-    int ahead = 0;                 // pages issued of cur, then of nxt
+    // Issued ahead of use: pages in runs of up to 32 of one (row, kv-head), lane i
+    // holding the block of a run's page i; the next run's are loaded while this one's
+    // pages are issued.
+    int issued = 0, consumed = 0;
+    OwnAt ahead = at;  // the run being issued
+    int32_t run_n = 0, run_at = 0, id = 0, next_n = 0, next_id = 0;
+    OwnAt next = at;
+    auto load_run = [&](OwnAt &a, int32_t left, int32_t &n, int32_t &ids) {
+        n = min(32, min(a.pages - a.page, left));
+        if (lane < n) {
+            ids = __ldg(p.block_tables + static_cast<int64_t>(a.row) * p.table_stride + p.rows[a.row].table + a.page + lane);
+            if (ids < 0 || ids >= p.num_blocks) {
+                report_error(p.err, PPAS_DEVERR_BAD_INDEX);
+                ids = 0;
+            }
+        }
+    };
+    auto after = [&](const OwnAt &a, int32_t n) {
+        OwnAt b = a;
+        b.page += n;
+        own_settle(p, b);
+        return b;
+    };
+    load_run(ahead, count, run_n, id);
+    if (count > run_n) {
+        next = after(ahead, run_n);
+        load_run(next, count - run_n, next_n, next_id);
+    }
     auto top_up = [&]() {
-        while (issued - consumed < kOwnStages && ahead < cur.pages + nxt.pages) {
-            const bool second = ahead >= cur.pages;
-            const int blk = __shfl_sync(0xffffffffu, second ? nxt.id : cur.id, second ? ahead - cur.pages : ahead);
-            const int kvh = second ? nxt.kvh : cur.kvh;
-            const int r = __shfl_sync(0xffffffffu, (blk * p.n_kv_heads + kvh) * kPage, 0);
+        while (issued - consumed < kOwnStages && issued < count) {
+            if (run_at == run_n) {
+                ahead = next;
+                run_n = next_n;
+                id = next_id;
+                run_at = 0;
+                const int32_t left = count - issued - run_n;
+                if (left > 0) {
+                    next = after(ahead, run_n);
+                    load_run(next, left, next_n, next_id);
+                }
+            }
+            const int blk = __shfl_sync(0xffffffffu, id, run_at);
+            const int r = __shfl_sync(0xffffffffu, (blk * p.n_kv_heads + ahead.kvh) * kPage, 0);
             const int st = issued % kOwnStages;
             if (elect_one()) {
                 const uint32_t dst = ring + st * kOwnStageBytes, b = bar(st);
@@ -482,15 +525,15 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
             }
             __syncwarp();
             ++issued;
-            ++ahead;
+            ++run_at;
         }
     };
     // Q as the B operand: n = the group's heads, k = head dims
     uint32_t qb[8][2], qn[8][2];
-    auto load_q = [&](const OwnItem &it, uint32_t(&q)[8][2]) {
-        const bool valid = hr < g && it.pages > 0;
+    auto load_q = [&](const OwnAt &a, uint32_t(&q)[8][2]) {
+        const bool valid = hr < g && a.row < p.n_rows;
         const uint32_t *qrow = reinterpret_cast<const uint32_t *>(
-            p.q + (static_cast<int64_t>(it.row) * p.n_q_heads + it.kvh * g + (valid ? hr : 0)) * kHeadDim);
+            p.q + (static_cast<int64_t>(valid ? a.row : 0) * p.n_q_heads + a.kvh * g + (valid ? hr : 0)) * kHeadDim);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {
             q[kk][0] = valid ? __ldg(qrow + kk * 8 + c) : 0u;
@@ -498,21 +541,25 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
         }
     };
     top_up();
-    load_q(cur, qb);
+    load_q(at, qb);
     bool ok = true;
-    while (cur.pages > 0) {
-        load_q(nxt, qn);
+    while (consumed < count) {
+        // the pages of (row, kv-head) at hand, and the pair after it
+        const int32_t here = min(at.pages - at.page, count - consumed);
+        const OwnAt then = after(at, here);
+        load_q(then, qn);
+        const int last = (p.rows[at.row].own + kPage - 1) % kPage + 1;  // keys of the pair's last page
         // this lane: tokens hr, hr + 8 of a page's S, head dims 16 n + hr (+ 8) of
         // O, heads 2c, 2c + 1 of both
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float o[8][4];
 #pragma unroll
         for (int n = 0; n < 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
-        for (int i = 0; i < cur.pages; ++i) {
+        for (int i = 0; i < here; ++i) {
             const int st = consumed % kOwnStages;
             ok = mbar_wait_warp(bar(st), (consumed / kOwnStages) & 1, p.err);
             if (!ok) break;
-            const int valid = i + 1 < cur.pages ? kPage : cur.last_valid;
+            const int valid = at.page + i + 1 < at.pages ? kPage : last;
             const uint32_t kb = ring + st * kOwnStageBytes, vb = kb + 2 * kBox;
             if (valid < kPage) {
                 // tokens past the context: zero their V rows so that 0 * V stays 0
@@ -573,14 +620,15 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
             top_up();
         }
         if (!ok) break;
-        // ---- the item's partial
+        // ---- the pair's partial
 #pragma unroll
         for (int o_ = 4; o_ <= 16; o_ <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, o_);
             l1 += __shfl_xor_sync(0xffffffffu, l1, o_);
         }
-        float *const po = p.own_o + static_cast<int64_t>(item) * g * kHeadDim;
-        float2 *const pml = reinterpret_cast<float2 *>(p.own_ml) + static_cast<int64_t>(item) * g;
+        const int64_t slot = static_cast<int64_t>(at.row) * p.n_kv_heads + at.kvh + w;
+        float *const po = p.own_o + slot * g * kHeadDim;
+        float2 *const pml = reinterpret_cast<float2 *>(p.own_ml) + slot * g;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int hh = 2 * c + x;
@@ -593,16 +641,12 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
                 __stcg(dst + 16 * n + 8, o[n][2 + x]);
             }
         }
-        ahead -= cur.pages;
-        item += p.own_warps;
-        cur = nxt;
-        nxt = own_item(p, item + p.own_warps, lane);
+        at = then;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {
             qb[kk][0] = qn[kk][0];
             qb[kk][1] = qn[kk][1];
         }
-        top_up();
     }
     // copies still in flight (only after a wait ran out)
     if (lane == 0)
@@ -611,9 +655,10 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
 
 }  // namespace
 
+template <class P>
 __global__ void __launch_bounds__(kThreads, 1)
     shared_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                       const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ SharedParams p) {
+                       const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ P p) {
     if (static_cast<int>(blockIdx.x) < p.n_pieces) {
         prefix_cta(tm_q, tm_k, tm_v, p, blockIdx.x);
         return;
@@ -631,7 +676,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 // row) and 8 columns of a tile, so a load of a prefix partial is 512 contiguous
 // bytes; `ways` warps of a CTA share the partials of their rows, in turn, and add
 // up in shared memory.
-__global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant__ SharedMergeParams p) {
+template <class P>
+__global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant__ P p) {
     __shared__ float s_ml[8][2][32];
     __shared__ float4 s_acc[8][2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -650,9 +696,13 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
     if (!__any_sync(0xffffffffu, valid) && p.ways == 1) return;
     const int row = grp.row0 + (valid ? q / p.group : 0), h = q % p.group;
     const SharedRow sr = p.rows[row];
-    const int n = valid ? u.n_pieces + sr.n_items : 0;
+    // the pair's own pages, the first and the last warp that had some of them
+    const int pages = (sr.own + kPage - 1) / kPage;
+    const int page0 = sr.page0 + u.kvh * pages;
+    const int w0 = page0 / p.warp_pages, n_own = pages ? (page0 + pages - 1) / p.warp_pages - w0 + 1 : 0;
+    const int n = valid ? u.n_pieces + n_own : 0;
     const int n_max = __reduce_max_sync(0xffffffffu, n);
-    const int64_t item0 = sr.item0 + static_cast<int64_t>(u.kvh) * sr.n_items - u.n_pieces;
+    const int64_t slot0 = static_cast<int64_t>(row) * p.n_kv_heads + u.kvh + w0 - u.n_pieces;
     grid_dep_wait();  // the partials come from the launch before this one
 
     float M = -INFINITY, L = 0.f;
@@ -674,7 +724,7 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
                 o[b][0] = __ldcg(src);
                 o[b][1] = __ldcg(src + kTileQ);
             } else {
-                const int64_t at = (item0 + k) * p.group + h;
+                const int64_t at = (slot0 + k) * p.group + h;
                 ml[b] = __ldcg(reinterpret_cast<const float2 *>(p.own_ml) + at);
                 const float4 *src = reinterpret_cast<const float4 *>(p.own_o) + at * (kHeadDim / 4) + 2 * col;
                 o[b][0] = __ldcg(src);
@@ -730,21 +780,29 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
                    pack_bf16x2(acc[1].x * inv, acc[1].y * inv), pack_bf16x2(acc[1].z * inv, acc[1].w * inv));
 }
 
-static std::atomic<uint64_t> g_shared_smem_set{0};
-
-cudaError_t launch_shared(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
-                          const SharedParams &p, int32_t own_ctas, cudaStream_t st) {
-    const cudaError_t e = ensure_smem_limit(shared_attn_kernel, static_cast<int>(kSmemBytes), g_shared_smem_set);
+template <class P>
+cudaError_t launch_shared(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const P &p,
+                          int32_t own_ctas, cudaStream_t st) {
+    static std::atomic<uint64_t> smem_set{0};
+    const cudaError_t e = ensure_smem_limit(shared_attn_kernel<P>, static_cast<int>(kSmemBytes), smem_set);
     if (e != cudaSuccess) return e;
     if (p.n_pieces + own_ctas <= 0) return cudaSuccess;
     PdlLaunch l(dim3(p.n_pieces + own_ctas), dim3(kThreads), kSmemBytes, st);
-    return cudaLaunchKernelEx(&l.cfg, shared_attn_kernel, tm_q, tm_k, tm_v, p);
+    return cudaLaunchKernelEx(&l.cfg, shared_attn_kernel<P>, tm_q, tm_k, tm_v, p);
 }
 
-cudaError_t launch_shared_merge(const SharedMergeParams &p, cudaStream_t st) {
+template <class P>
+cudaError_t launch_shared_merge(const P &p, cudaStream_t st) {
     if (p.n_units <= 0) return cudaSuccess;
     PdlLaunch l(dim3(p.n_units * p.tiles * 4 * 2 * p.ways), dim3(256), 0, st);
-    return cudaLaunchKernelEx(&l.cfg, shared_merge_kernel, p);
+    return cudaLaunchKernelEx(&l.cfg, shared_merge_kernel<P>, p);
 }
+
+template cudaError_t launch_shared(const CUtensorMap &, const CUtensorMap &, const CUtensorMap &, const SharedParams &,
+                                   int32_t, cudaStream_t);
+template cudaError_t launch_shared(const CUtensorMap &, const CUtensorMap &, const CUtensorMap &,
+                                   const SharedParamsSmall &, int32_t, cudaStream_t);
+template cudaError_t launch_shared_merge(const SharedMergeParams &, cudaStream_t);
+template cudaError_t launch_shared_merge(const SharedMergeParamsSmall &, cudaStream_t);
 
 }  // namespace ppas

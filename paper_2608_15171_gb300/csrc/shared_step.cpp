@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <iterator>
 #include <stdexcept>
 
 #include "attn_shared.cuh"
@@ -88,25 +89,13 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
         if (own_pages > 0 && tiles > 0)
             own_sms = std::max(1, std::min(num_sms - 1, static_cast<int32_t>(
                                                             num_sms * own_time / (own_time + tiles * kTileCost) + 0.5)));
+        // runs of at least 2 pages a warp: below that its fixed latency is all there is
+        if (own_pages > (int64_t{1} << 30)) throw std::length_error("own keys");
         const int64_t warps = std::max(1, own_sms) * static_cast<int64_t>(kSharedWarps);
-        l.item_pages = static_cast<int32_t>(
-            std::max<int64_t>(2, std::min<int64_t>(kSharedMaxItemPages, (own_pages + warps - 1) / warps)));
-        int64_t items = 0;
-        for (;; ++l.item_pages) {
-            items = 0;
-            int64_t longest = 0;
-            for (size_t i = i0; i < i1; ++i)
-                for (int32_t r = parts[i].row0; r < parts[i].row0 + parts[i].n_rows; ++r) {
-                    const int64_t pages = (ctx_lens[r] - parts[i].prefix + kPage - 1) / kPage;
-                    const int64_t n = (pages + l.item_pages - 1) / l.item_pages;
-                    longest = std::max(longest, n);
-                    items += n * n_kv_heads;
-                }
-            if (longest <= 0xFFFF || l.item_pages == kSharedMaxItemPages) break;
-        }
-        if (items > (1 << 27)) throw std::length_error("items");
-        l.own_ctas = static_cast<int32_t>(
-            std::min<int64_t>(own_sms, (items + kSharedWarps - 1) / kSharedWarps));
+        l.own_pages = static_cast<int32_t>(own_pages);
+        l.warp_pages = static_cast<int32_t>(std::max<int64_t>(2, (own_pages + warps - 1) / warps));
+        l.own_ctas = static_cast<int32_t>((own_pages + static_cast<int64_t>(l.warp_pages) * kSharedWarps - 1) /
+                                          (static_cast<int64_t>(l.warp_pages) * kSharedWarps));
         // ---- the prefixes' pieces: one length of piece for all, the shortest
         // that the SMs hold in one round
         const int32_t pre_sms = std::max(1, num_sms - own_sms);
@@ -124,17 +113,16 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
             if (pieces_at(mid) <= pre_sms) hi = mid;
             else len = mid + 1;
         }
-        int32_t first_item = 0, most_items = 0, most_pieces = 0;
+        int32_t page0 = 0, most_own = 0, most_pieces = 0;
         for (size_t i = i0; i < i1; ++i) {
             const Part &pt = parts[i];
             const uint16_t gi = static_cast<uint16_t>(i - i0);
             l.groups.push_back({pt.row0 - l.row0, pt.n_rows, pt.prefix});
             for (int32_t r = pt.row0; r < pt.row0 + pt.n_rows; ++r) {
-                const int32_t own = ctx_lens[r] - pt.prefix;
-                const int32_t n = ((own + kPage - 1) / kPage + l.item_pages - 1) / l.item_pages;
-                l.rows.push_back({own, first_item, static_cast<uint16_t>(n), gi});
-                first_item += n * n_kv_heads;
-                most_items = std::max(most_items, n);
+                const int32_t own = ctx_lens[r] - pt.prefix, pages = (own + kPage - 1) / kPage;
+                l.rows.push_back({own, page0, pt.prefix / kPage});
+                page0 += pages * n_kv_heads;
+                most_own = std::max(most_own, pages / l.warp_pages + 2);
             }
             const int32_t kt = (pt.prefix + kPrefillKT - 1) / kPrefillKT, np = (kt + len - 1) / len;
             for (int32_t mu = 0; mu < (pt.n_rows * g + per - 1) / per; ++mu)
@@ -149,13 +137,13 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
                 }
         }
         l.n_groups = static_cast<int32_t>(i1 - i0);
-        l.n_items = first_item;
-        const int32_t partials = most_pieces + most_items;
+        const int32_t partials = most_pieces + most_own;
         l.ways = partials > 32 ? 8 : partials > 16 ? 4 : partials > 8 ? 2 : 1;
+        const size_t slots = own_pages == 0 ? 0 : static_cast<size_t>(l.n_rows) * n_kv_heads + l.own_ctas * kSharedWarps;
         l.pre_o_bytes = align256(l.pieces.size() * l.tiles * kTileQ * kHeadDim * sizeof(float));
         l.pre_ml_bytes = align256(l.pieces.size() * l.tiles * kTileQ * 2 * sizeof(float));
-        l.own_o_bytes = align256(static_cast<size_t>(l.n_items) * g * kHeadDim * sizeof(float));
-        l.own_ml_bytes = align256(static_cast<size_t>(l.n_items) * g * 2 * sizeof(float));
+        l.own_o_bytes = align256(slots * g * kHeadDim * sizeof(float));
+        l.own_ml_bytes = align256(slots * g * 2 * sizeof(float));
         plan.bytes = std::max(plan.bytes, l.total_bytes());
         plan.launches.push_back(std::move(l));
         i0 = i1;
@@ -234,49 +222,57 @@ ppas_status run(const void *q, const void *k_cache, const void *v_cache, int32_t
     const int32_t g = hq / hk;
     if (!encode_kv_map(&tm_k, k_cache, num_blocks, hk) || !encode_kv_map(&tm_v, v_cache, num_blocks, hk))
         return PPAS_ERR_CUDA;
-    static thread_local SharedParams p;  // ~24 KB each: kept off the stack
-    static thread_local SharedMergeParams m;
+    static thread_local SharedParams big;  // ~24 KB each: kept off the stack
+    static thread_local SharedMergeParams big_merge;
+    static thread_local SharedParamsSmall small;
+    static thread_local SharedMergeParamsSmall small_merge;
     for (const SharedLaunch &l : plan.launches) {
         const __nv_bfloat16 *const q0 = static_cast<const __nv_bfloat16 *>(q) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
         if (!encode_q_group_map(&tm_q, q0, std::min(l.n_rows, n_rows - l.row0), hq, g)) return PPAS_ERR_CUDA;
         uint8_t *const ws = static_cast<uint8_t *>(workspace);
-        p.q = q0;
-        p.block_tables = d_block_tables + static_cast<int64_t>(l.row0) * max_blocks_per_seq;
-        p.table_stride = max_blocks_per_seq;
-        p.num_blocks = num_blocks;
-        p.n_q_heads = hq;
-        p.n_kv_heads = hk;
-        p.group = g;
-        p.tiles = l.tiles;
-        p.n_rows = l.n_rows;
-        p.n_pieces = static_cast<int32_t>(l.pieces.size());
-        p.n_items = l.n_items;
-        p.item_pages = l.item_pages;
-        p.own_warps = l.own_ctas * kSharedWarps;
-        p.scale_log2 = scale * 1.4426950408889634f;
-        p.err = err;
-        p.pre_o = reinterpret_cast<float *>(ws);
-        p.pre_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes);
-        p.own_o = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes);
-        p.own_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes + l.own_o_bytes);
-        std::copy(l.groups.begin(), l.groups.end(), p.groups);
-        std::copy(l.rows.begin(), l.rows.end(), p.rows);
-        std::copy(l.pieces.begin(), l.pieces.end(), p.pieces);
-        if (launch_shared(tm_q, tm_k, tm_v, p, l.own_ctas, st) != cudaSuccess) return PPAS_ERR_CUDA;
-        m.out = static_cast<__nv_bfloat16 *>(out) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
-        m.pre_o = p.pre_o;
-        m.pre_ml = p.pre_ml;
-        m.own_o = p.own_o;
-        m.own_ml = p.own_ml;
-        m.n_q_heads = hq;
-        m.group = g;
-        m.tiles = l.tiles;
-        m.n_units = static_cast<int32_t>(l.units.size());
-        m.ways = l.ways;
-        std::copy(l.groups.begin(), l.groups.end(), m.groups);
-        std::copy(l.rows.begin(), l.rows.end(), m.rows);
-        std::copy(l.units.begin(), l.units.end(), m.units);
-        if (launch_shared_merge(m, st) != cudaSuccess) return PPAS_ERR_CUDA;
+        auto launch = [&](auto &p, auto &m) {
+            p.q = q0;
+            p.block_tables = d_block_tables + static_cast<int64_t>(l.row0) * max_blocks_per_seq;
+            p.table_stride = max_blocks_per_seq;
+            p.num_blocks = num_blocks;
+            p.n_q_heads = hq;
+            p.n_kv_heads = hk;
+            p.group = g;
+            p.tiles = l.tiles;
+            p.n_rows = l.n_rows;
+            p.n_pieces = static_cast<int32_t>(l.pieces.size());
+            p.own_pages = l.own_pages;
+            p.warp_pages = l.warp_pages;
+            p.scale_log2 = scale * 1.4426950408889634f;
+            p.err = err;
+            p.pre_o = reinterpret_cast<float *>(ws);
+            p.pre_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes);
+            p.own_o = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes);
+            p.own_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes + l.own_o_bytes);
+            std::copy(l.groups.begin(), l.groups.end(), p.groups);
+            std::copy(l.rows.begin(), l.rows.end(), p.rows);
+            std::copy(l.pieces.begin(), l.pieces.end(), p.pieces);
+            if (launch_shared(tm_q, tm_k, tm_v, p, l.own_ctas, st) != cudaSuccess) return false;
+            m.out = static_cast<__nv_bfloat16 *>(out) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
+            m.pre_o = p.pre_o;
+            m.pre_ml = p.pre_ml;
+            m.own_o = p.own_o;
+            m.own_ml = p.own_ml;
+            m.n_q_heads = hq;
+            m.n_kv_heads = hk;
+            m.group = g;
+            m.tiles = l.tiles;
+            m.n_units = static_cast<int32_t>(l.units.size());
+            m.warp_pages = l.warp_pages;
+            m.ways = l.ways;
+            std::copy(l.groups.begin(), l.groups.end(), m.groups);
+            std::copy(l.rows.begin(), l.rows.end(), m.rows);
+            std::copy(l.units.begin(), l.units.end(), m.units);
+            return launch_shared_merge(m, st) == cudaSuccess;
+        };
+        const bool fits = l.rows.size() <= std::size(small.rows) && l.groups.size() <= std::size(small.groups) &&
+                          l.pieces.size() <= std::size(small.pieces) && l.units.size() <= std::size(small_merge.units);
+        if (!(fits ? launch(small, small_merge) : launch(big, big_merge))) return PPAS_ERR_CUDA;
     }
     return PPAS_OK;
 }

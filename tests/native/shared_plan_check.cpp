@@ -1,7 +1,7 @@
 // Checks the plan of the attention over shared prefixes against what its
 // kernels index from it.  A line of input: sms hq hk n_groups, then rows and
 // prefix of each group, then the contexts; a line of output each: "ok launches
-// pieces items own_ctas tiles ways longest_piece item_pages bytes" (of the first launch) or what is wrong.
+// pieces own_pages own_ctas tiles ways longest_piece warp_pages bytes" (of the first launch) or what is wrong.
 #include <cstdio>
 #include <iostream>
 #include <set>
@@ -27,29 +27,40 @@ static std::string check(int sms, int hq, int hk, const std::vector<int> &rows, 
         if (l.units.size() > kSharedMaxUnits) return "units table";
         if (l.pieces.size() > kSharedMaxPieces) return "pieces table";
         if (l.tiles != 1 && l.tiles != 2) return "tiles";
-        if (l.item_pages < 1 || l.item_pages > kSharedMaxItemPages) return "item pages";
+        if (l.warp_pages < 1) return "pages of a warp";
         if (l.ways != 1 && l.ways != 2 && l.ways != 4 && l.ways != 8) return "ways";
-        int r = 0, item = 0;
+        int r = 0, page = 0;
         for (size_t gi = 0; gi < l.groups.size(); ++gi) {
             const SharedGroup &gr = l.groups[gi];
             if (gr.row0 != r || gr.n_rows < 1 || gr.prefix % 16) return "group";
             for (int k = 0; k < gr.n_rows; ++k, ++r) {
                 const SharedRow &sr = l.rows[r];
-                if (sr.group != gi) return "group of a row";
-                const int want = gr.prefix;
-                if (want != prefix_of[row + r] && !(gr.n_rows == 1 && want == 0)) return "prefix of a row";
-                if (sr.own != ctx[row + r] - want || sr.own < 0) return "own keys";
-                const int pages = (sr.own + 15) / 16;
-                if (sr.item0 != item) return "first item";
-                if (static_cast<int64_t>(sr.n_items) * l.item_pages < pages ||
-                    static_cast<int64_t>(sr.n_items - 1) * l.item_pages >= pages) {
-                    if (!(sr.n_items == 0 && pages == 0)) return "items cover the pages, none empty";
-                }
-                item += sr.n_items * hk;
+                if (gr.prefix != prefix_of[row + r] && !(gr.n_rows == 1 && gr.prefix == 0)) return "prefix of a row";
+                if (sr.own != ctx[row + r] - gr.prefix || sr.own < 0) return "own keys";
+                if (sr.table != gr.prefix / 16 || sr.page0 != page) return "first page";
+                page += (sr.own + 15) / 16 * hk;
             }
         }
-        if (r != l.n_rows || item != l.n_items) return "items";
-        if ((l.own_ctas > 0) != (l.n_items > 0)) return "CTAs of own keys";
+        if (r != l.n_rows || page != l.own_pages) return "pages";
+        // every warp's slots, as the kernel numbers them: different, and inside the workspace
+        const int64_t warps = static_cast<int64_t>(l.own_ctas) * kSharedWarps;
+        if (warps * l.warp_pages < l.own_pages) return "warps cover the pages";
+        if (l.own_ctas > 0 && static_cast<int64_t>(l.own_ctas - 1) * kSharedWarps * l.warp_pages >= l.own_pages) return "a CTA without pages";
+        int64_t last_slot = -1;
+        for (int q = 0; q < l.n_rows; ++q) {
+            const int pages = (l.rows[q].own + 15) / 16;
+            for (int h = 0; h < hk && pages; ++h) {
+                const int64_t p0 = l.rows[q].page0 + static_cast<int64_t>(h) * pages;
+                const int64_t w0 = p0 / l.warp_pages, w1 = (p0 + pages - 1) / l.warp_pages;
+                for (int64_t w = w0; w <= w1; ++w) {
+                    const int64_t slot = static_cast<int64_t>(q) * hk + h + w;
+                    if (slot <= last_slot || w >= warps) return "slots";
+                    last_slot = slot;
+                }
+            }
+        }
+        if (l.own_o_bytes < static_cast<size_t>(last_slot + 1) * g * 512 || l.own_ml_bytes < static_cast<size_t>(last_slot + 1) * g * 8)
+            return "workspace of own keys";
         std::set<std::vector<int>> seen;
         size_t next = 0;
         for (const SharedUnit &u : l.units) {
@@ -71,8 +82,7 @@ static std::string check(int sms, int hq, int hk, const std::vector<int> &rows, 
         size_t want = 0;
         for (const SharedGroup &gr : l.groups) want += hk * ((gr.n_rows * g + 128 * l.tiles - 1) / (128 * l.tiles));
         if (want != l.units.size()) return "units";
-        if (l.pre_o_bytes < l.pieces.size() * l.tiles * 128 * 128 * 4 || l.pre_ml_bytes < l.pieces.size() * l.tiles * 1024 ||
-            l.own_o_bytes < static_cast<size_t>(l.n_items) * g * 512 || l.own_ml_bytes < static_cast<size_t>(l.n_items) * g * 8)
+        if (l.pre_o_bytes < l.pieces.size() * l.tiles * 128 * 128 * 4 || l.pre_ml_bytes < l.pieces.size() * l.tiles * 1024)
             return "workspace";
         if (l.pre_o_bytes % 256 || l.pre_ml_bytes % 256 || l.own_o_bytes % 256 || l.own_ml_bytes % 256) return "alignment";
         bytes = std::max(bytes, l.total_bytes());
@@ -83,8 +93,8 @@ static std::string check(int sms, int hq, int hk, const std::vector<int> &rows, 
     int longest = 0;
     for (const SharedPiece &pc : l.pieces) longest = std::max(longest, pc.kt1 - pc.kt0);
     std::ostringstream s;
-    s << "ok " << plan.launches.size() << " " << l.pieces.size() << " " << l.n_items << " " << l.own_ctas << " " << l.tiles
-      << " " << l.ways << " " << longest << " " << l.item_pages << " " << plan.bytes;
+    s << "ok " << plan.launches.size() << " " << l.pieces.size() << " " << l.own_pages << " " << l.own_ctas << " " << l.tiles
+      << " " << l.ways << " " << longest << " " << l.warp_pages << " " << plan.bytes;
     return s.str();
 }
 
