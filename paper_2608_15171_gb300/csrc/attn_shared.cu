@@ -75,8 +75,16 @@ constexpr uint32_t kIdescPV = idesc_bf16_f32(128, 128, false, true);   // B = V 
 // rings of own keys: one a warp
 constexpr int kOwnStages = 3;
 constexpr uint32_t kOwnStageBytes = 4 * kBox;  // K lo, K hi, V lo, V hi
-constexpr uint32_t kOwnOffBar = kSharedWarps * kOwnStages * kOwnStageBytes;
+constexpr uint32_t kOwnQBytes = 8 * kRowBytes;  // q-heads of a kv-head; a warp has two of them, pair by pair
+constexpr uint32_t kOwnOffQ = kSharedWarps * kOwnStages * kOwnStageBytes;
+constexpr uint32_t kOwnOffBar = kOwnOffQ + kSharedWarps * 2 * kOwnQBytes;
 static_assert(kOwnOffBar + kSharedWarps * kOwnStages * 8 + 1024 <= kSmemBytes, "own rings");
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 
 // One piece of a prefix (all 512 threads).
 template <class P>
@@ -424,6 +432,14 @@ __device__ __forceinline__ void own_settle(const P &p, OwnAt &a) {
         }
     }
 }
+// n places on, within the pair or just past its end
+template <class P>
+__device__ __forceinline__ OwnAt own_after(const P &p, const OwnAt &a, int32_t n) {
+    OwnAt b = a;
+    b.page += n;
+    own_settle(p, b);
+    return b;
+}
 
 // place `at` of the line
 template <class P>
@@ -442,6 +458,37 @@ __device__ __forceinline__ OwnAt own_place(const P &p, int32_t at) {
     return a;
 }
 
+// Block ids of 32 own pages of a row, a lane each.  A row of up to 32 pages has
+// one such window for all of its kv-heads.
+struct OwnIds {
+    int32_t row, page0, id;
+};
+template <class P>
+__device__ __forceinline__ OwnIds own_ids(const P &p, const OwnAt &a, int lane) {
+    OwnIds w = {a.row, a.page & ~31, 0};
+    if (a.row < p.n_rows && w.page0 + lane < a.pages) {
+        w.id = __ldg(p.block_tables + static_cast<int64_t>(a.row) * p.table_stride + p.rows[a.row].table + w.page0 + lane);
+        if (w.id < 0 || w.id >= p.num_blocks) {
+            report_error(p.err, PPAS_DEVERR_BAD_INDEX);
+            w.id = 0;
+        }
+    }
+    return w;
+}
+// the first place after a's window
+template <class P>
+__device__ __forceinline__ OwnAt own_past_window(const P &p, const OwnAt &a) {
+    OwnAt b = a;
+    if (a.pages <= 32) {
+        b.kvh = p.n_kv_heads - 1;
+        b.page = a.pages;
+    } else {
+        b.page = (a.page & ~31) + 32;
+    }
+    own_settle(p, b);
+    return b;
+}
+
 // Warp `w` of those that work on own keys: pages [w, w + 1) * p.warp_pages of the line.
 template <class P>
 __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const P &p, int w) {
@@ -453,6 +500,7 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
     const int lane = threadIdx.x & 31;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const uint32_t ring = sb + warp * kOwnStages * kOwnStageBytes;
+    const uint32_t q_slots = kOwnOffQ + warp * 2 * kOwnQBytes;  // from sb
     auto bar = [&](int st) { return sb + kOwnOffBar + (warp * kOwnStages + st) * 8u; };
     if (lane == 0) {
         for (int st = 0; st < kOwnStages; ++st) mbar_init(bar(st), 1);
@@ -461,93 +509,53 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
         prefetch_tmap(&tm_v);
     }
     const int32_t first = w * p.warp_pages;
-    const int32_t count = min(p.warp_pages, p.own_pages - first);
-    OwnAt at = {};
+    const int32_t count = max(0, min(p.warp_pages, p.own_pages - first));
+    OwnAt at = {p.n_rows, 0, 0, 1};  // past the end: no ids to load
     if (count > 0) at = own_place(p, first);
     __syncwarp();
     grid_dep_wait();
-    if (count <= 0) return;
 
     const int hr = lane >> 2, c = lane & 3, g = p.group;
     const int mi = lane >> 3, ri = lane & 7;
     const float sl2 = p.scale_log2;
-    // Issued ahead of use: pages in runs of up to 32 of one (row, kv-head), lane i
-    // holding the block of a run's page i; the next run's are loaded while this one's
-    // pages are issued.
-    int issued = 0, consumed = 0;
-    OwnAt ahead = at;  // the run being issued
-    int32_t run_n = 0, run_at = 0, id = 0, next_n = 0, next_id = 0;
-    OwnAt next = at;
-    auto load_run = [&](OwnAt &a, int32_t left, int32_t &n, int32_t &ids) {
-        n = min(32, min(a.pages - a.page, left));
-        if (lane < n) {
-            ids = __ldg(p.block_tables + static_cast<int64_t>(a.row) * p.table_stride + p.rows[a.row].table + a.page + lane);
-            if (ids < 0 || ids >= p.num_blocks) {
-                report_error(p.err, PPAS_DEVERR_BAD_INDEX);
-                ids = 0;
-            }
-        }
-    };
-    auto after = [&](const OwnAt &a, int32_t n) {
-        OwnAt b = a;
-        b.page += n;
-        own_settle(p, b);
-        return b;
-    };
-    load_run(ahead, count, run_n, id);
-    if (count > run_n) {
-        next = after(ahead, run_n);
-        load_run(next, count - run_n, next_n, next_id);
-    }
+    // pages are issued up to kOwnStages ahead of use, their ids loaded a window
+    // ahead; a pair's queries come with its first page, into one of two slots
+    int issued = 0, consumed = 0, pairs = 0, pairs_done = 0;
+    OwnAt ahead = at;
+    OwnIds ids = own_ids(p, at, lane), next_ids = own_ids(p, own_past_window(p, at), lane);
     auto top_up = [&]() {
         while (issued - consumed < kOwnStages && issued < count) {
-            if (run_at == run_n) {
-                ahead = next;
-                run_n = next_n;
-                id = next_id;
-                run_at = 0;
-                const int32_t left = count - issued - run_n;
-                if (left > 0) {
-                    next = after(ahead, run_n);
-                    load_run(next, left, next_n, next_id);
-                }
+            const bool opens = issued == 0 || ahead.page == 0;
+            if (opens && pairs - pairs_done == 2) break;
+            if (ahead.row != ids.row || (ahead.page & ~31) != ids.page0) {
+                ids = next_ids;
+                next_ids = own_ids(p, own_past_window(p, ahead), lane);
             }
-            const int blk = __shfl_sync(0xffffffffu, id, run_at);
+            const int blk = __shfl_sync(0xffffffffu, ids.id, ahead.page & 31);
             const int r = __shfl_sync(0xffffffffu, (blk * p.n_kv_heads + ahead.kvh) * kPage, 0);
             const int st = issued % kOwnStages;
             if (elect_one()) {
                 const uint32_t dst = ring + st * kOwnStageBytes, b = bar(st);
-                mbar_expect_tx(b, kOwnStageBytes);
+                mbar_expect_tx(b, kOwnStageBytes + (opens ? g * kRowBytes : 0));
                 tma_load_2d(dst, &tm_k, 0, r, b);
                 tma_load_2d(dst + kBox, &tm_k, 64, r, b);
                 tma_load_2d(dst + 2 * kBox, &tm_v, 0, r, b);
                 tma_load_2d(dst + 3 * kBox, &tm_v, 64, r, b);
+                if (opens)
+                    bulk_load(sb + q_slots + (pairs & 1) * kOwnQBytes,
+                              p.q + (static_cast<int64_t>(ahead.row) * p.n_q_heads + ahead.kvh * g) * kHeadDim,
+                              g * kRowBytes, b);
             }
             __syncwarp();
             ++issued;
-            ++run_at;
+            pairs += opens;
+            ahead = own_after(p, ahead, 1);
         }
     };
-    // Q as the B operand: n = the group's heads, k = head dims
-    uint32_t qb[8][2], qn[8][2];
-    auto load_q = [&](const OwnAt &a, uint32_t(&q)[8][2]) {
-        const bool valid = hr < g && a.row < p.n_rows;
-        const uint32_t *qrow = reinterpret_cast<const uint32_t *>(
-            p.q + (static_cast<int64_t>(valid ? a.row : 0) * p.n_q_heads + a.kvh * g + (valid ? hr : 0)) * kHeadDim);
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-            q[kk][0] = valid ? __ldg(qrow + kk * 8 + c) : 0u;
-            q[kk][1] = valid ? __ldg(qrow + kk * 8 + 4 + c) : 0u;
-        }
-    };
-    top_up();
-    load_q(at, qb);
+    if (count > 0) top_up();
     bool ok = true;
     while (consumed < count) {
-        // the pages of (row, kv-head) at hand, and the pair after it
-        const int32_t here = min(at.pages - at.page, count - consumed);
-        const OwnAt then = after(at, here);
-        load_q(then, qn);
+        const int here = min(at.pages - at.page, count - consumed);  // pages of the (row, kv-head) at hand
         const int last = (p.rows[at.row].own + kPage - 1) % kPage + 1;  // keys of the pair's last page
         // this lane: tokens hr, hr + 8 of a page's S, head dims 16 n + hr (+ 8) of
         // O, heads 2c, 2c + 1 of both
@@ -555,10 +563,20 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
         float o[8][4];
 #pragma unroll
         for (int n = 0; n < 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+        uint32_t qb[8][2];  // Q as the B operand: n = the group's heads, k = head dims
         for (int i = 0; i < here; ++i) {
             const int st = consumed % kOwnStages;
             ok = mbar_wait_warp(bar(st), (consumed / kOwnStages) & 1, p.err);
             if (!ok) break;
+            if (i == 0) {
+                const uint32_t *qrow =
+                    reinterpret_cast<const uint32_t *>(sg + q_slots + (pairs_done & 1) * kOwnQBytes + hr * kRowBytes);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) {
+                    qb[kk][0] = hr < g ? qrow[kk * 8 + c] : 0u;
+                    qb[kk][1] = hr < g ? qrow[kk * 8 + 4 + c] : 0u;
+                }
+            }
             const int valid = at.page + i + 1 < at.pages ? kPage : last;
             const uint32_t kb = ring + st * kOwnStageBytes, vb = kb + 2 * kBox;
             if (valid < kPage) {
@@ -641,12 +659,10 @@ __device__ __forceinline__ void own_warp(const CUtensorMap &tm_k, const CUtensor
                 __stcg(dst + 16 * n + 8, o[n][2 + x]);
             }
         }
-        at = then;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-            qb[kk][0] = qn[kk][0];
-            qb[kk][1] = qn[kk][1];
-        }
+        at = own_after(p, at, here);
+        ++pairs_done;
+        __syncwarp();
+        top_up();
     }
     // copies still in flight (only after a wait ran out)
     if (lane == 0)
@@ -672,15 +688,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     own_warp(tm_k, tm_v, p, (static_cast<int>(blockIdx.x) - p.n_pieces) * kSharedWarps + warp);
 }
 
-// Joins the partials of every (row, head).  A warp takes 32 query rows (a lane a
-// row) and 8 columns of a tile, so a load of a prefix partial is 512 contiguous
-// bytes; `ways` warps of a CTA share the partials of their rows, in turn, and add
-// up in shared memory.
+// Joins the partials of 32 query rows (a lane a row) of a tile: CTA of units x
+// tiles x 4 quarters x 2 ways.  A warp takes 8 columns, so a load of a prefix
+// partial is 512 contiguous bytes; `ways` of the warps share the partials of
+// their rows, in turn, and add up in shared memory.  (Joined by the CTAs of the
+// launch before instead, behind a barrier of all of them in a cooperative launch:
+// 24.6 us for 32 rows x 25k against 18.9, for such a launch does not overlap the
+// one before it, and 137 CTAs take the 256 tasks in two rounds.  Nor does an early
+// start pay: the CTAs then crowd on the SMs that are free first, 21.0 us.)
 template <class P>
-__global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant__ P p) {
-    __shared__ float s_ml[8][2][32];
-    __shared__ float4 s_acc[8][2][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__global__ void __launch_bounds__(256) shared_join_kernel(const __grid_constant__ P p) {
+    __shared__ float2 s_ml[8 * 32];       // [warp][lane]
+    __shared__ float4 s_acc[8 * 2 * 32];  // [warp][2][lane]
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sub = warp / p.ways, part = warp % p.ways;  // the warp's columns, its share of the partials
     const int cols_of_cta = 8 / p.ways, ctas = 16 / cols_of_cta;  // of 16 column groups
     const int col = (blockIdx.x % ctas) * cols_of_cta + sub;
@@ -689,12 +709,11 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
     rest /= 4;
     const int t = rest % p.tiles;
     const SharedUnit u = p.units[rest / p.tiles];
-    const SharedGroup grp = p.groups[u.group];
-    const int r = quarter * 32 + lane;  // of the tile
+    const int r = quarter * 32 + lane;                // of the tile
     const int q = (u.mu * p.tiles + t) * kTileQ + r;  // query row of the (group, kv-head)
-    const bool valid = q < grp.n_rows * p.group;
-    if (!__any_sync(0xffffffffu, valid) && p.ways == 1) return;
-    const int row = grp.row0 + (valid ? q / p.group : 0), h = q % p.group;
+    if (q - lane >= u.n_rows * p.group) return;     // none of the task's rows exists
+    const bool valid = q < u.n_rows * p.group;
+    const int row = u.row0 + (valid ? q / p.group : 0), h = q % p.group;
     const SharedRow sr = p.rows[row];
     // the pair's own pages, the first and the last warp that had some of them
     const int pages = (sr.own + kPage - 1) / kPage;
@@ -707,10 +726,11 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
 
     float M = -INFINITY, L = 0.f;
     float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    constexpr int kBatch = 4;
+    constexpr int kBatch = 6;
     for (int k0 = part; k0 < n_max; k0 += kBatch * p.ways) {
         float2 ml[kBatch];
         float4 o[kBatch][2];
+        float mn = M;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             const int k = k0 + b * p.ways;
@@ -731,7 +751,8 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
                 o[b][1] = __ldcg(src + 1);
             }
         }
-        const float mn = fmaxf(fmaxf(M, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x));
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) mn = fmaxf(mn, ml[b].x);
         if (mn == -INFINITY) continue;
         const float sc = M == -INFINITY ? 0.f : ex2(M - mn);
         L *= sc;
@@ -749,25 +770,25 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
         M = mn;
     }
     if (p.ways > 1) {
-        s_ml[warp][0][lane] = M;
-        s_ml[warp][1][lane] = L;
-        s_acc[warp][0][lane] = acc[0];
-        s_acc[warp][1][lane] = acc[1];
+        s_ml[warp * 32 + lane] = make_float2(M, L);
+        s_acc[warp * 64 + lane] = acc[0];
+        s_acc[warp * 64 + 32 + lane] = acc[1];
         __syncthreads();
         if (part != 0) return;
         float top = M;
-        for (int w = 1; w < p.ways; ++w) top = fmaxf(top, s_ml[warp + w][0][lane]);
+        for (int w = 1; w < p.ways; ++w) top = fmaxf(top, s_ml[(warp + w) * 32 + lane].x);
         const float f0 = M == -INFINITY ? 0.f : ex2(M - top);
         L *= f0;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) acc[c] = make_float4(acc[c].x * f0, acc[c].y * f0, acc[c].z * f0, acc[c].w * f0);
+        for (int c = 0; c < 2; ++c)
+            acc[c] = make_float4(acc[c].x * f0, acc[c].y * f0, acc[c].z * f0, acc[c].w * f0);
         for (int w = 1; w < p.ways; ++w) {
-            const float m = s_ml[warp + w][0][lane];
-            const float f = m == -INFINITY ? 0.f : ex2(m - top);
-            L += f * s_ml[warp + w][1][lane];
+            const float2 ml = s_ml[(warp + w) * 32 + lane];
+            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+            L += f * ml.y;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const float4 a = s_acc[warp + w][c][lane];
+                const float4 a = s_acc[(warp + w) * 64 + c * 32 + lane];
                 acc[c] = make_float4(acc[c].x + f * a.x, acc[c].y + f * a.y, acc[c].z + f * a.z, acc[c].w + f * a.w);
             }
         }
@@ -779,30 +800,32 @@ __global__ void __launch_bounds__(256) shared_merge_kernel(const __grid_constant
         make_uint4(pack_bf16x2(acc[0].x * inv, acc[0].y * inv), pack_bf16x2(acc[0].z * inv, acc[0].w * inv),
                    pack_bf16x2(acc[1].x * inv, acc[1].y * inv), pack_bf16x2(acc[1].z * inv, acc[1].w * inv));
 }
-
 template <class P>
 cudaError_t launch_shared(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const P &p,
-                          int32_t own_ctas, cudaStream_t st) {
+                          int32_t n_ctas, cudaStream_t st) {
     static std::atomic<uint64_t> smem_set{0};
     const cudaError_t e = ensure_smem_limit(shared_attn_kernel<P>, static_cast<int>(kSmemBytes), smem_set);
     if (e != cudaSuccess) return e;
-    if (p.n_pieces + own_ctas <= 0) return cudaSuccess;
-    PdlLaunch l(dim3(p.n_pieces + own_ctas), dim3(kThreads), kSmemBytes, st);
+    if (n_ctas <= 0) return cudaSuccess;
+    PdlLaunch l(dim3(n_ctas), dim3(kThreads), kSmemBytes, st);
     return cudaLaunchKernelEx(&l.cfg, shared_attn_kernel<P>, tm_q, tm_k, tm_v, p);
 }
 
 template <class P>
-cudaError_t launch_shared_merge(const P &p, cudaStream_t st) {
+cudaError_t launch_shared_join(const P &p, cudaStream_t st) {
     if (p.n_units <= 0) return cudaSuccess;
     PdlLaunch l(dim3(p.n_units * p.tiles * 4 * 2 * p.ways), dim3(256), 0, st);
-    return cudaLaunchKernelEx(&l.cfg, shared_merge_kernel<P>, p);
+    return cudaLaunchKernelEx(&l.cfg, shared_join_kernel<P>, p);
 }
 
-template cudaError_t launch_shared(const CUtensorMap &, const CUtensorMap &, const CUtensorMap &, const SharedParams &,
-                                   int32_t, cudaStream_t);
-template cudaError_t launch_shared(const CUtensorMap &, const CUtensorMap &, const CUtensorMap &,
-                                   const SharedParamsSmall &, int32_t, cudaStream_t);
-template cudaError_t launch_shared_merge(const SharedMergeParams &, cudaStream_t);
-template cudaError_t launch_shared_merge(const SharedMergeParamsSmall &, cudaStream_t);
+#define PPAS_LAUNCH_SHARED(P)                                                                                    \
+    template cudaError_t launch_shared(const CUtensorMap &, const CUtensorMap &, const CUtensorMap &, const P &, \
+                                       int32_t, cudaStream_t)
+PPAS_LAUNCH_SHARED(SharedParamsSmall);
+PPAS_LAUNCH_SHARED(SharedParamsMid);
+PPAS_LAUNCH_SHARED(SharedParamsBig);
+template cudaError_t launch_shared_join(const SharedParamsSmall &, cudaStream_t);
+template cudaError_t launch_shared_join(const SharedParamsMid &, cudaStream_t);
+template cudaError_t launch_shared_join(const SharedJoinBig &, cudaStream_t);
 
 }  // namespace ppas

@@ -35,21 +35,26 @@ struct SharedRow {
 struct SharedPiece {
     uint16_t group, kvh, mu, kt0, kt1, pad;
 };
+// the join's view: query rows [128 tiles mu, ...) of n_rows rows from row0 on
 struct SharedUnit {
-    uint16_t group, kvh, mu, piece0, n_pieces, pad;
+    int32_t row0;
+    uint16_t n_rows, kvh, mu, piece0, n_pieces, pad;
 };
 
-// Two sizes of the tables: a launch's parameters are copied by the host and read
-// by the device, 24 KB of them in 1.5 us or so
-template <int kRows, int kGroups, int kPieces>
+// The tables come in three sizes: a launch's parameters are copied by the host and
+// read by the device (4 rows: 13.5 us a call with 24 KB of them, 11.5 with 3).
+template <int kRows, int kGroups, int kPieces, int kUnits>
 struct SharedParamsT {
+    static constexpr int kMaxRows = kRows, kMaxGroups = kGroups, kMaxPieces = kPieces, kMaxUnits = kUnits;
     const __nv_bfloat16 *q;        // the launch's first row
+    __nv_bfloat16 *out;            // likewise
     const int32_t *block_tables;   // likewise
     int32_t table_stride, num_blocks;
     int32_t n_q_heads, n_kv_heads, group;  // group: q-heads of a kv-head
     int32_t tiles;                 // Q tiles of 128 query rows a piece has room for: 1 or 2
-    int32_t n_rows, n_pieces;
+    int32_t n_rows, n_pieces, n_units;
     int32_t own_pages, warp_pages;  // in all, and a warp's
+    int32_t ways;                  // warps that share a row's partials in the join: 1, 2, 4 or 8
     float scale_log2;
     int32_t *err;
     float *pre_o;   // [n_pieces, tiles, 32 chunks, 128 rows, 4]
@@ -59,24 +64,14 @@ struct SharedParamsT {
     SharedGroup groups[kGroups];
     SharedRow rows[kRows];
     SharedPiece pieces[kPieces];
-};
-using SharedParams = SharedParamsT<kSharedMaxRows, kSharedMaxGroups, kSharedMaxPieces>;
-using SharedParamsSmall = SharedParamsT<64, 8, 160>;
-static_assert(sizeof(SharedParams) + 3 * 128 <= 32764, "kernel parameter space");
-
-template <int kRows, int kGroups, int kUnits>
-struct SharedMergeParamsT {
-    __nv_bfloat16 *out;  // the launch's first row
-    const float *pre_o, *pre_ml, *own_o, *own_ml;
-    int32_t n_q_heads, n_kv_heads, group, tiles, n_units, warp_pages;
-    int32_t ways;        // warps that share a row's partials: 1, 2, 4 or 8
-    SharedGroup groups[kGroups];
-    SharedRow rows[kRows];
     SharedUnit units[kUnits];
 };
-using SharedMergeParams = SharedMergeParamsT<kSharedMaxRows, kSharedMaxGroups, kSharedMaxUnits>;
-using SharedMergeParamsSmall = SharedMergeParamsT<64, 8, 64>;
-static_assert(sizeof(SharedMergeParams) <= 32764, "kernel parameter space");
+using SharedParamsSmall = SharedParamsT<64, 8, 160, 64>;
+using SharedParamsMid = SharedParamsT<256, 32, 256, 256>;
+// (no room for the units beside the pieces: the join of these has its own tables)
+using SharedParamsBig = SharedParamsT<kSharedMaxRows, kSharedMaxGroups, kSharedMaxPieces, 1>;
+using SharedJoinBig = SharedParamsT<kSharedMaxRows, 1, 1, kSharedMaxUnits>;
+static_assert(sizeof(SharedParamsBig) + 3 * 128 <= 32764 && sizeof(SharedJoinBig) <= 32764, "kernel parameter space");
 
 // one launch of each kernel
 struct SharedLaunch {
@@ -88,6 +83,7 @@ struct SharedLaunch {
     std::vector<SharedUnit> units;
     size_t pre_o_bytes = 0, pre_ml_bytes = 0, own_o_bytes = 0, own_ml_bytes = 0;
     size_t total_bytes() const { return pre_o_bytes + pre_ml_bytes + own_o_bytes + own_ml_bytes; }
+    int32_t n_ctas() const { return static_cast<int32_t>(pieces.size()) + own_ctas; }
 };
 struct SharedPlan {
     std::vector<SharedLaunch> launches;
@@ -98,8 +94,8 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
 
 template <class P>
 cudaError_t launch_shared(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const P &p,
-                          int32_t own_ctas, cudaStream_t st);
+                          int32_t n_ctas, cudaStream_t st);
 template <class P>
-cudaError_t launch_shared_merge(const P &p, cudaStream_t st);
+cudaError_t launch_shared_join(const P &p, cudaStream_t st);
 
 }  // namespace ppas

@@ -114,7 +114,7 @@ static PyObject *py_sample_tokens(PyObject *self, PyObject *args) {
  *                       max_blocks_per_seq, group_rows, prefix_lens, ctx_lens,
  *                       n_q_heads, n_kv_heads, head_dim, scale, out, workspace,
  *                       workspace_bytes, d_err_flag, stream) -> ppas_status
- * (ctx_lens as long as the sum of group_rows: the binding checks it) */
+ */
 static PyObject *py_shared_attention_step(PyObject *self, PyObject *args) {
     unsigned long long q, k, v, tables, out, ws, ws_bytes, err, stream;
     int num_blocks, width, hq, hk, d;
@@ -126,8 +126,11 @@ static PyObject *py_shared_attention_step(PyObject *self, PyObject *args) {
         return NULL;
     PyObject *res = NULL;
     if (int32_buffer(&gr, "group_rows") && int32_buffer(&pl, "prefix_lens") && int32_buffer(&cl, "ctx_lens")) {
-        if (gr.len != pl.len) {
-            PyErr_SetString(PyExc_ValueError, "group_rows and prefix_lens differ in length");
+        /* the C call takes the lengths' number from group_rows */
+        long long rows = 0;
+        for (Py_ssize_t i = 0; i < gr.len / 4; ++i) rows += ((const int32_t *)gr.buf)[i];
+        if (gr.len != pl.len || rows != cl.len / 4) {
+            res = PyLong_FromLong(PPAS_ERR_INVALID_ARG);
         } else {
             const ppas_status st = ppas_shared_attention_step(
                 (const void *)(uintptr_t)q, (const void *)(uintptr_t)k, (const void *)(uintptr_t)v, num_blocks,

@@ -15,15 +15,17 @@ namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-// The time of a KV tile (64 KB) in a piece and of a page (8 KB) of own keys in a
-// warp's ring, in units of a tile streamed at an SM's share of the memory
-constexpr double kTileCost = 1.0, kPageCost = 1.0 / 8;
+// Times behind the split of the SMs, in us, fitted on GB300 to the best of splits
+// from 6 to 120 SMs for the own keys, 15 batches.  A piece takes 5.5 (ids, first K
+// tile, last softmax, writing O) and 1.2 a KV tile, 1.5 with two Q tiles; a warp's
+// run of own pages 4.2 and 1.1 a page.  (Alone, a tile takes 0.8 or 1.0 and a page
+// 0.75: side by side all of them wait for memory.)
+constexpr double kPieceUs = 5.5, kTileUs[2] = {1.2, 1.5}, kRunUs = 4.2, kPageUs = 1.1;
+
 // pieces of a prefix at the longest
 int32_t least_pieces(int32_t prefix) {
     return (prefix + kSharedMaxPiece * kPrefillKT - 1) / (kSharedMaxPiece * kPrefillKT);
 }
-
-constexpr double kItemCost = 0.25;  // an item besides its pages, in the same unit, over a CTA's 8 warps
 
 }  // namespace
 
@@ -73,46 +75,52 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
         // two Q tiles a piece where a group fills more than one (or the tables ask for it)
         l.tiles = most > kTileQ || units[0] > kSharedMaxUnits || pieces[0] > kSharedMaxPieces ? 2 : 1;
         const int32_t per = kTileQ * l.tiles;
-        // ---- own keys
-        int64_t own_pages = 0;
-        double tiles = 0;
+        int64_t own_pages = 0, tiles = 0;
         for (size_t i = i0; i < i1; ++i) {
             const Part &pt = parts[i];
             for (int32_t r = pt.row0; r < pt.row0 + pt.n_rows; ++r)
                 own_pages += static_cast<int64_t>((ctx_lens[r] - pt.prefix + kPage - 1) / kPage) * n_kv_heads;
-            tiles += static_cast<double>((pt.prefix + kPrefillKT - 1) / kPrefillKT) * n_kv_heads *
-                     ((pt.n_rows * g + per - 1) / per);
+            tiles += pt.prefix;
         }
-        // the SMs in proportion to the two kinds' time
-        const double own_time = own_pages * kPageCost + static_cast<double>(l.n_rows) * n_kv_heads * kItemCost / 8;
-        int32_t own_sms = own_pages == 0 ? 0 : num_sms;
-        if (own_pages > 0 && tiles > 0)
-            own_sms = std::max(1, std::min(num_sms - 1, static_cast<int32_t>(
-                                                            num_sms * own_time / (own_time + tiles * kTileCost) + 0.5)));
-        // runs of at least 2 pages a warp: below that its fixed latency is all there is
         if (own_pages > (int64_t{1} << 30)) throw std::length_error("own keys");
-        const int64_t warps = std::max(1, own_sms) * static_cast<int64_t>(kSharedWarps);
+        // The prefixes' pieces have one length, the shortest that sms SMs hold in
+        // one round; the own pages are cut into runs of at least 2 (below that a
+        // run's fixed latency is all there is).
+        auto piece_len = [&](int32_t sms) {
+            int32_t len = 1, hi = kSharedMaxPiece;
+            while (len < hi) {
+                const int32_t mid = (len + hi) / 2;
+                int64_t k = 0;
+                for (size_t i = i0; i < i1; ++i)
+                    k += static_cast<int64_t>(((parts[i].prefix + kPrefillKT - 1) / kPrefillKT + mid - 1) / mid) *
+                         units_of(parts[i], l.tiles);
+                if (k <= sms) hi = mid;
+                else len = mid + 1;
+            }
+            return len;
+        };
+        auto run_len = [&](int32_t sms) {
+            const int64_t warps = sms * static_cast<int64_t>(kSharedWarps);
+            return std::max<int64_t>(2, (own_pages + warps - 1) / warps);
+        };
+        // the SMs for the own keys with which the slower of the two kinds ends first
+        int32_t own_sms = own_pages == 0 ? 0 : num_sms;
+        if (own_pages > 0 && tiles > 0 && num_sms > 1) {
+            double best = INFINITY;
+            for (int32_t k = 1; k < num_sms; k += k < 32 ? 1 : 2) {
+                const double t = std::max(kPieceUs + kTileUs[l.tiles - 1] * piece_len(num_sms - k),
+                                          kRunUs + kPageUs * static_cast<double>(run_len(k)));
+                if (t < best) {
+                    best = t;
+                    own_sms = k;
+                }
+            }
+        }
         l.own_pages = static_cast<int32_t>(own_pages);
-        l.warp_pages = static_cast<int32_t>(std::max<int64_t>(2, (own_pages + warps - 1) / warps));
+        l.warp_pages = static_cast<int32_t>(run_len(std::max(1, own_sms)));
         l.own_ctas = static_cast<int32_t>((own_pages + static_cast<int64_t>(l.warp_pages) * kSharedWarps - 1) /
                                           (static_cast<int64_t>(l.warp_pages) * kSharedWarps));
-        // ---- the prefixes' pieces: one length of piece for all, the shortest
-        // that the SMs hold in one round
-        const int32_t pre_sms = std::max(1, num_sms - own_sms);
-        int32_t len = 1, hi = kSharedMaxPiece;
-        auto pieces_at = [&](int32_t n) {
-            int64_t k = 0;
-            for (size_t i = i0; i < i1; ++i) {
-                const int64_t kt = (parts[i].prefix + kPrefillKT - 1) / kPrefillKT;
-                k += (kt + n - 1) / n * n_kv_heads * ((parts[i].n_rows * g + per - 1) / per);
-            }
-            return k;
-        };
-        while (len < hi) {
-            const int32_t mid = (len + hi) / 2;
-            if (pieces_at(mid) <= pre_sms) hi = mid;
-            else len = mid + 1;
-        }
+        const int32_t len = piece_len(std::max(1, num_sms - own_sms));
         int32_t page0 = 0, most_own = 0, most_pieces = 0;
         for (size_t i = i0; i < i1; ++i) {
             const Part &pt = parts[i];
@@ -127,7 +135,8 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
             const int32_t kt = (pt.prefix + kPrefillKT - 1) / kPrefillKT, np = (kt + len - 1) / len;
             for (int32_t mu = 0; mu < (pt.n_rows * g + per - 1) / per; ++mu)
                 for (int32_t h = 0; h < n_kv_heads; ++h) {
-                    l.units.push_back({gi, static_cast<uint16_t>(h), static_cast<uint16_t>(mu),
+                    l.units.push_back({pt.row0 - l.row0, static_cast<uint16_t>(pt.n_rows), static_cast<uint16_t>(h),
+                                       static_cast<uint16_t>(mu),
                                        static_cast<uint16_t>(l.pieces.size()), static_cast<uint16_t>(np), 0});
                     for (int32_t k = 0; k < np; ++k)
                         l.pieces.push_back({gi, static_cast<uint16_t>(h), static_cast<uint16_t>(mu),
@@ -222,16 +231,17 @@ ppas_status run(const void *q, const void *k_cache, const void *v_cache, int32_t
     const int32_t g = hq / hk;
     if (!encode_kv_map(&tm_k, k_cache, num_blocks, hk) || !encode_kv_map(&tm_v, v_cache, num_blocks, hk))
         return PPAS_ERR_CUDA;
-    static thread_local SharedParams big;  // ~24 KB each: kept off the stack
-    static thread_local SharedMergeParams big_merge;
     static thread_local SharedParamsSmall small;
-    static thread_local SharedMergeParamsSmall small_merge;
+    static thread_local SharedParamsMid mid;  // (these are kept off the stack: up to 24 KB each)
+    static thread_local SharedParamsBig big;
+    static thread_local SharedJoinBig big_join;
     for (const SharedLaunch &l : plan.launches) {
         const __nv_bfloat16 *const q0 = static_cast<const __nv_bfloat16 *>(q) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
         if (!encode_q_group_map(&tm_q, q0, std::min(l.n_rows, n_rows - l.row0), hq, g)) return PPAS_ERR_CUDA;
         uint8_t *const ws = static_cast<uint8_t *>(workspace);
-        auto launch = [&](auto &p, auto &m) {
+        auto fill = [&](auto &p) {
             p.q = q0;
+            p.out = static_cast<__nv_bfloat16 *>(out) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
             p.block_tables = d_block_tables + static_cast<int64_t>(l.row0) * max_blocks_per_seq;
             p.table_stride = max_blocks_per_seq;
             p.num_blocks = num_blocks;
@@ -241,38 +251,42 @@ ppas_status run(const void *q, const void *k_cache, const void *v_cache, int32_t
             p.tiles = l.tiles;
             p.n_rows = l.n_rows;
             p.n_pieces = static_cast<int32_t>(l.pieces.size());
+            p.n_units = static_cast<int32_t>(l.units.size());
             p.own_pages = l.own_pages;
             p.warp_pages = l.warp_pages;
+            p.ways = l.ways;
             p.scale_log2 = scale * 1.4426950408889634f;
             p.err = err;
             p.pre_o = reinterpret_cast<float *>(ws);
-            p.pre_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes);
-            p.own_o = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes);
-            p.own_ml = reinterpret_cast<float *>(ws + l.pre_o_bytes + l.pre_ml_bytes + l.own_o_bytes);
-            std::copy(l.groups.begin(), l.groups.end(), p.groups);
+            p.pre_ml = p.pre_o + l.pre_o_bytes / sizeof(float);
+            p.own_o = p.pre_ml + l.pre_ml_bytes / sizeof(float);
+            p.own_ml = p.own_o + l.own_o_bytes / sizeof(float);
+            if (l.groups.size() <= std::size(p.groups)) std::copy(l.groups.begin(), l.groups.end(), p.groups);
             std::copy(l.rows.begin(), l.rows.end(), p.rows);
-            std::copy(l.pieces.begin(), l.pieces.end(), p.pieces);
-            if (launch_shared(tm_q, tm_k, tm_v, p, l.own_ctas, st) != cudaSuccess) return false;
-            m.out = static_cast<__nv_bfloat16 *>(out) + static_cast<int64_t>(l.row0) * hq * kHeadDim;
-            m.pre_o = p.pre_o;
-            m.pre_ml = p.pre_ml;
-            m.own_o = p.own_o;
-            m.own_ml = p.own_ml;
-            m.n_q_heads = hq;
-            m.n_kv_heads = hk;
-            m.group = g;
-            m.tiles = l.tiles;
-            m.n_units = static_cast<int32_t>(l.units.size());
-            m.warp_pages = l.warp_pages;
-            m.ways = l.ways;
-            std::copy(l.groups.begin(), l.groups.end(), m.groups);
-            std::copy(l.rows.begin(), l.rows.end(), m.rows);
-            std::copy(l.units.begin(), l.units.end(), m.units);
-            return launch_shared_merge(m, st) == cudaSuccess;
+            if (l.pieces.size() <= std::size(p.pieces)) std::copy(l.pieces.begin(), l.pieces.end(), p.pieces);
+            if (l.units.size() <= std::size(p.units)) std::copy(l.units.begin(), l.units.end(), p.units);
         };
-        const bool fits = l.rows.size() <= std::size(small.rows) && l.groups.size() <= std::size(small.groups) &&
-                          l.pieces.size() <= std::size(small.pieces) && l.units.size() <= std::size(small_merge.units);
-        if (!(fits ? launch(small, small_merge) : launch(big, big_merge))) return PPAS_ERR_CUDA;
+        auto fits = [&](const auto &p) {
+            return l.rows.size() <= std::size(p.rows) && l.groups.size() <= std::size(p.groups) &&
+                   l.pieces.size() <= std::size(p.pieces) && l.units.size() <= std::size(p.units);
+        };
+        auto launch = [&](auto &p, auto &join) {
+            const cudaError_t e = launch_shared(tm_q, tm_k, tm_v, p, l.n_ctas(), st);
+            return e == cudaSuccess ? launch_shared_join(join, st) : e;
+        };
+        cudaError_t e;
+        if (fits(small)) {
+            fill(small);
+            e = launch(small, small);
+        } else if (fits(mid)) {
+            fill(mid);
+            e = launch(mid, mid);
+        } else {
+            fill(big);
+            fill(big_join);
+            e = launch(big, big_join);
+        }
+        if (e != cudaSuccess) return PPAS_ERR_CUDA;
     }
     return PPAS_OK;
 }

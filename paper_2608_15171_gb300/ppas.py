@@ -340,14 +340,15 @@ def ppas_shared_attention_step(q, k_cache, v_cache, num_blocks: int, d_block_tab
                                ctx_lens, group_rows, prefix_lens, n_q_heads: int, n_kv_heads: int, head_dim: int,
                                scale: float, out, workspace=None, workspace_bytes: int = 0, d_err_flag=None,
                                stream=None) -> None:
-    cl, gr, pl = _group_lens(ctx_lens, group_rows, prefix_lens, "ppas_shared_attention_step")
     if _fast is not None:
         _check(_fast.shared_attention_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), int(num_blocks),
-                                           _ptr(d_block_tables), int(max_blocks_per_seq), gr, pl, cl, int(n_q_heads),
-                                           int(n_kv_heads), int(head_dim), float(scale), _ptr(out), _ptr(workspace),
+                                           _ptr(d_block_tables), int(max_blocks_per_seq), _i32(group_rows),
+                                           _i32(prefix_lens), _i32(ctx_lens), int(n_q_heads), int(n_kv_heads),
+                                           int(head_dim), float(scale), _ptr(out), _ptr(workspace),
                                            int(workspace_bytes), _ptr(d_err_flag), _stream(stream)),
                "ppas_shared_attention_step")
         return
+    cl, gr, pl = _group_lens(ctx_lens, group_rows, prefix_lens, "ppas_shared_attention_step")
     _check(_lib.ppas_shared_attention_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), int(num_blocks),
                                            _ptr(d_block_tables), int(max_blocks_per_seq), int(gr.size), _addr(gr),
                                            _addr(pl), _addr(cl), int(n_q_heads), int(n_kv_heads), int(head_dim),

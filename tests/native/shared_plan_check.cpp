@@ -64,15 +64,18 @@ static std::string check(int sms, int hq, int hk, const std::vector<int> &rows, 
         std::set<std::vector<int>> seen;
         size_t next = 0;
         for (const SharedUnit &u : l.units) {
-            const SharedGroup &gr = l.groups.at(u.group);
+            size_t gi = 0;
+            while (gi < l.groups.size() && l.groups[gi].row0 != u.row0) ++gi;
+            const SharedGroup &gr = l.groups.at(gi);
+            if (u.n_rows != gr.n_rows) return "rows of a unit";
             if (u.kvh >= hk || u.mu * l.tiles * 128 >= gr.n_rows * g) return "unit";
-            if (!seen.insert({u.group, u.kvh, u.mu}).second) return "a unit twice";
+            if (!seen.insert({u.row0, u.kvh, u.mu}).second) return "a unit twice";
             if (u.n_pieces > 0 && u.piece0 != next) return "first piece";
             const int kt = (gr.prefix + 127) / 128;
             int at = 0;
             for (int k = 0; k < u.n_pieces; ++k) {
                 const SharedPiece &pc = l.pieces.at(next++);
-                if (pc.group != u.group || pc.kvh != u.kvh || pc.mu != u.mu) return "piece of another unit";
+                if (pc.group != gi || pc.kvh != u.kvh || pc.mu != u.mu) return "piece of another unit";
                 if (pc.kt0 != at || pc.kt1 <= pc.kt0 || pc.kt1 - pc.kt0 > kSharedMaxPiece) return "piece's tiles";
                 at = pc.kt1;
             }
