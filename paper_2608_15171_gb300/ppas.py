@@ -144,6 +144,8 @@ def _check(status: int, where: str) -> None:
 
 
 def _i32(a) -> np.ndarray:
+    if type(a) is np.ndarray and a.dtype == np.int32 and a.ndim == 1 and a.flags.c_contiguous:
+        return a
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
 
@@ -316,7 +318,13 @@ def ppas_rope_append(q, k, v, q_stride: int, k_stride: int, v_stride: int, d_pos
                      n_tokens: int, d_inv_freq, rotary_dim: int, interleaved: bool, factor: float, q_out, k_cache,
                      v_cache, num_blocks: int, n_q_heads: int, n_kv_heads: int, head_dim: int, d_err_flag=None,
                      stream=None) -> None:
-    call = _lib.ppas_rope_append if _fast is None else _fast.rope_append
+    if _fast is not None:
+        _check(_fast.rope_append(_ptr(q), _ptr(k), _ptr(v), q_stride, k_stride, v_stride, _ptr(d_positions),
+                                 _ptr(d_slot_mapping), n_tokens, _ptr(d_inv_freq), rotary_dim, bool(interleaved),
+                                 factor, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), num_blocks, n_q_heads,
+                                 n_kv_heads, head_dim, _ptr(d_err_flag), _stream(stream)), "ppas_rope_append")
+        return
+    call = _lib.ppas_rope_append
     _check(call(_ptr(q), _ptr(k), _ptr(v), int(q_stride), int(k_stride), int(v_stride), _ptr(d_positions),
                 _ptr(d_slot_mapping), int(n_tokens), _ptr(d_inv_freq), int(rotary_dim), 1 if interleaved else 0,
                 float(factor), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), int(num_blocks), int(n_q_heads),
@@ -341,11 +349,10 @@ def ppas_shared_attention_step(q, k_cache, v_cache, num_blocks: int, d_block_tab
                                scale: float, out, workspace=None, workspace_bytes: int = 0, d_err_flag=None,
                                stream=None) -> None:
     if _fast is not None:
-        _check(_fast.shared_attention_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), int(num_blocks),
-                                           _ptr(d_block_tables), int(max_blocks_per_seq), _i32(group_rows),
-                                           _i32(prefix_lens), _i32(ctx_lens), int(n_q_heads), int(n_kv_heads),
-                                           int(head_dim), float(scale), _ptr(out), _ptr(workspace),
-                                           int(workspace_bytes), _ptr(d_err_flag), _stream(stream)),
+        _check(_fast.shared_attention_step(_ptr(q), _ptr(k_cache), _ptr(v_cache), num_blocks, _ptr(d_block_tables),
+                                           max_blocks_per_seq, _i32(group_rows), _i32(prefix_lens), _i32(ctx_lens),
+                                           n_q_heads, n_kv_heads, head_dim, scale, _ptr(out), _ptr(workspace),
+                                           workspace_bytes, _ptr(d_err_flag), _stream(stream)),
                "ppas_shared_attention_step")
         return
     cl, gr, pl = _group_lens(ctx_lens, group_rows, prefix_lens, "ppas_shared_attention_step")
@@ -359,7 +366,13 @@ def ppas_shared_attention_step(q, k_cache, v_cache, num_blocks: int, d_block_tab
 def ppas_sample_tokens(logits, logits_are_bf16: bool, row_stride: int, n_rows: int, vocab: int, d_temperature,
                        d_top_k, d_top_p, d_min_p, d_uniform, d_tokens, d_logprobs=None, d_err_flag=None,
                        stream=None) -> None:
-    call = _lib.ppas_sample_tokens if _fast is None else _fast.sample_tokens
+    if _fast is not None:
+        _check(_fast.sample_tokens(_ptr(logits), bool(logits_are_bf16), row_stride, n_rows, vocab,
+                                   _ptr(d_temperature), _ptr(d_top_k), _ptr(d_top_p), _ptr(d_min_p), _ptr(d_uniform),
+                                   _ptr(d_tokens), _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)),
+               "ppas_sample_tokens")
+        return
+    call = _lib.ppas_sample_tokens
     _check(call(_ptr(logits), 1 if logits_are_bf16 else 0, int(row_stride), int(n_rows), int(vocab),
                 _ptr(d_temperature), _ptr(d_top_k), _ptr(d_top_p), _ptr(d_min_p), _ptr(d_uniform), _ptr(d_tokens),
                 _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens")
