@@ -75,7 +75,7 @@ struct SShared {
     uint32_t fine_c[kSFine], fine_l[kSFine], fine_h[kSFine];  // first CTA: the histogram of a list
     SBinsOf bins;
     uint32_t ns[kStages], at[kStages];     // tokens in the lists (first CTA: all of them), this CTA's place there
-    float2 range[kSMaxCluster];            // (max, min finite) of each CTA
+    float2 range[kSMaxCluster];            // (max, about the least finite one) of each CTA
     uint64_t above[kSMaxCluster];          // weight with z >= ln p_min, or the lowest index of the maximum
     uint64_t warp_w[kSWarps];
     uint32_t warp_c[kSWarps];
@@ -139,7 +139,7 @@ __device__ __forceinline__ void place_range(float x_lo, float x_hi, uint64_t &lo
 }
 
 struct SRow {
-    float top, inv_t, lowest, bin_scale;  // all finite; the z of the lowest token that counts is in bin kSBins - 1
+    float top, inv_t, lowest, bin_scale;  // all finite; z = lowest, and all below, is in bin kSBins - 1
     float width;                          // x a bin (infinite where there is one bin)
     __device__ __forceinline__ float z(float x) const { return (x - top) * inv_t; }
     // (conversions between floats and whole numbers share a slow unit with exp:
@@ -455,18 +455,16 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         }
     };
     float mx = -INFINITY, mn = INFINITY;
+    // (a maximum passes over NaNs; the least of every fourth value will do to
+    // spread the bins, for what is below goes to the last one)
     stream(Loads<4>{}, [&](const float(&x)[4], int at) {
-        float y[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            y[k] = fmaxf(x[k], -INFINITY);  // a NaN is no candidate
-            mx = fmaxf(mx, y[k]);
-            mn = fminf(mn, y[k] > -INFINITY ? y[k] : INFINITY);
-        }
+        for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[k]);
+        if (x[0] > -INFINITY) mn = fminf(mn, x[0]);
         if constexpr (kResident) {
             const int to = at - i0 + pad;
-            if (at - i0 < head || at - i0 >= tail0) xs[to] = y[0];
-            else *reinterpret_cast<float4 *>(xs + to) = make_float4(y[0], y[1], y[2], y[3]);
+            if (at - i0 < head || at - i0 >= tail0) xs[to] = x[0];
+            else *reinterpret_cast<float4 *>(xs + to) = make_float4(x[0], x[1], x[2], x[3]);
         }
     });
     if constexpr (kResident) {
@@ -532,6 +530,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     row.inv_t = 1.f / temperature;
     // where z would not be a number: the largest alone are left, as equals
     const bool odd = mx == INFINITY || row.inv_t == INFINITY;
+    mn = fminf(mn, mx);
     if (odd) {
         row.top = mn = 0.f;
         row.inv_t = 1.f;
