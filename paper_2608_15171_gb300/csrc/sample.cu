@@ -18,6 +18,7 @@
 // over the cluster, gives the bin; its tokens (a few hundred) go to the first
 // CTA, which divides them further by the bits of (x, index).  Bins with more than
 // that (ties, flat rows) are divided so by the whole cluster first.
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -526,20 +527,12 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     const bool by_k = top_k > 0 && top_k < p.vocab, by_m = min_p > 0.f;
     const float ln_min_p = by_m ? logf(min_p) : -INFINITY;
     SRow row;
-    row.top = mx;
-    row.inv_t = 1.f / temperature;
-    // where z would not be a number: the largest alone are left, as equals
-    const bool odd = mx == INFINITY || row.inv_t == INFINITY;
-    mn = fminf(mn, mx);
-    if (odd) {
-        row.top = mn = 0.f;
-        row.inv_t = 1.f;
-    }
-    // a logit as the passes see it: one zero, and a NaN as -inf
-    auto logit = [&](float x) {
-        if (odd) return x == mx ? 0.f : -INFINITY;
-        return fmaxf(x, -INFINITY);
-    };
+    // all finite: +inf counts as the largest finite value, and so does 1 / T
+    row.top = fminf(mx, FLT_MAX);
+    row.inv_t = fminf(1.f / temperature, FLT_MAX);
+    mn = fminf(mn, row.top);
+    // a logit as the passes see it (a NaN as -inf)
+    auto logit = [](float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); };
     // (lowest * bin_scale is 1023 but for two roundings, so that no bin is past the last)
     row.lowest = fmaxf(row.z(mn), kSFloor);
     row.bin_scale = row.lowest < 0.f ? fminf((kSBins - 1.f) / -row.lowest, 1e30f) : 0.f;
@@ -724,20 +717,20 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                     s.lists[j][at] = (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(index);
             }
     };
-    if (!odd && bins.lo[kCutK] > bins.hi[kCutK] && bins.lo[kCutP] > bins.hi[kCutP]) {
+    if (bins.lo[kCutK] > bins.hi[kCutK] && bins.lo[kCutP] > bins.hi[kCutP]) {
         // (one range to compare with)
         pass(Loads<4>{}, [&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (x[k] >= bins.x_lo[kDraw] && x[k] <= bins.x_hi[kDraw]) gather(x[k], first + k);
+                if ((x[k] >= bins.x_lo[kDraw]) & (x[k] <= bins.x_hi[kDraw])) gather(x[k], first + k);
         });
     } else {
         pass(Loads<4>{}, [&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                bool maybe = odd;
+                bool maybe = false;  // (no short circuits: six comparisons take less than their branches)
 #pragma unroll
-                for (int j = 0; j < kStages; ++j) maybe = maybe || (x[k] >= bins.x_lo[j] && x[k] <= bins.x_hi[j]);
+                for (int j = 0; j < kStages; ++j) maybe |= (x[k] >= bins.x_lo[j]) & (x[k] <= bins.x_hi[j]);
                 if (maybe) gather(x[k], first + k);
             }
         });
@@ -796,7 +789,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         pass(Loads<2>{}, [&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (!odd && !(x[k] >= cmd.x_lo && x[k] <= cmd.x_hi)) continue;
+                if (!((x[k] >= cmd.x_lo) & (x[k] <= cmd.x_hi))) continue;
                 const float y = logit(x[k]) + 0.f, z = row.z(y);
                 if (!SRow::counts(z)) continue;
                 const uint64_t place =
