@@ -22,6 +22,10 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // 0.75: side by side all of them wait for memory.)
 constexpr double kPieceUs = 5.5, kTileUs[2] = {1.2, 1.5}, kRunUs = 4.2, kPageUs = 1.1;
 
+// a single row's prefix of up to this many pages is cheaper as its own keys; a longer
+// one would leave the join too many partials
+constexpr int32_t kOwnPrefixPages = 256;
+
 // pieces of a prefix at the longest
 int32_t least_pieces(int32_t prefix) {
     return (prefix + kSharedMaxPiece * kPrefillKT - 1) / (kSharedMaxPiece * kPrefillKT);
@@ -43,15 +47,24 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
     auto pieces_of = [&](const Part &pt, int32_t tiles) {
         return units_of(pt, tiles) * least_pieces(pt.prefix);
     };
-    // A group of more rows than a launch's tables hold is several parts; rows that
-    // have their prefix to themselves read it as their own keys.
+    // A group of more rows than a launch's tables hold is several parts.  Rows read
+    // a short prefix as their own keys, where that takes less of the SMs' time than
+    // a piece's fixed latency: 100 groups of 2 rows x 512 (16/2 heads) 25.5 us, in
+    // pieces 157.6; 60 of 2 x 320 (8/8) 34.6 and 278.5; the other way, 4 rows x 2048
+    // 9.4 us in pieces and 11.0 as own keys, 1 x 8000 9.1 and 11.5, 1 x 25k 11.2 and
+    // 17.6, 4 groups of 1 x 25k 23.4 and 26.2.
+    auto as_own = [](int32_t n, int32_t prefix) {
+        const double pages = prefix / kPage;
+        return n == 1 ? pages <= kOwnPrefixPages
+                      : n * pages * kPageUs / kSharedWarps < kPieceUs + pages * kTileUs[0] / (kPrefillKT / kPage);
+    };
     std::vector<Part> parts;
     for (int32_t i = 0, row = 0; i < n_groups; row += group_rows[i++]) {
         const int32_t tables = kSharedMaxPieces / (n_kv_heads * std::max(1, least_pieces(prefix_lens[i])));
         const int32_t most = std::min<int64_t>(kSharedMaxRows, static_cast<int64_t>(tables) * 2 * kTileQ / g);
         for (int32_t r = 0; r < group_rows[i]; r += most) {
             const int32_t n = std::min(most, group_rows[i] - r);
-            parts.push_back({row + r, n, n == 1 ? 0 : prefix_lens[i]});
+            parts.push_back({row + r, n, as_own(n, prefix_lens[i]) ? 0 : prefix_lens[i]});
         }
     }
     for (size_t i0 = 0; i0 < parts.size();) {
@@ -75,17 +88,21 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
         // two Q tiles a piece where a group fills more than one (or the tables ask for it)
         l.tiles = most > kTileQ || units[0] > kSharedMaxUnits || pieces[0] > kSharedMaxPieces ? 2 : 1;
         const int32_t per = kTileQ * l.tiles;
-        int64_t own_pages = 0, tiles = 0;
+        int64_t own_pages = 0, most_pages = 0, tiles = 0;
         for (size_t i = i0; i < i1; ++i) {
             const Part &pt = parts[i];
-            for (int32_t r = pt.row0; r < pt.row0 + pt.n_rows; ++r)
-                own_pages += static_cast<int64_t>((ctx_lens[r] - pt.prefix + kPage - 1) / kPage) * n_kv_heads;
+            for (int32_t r = pt.row0; r < pt.row0 + pt.n_rows; ++r) {
+                const int64_t pages = (ctx_lens[r] - pt.prefix + kPage - 1) / kPage;
+                own_pages += pages * n_kv_heads;
+                most_pages = std::max(most_pages, pages);
+            }
             tiles += pt.prefix;
         }
         if (own_pages > (int64_t{1} << 30)) throw std::length_error("own keys");
         // The prefixes' pieces have one length, the shortest that sms SMs hold in
         // one round; the own pages are cut into runs of at least 2 (below that a
-        // run's fixed latency is all there is).
+        // run's fixed latency is all there is), and at most 128 to a (row, kv-head)
+        // (one row's 25k tokens in 521 runs: 18.9 us, most of it the join).
         auto piece_len = [&](int32_t sms) {
             int32_t len = 1, hi = kSharedMaxPiece;
             while (len < hi) {
@@ -101,7 +118,7 @@ SharedPlan plan_shared(int32_t n_groups, const int32_t *group_rows, const int32_
         };
         auto run_len = [&](int32_t sms) {
             const int64_t warps = sms * static_cast<int64_t>(kSharedWarps);
-            return std::max<int64_t>(2, (own_pages + warps - 1) / warps);
+            return std::max({int64_t{2}, (own_pages + warps - 1) / warps, (most_pages + 127) / 128});
         };
         // the SMs for the own keys with which the slower of the two kinds ends first
         int32_t own_sms = own_pages == 0 ? 0 : num_sms;

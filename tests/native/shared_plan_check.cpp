@@ -35,7 +35,7 @@ static std::string check(int sms, int hq, int hk, const std::vector<int> &rows, 
             if (gr.row0 != r || gr.n_rows < 1 || gr.prefix % 16) return "group";
             for (int k = 0; k < gr.n_rows; ++k, ++r) {
                 const SharedRow &sr = l.rows[r];
-                if (gr.prefix != prefix_of[row + r] && !(gr.n_rows == 1 && gr.prefix == 0)) return "prefix of a row";
+                if (gr.prefix != prefix_of[row + r] && !(gr.prefix == 0 && (gr.n_rows == 1 || prefix_of[row + r] < 1024))) return "prefix of a row";
                 if (sr.own != ctx[row + r] - gr.prefix || sr.own < 0) return "own keys";
                 if (sr.table != gr.prefix / 16 || sr.page0 != page) return "first page";
                 page += (sr.own + 15) / 16 * hk;

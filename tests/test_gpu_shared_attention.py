@@ -105,6 +105,24 @@ def test_rows_of_a_group(ppas, hq, hk, rows):
     b.check(b.call(ppas))
 
 
+@pytest.mark.parametrize("rows,prefix", [(1, 4096), (1, 4112), (1, 9040), (2, 688), (2, 704), (2, 1040), (3, 1040),
+                                         (8, 80), (8, 96), (8, 112)])
+@pytest.mark.parametrize("hq,hk", GEOMETRIES)
+def test_few_rows_of_a_prefix(ppas, rows, prefix, hq, hk):
+    """Both sides of the lengths from which few rows read their prefix as one."""
+    b = Batch(hq, hk, [rows, 1, rows], [prefix, 32, prefix + 16], [1 + 11 * r for r in range(2 * rows + 1)], seed=rows)
+    b.check(b.call(ppas))
+
+
+def test_long_own_keys(ppas):
+    """One row's long context without a prefix, and beside rows with a few keys: many
+    runs of one (row, kv-head), and runs of many."""
+    b = Batch(16, 2, [1], [0], [30001], seed=20)
+    b.check(b.call(ppas))
+    b = Batch(16, 2, [3, 20], [64, 2048], [9000, 1, 0] + [r % 4 for r in range(20)], seed=21)
+    b.check(b.call(ppas))
+
+
 @pytest.mark.parametrize("prefix", [16, 32, 112, 128, 144, 256, 400, 512, 1024, 2000, 5008])
 @pytest.mark.parametrize("hq,hk,rows", [(16, 2, 5), (32, 8, 40), (8, 8, 130)])
 def test_prefix_lengths(ppas, prefix, hq, hk, rows):
