@@ -449,7 +449,7 @@ ppas_status ppas_shared_attention_step(const void *q, const void *k_cache, const
  * A logit of -inf (a banned token) or NaN is never drawn; +inf counts
  * as the largest finite value.  A row with nothing else gives token -1, logprob -inf.
  * vocab at most 262144, else PPAS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op.
- * One launch (of thread-block clusters, up to 8 CTAs a row), with programmatic
+ * One launch (of thread-block clusters, up to 16 CTAs a row), with programmatic
  * stream serialization; no workspace.
  * ------------------------------------------------------------------------- */
 ppas_status ppas_sample_tokens(const void *logits, int32_t logits_are_bf16, int64_t row_stride, int32_t n_rows,

@@ -35,7 +35,7 @@ constexpr int kSBins = 1024;      // bins of z
 constexpr int kSFine = 512;       // bins of a bin's (x, index)
 constexpr int kSList = 512;       // tokens that the first CTA takes
 constexpr int kSIndexBits = 18;   // vocabularies of up to 2^18 tokens
-constexpr int kSMaxCluster = 8;
+constexpr int kSMaxCluster = 16;
 constexpr float kSFloor = -28.f;  // z below this: W = 0 (exp(-28) 2^40 < 1)
 constexpr int kSMaxCommands = 40;
 static_assert(kSMaxVocab == 1 << kSIndexBits, "index bits");
@@ -873,28 +873,74 @@ size_t sample_smem_bytes(int32_t chunk) {
     return (sizeof(SShared) + 15) / 16 * 16 + (static_cast<size_t>(chunk) + 12) * sizeof(float);
 }
 
-static std::atomic<uint64_t> g_sample_smem_set[2] = {};
+// two CTAs share an SM
+constexpr int kHalfSm = 115712;
+constexpr int kPortableCluster = 8;
+
+using SampleKernel = void (*)(SampleParams);
+SampleKernel sample_kernel_of(bool bf16, bool resident) {
+    return bf16 ? (resident ? sample_kernel<__nv_bfloat16, true> : sample_kernel<__nv_bfloat16, false>)
+                : (resident ? sample_kernel<float, true> : sample_kernel<float, false>);
+}
+
+// Sets the kernel's limits, once per device, and says whether the current device
+// runs it in clusters of kSMaxCluster (more than every device has to).
+cudaError_t prepare_sample(SampleKernel kernel, int which, bool *wide) {
+    static std::atomic<uint64_t> limit_set[4] = {}, yes[4] = {}, no[4] = {};
+    *wide = false;
+    cudaError_t e = ensure_smem_limit(kernel, kHalfSm, limit_set[which]);
+    int dev = 0;
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t{1} << dev : 0;
+    if (!bit || (no[which].load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    if (!(yes[which].load(std::memory_order_acquire) & bit)) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(kSMaxCluster);
+        cfg.blockDim = dim3(kSThreads);
+        cfg.dynamicSmemBytes = kHalfSm;
+        cudaLaunchAttribute a = {};
+        a.id = cudaLaunchAttributeClusterDimension;
+        a.val.clusterDim.x = kSMaxCluster;
+        a.val.clusterDim.y = a.val.clusterDim.z = 1;
+        cfg.attrs = &a;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            no[which].fetch_or(bit, std::memory_order_release);
+            return cudaSuccess;
+        }
+        yes[which].fetch_or(bit, std::memory_order_release);
+    }
+    *wide = true;
+    return cudaSuccess;
+}
 
 cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_t st) {
-    // two CTAs share an SM
-    constexpr int kHalfSm = 115712;
     const int64_t slots = 2 * static_cast<int64_t>(device_sm_count());
     auto chunk_of = [&](int32_t c) { return ((p.vocab + c - 1) / c + 7) / 8 * 8; };
-    // As many CTAs a row as one round holds (64 rows x 32003: 4 CTAs 20.2 us, 2 25.7,
-    // 8 27.9), and parts of at most 80 K logits: large batches in several rounds,
-    // whose passes then overlap and find more in L2 (256 x 152000: 154 us with 1
-    // CTA a row, 135 with 2 or 4, 161 with 8; 256 x 32003: 41.8, 46.0, 56.1).
+    auto fits = [&](int32_t c) { return sample_smem_bytes(chunk_of(c)) <= static_cast<size_t>(kHalfSm); };
+    // As many CTAs a row as one round holds, 2048 logits each at least (1 row x
+    // 152000: 16 CTAs 17.4 us, 8 20.5, 4 28.5; 8 rows 20.1, 25.3, 33.9; 64 x 32003: 4
+    // CTAs 21.0, 8 28.6, 2 25.7; 20 x 5000: 4 CTAs 13.7, 8 14.6, 16 21.7), and parts
+    // of at most 80 K logits: large batches in several rounds, whose passes then
+    // overlap and find more in L2 (256 x 152000: 154 us with 1 CTA a row, 131 with 2
+    // or 4, 161 with 8; 256 x 32003: 41, 46, 58).
     int32_t c = 1;
     while (c < kSMaxCluster &&
-           ((2 * c * static_cast<int64_t>(n_rows) <= slots && chunk_of(c) > 1024) || chunk_of(c) > 80 * 1024))
+           ((2 * c * static_cast<int64_t>(n_rows) <= slots && chunk_of(c) > 2048) || chunk_of(c) > 80 * 1024))
         c *= 2;
-    const bool resident = sample_smem_bytes(chunk_of(c)) <= static_cast<size_t>(kHalfSm);
-    const auto kernel = bf16 ? (resident ? sample_kernel<__nv_bfloat16, true> : sample_kernel<__nv_bfloat16, false>)
-                             : (resident ? sample_kernel<float, true> : sample_kernel<float, false>);
-    if (resident) {
-        const cudaError_t e = ensure_smem_limit(kernel, kHalfSm, g_sample_smem_set[bf16]);
-        if (e != cudaSuccess) return e;
+    bool resident = fits(c), wide = false;
+    cudaError_t e = prepare_sample(sample_kernel_of(bf16, resident), 2 * bf16 + resident, &wide);
+    if (e == cudaSuccess && c > kPortableCluster && !wide) {
+        c = kPortableCluster;
+        resident = fits(c);
+        e = prepare_sample(sample_kernel_of(bf16, resident), 2 * bf16 + resident, &wide);
     }
+    if (e != cudaSuccess) return e;
+    const SampleKernel kernel = sample_kernel_of(bf16, resident);
     p.chunk = chunk_of(c);
     const size_t smem = resident ? sample_smem_bytes(p.chunk) : sizeof(SShared);
     PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kSThreads), smem, st);
