@@ -119,9 +119,6 @@ __device__ __forceinline__ uint32_t atom_cluster_add(uint32_t a, uint32_t v) {
     asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
     return old;
 }
-// the cluster barrier in two halves
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait_acquire() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_cluster_u64(uint32_t a, uint64_t v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
@@ -459,8 +456,9 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         else return __bfloat162float(x);
     };
     // f(four values, index of the first in the row) over the part as it lies in
-    // global memory, kLoads x 16 bytes a thread under way
-    auto stream = [&](auto loads, auto &&f) {
+    // global memory, in batches of kLoads x 16 bytes a thread, all under way at
+    // once; then done(place of the batch in `tops`), where wanted(place) was true
+    auto stream = [&](auto loads, auto &&f, auto &&wanted, auto &&done) {
         constexpr int kLoads = decltype(loads)::value;
         // what is before the first and after the last boundary, a value a thread
         const int ends = head + n - tail0;
@@ -469,7 +467,9 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             const float x[4] = {widen(src[at]), -INFINITY, -INFINITY, -INFINITY};
             f(x, i0 + at);
         }
-        for (int v0 = tid; v0 < vecs; v0 += kLoads * kSThreads) {
+        int place = tid;
+        for (int v0 = tid; v0 < vecs; v0 += kLoads * kSThreads, place += kSThreads) {
+            if (!wanted(place)) continue;
             uint4 q[kLoads];
 #pragma unroll
             for (int k = 0; k < kLoads; ++k)
@@ -493,8 +493,11 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                     }
                 }
             }
+            done(place);
         }
     };
+    auto always = [](int) { return true; };
+    auto nothing = [](int) {};
     // a pass over the part once the maximum is known
     auto pass = [&](auto loads, auto &&f) {
         if constexpr (kResident) {
@@ -504,22 +507,29 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 f(x, i0 - pad + 4 * i);
             }
         } else {
-            stream(loads, f);
+            stream(loads, f, always, nothing);
         }
     };
-    float mx = -INFINITY, mn = INFINITY;
+    float mx = -INFINITY, mn = INFINITY, top = -INFINITY;
     // (a maximum passes over NaNs; the least of every fourth value will do to
     // spread the bins, for what is below goes to the last one)
     stream(Loads<4>{}, [&](const float(&x)[4], int at) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mx = fmaxf(mx, x[k]);
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, x[k]);
         if (x[0] > -INFINITY) mn = fminf(mn, x[0]);
         if constexpr (kResident) {
             const int to = at - i0 + pad;
             if (at - i0 < head || at - i0 >= tail0) xs[to] = x[0];
             else *reinterpret_cast<float4 *>(xs + to) = make_float4(x[0], x[1], x[2], x[3]);
         }
+    }, always, [&](int place) {
+        if constexpr (!kResident) {  // each batch's maximum, of which the gather makes use
+            xs[place] = top;
+            mx = fmaxf(mx, top);
+            top = -INFINITY;
+        }
     });
+    mx = fmaxf(mx, top);
     if constexpr (kResident) {
         if (tid < pad) xs[tid] = -INFINITY;
         if (tid < 4 * n4 - pad - n) xs[pad + n + tid] = -INFINITY;
@@ -751,15 +761,25 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                     s.lists[j][at] = (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(index);
             }
     };
+    // (resident or not: without the batches of which no logit is that large.  256 x
+    // 152000: 117.4 -> XXX us)
+    auto gather_pass = [&](auto &&f) {
+        if constexpr (kResident) {
+            pass(Loads<4>{}, f);
+        } else {
+            const float least = fminf(fminf(bins.x_lo[kCutK], bins.x_lo[kCutP]), bins.x_lo[kDraw]);
+            stream(Loads<4>{}, f, [&](int place) { return xs[place] >= least; }, nothing);
+        }
+    };
     if (bins.lo[kCutK] > bins.hi[kCutK] && bins.lo[kCutP] > bins.hi[kCutP]) {
         // (one range to compare with)
-        pass(Loads<4>{}, [&](const float(&x)[4], int first) {
+        gather_pass([&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if ((x[k] >= bins.x_lo[kDraw]) & (x[k] <= bins.x_hi[kDraw])) gather(x[k], first + k);
         });
     } else {
-        pass(Loads<4>{}, [&](const float(&x)[4], int first) {
+        gather_pass([&](const float(&x)[4], int first) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 bool maybe = false;  // (no short circuits: six comparisons take less than their branches)
@@ -785,7 +805,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
 #pragma unroll
     for (int j = 0; j < kStages; ++j) most = max(most, ld_cluster_u32(dsmem_addr(smem_u32(&s.ns[j]), 0)));
     if (most <= kSList) {
-        cluster_arrive();  // this CTA has read the first one's counts
+        cluster_arrive_relaxed();  // this CTA has read the first one's counts
         if (rank != 0) return;
         if (most <= kSRank) {
             rank_lists(s, row);
@@ -838,7 +858,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             }
             if (tid == 0) write_token();
         }
-        cluster_wait_acquire();
+        cluster_wait();
         return;
     }
     // ---- one search after the other, each bin divided while it holds too many tokens
@@ -940,6 +960,12 @@ size_t sample_smem_bytes(int32_t chunk) {
     return (sizeof(SShared) + 15) / 16 * 16 + (static_cast<size_t>(chunk) + 12) * sizeof(float);
 }
 
+// the maximum of each batch of the first pass (4 x 16 bytes a thread)
+size_t sample_stream_smem_bytes(int32_t chunk, bool bf16) {
+    const int32_t round = 4 * kSThreads * (bf16 ? 8 : 4);
+    return (sizeof(SShared) + 15) / 16 * 16 + static_cast<size_t>((chunk + round - 1) / round) * kSThreads * sizeof(float);
+}
+
 // two CTAs share an SM
 constexpr int kHalfSm = 115712;
 constexpr int kPortableCluster = 8;
@@ -1009,7 +1035,7 @@ cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_
     if (e != cudaSuccess) return e;
     const SampleKernel kernel = sample_kernel_of(bf16, resident);
     p.chunk = chunk_of(c);
-    const size_t smem = resident ? sample_smem_bytes(p.chunk) : sizeof(SShared);
+    const size_t smem = resident ? sample_smem_bytes(p.chunk) : sample_stream_smem_bytes(p.chunk, bf16);
     PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kSThreads), smem, st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
