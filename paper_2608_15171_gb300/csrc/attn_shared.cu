@@ -16,7 +16,7 @@
 // as 8 columns, on the CTAs after those of the pieces.
 // Every partial goes to the workspace in fp32 and a second launch joins them.
 //
-// Bound by HBM where prefixes and own keys are long (64 rows of 2k own keys after
+// Bound by HBM where prefixes and own keys are long (64 rows of up to 1000 own keys after
 // 30k shared, 32/8 heads: 53.5 us for 264 MB, 49 of them this launch), by the start
 // and end of two launches where they are short (32 rows after 25k, 16/2 heads: 17.6
 // us, of which the tiles take 4 and the join 4), and by the tensor cores in large

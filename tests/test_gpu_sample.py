@@ -154,6 +154,51 @@ def test_few_distinct_values(ppas):
         _check(y, rules, u, tokens, lp)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n", [1, 2, 31, 127, 128, 129, 300, 511, 512, 513, 1000])
+def test_tokens_of_one_value(ppas, n, bf16):
+    """n ties, some larger and many smaller logits: top-k, top-p and the draw all end inside the ties."""
+    v, reps = 20000, 8
+    g = np.random.default_rng(n)
+    x = np.full((reps, v), -math.inf, np.float32)
+    for r in range(reps):
+        at = g.permutation(v)
+        x[r, at[:n]] = 1.0
+        x[r, at[n:n + 5]] = [1.25, 1.5, 1.5, 2.0, 3.0]
+        x[r, at[n + 5:]] = -9.0 - g.integers(0, 64, v - n - 5) / 8
+    x = torch.from_numpy(x).cuda()
+    x = x.to(torch.bfloat16) if bf16 else x
+    rules = [(1.0, 0, 1.0, 0.0), (0.8, n // 2 + 6, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (1.0, n // 2 + 6, 0.95, 0.1)] * 2
+    u = np.array([0.5, 0.9, 0.97, 0.8, 0.9999, 0.99999, 0.999, 0.98], np.float32)
+    tokens, lp = _call(ppas, x, *zip(*rules), u)
+    for r in range(reps):
+        assert tokens[r] == _whole_numbers(x[r], *rules[r], u[r]), (r, rules[r])
+    _check(x, rules, u, tokens, lp)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("stride", [90000, 90003])
+def test_few_large_logits_in_long_rows(ppas, stride, bf16):
+    """Rows too many and long for shared memory, of nothing, NaN or far smaller logits but for a handful of
+    tokens at the start, the end and between: the passes over most of a row have nothing to find."""
+    n, v = 320, 90000
+    x = torch.full((n, stride), -math.inf, device="cuda", dtype=torch.bfloat16 if bf16 else torch.float32)
+    g = np.random.default_rng(6)
+    for r in range(n):
+        if r % 3 == 1:
+            x[r] = math.nan
+        elif r % 3 == 2:
+            x[r] = -20.0
+        where = g.choice([0, 1, 2, 3, 7, 8191, 8192, 8193, 44999, 45000, 45001, 65535, v - 9, v - 2, v - 1], 6,
+                         replace=False)
+        x[r, torch.from_numpy(where).cuda()] = torch.from_numpy(g.integers(-8, 9, 6) / 4).to(x)
+    rules = [RULES[r % len(RULES)] for r in range(n)]
+    u = g.random(n).astype(np.float32)
+    tokens, _ = _call(ppas, x[:, :v], *zip(*rules), u)
+    for r in range(n):
+        assert tokens[r] == _whole_numbers(x[r, :v], *rules[r], u[r]), (r, rules[r])
+
+
 def test_special_values(ppas):
     inf, nan = math.inf, math.nan
     low32, low16 = -3.4028234663852886e38, -3.3895313892515355e38
