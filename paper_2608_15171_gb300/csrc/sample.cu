@@ -40,7 +40,10 @@ constexpr int kSThreads = 512;
 constexpr int kSWarps = kSThreads / 32;
 constexpr int kSBins = 1024;      // bins of z
 constexpr int kSFine = 512;       // bins of a bin's (x, index)
-constexpr int kSList = 512;       // tokens that the first CTA takes
+// tokens of a search that the first CTA takes (64 rows of 152000 logits that vary by
+// 1: 42.3 us, with 512 of them 70.4; 1 row by 0.5: 19.4 and 29.3)
+constexpr int kSList = 1024;
+constexpr int kOfThread = 2;      // of these a thread has
 constexpr int kSRank = 128;       // tokens of a search that are ranked by comparing all pairs
 constexpr int kSIndexBits = 18;   // vocabularies of up to 2^18 tokens
 constexpr int kSMaxCluster = 16;
@@ -49,7 +52,7 @@ constexpr int kSMaxCommands = 40;
 enum { kCutK, kCutP, kDraw, kStages };  // the searches
 static_assert(kSMaxVocab == 1 << kSIndexBits, "index bits");
 static_assert(kSBins % (2 * kSMaxCluster) == 0 && kSFine % kSMaxCluster == 0 && kSBins == 2 * kSFine &&
-                  kSBins == 2 * kSThreads && kSFine == kSThreads && kSList <= kSThreads && kStages * kSRank <= kSThreads,
+                  kSBins == 2 * kSThreads && kSFine == kSThreads && kSList == kOfThread * kSThreads && kStages * kSRank <= kSThreads,
               "the scans give each thread two bins or one");
 
 enum : uint32_t { kDone, kGather, kDivide };
@@ -77,14 +80,11 @@ struct SShared {
             uint32_t cnt[kSBins], wl[kSBins], wh[kSBins];
         };
         uint64_t lists[kStages][kSList];  // places (key, index)
+        uint64_t list[kSList];            // tokens of a single search's bin
     };
     uint64_t sum_w[kSBins];                // first CTA: the bins' sums over the cluster, then their running sums
     uint32_t sum_c[kSBins];
-    // tokens of a single search's bin, or the running weights of each search's ranked ones
-    union {
-        uint64_t list[kSList];
-        uint64_t run_w[kStages][kSRank];
-    };
+    uint64_t run_w[kStages][kSRank];       // running weights of the ranked tokens
     // first CTA: the histogram of a list, or (place, weight) of the tokens to rank
     union {
         struct {
@@ -355,12 +355,12 @@ __device__ __forceinline__ void send(SShared &s, const SCommand &c, uint32_t cta
     dsmem_st_f32(a + offsetof(SCommand, x_hi), c.x_hi);
 }
 
-// Entry threadIdx.x of the cluster's n gathered tokens (lists of all_n(rank)
+// Entry `at` of the cluster's n gathered tokens (lists of all_n(rank)
 // tokens each, at the same place in every CTA); behind every token past them.
 template <class Count>
-__device__ __forceinline__ uint64_t list_entry(const uint64_t *list, uint32_t n, uint32_t ctas, Count all_n) {
-    if (threadIdx.x >= n) return ~uint64_t{0};
-    uint32_t at = threadIdx.x, r = 0;
+__device__ __forceinline__ uint64_t list_entry(const uint64_t *list, uint32_t at, uint32_t n, uint32_t ctas, Count all_n) {
+    if (at >= n) return ~uint64_t{0};
+    uint32_t r = 0;
     for (; r + 1 < ctas; ++r) {
         const uint32_t nr = all_n(r);
         if (at < nr) break;
@@ -369,17 +369,22 @@ __device__ __forceinline__ uint64_t list_entry(const uint64_t *list, uint32_t n,
     return ld_cluster_u64(dsmem_addr(smem_u32(list + at), r));
 }
 
-// Finds among n gathered tokens (one place v a thread, all within lo .. hi) the
-// one at which the target is reached, s.base_w and s.base_c being the sums before
+// Finds among n gathered tokens (places v, a thread's kSThreads apart, all within
+// lo .. hi) the one at which the target is reached, s.base_w and s.base_c being the sums before
 // them: got_w (the running weight up to it), got_mass, got_index, got_z.  Their
 // places are spread over kSFine bins, and the bin with the target again, until
 // it holds one token: mostly once or twice.  (Sorting 300 of them took 4 us,
 // bound by the shuffles; this takes 1.)
-__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t, uint64_t v, uint32_t n,
-                                            uint64_t lo, uint64_t hi) {
+__device__ __forceinline__ void search_list(SShared &s, const SRow &row, const STarget &t,
+                                            const uint64_t (&v)[kOfThread], uint32_t n, uint64_t lo, uint64_t hi) {
     const uint32_t i = threadIdx.x;
-    const float z = row.z(key_value(static_cast<uint32_t>(v >> kSIndexBits)));
-    const uint2 mass = SRow::weight2(expf(z));
+    float z[kOfThread];
+    uint2 mass[kOfThread];
+#pragma unroll
+    for (int k = 0; k < kOfThread; ++k) {
+        z[k] = row.z(key_value(static_cast<uint32_t>(v[k] >> kSIndexBits)));
+        mass[k] = SRow::weight2(expf(z[k]));
+    }
     if (i == 0) s.got_index = 0xFFFFFFFFu;
     uint64_t base_w = s.base_w, base_c = s.base_c;
     for (int level = 0; level < 8; ++level) {
@@ -388,11 +393,15 @@ __device__ __forceinline__ void search_list(SShared &s, const SRow &row, const S
         s.fine_c[i] = s.fine_l[i] = s.fine_h[i] = 0;
         if (i == 0) s.got_bin = 0xFFFFFFFFu;
         __syncthreads();
-        const bool in = i < n && lo <= v && v <= hi;
-        const uint32_t b = static_cast<uint32_t>((v - lo) >> shift);
-        if (in) {
-            atomicAdd(&s.fine_c[b], 1u);
-            add_weight(&s.fine_l[b], &s.fine_h[b], mass);
+        uint32_t b[kOfThread];
+#pragma unroll
+        for (int k = 0; k < kOfThread; ++k) {
+            const bool in = i + k * kSThreads < n && lo <= v[k] && v[k] <= hi;
+            b[k] = in ? static_cast<uint32_t>((v[k] - lo) >> shift) : 0xFFFFFFFFu;
+            if (in) {
+                atomicAdd(&s.fine_c[b[k]], 1u);
+                add_weight(&s.fine_l[b[k]], &s.fine_h[b[k]], mass[k]);
+            }
         }
         __syncthreads();
         const uint64_t own_w = s.fine_l[i] + (static_cast<uint64_t>(s.fine_h[i]) << 32);
@@ -412,11 +421,13 @@ __device__ __forceinline__ void search_list(SShared &s, const SRow &row, const S
         const uint32_t got = s.got_bin;
         if (got == 0xFFFFFFFFu) return;
         if (s.got_n == 1) {
-            if (in && b == got) {
-                s.got_mass = (static_cast<uint64_t>(mass.y) << 32) | mass.x;
-                s.got_index = static_cast<uint32_t>(v) & (kSMaxVocab - 1);
-                s.got_z = z;
-            }
+#pragma unroll
+            for (int k = 0; k < kOfThread; ++k)
+                if (b[k] == got) {
+                    s.got_mass = (static_cast<uint64_t>(mass[k].y) << 32) | mass[k].x;
+                    s.got_index = static_cast<uint32_t>(v[k]) & (kSMaxVocab - 1);
+                    s.got_z = z[k];
+                }
             __syncthreads();
             return;
         }
@@ -837,11 +848,10 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         if (tid < kStages) s.at[tid] = s.ns[tid] ? atom_cluster_add(dsmem_addr(smem_u32(&s.ns[tid]), 0), s.ns[tid]) : 0;
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kStages; ++j) {
-            const uint32_t at = s.at[j] + tid;
-            if (tid < static_cast<int>(min(s.ns[j], static_cast<uint32_t>(kSList))) && at < kSList)
-                st_cluster_u64(dsmem_addr(smem_u32(&s.lists[j][at]), 0), s.lists[j][tid]);
-        }
+        for (int j = 0; j < kStages; ++j)
+            for (uint32_t i = tid; i < min(s.ns[j], static_cast<uint32_t>(kSList)); i += kSThreads)
+                if (s.at[j] + i < kSList)
+                    st_cluster_u64(dsmem_addr(smem_u32(&s.lists[j][s.at[j] + i]), 0), s.lists[j][i]);
     }
     cluster_sync_all();
     uint32_t most = 0;
@@ -895,7 +905,8 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
                 next_target();
                 uint64_t lo, hi;
                 place_range<T>(s.bins.x_lo[j], fminf(s.bins.x_hi[j], row.top), lo, hi);
-                search_list(s, row, want, s.lists[j][tid], s.ns[j], lo, hi);
+                const uint64_t v[kOfThread] = {s.lists[j][tid], s.lists[j][tid + kSThreads]};
+                search_list(s, row, want, v, s.ns[j], lo, hi);
                 if (s.got_index == 0xFFFFFFFFu) break;
                 if (j < kDraw) sum = s.got_w;
             }
@@ -984,8 +995,10 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             send(s, c, ctas);
             continue;
         }
-        search_list(s, row, want, list_entry(s.list, total, ctas, [&](uint32_t q) { return s.all_n[q]; }), total, cmd.lo,
-                    cmd.hi);
+        auto n_of = [&](uint32_t q) { return s.all_n[q]; };
+        const uint64_t v[kOfThread] = {list_entry(s.list, tid, total, ctas, n_of),
+                                       list_entry(s.list, tid + kSThreads, total, ctas, n_of)};
+        search_list(s, row, want, v, total, cmd.lo, cmd.hi);
         if (s.got_index == 0xFFFFFFFFu || stage == kDraw) {
             if (tid == 0) write_token();
             send(s, c, ctas);  // kDone
