@@ -391,8 +391,8 @@ __device__ __forceinline__ void search_list(SShared &s, const SRow &row, const S
         const int bits = 64 - __clzll(static_cast<long long>(hi - lo));
         const int shift = bits > 9 ? bits - 9 : 0;  // kSFine parts of 2^shift places
         s.fine_c[i] = s.fine_l[i] = s.fine_h[i] = 0;
-        if (i == 0) s.got_bin = 0xFFFFFFFFu;
         __syncthreads();
+        if (i == 0) s.got_bin = 0xFFFFFFFFu;  // (every thread has read the one of the level before)
         uint32_t b[kOfThread];
 #pragma unroll
         for (int k = 0; k < kOfThread; ++k) {
