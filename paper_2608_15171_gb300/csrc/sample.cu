@@ -24,7 +24,7 @@
 // Few rows are bound by the chain of passes, exchanges and searches: 1 row x 152000
 // 12.8 us a call, 32 x 128000 bf16 20.5, 64 x 32003 15.3.  Many are bound by the
 // instructions of the histogram (about 25 a logit, of which exp is 8): 256 x 152000
-// in 105 us, 1.5 TB/s of the logits' own bytes.
+// in 106 us, 1.5 TB/s of the logits' own bytes.
 #include <float.h>
 #include <math.h>
 
