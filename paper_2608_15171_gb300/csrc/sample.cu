@@ -483,6 +483,8 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ctas = cluster_nctarank(), rank = ctas > 1 ? cluster_ctarank() : 0;
     const int32_t r = blockIdx.x / ctas;
+    // (the other half of this barrier is before the first store to another CTA)
+    cluster_arrive_relaxed();
     for (int b = tid; b < kSBins; b += kSThreads) s.cnt[b] = s.wl[b] = s.wh[b] = 0;
     grid_dep_launch();
     grid_dep_wait();
@@ -591,6 +593,9 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     }
     if (lane == 0) s.warp_range[warp] = make_float2(mx, mn);
     __syncthreads();
+    // every CTA of the cluster has started: its shared memory may be written
+    // (the pass over the logits hides the wait)
+    cluster_wait();
     if (tid < static_cast<int>(ctas)) {
         for (int w = 0; w < kSWarps; ++w) {
             mx = fmaxf(mx, s.warp_range[w].x);
