@@ -221,19 +221,22 @@ ppas_status check_lengths(int32_t n_groups, const int32_t *rows, const int32_t *
     const int32_t g = hq / hk;
     if (g != 1 && g != 2 && g != 4 && g != 8) return PPAS_ERR_UNSUPPORTED;
     if (hq / (g >= 2 ? 2 : 1) > 256) return PPAS_ERR_UNSUPPORTED;
+    // every group first: the number of contexts follows from all of them, and a
+    // context is read only where that many are there
     int64_t n = 0;
     for (int32_t i = 0; i < n_groups; ++i) {
         if (rows[i] < 1 || prefixes[i] < 0 || prefixes[i] % kPage != 0) return PPAS_ERR_INVALID_ARG;
+        n += rows[i];
+    }
+    if (n > INT32_MAX / 1024) return PPAS_ERR_UNSUPPORTED;
+    for (int32_t i = 0, r = 0; i < n_groups; ++i) {
         // a launch's table of pieces
         if (static_cast<int64_t>(hk) * least_pieces(std::min(prefixes[i], 65535 * kPrefillKT)) > kSharedMaxPieces)
             return PPAS_ERR_UNSUPPORTED;
-        if (n + rows[i] > INT32_MAX / 1024) return PPAS_ERR_UNSUPPORTED;
-        for (int32_t r = 0; r < rows[i]; ++r) {
-            const int32_t c = ctx[n + r];
-            if (c < 1 || c < prefixes[i]) return PPAS_ERR_INVALID_ARG;
-            if (c > 65535 * kPrefillKT) return PPAS_ERR_UNSUPPORTED;  // 16-bit KV tiles
+        for (const int32_t end = r + rows[i]; r < end; ++r) {
+            if (ctx[r] < 1 || ctx[r] < prefixes[i]) return PPAS_ERR_INVALID_ARG;
+            if (ctx[r] > 65535 * kPrefillKT) return PPAS_ERR_UNSUPPORTED;  // 16-bit KV tiles
         }
-        n += rows[i];
     }
     *n_rows = static_cast<int32_t>(n);
     return PPAS_OK;
