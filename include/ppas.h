@@ -446,8 +446,9 @@ ppas_status ppas_shared_attention_step(const void *q, const void *k_cache, const
  *   d_uniform     : device fp32 [n_rows] in [0, 1)
  *   d_tokens      : device int32 [n_rows]
  *   d_logprobs    : device fp32 [n_rows] or NULL
- * A logit of -inf (a banned token) or NaN is never drawn; +inf counts
- * as the largest finite value.  A row with nothing else gives token -1, logprob -inf.
+ * A logit of -inf (a banned token) or NaN is never drawn; +inf counts as the
+ * largest finite value of the logits' type.  A row with no other logit gives
+ * token -1, logprob -inf.
  * vocab at most 262144, else PPAS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op.
  * One launch (of thread-block clusters, up to 16 CTAs a row), with programmatic
  * stream serialization; no workspace.

@@ -139,6 +139,11 @@ __device__ __forceinline__ float key_value(uint32_t k) {
     return __uint_as_float((k >> 31) ? k : ~k & 0x7FFFFFFFu);
 }
 
+// The largest finite logit of type T, as which +inf counts.  (Of bf16 not FLT_MAX,
+// which is none of its values: place_range would leave it out.)
+template <class T>
+constexpr float kLargest = sizeof(T) == 4 ? FLT_MAX : 0x1.FEp127f;
+
 // The places of the logits of type T from x_hi down to x_lo.  (Of bf16 logits a
 // bin of z holds one value or two, of many tokens each: with the range closed
 // to them the first division tells tokens apart, and not 2^16 values that are
@@ -617,12 +622,13 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         }
         return;
     }
+    const float largest = fminf(mx, kLargest<T>);
     if (!(temperature > 0.f)) {  // the largest logit, the lowest index of several
         uint32_t first = 0xFFFFFFFFu;
         pass(Loads<4>{}, [&](const float(&x)[4], int at) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (x[k] == mx) first = min(first, static_cast<uint32_t>(at + k));
+                if (x[k] >= largest) first = min(first, static_cast<uint32_t>(at + k));
         });
         first = __reduce_min_sync(0xffffffffu, first);
         if (lane == 0) s.warp_c[warp] = first;
@@ -644,12 +650,12 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     const bool by_k = top_k > 0 && top_k < p.vocab, by_m = min_p > 0.f;
     const float ln_min_p = by_m ? logf(min_p) : -INFINITY;
     SRow row;
-    // all finite: +inf counts as the largest finite value, and so does 1 / T
-    row.top = fminf(mx, FLT_MAX);
+    // all finite, 1 / T too
+    row.top = largest;
     row.inv_t = fminf(1.f / temperature, FLT_MAX);
     mn = fminf(mn, row.top);
     // a logit as the passes see it (a NaN as -inf)
-    auto logit = [](float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); };
+    auto logit = [](float x) { return fminf(fmaxf(x, -INFINITY), kLargest<T>); };
     // (lowest * bin_scale is 1023 but for two roundings, so that no bin is past the last)
     row.lowest = fmaxf(row.z(mn), kSFloor);
     row.bin_scale = row.lowest < 0.f ? fminf((kSBins - 1.f) / -row.lowest, 1e30f) : 0.f;
@@ -985,6 +991,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             c.hi = min(cmd.hi, c.lo + (uint64_t{1} << cmd.shift) - 1);
             c.x_lo = key_value(static_cast<uint32_t>(c.hi >> kSIndexBits));
             c.x_hi = key_value(static_cast<uint32_t>(c.lo >> kSIndexBits));
+            if (c.x_hi >= kLargest<T>) c.x_hi = INFINITY;  // (the passes compare the logits as they are)
             if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
             send(s, c, ctas);
             continue;
