@@ -46,6 +46,7 @@ typedef int32_t ppas_status;
 /* codes a kernel writes to *d_err_flag (0 = no error) */
 #define PPAS_DEVERR_TIMEOUT 1       /* a bounded wait on a barrier ran out            */
 #define PPAS_DEVERR_BAD_INDEX 2     /* a slot or block id outside the cache           */
+#define PPAS_DEVERR_SEARCH 3        /* sampling found no token (a defect of its own)  */
 
 /* page geometry of the KV cache: 16 tokens per block */
 #define PPAS_PAGE_TOKENS 16
@@ -448,7 +449,8 @@ ppas_status ppas_shared_attention_step(const void *q, const void *k_cache, const
  *   d_logprobs    : device fp32 [n_rows] or NULL
  * A logit of -inf (a banned token) or NaN is never drawn; +inf counts as the
  * largest finite value of the logits' type.  A row with no other logit gives
- * token -1, logprob -inf.
+ * token -1, logprob -inf, and so does one whose search fails (which no input is
+ * known to bring about; *d_err_flag is then PPAS_DEVERR_SEARCH).
  * vocab at most 262144, else PPAS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op.
  * One launch (of thread-block clusters, up to 16 CTAs a row), with programmatic
  * stream serialization; no workspace.

@@ -48,6 +48,8 @@ constexpr int kSRank = 128;       // tokens of a search that are ranked by compa
 constexpr int kSIndexBits = 18;   // vocabularies of up to 2^18 tokens
 constexpr int kSMaxCluster = 16;
 constexpr float kSFloor = -28.f;  // z below this: W = 0 (exp(-28) 2^40 < 1)
+// A search divides its 50 bits of (x, index) by 2^9 until 2^10 places are left, at
+// most 5 times, and gathers before and after: three searches and the end take 34.
 constexpr int kSMaxCommands = 40;
 enum { kCutK, kCutP, kDraw, kStages };  // the searches
 static_assert(kSMaxVocab == 1 << kSIndexBits, "index bits");
@@ -712,6 +714,12 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
     STarget want = {};
     uint64_t sum = 0;  // S so far
     uint64_t m_sum = ~uint64_t{0};
+    // a search without a result, by one thread: no old token stays
+    auto found_none = [&]() {
+        report_error(p.err, PPAS_DEVERR_SEARCH);
+        p.tokens[r] = -1;
+        if (p.logprobs) p.logprobs[r] = -INFINITY;
+    };
     // the search that comes next: its stage, and what it has to reach
     auto next_target = [&]() {
         if (stage == kCutK && !(by_k && static_cast<uint32_t>(top_k) < s.sum_c[kSBins - 1])) stage = kCutP;
@@ -734,13 +742,13 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         c.bin = s.got_bin;
         row.bin_range(static_cast<int>(c.bin), c.x_lo, c.x_hi);
         place_range<T>(c.x_lo, fminf(c.x_hi, row.top), c.lo, c.hi);
-        if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
+        if (c.op == kDone && tid == 0) found_none();
         send(s, c, ctas);
     };
     // the token that was found, by one thread
     auto write_token = [&]() {
         if (s.got_index == 0xFFFFFFFFu) {
-            report_error(p.err, PPAS_DEVERR_TIMEOUT);
+            found_none();
             return;
         }
         p.tokens[r] = static_cast<int32_t>(s.got_index);
@@ -992,7 +1000,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
             c.x_lo = key_value(static_cast<uint32_t>(c.hi >> kSIndexBits));
             c.x_hi = key_value(static_cast<uint32_t>(c.lo >> kSIndexBits));
             if (c.x_hi >= kLargest<T>) c.x_hi = INFINITY;  // (the passes compare the logits as they are)
-            if (c.op == kDone && tid == 0) report_error(p.err, PPAS_DEVERR_TIMEOUT);
+            if (c.op == kDone && tid == 0) found_none();
             send(s, c, ctas);
             continue;
         }
@@ -1020,6 +1028,7 @@ __global__ void __launch_bounds__(kSThreads, 2) sample_kernel(const __grid_const
         stage = stage == kCutK ? kCutP : kDraw;
         next_search();
     }
+    if (rank == 0 && tid == 0) found_none();  // out of commands
 }
 static_assert(kSFine == 1 << 9, "shift of a divided range");
 

@@ -37,6 +37,7 @@ PPAS_ERR_UNSUPPORTED = -4
 PPAS_ERR_CUDA = -5
 PPAS_DEVERR_TIMEOUT = 1
 PPAS_DEVERR_BAD_INDEX = 2
+PPAS_DEVERR_SEARCH = 3
 PPAS_PAGE_TOKENS = 16
 PPAS_REQ_PENDING, PPAS_REQ_WAITING, PPAS_REQ_RUNNING, PPAS_REQ_FINISHED = 0, 1, 2, 3
 
