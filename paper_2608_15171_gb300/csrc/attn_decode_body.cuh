@@ -265,10 +265,12 @@ __device__ __forceinline__ void decode_cta(const CUtensorMap &tm_k, const CUtens
         }
         mx0 = fmaxf(m0, mx0);
         mx1 = fmaxf(m1, mx1);
-        const float al0 = ex2(m0 - mx0), al1 = ex2(m1 - mx1);
+        // (while every score so far is -inf, all weights are 0 and not 2^(-inf + inf))
+        const float s0 = mx0 == -INFINITY ? 0.f : mx0, s1 = mx1 == -INFINITY ? 0.f : mx1;
+        const float al0 = ex2(m0 - s0), al1 = ex2(m1 - s1);
         m0 = mx0;
         m1 = mx1;
-        const float e0 = ex2(x0 - m0), e1 = ex2(x1 - m1), e2 = ex2(x2 - m0), e3 = ex2(x3 - m1);
+        const float e0 = ex2(x0 - s0), e1 = ex2(x1 - s1), e2 = ex2(x2 - s0), e3 = ex2(x3 - s1);
         l0 = l0 * al0 + (e0 + e2);
         l1 = l1 * al1 + (e1 + e3);
 #pragma unroll
