@@ -324,8 +324,8 @@ ppas_status ppas_attention_step_noalloc(const void *q, const void *k_cache, cons
  * and dims from rotary_dim on are unchanged.  The rotated queries go to q_out,
  * the rotated keys and the values to the token's slot of the paged cache, as
  * ppas_kv_append stores them.  Arithmetic in fp32, rounded once to bf16; the
- * phase is reduced modulo one turn in 64-bit fixed point, so its error does
- * not grow with the position.
+ * phase is reduced modulo one turn in 64-bit fixed point: the angle is good to
+ * 2^-25 turn for every position and every finite frequency.
  *   q, k, v        : device bf16, head h of token t at x + t * x_stride +
  *                    h * head_dim (strides in elements, heads contiguous), so
  *                    the three may be columns of one fused projection

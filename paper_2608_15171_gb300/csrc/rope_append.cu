@@ -6,9 +6,10 @@
 // interleaved one, i < r/2; dims from r on pass through.
 //
 // The phase is kept as a fraction of a turn in 64-bit fixed point: f / 2 pi in
-// units of 2^-64 turn is computed exactly from f's 24-bit significand, its
-// product with the position wraps modulo one turn, and the top 32 bits go to
-// sincospif().  So the angle of any 32-bit position is good to 2^-25 turn,
+// units of 2^-64 turn comes from f's 24-bit significand and the digits of 1 / 2 pi,
+// its product with the position wraps modulo one turn (2^-31 turn off at the
+// most, for |t| <= 2^31), and the top 32 bits go to sincospif().
+// So the angle of any 32-bit position and any finite f is good to 2^-25 turn,
 // where t * f in fp32 is off by up to 0.004 rad at 131072.  (No 64-bit floating
 // point: its rate is low here.)
 //
@@ -34,17 +35,35 @@ constexpr int kRopeMaxDim = 512;     // head_dim: 16 values a lane
 // reads of 8 neighbouring lanes then hit all banks once
 constexpr int kUnitPitch = 10;
 
-// f / (2 pi) modulo 1 as a 64-bit fraction of a turn, f finite
+// 2^192 / (2 pi), rounded down
+constexpr uint64_t kInv2 = 0x28BE60DB9391054Aull, kInv1 = 0x7F09D5F47D4D3770ull, kInv0 = 0x36D8A5664F10E410ull;
+
+// f / (2 pi) modulo 1 as a 64-bit fraction of a turn, to 2^-63 turn, of f = m 2^-shift.
+// The digits of 1 / (2 pi) that matter are those which f's exponent moves to the 64
+// places behind the point (Payne and Hanek's reduction): 192 for the largest fp32
+// numbers.  For f of 2 and more, which are rare: as a call it leaves the kernel's time
+// as it is without it (2056 tokens 5.64 us, 5.93 inline).
+__device__ __noinline__ uint64_t turns_of_large(uint64_t m, int shift) {
+    // the product p3 p2 p1 p0 of m and the digits, the point in front of p2
+    const uint64_t c0 = __umul64hi(m, kInv0), p1 = m * kInv1 + c0;
+    const uint64_t c1 = __umul64hi(m, kInv1) + (p1 < c0 ? 1 : 0), p2 = m * kInv2 + c1;
+    const uint64_t p3 = __umul64hi(m, kInv2) + (p2 < c1 ? 1 : 0);
+    if (shift > 0) return (p2 >> shift) | (p3 << (64 - shift));
+    if (shift == 0) return p2;
+    if (shift > -64) return (p2 << -shift) | (p1 >> (64 + shift));
+    if (shift == -64) return p1;
+    return (p1 << (-shift - 64)) | (m * kInv0 >> (128 + shift));
+}
+
+// the same of any finite f; below 2 the first 64 digits do
 __device__ __forceinline__ uint64_t turns_per_position(float f) {
     const uint32_t b = __float_as_uint(f);
     const int e = static_cast<int>((b >> 23) & 0xFF);
     const uint64_t m = e ? ((b & 0x7FFFFFu) | 0x800000u) : (b & 0x7FFFFFu);
     const int shift = 150 - (e ? e : 1);  // f = m 2^-shift
-    // 2^64 / (2 pi), rounded down: 62 significant bits
-    constexpr uint64_t kInv2Pi = 0x28BE60DB9391054Aull;
-    const uint64_t lo = m * kInv2Pi, hi = __umul64hi(m, kInv2Pi);
+    const uint64_t lo = m * kInv2, hi = __umul64hi(m, kInv2);
     uint64_t t;
-    if (shift <= 0) t = shift > -64 ? lo << -shift : 0;
+    if (shift < 23) t = turns_of_large(m, shift);
     else if (shift < 64) t = (lo >> shift) | (hi << (64 - shift));
     else t = shift < 128 ? hi >> (shift - 64) : 0;
     return (b >> 31) ? 0 - t : t;
