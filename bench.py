@@ -45,10 +45,10 @@ HEADLINE_WORKLOAD = ("MBT 16384 low pressure: 25,000-token prompt planned into c
                      "plan + kv append + attention per layer")
 
 # DRAM traffic of one prefill-kernel launch measured by ncu, keyed by the
-# sha256 of the kernel's device code it was measured on (reported only while
-# that code is unchanged).
+# sha256 of the kernel's device code, headers included, it was measured on
+# (reported only while that code is unchanged).
 PREFILL_TRAFFIC = {
-    "9a920992b133d847": 83945216 + 27287296,   # ncu capture of one (16384, p=0) layer
+    "c25fb19df49305a1": 84055296 + 27506944,   # ncu capture of one (16384, p=0) layer
 }
 
 
@@ -61,20 +61,27 @@ def _peaks():
     return PEAKS_FALLBACK, "fallback"
 
 
-def _src_hash(name):
-    """Hash of a kernel source's device code: the text before its host
-    launchers (the first ``cudaError_t launch_`` definition), comments and
-    blank space removed, so that the ncu figures keyed by it stay valid across
-    comment and launcher edits and go null when the kernel's code changes."""
+def _device_code(name, headers):
+    """A kernel source's device code, comments and blank space removed: its text before the host launchers
+    (the first ``cudaError_t launch_`` definition), and that of the device headers (``*.cuh``) it includes."""
     with open(os.path.join(ROOT, "paper_2608_15171_gb300", "csrc", name), encoding="utf-8") as f:
         text = f.read()
     cut = text.find("\ncudaError_t launch_")
     if cut >= 0:
         text = text[:cut]
     text = re.sub(r"/\*.*?\*/", " ", text, flags=re.S)
-    text = re.sub(r"//[^\n]*", " ", text)
-    text = " ".join(text.split())
-    return hashlib.sha256(text.encode()).hexdigest()[:16]
+    text = " ".join(re.sub(r"//[^\n]*", " ", text).split())
+    for header in re.findall(r'#include "([^"]+\.cuh)"', text):
+        if header not in headers and os.path.exists(os.path.join(ROOT, "paper_2608_15171_gb300", "csrc", header)):
+            headers.append(header)
+            text += "\n" + _device_code(header, headers)
+    return text
+
+
+def _src_hash(name):
+    """Hash of a kernel source's device code and of its device headers', so that the ncu figures keyed by it
+    stay valid across comment and launcher edits and go null when the kernel's code changes."""
+    return hashlib.sha256(_device_code(name, []).encode()).hexdigest()[:16]
 
 
 class ClockSampler:
