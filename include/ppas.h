@@ -391,8 +391,9 @@ ppas_status ppas_rope_frequencies(int32_t kind, int32_t rotary_dim, double base,
  *   k_cache,v_cache: device bf16 [num_blocks, n_kv_heads, 16, head_dim],
  *                    16-byte aligned
  *   d_block_tables : device int32 [n_rows, max_blocks_per_seq]; the first
- *                    prefix / 16 entries of a group's rows are the same blocks
- *                    (those of its first row are read for all)
+ *                    prefix / 16 entries of a group's rows are the same blocks,
+ *                    written in every row (a short prefix is read by each row's
+ *                    own entries, a long one by those of one row for several)
  *   h_group_rows   : HOST int32 [n_groups], >= 1
  *   h_prefix_lens  : HOST int32 [n_groups], multiples of 16, 0 for none
  *   h_ctx_lens     : HOST int32 [n_rows], the row's whole context, prefix and
@@ -412,6 +413,8 @@ ppas_status ppas_rope_frequencies(int32_t kind, int32_t rotary_dim, double base,
  * 1024 units of (group, kv-head, 256 query rows), with programmatic stream
  * serialization.  Plans, and the workspace size, follow the current device's
  * SM count; a call's plan is kept for the next calls with the same lengths.
+ * Lengths are checked group by group before a context is read.  A key with a
+ * score of -inf has weight 0.
  * ------------------------------------------------------------------------- */
 size_t ppas_shared_attention_workspace_size(int32_t n_groups, const int32_t *h_group_rows,
                                             const int32_t *h_prefix_lens, const int32_t *h_ctx_lens,

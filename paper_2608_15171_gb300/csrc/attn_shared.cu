@@ -18,9 +18,10 @@
 //
 // Bound by HBM where prefixes and own keys are long (64 rows of up to 1000 own keys after
 // 30k shared, 32/8 heads: 53.5 us for 264 MB, 49 of them this launch), by the start
-// and end of two launches where they are short (32 rows after 25k, 16/2 heads: 17.6
-// us, of which the tiles take 4 and the join 4), and by the tensor cores in large
-// groups (512 rows after 25k: 86.6 us, 1213 TFLOP/s).
+// and end of two launches where they are short (32 rows after 25k, 16/2 heads: 17.7
+// us, of which the tiles take 4 and the join 4), and by the tensor cores of the SMs
+// that have a piece in large groups (512 rows after 25k: 88.7 us, 1195 TFLOP/s; 128
+// pieces of 49 tiles on 152 SMs).
 #include <math.h>
 
 #include "attn_decode_body.cuh"

@@ -22,9 +22,11 @@
 // rows) are divided so by the whole cluster first.
 //
 // Few rows are bound by the chain of passes, exchanges and searches: 1 row x 152000
-// 12.8 us a call, 32 x 128000 bf16 20.5, 64 x 32003 15.3.  Many are bound by the
-// instructions of the histogram (about 25 a logit, of which exp is 8): 256 x 152000
-// in 106 us, 1.5 TB/s of the logits' own bytes.
+// 12.7 us a call, 32 x 128000 bf16 20.2, 64 x 32003 15.4.  Many are bound by phases
+// that do not overlap: 256 x 152000 in 105 us, 1.5 TB/s of the logits' own bytes, at
+// 42 instructions a logit (25 of them the histogram's, of which exp is 8) with the
+// issue slots busy half of the time and DRAM a fifth of it, for the two CTAs of an SM
+// read, add up and gather in step, and 512 CTAs take two rounds of 304.
 #include <float.h>
 #include <math.h>
 
