@@ -45,7 +45,8 @@ typedef int32_t ppas_status;
 
 /* codes a kernel writes to *d_err_flag (0 = no error) */
 #define PPAS_DEVERR_TIMEOUT 1       /* a bounded wait on a barrier ran out            */
-#define PPAS_DEVERR_BAD_INDEX 2     /* a slot or block id outside the cache           */
+#define PPAS_DEVERR_BAD_INDEX 2     /* a slot or block id outside the cache, a token
+                                       outside the vocabulary                         */
 #define PPAS_DEVERR_SEARCH 3        /* sampling found no token (a defect of its own)  */
 
 /* page geometry of the KV cache: 16 tokens per block */
@@ -462,6 +463,97 @@ ppas_status ppas_sample_tokens(const void *logits, int32_t logits_are_bf16, int6
                                int32_t vocab, const float *d_temperature, const int32_t *d_top_k,
                                const float *d_top_p, const float *d_min_p, const float *d_uniform,
                                int32_t *d_tokens, float *d_logprobs, int32_t *d_err_flag, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Norms of queries and keys for each head, rotary positions and KV append in one
+ * pass (device): ppas_rope_append for models that normalise each query and key
+ * head before its rotation.  With a head x of head_dim values, every dim of it,
+ *   y_i = x_i w_i / sqrt(mean_j x_j^2 + eps),
+ * and y is then rotated and stored as ppas_rope_append does with x (the same
+ * arguments, layouts, limits and launches; values are stored as they are).
+ * Sums, norms and the rotation in fp32, rounded once to bf16.
+ *   d_q_weight, d_k_weight : device fp32 [head_dim], the weights w of query and
+ *                    of key heads; NULL for ones
+ *   eps            : finite, > 0
+ * Rows that move 16 bytes at a time (see ppas_rope_append) need weights on a
+ * 16-byte boundary too; others take a warp a row.  In place (q_out == q,
+ * contiguous rows) as there.
+ * ------------------------------------------------------------------------- */
+ppas_status ppas_norm_rope_append(const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                                  int64_t v_stride, const float *d_q_weight, const float *d_k_weight, float eps,
+                                  const int32_t *d_positions, const int32_t *d_slot_mapping, int32_t n_tokens,
+                                  const float *d_inv_freq, int32_t rotary_dim, int32_t interleaved, float factor,
+                                  void *q_out, void *k_cache, void *v_cache, int32_t num_blocks, int32_t n_q_heads,
+                                  int32_t n_kv_heads, int32_t head_dim, int32_t *d_err_flag, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a projection that they share
+ * (device).  The rows of x and y are the step's new tokens, sequences packed in
+ * order; those of sequence s, h_q_lens[s] of them, have adapter h_adapters[s].
+ * With A, B and scale of that adapter, and j the slice of column c:
+ *   out[t, c] = y[t, c] + scale * sum_r (sum_k x[t, k] A[j * rank + r, k]) B[c, r]
+ * and out[t] = y[t] for rows without an adapter (-1).  Slices are projections
+ * side by side (query, key and value), each with its own inner sums.  Products
+ * accumulate in fp32; the inner sums enter the second product as two bf16
+ * numbers (2^-17 relative); the result is rounded once to bf16.
+ *   x              : device bf16, row t at x + t * x_stride, [rows, hidden]
+ *   y, out         : device bf16, [rows, cols] with strides; out may be y (with
+ *                    the same stride), else they must not overlap; out must
+ *                    not overlap x
+ *   h_q_lens       : HOST int32 [n_seqs], >= 1
+ *   h_adapters     : HOST int32 [n_seqs], -1 or 0 .. n_adapters - 1; any number
+ *                    of sequences may have the same
+ *   a              : device bf16 [n_adapters, n_slices * rank, hidden]
+ *   b              : device bf16 [n_adapters, cols, rank]
+ *   d_scales       : device fp32 [n_adapters], or NULL (1)
+ *   h_slice_cols   : HOST int32 [n_slices], the columns of each slice; cols is
+ *                    their sum
+ *   d_err_flag     : device int32 or NULL; PPAS_DEVERR_TIMEOUT if a bounded wait
+ *                    runs out
+ * Pointers are 16-byte aligned, strides multiples of 8 and at least the row's
+ * width, else PPAS_ERR_INVALID_ARG.  Supported: hidden, rank and each slice's
+ * columns multiples of 8, rank up to 128 (smaller ones of some adapters padded
+ * with zeros), up to 4 slices, 2^24 rows, hidden and cols up to 2^24,
+ * n_adapters * n_slices * rank and n_adapters * cols below 2^31; otherwise
+ * PPAS_ERR_UNSUPPORTED.  n_seqs == 0 is a no-op.  A row's result depends on its
+ * own x, y and adapter alone, but for the order of its sums over k, which follows
+ * the step's size; equal calls give equal bits.  No workspace; launches with
+ * programmatic stream serialization.
+ * ------------------------------------------------------------------------- */
+ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const void *y, int64_t y_stride, void *out,
+                             int64_t out_stride, int32_t n_seqs, const int32_t *h_q_lens, const int32_t *h_adapters,
+                             const void *a, const void *b, const float *d_scales, int32_t n_adapters, int32_t hidden,
+                             int32_t n_slices, const int32_t *h_slice_cols, int32_t rank, int32_t *d_err_flag,
+                             void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Log probabilities of given tokens, entropy and top alternatives (device).  For
+ * a row x of logits with maximum M, z_i = x_i - M and S = sum_i exp(z_i):
+ *   log p_i = z_i - ln S,   entropy = -sum_i p_i log p_i = ln S - sum_i z_i p_i,
+ * natural logarithms, in fp32.
+ *   logits        : device fp32, or bf16 (logits_are_bf16 != 0), row r at
+ *                   logits + r * row_stride elements, any alignment
+ *   d_tokens      : device int32 [n_rows], or NULL (then d_logprobs is NULL too)
+ *   d_logprobs    : device fp32 [n_rows], log p of the row's given token; 0 for a
+ *                   negative token (none is asked for); -inf for one >= vocab
+ *                   (*d_err_flag is then PPAS_DEVERR_BAD_INDEX)
+ *   d_entropy     : device fp32 [n_rows] or NULL
+ *   n_top         : alternatives a row, 0 .. 32
+ *   d_top_tokens  : device int32 [n_rows, n_top], the tokens of the largest
+ *                   logits, descending, the lower index first of equal ones
+ *   d_top_logprobs: device fp32 [n_rows, n_top]
+ * (both may be NULL when n_top is 0).  As for ppas_sample_tokens a logit of -inf
+ * or NaN has probability 0 and is no alternative, +inf counts as the largest
+ * finite value of the logits' type; alternatives that a row does not have are
+ * token -1, log probability -inf.  A row with no other logit has entropy 0 and
+ * log probabilities -inf.  vocab at most 262144, else PPAS_ERR_UNSUPPORTED.
+ * n_rows == 0 is a no-op.  A row's answers do not depend on the other rows.  One
+ * launch, with programmatic stream serialization; no workspace.
+ * ------------------------------------------------------------------------- */
+ppas_status ppas_token_logprobs(const void *logits, int32_t logits_are_bf16, int64_t row_stride, int32_t n_rows,
+                                int32_t vocab, const int32_t *d_tokens, float *d_logprobs, float *d_entropy,
+                                int32_t n_top, int32_t *d_top_tokens, float *d_top_logprobs, int32_t *d_err_flag,
+                                void *stream);
 
 /* Failure-path check (device).  Launches one thread that waits, with a
  * limit of limit_us microseconds (1 .. 2,000,000), on a barrier nothing

@@ -345,6 +345,10 @@ struct RopeParams {
     int32_t n_tokens, num_blocks, n_q_heads, n_kv_heads, head_dim, rotary_dim, interleaved;
     // a warp's task: `iters` passes of 32 lanes over a token's head rows
     int32_t iters, tasks_per_token, n_tasks;
+    // norms of the query and key heads first (weights [head_dim], or NULL: ones)
+    int32_t norm;
+    const float *q_weight, *k_weight;
+    float eps, inv_dim;
 };
 cudaError_t launch_rope_append(RopeParams p, cudaStream_t st);
 
@@ -363,6 +367,51 @@ struct SampleParams {
     int32_t chunk;  // logits of a row in each CTA of its cluster, a multiple of 8
 };
 cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_t st);
+
+// ------------------------------------------------------------------ log probabilities
+constexpr int kLMaxTop = 32;      // alternatives of a row
+constexpr int kLMaxCluster = 16;  // CTAs of a row
+struct LogprobParams {
+    const void *logits;  // fp32 or bf16, row r at logits + r * row_stride
+    int64_t row_stride;
+    const int32_t *tokens;  // given, per row; or NULL
+    float *logprobs, *entropy;  // or NULL
+    int32_t *top_tokens;  // [n_rows, n_top]
+    float *top_logprobs;
+    int32_t *err;
+    int32_t vocab, n_top;
+};
+cudaError_t launch_token_logprobs(const LogprobParams &p, int32_t n_rows, bool bf16, cudaStream_t st);
+
+// ------------------------------------------------------------------ low-rank adapters
+constexpr int kAMaxSlices = 4;   // projections fused side by side
+constexpr int kAMaxRank = 128;
+constexpr int kAUnitRows = 16;   // rows of a unit
+// Rows of one adapter: n of them from row `first` on (or, listed, the rows
+// rows[first ..]); adapter -1: rows that are only copied.
+struct AdapterUnit {
+    int32_t first;
+    int32_t adapter;
+    int32_t n;
+    int32_t listed;
+};
+struct AdapterParams {
+    const __nv_bfloat16 *x, *y;
+    __nv_bfloat16 *out;
+    int64_t x_stride, y_stride, out_stride;
+    const __nv_bfloat16 *a;  // [n_adapters, n_slices * rank, hidden]
+    const __nv_bfloat16 *b;  // [n_adapters, cols, rank]
+    const float *scales;     // [n_adapters] or NULL
+    int32_t hidden, rank, n_slices, cols;
+    int32_t slice_at[kAMaxSlices + 1];  // first column of each slice; cols
+};
+struct AdapterPlan {
+    std::vector<AdapterUnit> units;
+    std::vector<int32_t> rows;  // of the listed units
+};
+// the units of sequences of q_lens rows with these adapters (-1: none); copies:
+// rows without an adapter have to be copied
+AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies);
 
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its

@@ -146,7 +146,84 @@ static PyObject *py_shared_attention_step(PyObject *self, PyObject *args) {
     return res;
 }
 
+/* norm_rope_append(q, k, v, q_stride, k_stride, v_stride, d_q_weight,
+ *                  d_k_weight, eps, d_positions, d_slot_mapping, n_tokens,
+ *                  d_inv_freq, rotary_dim, interleaved, factor, q_out, k_cache,
+ *                  v_cache, num_blocks, n_q_heads, n_kv_heads, head_dim,
+ *                  d_err_flag, stream) -> ppas_status */
+static PyObject *py_norm_rope_append(PyObject *self, PyObject *args) {
+    unsigned long long q, k, v, qw, kw, pos, slots, freq, qo, kc, vc, err, stream;
+    long long qs, ks, vs;
+    int n_tokens, rotary, inter, num_blocks, hq, hk, d;
+    float factor, eps;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KKKLLLKKfKKiKiifKKKiiiiKK", &q, &k, &v, &qs, &ks, &vs, &qw, &kw, &eps, &pos, &slots,
+                          &n_tokens, &freq, &rotary, &inter, &factor, &qo, &kc, &vc, &num_blocks, &hq, &hk, &d, &err,
+                          &stream))
+        return NULL;
+    const ppas_status st = ppas_norm_rope_append(
+        (const void *)(uintptr_t)q, (const void *)(uintptr_t)k, (const void *)(uintptr_t)v, qs, ks, vs,
+        (const float *)(uintptr_t)qw, (const float *)(uintptr_t)kw, eps, (const int32_t *)(uintptr_t)pos,
+        (const int32_t *)(uintptr_t)slots, n_tokens, (const float *)(uintptr_t)freq, rotary, inter, factor,
+        (void *)(uintptr_t)qo, (void *)(uintptr_t)kc, (void *)(uintptr_t)vc, num_blocks, hq, hk, d,
+        (int32_t *)(uintptr_t)err, (void *)(uintptr_t)stream);
+    return PyLong_FromLong((long)st);
+}
+
+/* adapter_add(x, x_stride, y, y_stride, out, out_stride, q_lens, adapters, a, b,
+ *             d_scales, n_adapters, hidden, slice_cols, rank, d_err_flag,
+ *             stream) -> ppas_status */
+static PyObject *py_adapter_add(PyObject *self, PyObject *args) {
+    unsigned long long x, y, out, a, b, scales, err, stream;
+    long long xs, ys, os;
+    int n_adapters, hidden, rank;
+    Py_buffer ql, ad, sc;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KLKLKLy*y*KKKiiy*iKK", &x, &xs, &y, &ys, &out, &os, &ql, &ad, &a, &b, &scales,
+                          &n_adapters, &hidden, &sc, &rank, &err, &stream))
+        return NULL;
+    PyObject *res = NULL;
+    if (int32_buffer(&ql, "q_lens") && int32_buffer(&ad, "adapters") && int32_buffer(&sc, "slice_cols")) {
+        if (ql.len != ad.len) {
+            res = PyLong_FromLong(PPAS_ERR_INVALID_ARG);
+        } else {
+            const ppas_status st = ppas_adapter_add(
+                (const void *)(uintptr_t)x, xs, (const void *)(uintptr_t)y, ys, (void *)(uintptr_t)out, os,
+                (int32_t)(ql.len / 4), (const int32_t *)ql.buf, (const int32_t *)ad.buf, (const void *)(uintptr_t)a,
+                (const void *)(uintptr_t)b, (const float *)(uintptr_t)scales, n_adapters, hidden,
+                (int32_t)(sc.len / 4), (const int32_t *)sc.buf, rank, (int32_t *)(uintptr_t)err,
+                (void *)(uintptr_t)stream);
+            res = PyLong_FromLong((long)st);
+        }
+    }
+    PyBuffer_Release(&ql);
+    PyBuffer_Release(&ad);
+    PyBuffer_Release(&sc);
+    return res;
+}
+
+/* token_logprobs(logits, logits_are_bf16, row_stride, n_rows, vocab, d_tokens,
+ *                d_logprobs, d_entropy, n_top, d_top_tokens, d_top_logprobs,
+ *                d_err_flag, stream) -> ppas_status */
+static PyObject *py_token_logprobs(PyObject *self, PyObject *args) {
+    unsigned long long x, tok, lp, ent, tt, tl, err, stream;
+    long long stride;
+    int bf16, n_rows, vocab, n_top;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "KiLiiKKKiKKKK", &x, &bf16, &stride, &n_rows, &vocab, &tok, &lp, &ent, &n_top, &tt, &tl,
+                          &err, &stream))
+        return NULL;
+    const ppas_status st = ppas_token_logprobs(
+        (const void *)(uintptr_t)x, bf16, stride, n_rows, vocab, (const int32_t *)(uintptr_t)tok,
+        (float *)(uintptr_t)lp, (float *)(uintptr_t)ent, n_top, (int32_t *)(uintptr_t)tt, (float *)(uintptr_t)tl,
+        (int32_t *)(uintptr_t)err, (void *)(uintptr_t)stream);
+    return PyLong_FromLong((long)st);
+}
+
 static PyMethodDef methods[] = {
+    {"norm_rope_append", py_norm_rope_append, METH_VARARGS, "ppas_norm_rope_append (see include/ppas.h)"},
+    {"adapter_add", py_adapter_add, METH_VARARGS, "ppas_adapter_add (see include/ppas.h)"},
+    {"token_logprobs", py_token_logprobs, METH_VARARGS, "ppas_token_logprobs (see include/ppas.h)"},
     {"shared_attention_step", py_shared_attention_step, METH_VARARGS,
      "ppas_shared_attention_step (see include/ppas.h)"},
     {"sample_tokens", py_sample_tokens, METH_VARARGS, "ppas_sample_tokens (see include/ppas.h)"},

@@ -20,6 +20,12 @@
 // pairs, so rotation needs no exchange and may run in place.  16384 tokens of 32/8
 // heads in 64.7 us (403 MB: 6.2 TB/s, 0.92 of a plain copy's rate); 2056 tokens of
 // 16/2 heads take 5.6 us and one token 4.6, what a call costs the host.
+//
+// With norms (kNorm) each query and key head x becomes x r w first, w a weight a
+// dim, r = 1 / sqrt(mean x^2 + eps), all in fp32 and rounded once behind the
+// rotation.  A row is in the registers of one warp, so its sum of squares takes a
+// few shuffles and no memory: the bytes are those of the rotation alone.
+#include <float.h>
 #include <math.h>
 
 #include "ppas_device.cuh"
@@ -82,6 +88,28 @@ __device__ __forceinline__ float2 unpack_bf16x2(uint32_t v) {
     return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
 }
 
+// sum of the squares of 8 values, each times `scale` first
+__device__ __forceinline__ float squares(uint4 v, float scale) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 x = unpack_bf16x2(w[k]);
+        const float a = x.x * scale, b = x.y * scale;
+        s = fmaf(a, a, fmaf(b, b, s));
+    }
+    return s;
+}
+
+// Heads whose squares pass the fp32 range (values from 1.8e19 on) are summed again
+// times this; the largest bf16 numbers then stay below 2^59, 512 squares of them in range.
+constexpr float kSquareScale = 0x1p-70f;
+
+// 1 / sqrt(mean + eps) of a head's sum of squares, or of the scaled one
+__device__ __forceinline__ float norm_factor(float sum, float scaled, float inv_dim, float eps) {
+    return sum <= FLT_MAX ? rsqrtf(fmaf(sum, inv_dim, eps)) : rsqrtf(scaled * inv_dim) * kSquareScale;
+}
+
 // where a token's keys and values go; -1: nowhere
 __device__ __forceinline__ int32_t checked_slot(const RopeParams &p, int32_t token, bool reports) {
     const int32_t slot = __ldg(p.slots + token);
@@ -97,7 +125,8 @@ __device__ __forceinline__ int32_t checked_slot(const RopeParams &p, int32_t tok
 struct RopeRow {
     const __nv_bfloat16 *src;
     __nv_bfloat16 *dst;  // NULL: not written
-    bool turns;
+    bool turns;           // (and has a norm)
+    bool is_q;
 };
 __device__ __forceinline__ RopeRow rope_row(const RopeParams &p, int32_t token, int32_t slot, int32_t row) {
     RopeRow r;
@@ -105,10 +134,11 @@ __device__ __forceinline__ RopeRow rope_row(const RopeParams &p, int32_t token, 
     if (row < p.n_q_heads) {
         r.src = p.q + t * p.q_stride + row * p.head_dim;
         r.dst = p.q_out + (t * p.n_q_heads + row) * p.head_dim;
-        r.turns = true;
+        r.turns = r.is_q = true;
         return r;
     }
     row -= p.n_q_heads;
+    r.is_q = false;
     r.turns = row < p.n_kv_heads;
     const int32_t h = r.turns ? row : row - p.n_kv_heads;
     r.src = r.turns ? p.k + t * p.k_stride + h * p.head_dim : p.v + t * p.v_stride + h * p.head_dim;
@@ -123,7 +153,7 @@ __device__ __forceinline__ RopeRow rope_row(const RopeParams &p, int32_t token, 
 }  // namespace
 
 // 16-byte accesses: rotary_dim a multiple of 16, every row 16-byte aligned.
-template <bool kInterleaved>
+template <bool kInterleaved, bool kNorm>
 __global__ void __launch_bounds__(kRopeWarps * 32) rope_append_kernel(const __grid_constant__ RopeParams p) {
     // the launch that follows may start its set-up now
     grid_dep_launch();
@@ -175,10 +205,84 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_append_kernel(const __gr
             cs[2 * k + 1] = make_float2(v.z, v.w);
         }
     }
+    float w[16];                    // (kNorm) the weights of the lane's two chunks
+    const float *w_of = nullptr;    // where they come from, once there are any
+    bool w_there = false;
 #pragma unroll
     for (int i = 0; i < kRopeMaxIter; ++i) {
+        if constexpr (kNorm) {
+            if (i >= p.iters) break;
+            // (every lane of the warp: a row's lanes are its units)
+            const bool mine = r[i].dst != nullptr;
+            auto row_sum = [&](float scale) {
+                float s = 0.f;
+                if (mine) s = squares(a[i], scale) + (cb < chunks ? squares(b[i], scale) : 0.f);
+                if ((units & (units - 1)) == 0) {
+                    for (int o = 1; o < units; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                    return s;
+                }
+                float all = 0.f;
+                for (int j = 0; j < units; ++j) all += __shfl_sync(0xffffffffu, s, (sub * units + j) & 31);
+                return all;
+            };
+            const float sum = row_sum(1.f);
+            const bool large = !(sum <= FLT_MAX);
+            const float scaled = __any_sync(0xffffffffu, large) ? row_sum(kSquareScale) : 0.f;
+            if (mine && r[i].turns) {
+                const float f = norm_factor(sum, scaled, p.inv_dim, p.eps);
+                const float *from = r[i].is_q ? p.q_weight : p.k_weight;
+                if (from != w_of || !w_there) {  // (queries come first: mostly once)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int chunk = h ? cb : ca;
+                        const bool there = from && chunk < chunks;
+                        const float4 *src = reinterpret_cast<const float4 *>(from + chunk * 8);
+                        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+                        const float4 w0 = there ? __ldg(src) : one, w1 = there ? __ldg(src + 1) : one;
+                        w[8 * h] = w0.x, w[8 * h + 1] = w0.y, w[8 * h + 2] = w0.z, w[8 * h + 3] = w0.w;
+                        w[8 * h + 4] = w1.x, w[8 * h + 5] = w1.y, w[8 * h + 6] = w1.z, w[8 * h + 7] = w1.w;
+                    }
+                    w_of = from;
+                    w_there = true;
+                }
+                const uint32_t xa[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, xb[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+                float fa[8], fb[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 v = unpack_bf16x2(xa[k]), u2 = unpack_bf16x2(xb[k]);
+                    fa[2 * k] = v.x * f * w[2 * k];
+                    fa[2 * k + 1] = v.y * f * w[2 * k + 1];
+                    fb[2 * k] = u2.x * f * w[8 + 2 * k];
+                    fb[2 * k + 1] = u2.y * f * w[8 + 2 * k + 1];
+                }
+                if (turned) {
+                    if constexpr (kInterleaved) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 c = cs[k], d = cs[k + 4];
+                            const float v0 = fa[2 * k], v1 = fa[2 * k + 1], u0 = fb[2 * k], u1 = fb[2 * k + 1];
+                            fa[2 * k] = v0 * c.x - v1 * c.y;
+                            fa[2 * k + 1] = v1 * c.x + v0 * c.y;
+                            fb[2 * k] = u0 * d.x - u1 * d.y;
+                            fb[2 * k + 1] = u1 * d.x + u0 * d.y;
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float v0 = fa[k], u0 = fb[k];
+                            fa[k] = v0 * cs[k].x - u0 * cs[k].y;
+                            fb[k] = u0 * cs[k].x + v0 * cs[k].y;
+                        }
+                    }
+                }
+                a[i] = make_uint4(pack_bf16x2(fa[0], fa[1]), pack_bf16x2(fa[2], fa[3]), pack_bf16x2(fa[4], fa[5]),
+                                  pack_bf16x2(fa[6], fa[7]));
+                b[i] = make_uint4(pack_bf16x2(fb[0], fb[1]), pack_bf16x2(fb[2], fb[3]), pack_bf16x2(fb[4], fb[5]),
+                                  pack_bf16x2(fb[6], fb[7]));
+            }
+        }
         if (!r[i].dst) continue;
-        if (turned && r[i].turns) {
+        if (!kNorm && turned && r[i].turns) {
             uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -236,10 +340,52 @@ __global__ void __launch_bounds__(256) rope_append_any_kernel(const __grid_const
     }
 }
 
+// The same with norms: a warp has a head row.
+__global__ void __launch_bounds__(256) norm_rope_append_any_kernel(const __grid_constant__ RopeParams p) {
+    grid_dep_launch();
+    grid_dep_wait();
+    const int lane = threadIdx.x & 31, half = p.rotary_dim / 2;
+    const int32_t n_rows = p.n_q_heads + 2 * p.n_kv_heads;
+    const int64_t total = static_cast<int64_t>(p.n_tokens) * n_rows;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); i < total;
+         i += static_cast<int64_t>(gridDim.x) * 8) {
+        const int32_t token = static_cast<int32_t>(i / n_rows), row = static_cast<int32_t>(i % n_rows);
+        const RopeRow r = rope_row(p, token, checked_slot(p, token, lane == 0), row);
+        if (!r.dst) continue;  // (the whole warp)
+        if (!r.turns) {
+            for (int e = lane; e < p.head_dim; e += 32) r.dst[e] = r.src[e];
+            continue;
+        }
+        auto row_sum = [&](float scale) {
+            float s = 0.f;
+            for (int e = lane; e < p.head_dim; e += 32) {
+                const float x = __bfloat162float(r.src[e]) * scale;
+                s = fmaf(x, x, s);
+            }
+            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            return s;
+        };
+        const float sum = row_sum(1.f);
+        const float f = norm_factor(sum, sum <= FLT_MAX ? 0.f : row_sum(kSquareScale), p.inv_dim, p.eps);
+        const float *const weight = r.is_q ? p.q_weight : p.k_weight;
+        const int32_t position = __ldg(p.positions + token);
+        auto normed = [&](int e) { return __bfloat162float(r.src[e]) * f * (weight ? __ldg(weight + e) : 1.f); };
+        __syncwarp();  // in place: every lane has read the row
+        for (int e = lane; e < half; e += 32) {
+            const int x = p.interleaved ? 2 * e : e, y = p.interleaved ? 2 * e + 1 : e + half;
+            const float2 cs = rope_angle(position, __ldg(p.inv_freq + e), p.factor);
+            const float fu = normed(x), fw = normed(y);
+            r.dst[x] = __float2bfloat16_rn(fu * cs.x - fw * cs.y);
+            r.dst[y] = __float2bfloat16_rn(fw * cs.x + fu * cs.y);
+        }
+        for (int e = 2 * half + lane; e < p.head_dim; e += 32) r.dst[e] = __float2bfloat16_rn(normed(e));
+    }
+}
+
 cudaError_t launch_rope_append(RopeParams p, cudaStream_t st) {
     auto on16 = [](const void *x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; };
     const bool wide = p.rotary_dim % 16 == 0 && p.q_stride % 8 == 0 && p.k_stride % 8 == 0 && p.v_stride % 8 == 0 &&
-                      on16(p.q) && on16(p.k) && on16(p.v) && on16(p.q_out);
+                      on16(p.q) && on16(p.k) && on16(p.v) && on16(p.q_out) && on16(p.q_weight) && on16(p.k_weight);
     const int64_t sms = device_sm_count();
     const int32_t n_rows = p.n_q_heads + 2 * p.n_kv_heads;
     const int32_t passes = (n_rows + 32 / ((p.head_dim + 15) / 16) - 1) / (32 / ((p.head_dim + 15) / 16));
@@ -254,8 +400,16 @@ cudaError_t launch_rope_append(RopeParams p, cudaStream_t st) {
         const size_t smem = static_cast<size_t>(kRopeWarps) * (p.rotary_dim / 16) * kUnitPitch * sizeof(float2);
         PdlLaunch l(dim3(static_cast<unsigned>((tasks + kRopeWarps - 1) / kRopeWarps)), dim3(kRopeWarps * 32), smem,
                     st);
-        return p.interleaved ? cudaLaunchKernelEx(&l.cfg, rope_append_kernel<true>, p)
-                             : cudaLaunchKernelEx(&l.cfg, rope_append_kernel<false>, p);
+        if (p.norm)
+            return p.interleaved ? cudaLaunchKernelEx(&l.cfg, rope_append_kernel<true, true>, p)
+                                 : cudaLaunchKernelEx(&l.cfg, rope_append_kernel<false, true>, p);
+        return p.interleaved ? cudaLaunchKernelEx(&l.cfg, rope_append_kernel<true, false>, p)
+                             : cudaLaunchKernelEx(&l.cfg, rope_append_kernel<false, false>, p);
+    }
+    if (p.norm) {
+        const int64_t warps = (static_cast<int64_t>(p.n_tokens) * n_rows + 7) / 8;
+        PdlLaunch l(dim3(static_cast<unsigned>(warps < sms * 16 ? warps : sms * 16)), dim3(256), 0, st);
+        return cudaLaunchKernelEx(&l.cfg, norm_rope_append_any_kernel, p);
     }
     const int64_t total = static_cast<int64_t>(p.n_tokens) * n_rows * (p.head_dim - p.rotary_dim / 2);
     const int64_t blocks = (total + 255) / 256;
@@ -301,12 +455,15 @@ extern "C" ppas_status ppas_rope_frequencies(int32_t kind, int32_t rotary_dim, d
     return PPAS_OK;
 }
 
-extern "C" ppas_status ppas_rope_append(const void *q, const void *k, const void *v, int64_t q_stride,
-                                        int64_t k_stride, int64_t v_stride, const int32_t *d_positions,
-                                        const int32_t *d_slot_mapping, int32_t n_tokens, const float *d_inv_freq,
-                                        int32_t rotary_dim, int32_t interleaved, float factor, void *q_out,
-                                        void *k_cache, void *v_cache, int32_t num_blocks, int32_t n_q_heads,
-                                        int32_t n_kv_heads, int32_t head_dim, int32_t *d_err_flag, void *stream) {
+namespace {
+
+// the checks and the launch of both entry points; norm: with q_weight, k_weight (or NULL) and eps
+ppas_status rope_call(const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                      int64_t v_stride, const int32_t *d_positions, const int32_t *d_slot_mapping, int32_t n_tokens,
+                      const float *d_inv_freq, int32_t rotary_dim, int32_t interleaved, float factor, void *q_out,
+                      void *k_cache, void *v_cache, int32_t num_blocks, int32_t n_q_heads, int32_t n_kv_heads,
+                      int32_t head_dim, int32_t *d_err_flag, void *stream, bool norm, const float *d_q_weight,
+                      const float *d_k_weight, float eps) {
     if (n_tokens < 0 || n_q_heads < 0 || n_kv_heads < 1 || head_dim < 8 || head_dim % 8 != 0 || num_blocks < 1)
         return PPAS_ERR_INVALID_ARG;
     if (rotary_dim < 0 || rotary_dim % 2 || rotary_dim > head_dim || !std::isfinite(factor))
@@ -323,6 +480,7 @@ extern "C" ppas_status ppas_rope_append(const void *q, const void *k, const void
     if (!on(q, 2) || !on(k, 2) || !on(v, 2) || !on(q_out, 2) || !on(k_cache, 16) || !on(v_cache, 16) ||
         !on(d_positions, 4) || !on(d_slot_mapping, 4) || !on(d_inv_freq, 4) || !on(d_err_flag, 4))
         return PPAS_ERR_INVALID_ARG;
+    if (!on(d_q_weight, 4) || !on(d_k_weight, 4)) return PPAS_ERR_INVALID_ARG;
     if (n_q_heads > 0 && q_out == q && q_stride != q_row) return PPAS_ERR_INVALID_ARG;  // in place: contiguous rows
     RopeParams p = {};
     if (n_q_heads > 0) {
@@ -348,5 +506,36 @@ extern "C" ppas_status ppas_rope_append(const void *q, const void *k, const void
     p.head_dim = head_dim;
     p.rotary_dim = rotary_dim;
     p.interleaved = interleaved ? 1 : 0;
+    p.norm = norm ? 1 : 0;
+    p.q_weight = d_q_weight;
+    p.k_weight = d_k_weight;
+    p.eps = eps;
+    p.inv_dim = 1.f / static_cast<float>(head_dim);
     return launch_rope_append(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PPAS_OK : PPAS_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" ppas_status ppas_rope_append(const void *q, const void *k, const void *v, int64_t q_stride,
+                                        int64_t k_stride, int64_t v_stride, const int32_t *d_positions,
+                                        const int32_t *d_slot_mapping, int32_t n_tokens, const float *d_inv_freq,
+                                        int32_t rotary_dim, int32_t interleaved, float factor, void *q_out,
+                                        void *k_cache, void *v_cache, int32_t num_blocks, int32_t n_q_heads,
+                                        int32_t n_kv_heads, int32_t head_dim, int32_t *d_err_flag, void *stream) {
+    return rope_call(q, k, v, q_stride, k_stride, v_stride, d_positions, d_slot_mapping, n_tokens, d_inv_freq,
+                     rotary_dim, interleaved, factor, q_out, k_cache, v_cache, num_blocks, n_q_heads, n_kv_heads,
+                     head_dim, d_err_flag, stream, false, nullptr, nullptr, 0.f);
+}
+
+extern "C" ppas_status ppas_norm_rope_append(const void *q, const void *k, const void *v, int64_t q_stride,
+                                             int64_t k_stride, int64_t v_stride, const float *d_q_weight,
+                                             const float *d_k_weight, float eps, const int32_t *d_positions,
+                                             const int32_t *d_slot_mapping, int32_t n_tokens, const float *d_inv_freq,
+                                             int32_t rotary_dim, int32_t interleaved, float factor, void *q_out,
+                                             void *k_cache, void *v_cache, int32_t num_blocks, int32_t n_q_heads,
+                                             int32_t n_kv_heads, int32_t head_dim, int32_t *d_err_flag, void *stream) {
+    if (!(eps > 0.f) || !std::isfinite(eps)) return PPAS_ERR_INVALID_ARG;
+    return rope_call(q, k, v, q_stride, k_stride, v_stride, d_positions, d_slot_mapping, n_tokens, d_inv_freq,
+                     rotary_dim, interleaved, factor, q_out, k_cache, v_cache, num_blocks, n_q_heads, n_kv_heads,
+                     head_dim, d_err_flag, stream, true, d_q_weight, d_k_weight, eps);
 }

@@ -46,7 +46,8 @@ EXPORTED = ("ppas_sched_create", "ppas_sched_destroy", "ppas_sched_free_blocks",
             "ppas_status_string", "ppas_abi_version", "ppas_attention_step_noalloc",
             "ppas_debug_wait_timeout", "ppas_attention_kernel_count", "ppas_gateup_pack",
             "ppas_gateup_swiglu", "ppas_rope_append", "ppas_rope_frequencies", "ppas_sample_tokens",
-            "ppas_shared_attention_workspace_size", "ppas_shared_attention_step")
+            "ppas_shared_attention_workspace_size", "ppas_shared_attention_step",
+            "ppas_norm_rope_append", "ppas_adapter_add", "ppas_token_logprobs")
 PPAS_ROPE_PLAIN, PPAS_ROPE_LINEAR, PPAS_ROPE_BASE, PPAS_ROPE_BANDS, PPAS_ROPE_RAMP = 0, 1, 2, 3, 4
 PPAS_NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024
 
@@ -115,6 +116,21 @@ _lib.ppas_sample_tokens.argtypes = [_c.c_void_p, _c.c_int32, _c.c_int64, _c.c_in
                                     _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p,
                                     _c.c_void_p, _c.c_void_p]
 _lib.ppas_sample_tokens.restype = _c.c_int32
+_lib.ppas_norm_rope_append.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64,
+                                       _c.c_void_p, _c.c_void_p, _c.c_float, _c.c_void_p, _c.c_void_p, _c.c_int32,
+                                       _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_float, _c.c_void_p, _c.c_void_p,
+                                       _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_void_p,
+                                       _c.c_void_p]
+_lib.ppas_norm_rope_append.restype = _c.c_int32
+_lib.ppas_adapter_add.argtypes = [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                  _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p,
+                                  _c.c_int32, _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_int32, _c.c_void_p,
+                                  _c.c_void_p]
+_lib.ppas_adapter_add.restype = _c.c_int32
+_lib.ppas_token_logprobs.argtypes = [_c.c_void_p, _c.c_int32, _c.c_int64, _c.c_int32, _c.c_int32, _c.c_void_p,
+                                     _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p,
+                                     _c.c_void_p]
+_lib.ppas_token_logprobs.restype = _c.c_int32
 _lib.ppas_attention_step.argtypes = [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_void_p,
                                      _c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int32,
                                      _c.c_float, _c.c_void_p, _c.c_int32, _c.c_void_p, _c.c_size_t,
@@ -377,6 +393,55 @@ def ppas_sample_tokens(logits, logits_are_bf16: bool, row_stride: int, n_rows: i
     _check(call(_ptr(logits), 1 if logits_are_bf16 else 0, int(row_stride), int(n_rows), int(vocab),
                 _ptr(d_temperature), _ptr(d_top_k), _ptr(d_top_p), _ptr(d_min_p), _ptr(d_uniform), _ptr(d_tokens),
                 _ptr(d_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_sample_tokens")
+
+
+def ppas_norm_rope_append(q, k, v, q_stride: int, k_stride: int, v_stride: int, d_q_weight, d_k_weight, eps: float,
+                          d_positions, d_slot_mapping, n_tokens: int, d_inv_freq, rotary_dim: int, interleaved: bool,
+                          factor: float, q_out, k_cache, v_cache, num_blocks: int, n_q_heads: int, n_kv_heads: int,
+                          head_dim: int, d_err_flag=None, stream=None) -> None:
+    if _fast is not None:
+        _check(_fast.norm_rope_append(_ptr(q), _ptr(k), _ptr(v), q_stride, k_stride, v_stride, _ptr(d_q_weight),
+                                      _ptr(d_k_weight), eps, _ptr(d_positions), _ptr(d_slot_mapping), n_tokens,
+                                      _ptr(d_inv_freq), rotary_dim, bool(interleaved), factor, _ptr(q_out),
+                                      _ptr(k_cache), _ptr(v_cache), num_blocks, n_q_heads, n_kv_heads, head_dim,
+                                      _ptr(d_err_flag), _stream(stream)), "ppas_norm_rope_append")
+        return
+    call = _lib.ppas_norm_rope_append
+    _check(call(_ptr(q), _ptr(k), _ptr(v), int(q_stride), int(k_stride), int(v_stride), _ptr(d_q_weight),
+                _ptr(d_k_weight), float(eps), _ptr(d_positions), _ptr(d_slot_mapping), int(n_tokens),
+                _ptr(d_inv_freq), int(rotary_dim), 1 if interleaved else 0, float(factor), _ptr(q_out), _ptr(k_cache),
+                _ptr(v_cache), int(num_blocks), int(n_q_heads), int(n_kv_heads), int(head_dim), _ptr(d_err_flag),
+                _stream(stream)), "ppas_norm_rope_append")
+
+
+def ppas_adapter_add(x, x_stride: int, y, y_stride: int, out, out_stride: int, q_lens, adapters, a, b, d_scales,
+                     n_adapters: int, hidden: int, slice_cols, rank: int, d_err_flag=None, stream=None) -> None:
+    ql, ad, sc = _i32(q_lens), _i32(adapters), _i32(slice_cols)
+    if ql.size != ad.size:
+        raise PpasError(PPAS_ERR_INVALID_ARG, "ppas_adapter_add")
+    if _fast is not None:
+        _check(_fast.adapter_add(_ptr(x), x_stride, _ptr(y), y_stride, _ptr(out), out_stride, ql, ad, _ptr(a), _ptr(b),
+                                 _ptr(d_scales), n_adapters, hidden, sc, rank, _ptr(d_err_flag), _stream(stream)),
+               "ppas_adapter_add")
+        return
+    call = _lib.ppas_adapter_add
+    _check(call(_ptr(x), int(x_stride), _ptr(y), int(y_stride), _ptr(out), int(out_stride), int(ql.size), _addr(ql),
+                _addr(ad), _ptr(a), _ptr(b), _ptr(d_scales), int(n_adapters), int(hidden), int(sc.size), _addr(sc),
+                int(rank), _ptr(d_err_flag), _stream(stream)), "ppas_adapter_add")
+
+
+def ppas_token_logprobs(logits, logits_are_bf16: bool, row_stride: int, n_rows: int, vocab: int, d_tokens, d_logprobs,
+                        d_entropy=None, n_top: int = 0, d_top_tokens=None, d_top_logprobs=None, d_err_flag=None,
+                        stream=None) -> None:
+    if _fast is not None:
+        _check(_fast.token_logprobs(_ptr(logits), bool(logits_are_bf16), row_stride, n_rows, vocab, _ptr(d_tokens),
+                                    _ptr(d_logprobs), _ptr(d_entropy), n_top, _ptr(d_top_tokens),
+                                    _ptr(d_top_logprobs), _ptr(d_err_flag), _stream(stream)), "ppas_token_logprobs")
+        return
+    call = _lib.ppas_token_logprobs
+    _check(call(_ptr(logits), 1 if logits_are_bf16 else 0, int(row_stride), int(n_rows), int(vocab), _ptr(d_tokens),
+                _ptr(d_logprobs), _ptr(d_entropy), int(n_top), _ptr(d_top_tokens), _ptr(d_top_logprobs),
+                _ptr(d_err_flag), _stream(stream)), "ppas_token_logprobs")
 
 
 def ppas_debug_wait_timeout(d_err_flag, limit_us: int, stream=None) -> None:
