@@ -371,6 +371,7 @@ cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_
 // ------------------------------------------------------------------ log probabilities
 constexpr int kLMaxTop = 32;      // alternatives of a row
 constexpr int kLMaxCluster = 16;  // CTAs of a row
+constexpr int kPortableLCluster = 8;
 struct LogprobParams {
     const void *logits;  // fp32 or bf16, row r at logits + r * row_stride
     int64_t row_stride;
@@ -380,6 +381,7 @@ struct LogprobParams {
     float *top_logprobs;
     int32_t *err;
     int32_t vocab, n_top;
+    int32_t chunk;  // logits of a row in each CTA of its cluster, a multiple of 16
 };
 cudaError_t launch_token_logprobs(const LogprobParams &p, int32_t n_rows, bool bf16, cudaStream_t st);
 
