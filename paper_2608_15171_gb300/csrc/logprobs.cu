@@ -19,6 +19,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "ppas_device.cuh"
 #include "ppas_internal.h"
 
@@ -27,12 +29,15 @@ namespace {
 
 constexpr int kLThreads = 256;
 constexpr int kLWarps = kLThreads / 32;
-constexpr int kLLoads = 4;       // 16-byte loads that a thread has under way
+constexpr int kLLoads = 4;       // 16-byte loads of a round, a thread
+constexpr int kLStages = 3;      // rounds that are under way
+constexpr int kLAnSm = 4;        // CTAs an SM holds
 constexpr int kLGroups = kLThreads / 2;
-constexpr int kLList = 1024;     // places of a list
+constexpr int kLList = 640;     // places of a list
+constexpr uint32_t kLFew = 64;   // lists that are ranked as they are
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLLimit = 0x1p22f;  // |x L| from here on: the whole numbers c have no room left
-constexpr float kLFloor = -200.f;   // 2^-200 is 0, and so is its product with -200
+constexpr float kLFloor = -1e30f;   // logits below count as this: 2^(x L - c) is 0, and 0 times x L - c too
 constexpr float kLRaise = 8.f;      // c follows logits that are 2^8 past it
 static_assert(kLMaxTop <= kLGroups, "each alternative has a group");
 
@@ -40,27 +45,39 @@ static_assert(kLMaxTop <= kLGroups, "each alternative has a group");
 template <class T>
 constexpr float kLLargest = sizeof(T) == 4 ? FLT_MAX : 0x1.FEp127f;
 
+template <class T>
+__device__ __forceinline__ float value_of(T x) {
+    if constexpr (sizeof(T) == 4) return x;
+    else return __bfloat162float(x);
+}
 // a logit as it counts: a NaN as -inf, +inf as the largest finite one, -0 as 0
 template <class T>
 __device__ __forceinline__ float logit_of(T x) {
-    float v;
-    if constexpr (sizeof(T) == 4) v = x;
-    else v = __bfloat162float(x);
-    return fminf(fmaxf(v, -INFINITY), kLLargest<T>) + 0.f;
+    return fminf(fmaxf(value_of(x), -INFINITY), kLLargest<T>) + 0.f;
 }
 
+// a logit as a whole number that ascends with it
+__device__ __forceinline__ uint32_t ascending(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return (b >> 31) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float of_ascending(uint32_t key) {
+    return __uint_as_float((key >> 31) ? key & 0x7FFFFFFFu : ~key);
+}
 // (x, index) as a whole number: larger logits first, of equal ones the lower index; never 0
 __device__ __forceinline__ uint64_t place_of(float x, uint32_t index) {
-    const uint32_t b = __float_as_uint(x);
-    const uint32_t key = (b >> 31) ? ~b : b | 0x80000000u;  // ascending with x
-    return (static_cast<uint64_t>(key) << 32) | (0xFFFFFFFFu - index);
+    return (static_cast<uint64_t>(ascending(x)) << 32) | (0xFFFFFFFFu - index);
 }
 __device__ __forceinline__ float place_logit(uint64_t place) {
-    const uint32_t key = static_cast<uint32_t>(place >> 32);
-    return __uint_as_float((key >> 31) ? key & 0x7FFFFFFFu : ~key);
+    return of_ascending(static_cast<uint32_t>(place >> 32));
 }
 __device__ __forceinline__ int32_t place_index(uint64_t place) {
     return static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(place));
+}
+
+// the rounds that raise the bound: 0, 1, 3, 7, ... where as many are to come
+__device__ __forceinline__ bool raises(int round, int rounds) {
+    return ((round + 1) & round) == 0 && (round == 0 || rounds >= 2 * (round + 1));
 }
 
 // what a CTA found in its part of a row: the maximum, and the sums relative to it
@@ -68,13 +85,18 @@ struct LPart {
     float top, s, t;
 };
 struct LShared {
+    union {
+        uint4 ring[kLStages][kLLoads][kLThreads];  // each thread's own logits under way
+        struct {
+            uint64_t kept[kLList];                  // of the list the places at or above the last bound
+            uint64_t all[kLMaxCluster * kLMaxTop];  // first CTA: every CTA's alternatives
+        };
+    };
     uint64_t list[kLList];    // places at or above the bound
-    uint64_t kept[kLList];    // of these the ones at or above the last bound
     uint64_t best[kLMaxTop];  // this CTA's alternatives, in order; 0: none
-    uint64_t all[kLMaxCluster * kLMaxTop];  // first CTA: every CTA's
     LPart parts[kLMaxCluster];
     union {
-        float group[kLGroups];
+        uint32_t group[kLGroups];
         uint64_t group_place[kLGroups];
     };
     uint64_t place[kLWarps];
@@ -97,44 +119,55 @@ __device__ __forceinline__ uint64_t block_max(LShared &sh, uint64_t v) {
     return v;
 }
 
+__device__ __forceinline__ void cluster_arrive() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void st_cluster_u64(uint32_t a, uint64_t v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 
-// The n-th largest of the groups' maxima, given every thread's.
+// The n-th largest of the groups' maxima (or a little less), given every thread's:
+// a warp takes the largest key out n times.
 __device__ __forceinline__ float bound_of(LShared &sh, float top, int n) {
+    constexpr uint32_t kIndex = kLGroups - 1;  // a key's low bits tell equal maxima apart
     const int tid = threadIdx.x;
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    if ((tid & 1) == 0) sh.group[tid >> 1] = top;
+    if ((tid & 1) == 0) sh.group[tid >> 1] = (ascending(top) & ~kIndex) | static_cast<uint32_t>(tid >> 1);
     __syncthreads();
-    if (tid < kLGroups) {
-        const float mine = sh.group[tid];
-        const float4 *g4 = reinterpret_cast<const float4 *>(sh.group);
-        int before = 0;
-#pragma unroll 8
-        for (int j = 0; j < kLGroups / 4; ++j) {
-            const float4 g = g4[j];
-            before += g.x > mine || (g.x == mine && 4 * j < tid);
-            before += g.y > mine || (g.y == mine && 4 * j + 1 < tid);
-            before += g.z > mine || (g.z == mine && 4 * j + 2 < tid);
-            before += g.w > mine || (g.w == mine && 4 * j + 3 < tid);
+    if (tid < 32) {
+        const uint4 g = reinterpret_cast<const uint4 *>(sh.group)[tid];
+        uint32_t a = max(g.x, g.y), b = min(g.x, g.y), c = max(g.z, g.w), d = min(g.z, g.w), u;
+        u = max(a, c), c = min(a, c), a = u;
+        u = max(b, d), d = min(b, d), b = u;
+        u = max(b, c), c = min(b, c), b = u;
+        uint32_t m = 0;
+        for (int i = 0; i < n; ++i) {
+            m = __reduce_max_sync(0xffffffffu, a);
+            if (a == m) a = b, b = c, c = d, d = 0;
         }
-        if (before == n - 1) sh.bound = mine;
+        m &= ~kIndex;
+        if (tid == 0) sh.bound = m <= ascending(-INFINITY) ? -INFINITY : of_ascending(m);
     }
     __syncthreads();
     return sh.bound;
 }
 
-// best[0 .. n) of the m places in `from` (a 0 is none), in order (0 where there are fewer)
+// best[0 .. n) of the m places in `from` (a 0 is none), in order (0 where there are
+// fewer): a place's rank is the number of larger ones, counted by several lanes.
 __device__ __forceinline__ void rank_places(const uint64_t *from, int m, uint64_t *best, int n) {
-    for (int i = threadIdx.x; i < n; i += kLThreads) best[i] = 0;
+    if (static_cast<int>(threadIdx.x) < n) best[threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < m; i += kLThreads) {
-        const uint64_t mine = from[i];
+    int lanes = 32;
+    while (lanes > 1 && m * lanes > kLThreads) lanes >>= 1;
+    const int l = threadIdx.x & (lanes - 1);
+    for (int base = 0; base < m; base += kLThreads / lanes) {
+        const int i = base + static_cast<int>(threadIdx.x) / lanes;
+        const uint64_t mine = i < m ? from[i] : 0;
         int before = 0;
 #pragma unroll 4
-        for (int j = 0; j < m; ++j) before += from[j] > mine;
-        if (before < n && mine != 0) best[before] = mine;
+        for (int j = l; j < m; j += lanes) before += from[j] > mine;
+        for (int o = lanes >> 1; o; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+        if (l == 0 && before < n && mine != 0) best[before] = mine;
     }
     __syncthreads();
 }
@@ -209,7 +242,7 @@ __device__ __noinline__ float2 slow_sums(const T *src, int n, float top) {
     return make_float2(s, t);
 }
 
-// the values of 16 bytes
+// the values of 16 bytes, as they are and for the sums (none below kLFloor, no NaN), and their maximum with `top`
 template <class T>
 __device__ __forceinline__ void widen(uint4 q, float (&x)[16 / sizeof(T)]) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -223,18 +256,75 @@ __device__ __forceinline__ void widen(uint4 q, float (&x)[16 / sizeof(T)]) {
         }
     }
 }
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <class T>
+__device__ __forceinline__ uint4 floored(uint4 q) {
+    if constexpr (sizeof(T) == 4) {
+        auto f = [](uint32_t w) { return __float_as_uint(fmaxf(__uint_as_float(w), kLFloor)); };
+        return make_uint4(f(q.x), f(q.y), f(q.z), f(q.w));
+    } else {
+        constexpr uint32_t kFloors = 0xF149F149u;  // twice -1e30 in bf16
+        return make_uint4(max_bf16x2(q.x, kFloors), max_bf16x2(q.y, kFloors), max_bf16x2(q.z, kFloors),
+                          max_bf16x2(q.w, kFloors));
+    }
+}
+// the maximum of 16 bytes' values, NaNs passed over: of bf16 the two halves' each
+template <class T>
+__device__ __forceinline__ uint32_t max_bits(uint4 q) {
+    if constexpr (sizeof(T) == 4)
+        return __float_as_uint(fmaxf(max3(__uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z)),
+                                     __uint_as_float(q.w)));
+    else return max_bf16x2(max_bf16x2(q.x, q.y), max_bf16x2(q.z, q.w));
+}
+template <class T>
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    else return max_bf16x2(a, b);
+}
+template <class T>
+__device__ __forceinline__ float max_value(uint32_t bits) {
+    if constexpr (sizeof(T) == 4) return fmaxf(__uint_as_float(bits), -INFINITY);
+    else return fmaxf(fmaxf(__uint_as_float(bits << 16), __uint_as_float(bits & 0xFFFF0000u)), -INFINITY);
+}
+// 16 bytes that are not all of the part, from its value `first` on: value by value, -inf where there is none
+template <class T>
+__device__ __noinline__ uint4 edge_vector(const T *src, int first, int n) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        auto bits = [&](int i) -> uint32_t {
+            const bool in = i >= 0 && i < n;
+            if constexpr (sizeof(T) == 4) return in ? __float_as_uint(src[i]) : 0xFF800000u;
+            else return in ? __bfloat16_as_ushort(src[i]) : 0xFF80u;
+        };
+        if constexpr (sizeof(T) == 4) w[k] = bits(first + k);
+        else w[k] = bits(first + 2 * k) | (bits(first + 2 * k + 1) << 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void copy16_async(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory");
+}
 
 }  // namespace
 
 template <class T, bool kTop>
 __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_constant__ LogprobParams p) {
-    __shared__ __align__(16) LShared sh;
+    extern __shared__ __align__(16) uint8_t logprob_smem[];
+    LShared &sh = *reinterpret_cast<LShared *>(logprob_smem);
     constexpr int kPer = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ctas = cluster_nctarank(), rank = ctas > 1 ? cluster_ctarank() : 0;
     const int64_t r = blockIdx.x / ctas;
-    // (the other half of this barrier is before the first store to another CTA)
-    cluster_arrive_relaxed();
     if (tid == 0) sh.n_list = sh.n_kept = 0;
     grid_dep_launch();
     grid_dep_wait();
@@ -250,39 +340,46 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     const int vecs = (pad + n + kPer - 1) / kPer;
     const int whole0 = pad ? 1 : 0, whole1 = (pad + n) / kPer;  // [whole0, whole1) have all their values
     const uint4 *const src4 = reinterpret_cast<const uint4 *>(src - pad);
-    auto load = [&](int v) {
-        if (v >= whole0 && v < whole1) return __ldg(src4 + v);
-        uint32_t w[4];  // the first and the last ones: value by value (and past them -inf)
+    // A thread's copies go to its own places of the ring, from which it alone reads:
+    // its own waits are all that it takes.
+    constexpr int kRound = kLThreads * kLLoads;
+    const int rounds = (vecs + kRound - 1) / kRound;
+    auto fetch = [&](int round, int stage) {
+        const int v0 = round * kRound;
+        if (v0 >= whole0 && v0 + kRound <= whole1) {
+            const uint4 *from = src4 + v0 + tid;
+            const uint32_t to = smem_u32(&sh.ring[stage][0][tid]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            auto bits = [&](int e) -> uint32_t {
-                const int i = v * kPer + e - pad;
-                const bool in = i >= 0 && i < n;
-                if constexpr (sizeof(T) == 4) return in ? __float_as_uint(src[i]) : 0xFF800000u;
-                else return in ? __bfloat16_as_ushort(src[i]) : 0xFF80u;
-            };
-            if constexpr (sizeof(T) == 4) w[k] = bits(k);
-            else w[k] = bits(2 * k) | (bits(2 * k + 1) << 16);
+            for (int k = 0; k < kLLoads; ++k) copy16_async(to + k * kLThreads * 16, from + k * kLThreads);
+        } else if (round < rounds) {
+#pragma unroll 1
+            for (int k = 0; k < kLLoads; ++k) {
+                const int v = v0 + k * kLThreads + tid;
+                if (v >= whole0 && v < whole1) copy16_async(smem_u32(&sh.ring[stage][k][tid]), src4 + v);
+                else sh.ring[stage][k][tid] = edge_vector(src, v * kPer - pad, n);
+            }
         }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        copies_commit();
     };
+#pragma unroll
+    for (int i = 0; i < kLStages - 1; ++i) fetch(i, i);
     float top = -INFINITY, c = -1e30f, s = 0.f, t = 0.f, bound = INFINITY;
     bool bad = false;
-    int rounds = 0;
-    for (int base = 0; base < vecs; base += kLThreads * kLLoads, ++rounds) {
+    for (int round = 0, stage = 0; round < rounds; ++round, stage = stage + 1 == kLStages ? 0 : stage + 1) {
+        fetch(round + kLStages - 1, stage == 0 ? kLStages - 1 : stage - 1);
+        copies_wait<kLStages - 1>();
         uint4 q[kLLoads];
 #pragma unroll
-        for (int k = 0; k < kLLoads; ++k) q[k] = load(base + k * kLThreads + tid);
-        float here = -INFINITY;  // (a maximum passes over NaNs)
+        for (int k = 0; k < kLLoads; ++k) q[k] = sh.ring[stage][k][tid];
+        uint32_t most[kLLoads], all = 0;
 #pragma unroll
         for (int k = 0; k < kLLoads; ++k) {
-            float x[kPer];
-            widen<T>(q[k], x);
-#pragma unroll
-            for (int e = 0; e < kPer; e += 2) here = max3(here, x[e], x[e + 1]);
+            most[k] = max_bits<T>(q[k]);
+            all = k ? max_bits<T>(all, most[k]) : most[k];
         }
+        const float here = max_value<T>(all);
         top = fmaxf(top, here);
-        if (kTop && (rounds & (rounds + 1)) == 0) bound = bound_of(sh, top, p.n_top);
+        if (kTop && raises(round, rounds)) bound = bound_of(sh, top, p.n_top);
         if (here * kLog2E - c > kLRaise) {  // (not where all are -inf)
             bad = bad || !(fabsf(here) * kLog2E < kLLimit);
             const float now = ceilf(here * kLog2E), d = now - c, f = ex2(-d);
@@ -294,12 +391,10 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
 #pragma unroll
         for (int k = 0; k < kLLoads; ++k) {
             float x[kPer];
-            widen<T>(q[k], x);
+            widen<T>(floored<T>(q[k]), x);
 #pragma unroll
             for (int e = 0; e < kPer; e += 2) {
-                float2 z = fma2(make_float2(x[e], x[e + 1]), make_float2(kLog2E, kLog2E), make_float2(-c, -c));
-                z.x = fmaxf(z.x, kLFloor);
-                z.y = fmaxf(z.y, kLFloor);
+                const float2 z = fma2(make_float2(x[e], x[e + 1]), make_float2(kLog2E, kLog2E), make_float2(-c, -c));
                 const float2 w = make_float2(ex2(z.x), ex2(z.y));
                 s2 = add2(s2, w);
                 t2 = fma2(z, w, t2);
@@ -307,22 +402,38 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         }
         s += s2.x + s2.y;
         t += t2.x + t2.y;
-        if (kTop && here >= bound && here > -INFINITY) {
+        if (kTop) {
+            // the logits at or above the bound go to the list: the warp looks through the
+            // values of one of its lanes after another (a lane by itself through its own: a
+            // few of them at a time keep the whole warp, and 256 x 152000 takes 36.5 us)
+            uint32_t hits = __ballot_sync(0xffffffffu, here >= bound && here > -INFINITY);
+            if (hits) {
+                constexpr int kValues = kLLoads * kPer;
+                __syncwarp();
+                do {
+                    const int from = (tid & ~31) + __ffs(hits) - 1;
+                    hits &= hits - 1;
 #pragma unroll
-            for (int k = 0; k < kLLoads; ++k) {
-                float x[kPer];
-                widen<T>(q[k], x);
-#pragma unroll
-                for (int e = 0; e < kPer; ++e)
-                    if (x[e] >= bound && x[e] > -INFINITY) {
-                        const uint32_t at = atomicAdd(&sh.n_list, 1u);
-                        if (at < kLList)
-                            sh.list[at] = place_of(x[e] + 0.f, static_cast<uint32_t>(
-                                                                  i0 + (base + k * kLThreads + tid) * kPer + e - pad));
+                    for (int j0 = 0; j0 < kValues; j0 += 32) {
+                        const int j = j0 + lane, k = j / kPer, e = j % kPer;
+                        if (j < kValues) {
+                            const float x = value_of(reinterpret_cast<const T *>(&sh.ring[stage][k][from])[e]);
+                            if (x >= bound && x > -INFINITY) {
+                                const uint32_t at = atomicAdd(&sh.n_list, 1u);
+                                const int index = i0 + ((round * kLLoads + k) * kLThreads + from) * kPer + e - pad;
+                                if (at < kLList) sh.list[at] = place_of(x + 0.f, static_cast<uint32_t>(index));
+                            }
+                        }
                     }
+                } while (hits);
+                __syncwarp();
             }
         }
     }
+    __syncthreads();  // (the ring's memory has other uses from here on)
+    // the first CTA's ring may take the others' finds once every CTA is here (the other
+    // half of this barrier is before the first store to it)
+    cluster_arrive();
 
     // ---- the part's maximum and sums
     float part_top = top;
@@ -358,18 +469,23 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         } else if (m > kLList || part_bad) {
             slow_top(sh, src, n, i0, p.n_top);
         } else {
-            const float last = (rounds & (rounds - 1)) == 0 ? bound : bound_of(sh, top, p.n_top);
-            for (uint32_t i = tid; i < m; i += kLThreads) {
-                const uint64_t v = sh.list[i];
-                if (place_logit(v) >= last) sh.kept[atomicAdd(&sh.n_kept, 1u)] = v;
+            const uint64_t *from = sh.list;
+            uint32_t left = m;
+            if (m > kLFew) {  // without those that only an earlier bound let in
+                for (uint32_t i = tid; i < m; i += kLThreads) {
+                    const uint64_t v = sh.list[i];
+                    if (place_logit(v) >= bound) sh.kept[atomicAdd(&sh.n_kept, 1u)] = v;
+                }
+                __syncthreads();
+                from = sh.kept;
+                left = sh.n_kept;
             }
-            __syncthreads();
-            rank_places(sh.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
+            rank_places(from, static_cast<int>(left), sh.best, p.n_top);
         }
     }
     __syncthreads();
     // ---- the first CTA joins the parts
-    cluster_wait();  // every CTA of the cluster has started
+    cluster_wait();
     if (tid == 0) {
         s = t = 0.f;
         for (int w = 0; w < kLWarps; ++w) {
@@ -402,13 +518,23 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     if (kTop) {
         const uint64_t *found = sh.best;
         if (ctas > 1) {
-            rank_places(sh.all, static_cast<int>(ctas) * p.n_top, sh.kept, p.n_top);
-            found = sh.kept;
+            // the n-th largest of all is at least the least of every CTA's (n / CTAs)-th
+            const int at = (p.n_top + static_cast<int>(ctas) - 1) / static_cast<int>(ctas) - 1;
+            const uint32_t least = __reduce_min_sync(
+                0xffffffffu, static_cast<uint32_t>(sh.all[min(lane, static_cast<int>(ctas) - 1) * p.n_top + at] >> 32));
+            if (tid == 0) sh.n_kept = 0;
+            __syncthreads();
+            for (int i = tid; i < static_cast<int>(ctas) * p.n_top; i += kLThreads) {
+                const uint64_t v = sh.all[i];
+                if (v != 0 && static_cast<uint32_t>(v >> 32) >= least) sh.kept[atomicAdd(&sh.n_kept, 1u)] = v;
+            }
+            __syncthreads();
+            rank_places(sh.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
         }
+        const uint64_t mine = tid < p.n_top ? found[tid] : 0;
         if (tid < p.n_top) {
-            const uint64_t v = found[tid];
-            p.top_tokens[r * p.n_top + tid] = v ? place_index(v) : -1;
-            p.top_logprobs[r * p.n_top + tid] = v ? place_logit(v) - m - ln_s : -INFINITY;
+            p.top_tokens[r * p.n_top + tid] = mine ? place_index(mine) : -1;
+            p.top_logprobs[r * p.n_top + tid] = mine ? place_logit(mine) - m - ln_s : -INFINITY;
         }
     }
     if (tid == 0) {
@@ -422,14 +548,60 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     }
 }
 
-template <class T>
+static_assert(kLMaxCluster * kLMaxTop <= kLList, "the first CTA ranks them in `kept`");
+static_assert(kLAnSm * (sizeof(LShared) + 1024) <= 233472, "shared memory of an SM");
+
+// A kernel's shared memory limit, and whether this device holds a cluster of
+// kLMaxCluster of its CTAs (more than the portable 8); once per device.
+template <class T, bool kTop>
+cudaError_t prepare_logprobs(bool *wide) {
+    const auto kernel = token_logprobs_kernel<T, kTop>;
+    static std::atomic<uint64_t> limit_set{0}, yes{0}, no{0};
+    *wide = false;
+    cudaError_t e = ensure_smem_limit(kernel, sizeof(LShared), limit_set);
+    int dev = 0;
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t{1} << dev : 0;
+    if (!bit || (no.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    if (!(yes.load(std::memory_order_acquire) & bit)) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(kLMaxCluster);
+        cfg.blockDim = dim3(kLThreads);
+        cfg.dynamicSmemBytes = sizeof(LShared);
+        cudaLaunchAttribute a = {};
+        a.id = cudaLaunchAttributeClusterDimension;
+        a.val.clusterDim.x = kLMaxCluster;
+        a.val.clusterDim.y = a.val.clusterDim.z = 1;
+        cfg.attrs = &a;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            no.fetch_or(bit, std::memory_order_release);
+            return cudaSuccess;
+        }
+        yes.fetch_or(bit, std::memory_order_release);
+    }
+    *wide = true;
+    return cudaSuccess;
+}
+
+template <class T, bool kTop>
 cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
-    // as many CTAs a row as the SMs hold at a time, 4096 logits each at least
-    const int64_t slots = 4 * static_cast<int64_t>(device_sm_count());
+    // As many CTAs a row as the SMs hold at a time, 4096 logits each at least
+    // (64 x 32003 bf16: 8 CTAs 6.4 us, 4 7.3; 1 x 152000: 16 CTAs 9.5, 8 11.0; 256 x
+    // 152000: 2 CTAs 33.6, 1 41.7; 4, in two rounds, 44.6).
+    bool wide = false;
+    const cudaError_t e = prepare_logprobs<T, kTop>(&wide);
+    if (e != cudaSuccess) return e;
+    const int64_t slots = kLAnSm * static_cast<int64_t>(device_sm_count());
+    const int32_t most = wide ? kLMaxCluster : kPortableLCluster;
     int32_t c = 1;
-    while (c < kPortableLCluster && 2 * c * static_cast<int64_t>(n_rows) <= slots && p.vocab >= 2 * c * 4096) c *= 2;
+    while (c < most && 2 * c * static_cast<int64_t>(n_rows) <= slots && p.vocab >= 2 * c * 4096) c *= 2;
     p.chunk = ((p.vocab + c - 1) / c + 15) / 16 * 16;
-    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), 0, st);
+    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), sizeof(LShared), st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
         attrs[1].id = cudaLaunchAttributeClusterDimension;
@@ -439,12 +611,13 @@ cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
         l.cfg.attrs = attrs;
         l.cfg.numAttrs = 2;
     }
-    return p.n_top > 0 ? cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, true>, p)
-                       : cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, false>, p);
+    return cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, kTop>, p);
 }
 
 cudaError_t launch_token_logprobs(const LogprobParams &p, int32_t n_rows, bool bf16, cudaStream_t st) {
-    return bf16 ? launch_logprobs<__nv_bfloat16>(p, n_rows, st) : launch_logprobs<float>(p, n_rows, st);
+    if (p.n_top > 0)
+        return bf16 ? launch_logprobs<__nv_bfloat16, true>(p, n_rows, st) : launch_logprobs<float, true>(p, n_rows, st);
+    return bf16 ? launch_logprobs<__nv_bfloat16, false>(p, n_rows, st) : launch_logprobs<float, false>(p, n_rows, st);
 }
 
 }  // namespace ppas
