@@ -24,7 +24,8 @@
 // With norms (kNorm) each query and key head x becomes x r w first, w a weight a
 // dim, r = 1 / sqrt(mean x^2 + eps), all in fp32 and rounded once behind the
 // rotation.  A row is in the registers of one warp, so its sum of squares takes a
-// few shuffles and no memory: the bytes are those of the rotation alone.
+// few shuffles and no memory: the bytes are those of the rotation alone.  16384 tokens
+// of 32/8 heads in 68.4 us (5.9 TB/s), 2056 of 16/2 in 7.0.
 #include <float.h>
 #include <math.h>
 
@@ -35,11 +36,22 @@ namespace ppas {
 namespace {
 
 constexpr int kRopeWarps = 8;
+// CTAs an SM holds of the kernel with norms (of 80 registers; 16384 tokens of 32/8
+// heads: 68.4 us, with 4 of 64 73.2, with 2 74.5)
+constexpr int kNormCtas = 3;
 constexpr int kRopeMaxIter = 4;      // 32-lane passes over head rows a warp makes, loads of all in flight
 constexpr int kRopeMaxDim = 512;     // head_dim: 16 values a lane
 // a unit's 8 (cos, sin) pairs, two pairs of padding after them: the 16-byte
 // reads of 8 neighbouring lanes then hit all banks once
 constexpr int kUnitPitch = 10;
+
+// the same of a unit's 16 weights, and of 8 cosines, sines and negative sines
+constexpr int kWeightPitch = 20, kAnglePitch = 28;
+constexpr size_t norm_rope_smem(int head_dim, int rotary_dim) {
+    return (2 * ((head_dim + 15) / 16) * static_cast<size_t>(kWeightPitch) +
+            static_cast<size_t>(kRopeWarps) * (rotary_dim / 16) * kAnglePitch) * sizeof(float);
+}
+static_assert(norm_rope_smem(kRopeMaxDim, kRopeMaxDim) <= 48 * 1024, "shared memory without a raised limit");
 
 // 2^192 / (2 pi), rounded down
 constexpr uint64_t kInv2 = 0x28BE60DB9391054Aull, kInv1 = 0x7F09D5F47D4D3770ull, kInv0 = 0x36D8A5664F10E410ull;
@@ -88,18 +100,7 @@ __device__ __forceinline__ float2 unpack_bf16x2(uint32_t v) {
     return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
 }
 
-// sum of the squares of 8 values, each times `scale` first
-__device__ __forceinline__ float squares(uint4 v, float scale) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float2 x = unpack_bf16x2(w[k]);
-        const float a = x.x * scale, b = x.y * scale;
-        s = fmaf(a, a, fmaf(b, b, s));
-    }
-    return s;
-}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return fma2(a, b, make_float2(-0.f, -0.f)); }
 
 // Heads whose squares pass the fp32 range (values from 1.8e19 on) are summed again
 // times this; the largest bf16 numbers then stay below 2^59, 512 squares of them in range.
@@ -125,7 +126,7 @@ __device__ __forceinline__ int32_t checked_slot(const RopeParams &p, int32_t tok
 struct RopeRow {
     const __nv_bfloat16 *src;
     __nv_bfloat16 *dst;  // NULL: not written
-    bool turns;           // (and has a norm)
+    bool turns;  // (and has a norm)
     bool is_q;
 };
 __device__ __forceinline__ RopeRow rope_row(const RopeParams &p, int32_t token, int32_t slot, int32_t row) {
@@ -153,7 +154,7 @@ __device__ __forceinline__ RopeRow rope_row(const RopeParams &p, int32_t token, 
 }  // namespace
 
 // 16-byte accesses: rotary_dim a multiple of 16, every row 16-byte aligned.
-template <bool kInterleaved, bool kNorm>
+template <bool kInterleaved>
 __global__ void __launch_bounds__(kRopeWarps * 32) rope_append_kernel(const __grid_constant__ RopeParams p) {
     // the launch that follows may start its set-up now
     grid_dep_launch();
@@ -205,84 +206,10 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_append_kernel(const __gr
             cs[2 * k + 1] = make_float2(v.z, v.w);
         }
     }
-    float w[16];                    // (kNorm) the weights of the lane's two chunks
-    const float *w_of = nullptr;    // where they come from, once there are any
-    bool w_there = false;
 #pragma unroll
     for (int i = 0; i < kRopeMaxIter; ++i) {
-        if constexpr (kNorm) {
-            if (i >= p.iters) break;
-            // (every lane of the warp: a row's lanes are its units)
-            const bool mine = r[i].dst != nullptr;
-            auto row_sum = [&](float scale) {
-                float s = 0.f;
-                if (mine) s = squares(a[i], scale) + (cb < chunks ? squares(b[i], scale) : 0.f);
-                if ((units & (units - 1)) == 0) {
-                    for (int o = 1; o < units; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                    return s;
-                }
-                float all = 0.f;
-                for (int j = 0; j < units; ++j) all += __shfl_sync(0xffffffffu, s, (sub * units + j) & 31);
-                return all;
-            };
-            const float sum = row_sum(1.f);
-            const bool large = !(sum <= FLT_MAX);
-            const float scaled = __any_sync(0xffffffffu, large) ? row_sum(kSquareScale) : 0.f;
-            if (mine && r[i].turns) {
-                const float f = norm_factor(sum, scaled, p.inv_dim, p.eps);
-                const float *from = r[i].is_q ? p.q_weight : p.k_weight;
-                if (from != w_of || !w_there) {  // (queries come first: mostly once)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int chunk = h ? cb : ca;
-                        const bool there = from && chunk < chunks;
-                        const float4 *src = reinterpret_cast<const float4 *>(from + chunk * 8);
-                        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-                        const float4 w0 = there ? __ldg(src) : one, w1 = there ? __ldg(src + 1) : one;
-                        w[8 * h] = w0.x, w[8 * h + 1] = w0.y, w[8 * h + 2] = w0.z, w[8 * h + 3] = w0.w;
-                        w[8 * h + 4] = w1.x, w[8 * h + 5] = w1.y, w[8 * h + 6] = w1.z, w[8 * h + 7] = w1.w;
-                    }
-                    w_of = from;
-                    w_there = true;
-                }
-                const uint32_t xa[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, xb[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
-                float fa[8], fb[8];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 v = unpack_bf16x2(xa[k]), u2 = unpack_bf16x2(xb[k]);
-                    fa[2 * k] = v.x * f * w[2 * k];
-                    fa[2 * k + 1] = v.y * f * w[2 * k + 1];
-                    fb[2 * k] = u2.x * f * w[8 + 2 * k];
-                    fb[2 * k + 1] = u2.y * f * w[8 + 2 * k + 1];
-                }
-                if (turned) {
-                    if constexpr (kInterleaved) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float2 c = cs[k], d = cs[k + 4];
-                            const float v0 = fa[2 * k], v1 = fa[2 * k + 1], u0 = fb[2 * k], u1 = fb[2 * k + 1];
-                            fa[2 * k] = v0 * c.x - v1 * c.y;
-                            fa[2 * k + 1] = v1 * c.x + v0 * c.y;
-                            fb[2 * k] = u0 * d.x - u1 * d.y;
-                            fb[2 * k + 1] = u1 * d.x + u0 * d.y;
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float v0 = fa[k], u0 = fb[k];
-                            fa[k] = v0 * cs[k].x - u0 * cs[k].y;
-                            fb[k] = u0 * cs[k].x + v0 * cs[k].y;
-                        }
-                    }
-                }
-                a[i] = make_uint4(pack_bf16x2(fa[0], fa[1]), pack_bf16x2(fa[2], fa[3]), pack_bf16x2(fa[4], fa[5]),
-                                  pack_bf16x2(fa[6], fa[7]));
-                b[i] = make_uint4(pack_bf16x2(fb[0], fb[1]), pack_bf16x2(fb[2], fb[3]), pack_bf16x2(fb[4], fb[5]),
-                                  pack_bf16x2(fb[6], fb[7]));
-            }
-        }
         if (!r[i].dst) continue;
-        if (!kNorm && turned && r[i].turns) {
+        if (turned && r[i].turns) {
             uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -305,6 +232,183 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_append_kernel(const __gr
         uint4 *dst = reinterpret_cast<uint4 *>(r[i].dst);
         dst[ca] = a[i];
         if (cb < chunks) dst[cb] = b[i];
+    }
+}
+
+// The same with norms.  A warp takes a run of tasks, and a token's angles with its
+// first one; angles and weights lie in shared memory in the order of the lanes that
+// read them (in registers they left room for two CTAs an SM: 16384 tokens of 32/8 heads
+// 103 us).  What bounds it next is the number of instructions: heads of 128 have a
+// kernel of their own (kDim; 0: any), products run on two values at once.
+template <bool kInterleaved, int kDim>
+__global__ void __launch_bounds__(kRopeWarps * 32, kDim ? kNormCtas : 2)
+    norm_rope_append_kernel(const __grid_constant__ RopeParams p) {
+    grid_dep_launch();
+    extern __shared__ float4 rope_smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int dim = kDim ? kDim : p.head_dim;
+    const int units = (dim + 15) / 16, half = p.rotary_dim / 2, rot_units = half / 8;
+    const int rows_at_once = 32 / units, chunks = dim / 8;
+    const int u = lane % units, sub = lane / units;
+    const bool turned = u < rot_units;
+    auto first_chunk = [&](int unit) { return kInterleaved || unit >= rot_units ? 2 * unit : unit; };
+    auto second_chunk = [&](int unit) { return kInterleaved || unit >= rot_units ? 2 * unit + 1 : unit + rot_units; };
+    const int ca = first_chunk(u), cb = second_chunk(u);
+    const bool has_row = kDim == 128 || sub < rows_at_once, has_b = kDim == 128 || cb < chunks;
+    constexpr int kPitch = kWeightPitch, kTurnPitch = kAnglePitch;
+    // [queries, keys][unit][16 weights]; then each warp's angles [unit][8 cosines, 8 sines, the sines' negatives]
+    float *const weights = reinterpret_cast<float *>(rope_smem);
+    float *const table = weights + 2 * units * kPitch + warp * rot_units * kTurnPitch;
+    const int32_t n_turned = p.n_q_heads + p.n_kv_heads, n_rows = n_turned + p.n_kv_heads;
+    // this warp's tasks
+    const int64_t w = static_cast<int64_t>(blockIdx.x) * kRopeWarps + warp;
+    const int64_t n_warps = static_cast<int64_t>(gridDim.x) * kRopeWarps;
+    int32_t task = static_cast<int32_t>(p.n_tasks * w / n_warps);
+    const int32_t task_end = static_cast<int32_t>(p.n_tasks * (w + 1) / n_warps);
+    grid_dep_wait();
+    for (int i = threadIdx.x; i < 2 * units * 16; i += kRopeWarps * 32) {
+        const int which = i / (units * 16), unit = i / 16 % units, e = i % 16;
+        const int d = (e < 8 ? first_chunk(unit) : second_chunk(unit)) * 8 + e % 8;
+        const float *const from = which ? p.k_weight : p.q_weight;
+        weights[(which * units + unit) * kPitch + e] = from && d < dim ? __ldg(from + d) : 1.f;
+    }
+    __syncthreads();
+    int32_t token = task / p.tasks_per_token, part = task - token * p.tasks_per_token;
+    bool angles = false;  // the token's are in the table
+    for (; task < task_end; ++task) {
+        const int32_t slot = checked_slot(p, token, lane == 0 && part == 0);
+        const __nv_bfloat16 *const q = p.q + token * p.q_stride, *const k = p.k + token * p.k_stride;
+        const __nv_bfloat16 *const v = p.v + token * p.v_stride;
+        const int32_t row0 = part * p.iters * rows_at_once + sub;
+        uint4 a[kRopeMaxIter], b[kRopeMaxIter];
+#pragma unroll
+        for (int i = 0; i < kRopeMaxIter; ++i) {
+            const int32_t row = row0 + i * rows_at_once;
+            a[i] = b[i] = make_uint4(0, 0, 0, 0);
+            if (i < p.iters && has_row && row < n_rows) {
+                const __nv_bfloat16 *src = row < p.n_q_heads ? q + row * dim
+                                           : row < n_turned  ? k + (row - p.n_q_heads) * dim
+                                                             : v + (row - n_turned) * dim;
+                const uint4 *from = reinterpret_cast<const uint4 *>(src);
+                a[i] = from[ca];
+                if (has_b) b[i] = from[cb];
+            }
+        }
+        if (!angles) {
+            const int32_t position = __ldg(p.positions + token);
+            for (int f = lane; f < half; f += 32) {
+                const float2 cs = rope_angle(position, __ldg(p.inv_freq + f), p.factor);
+                float *const to = table + (f >> 3) * kTurnPitch + (f & 7);
+                to[0] = cs.x;
+                to[8] = cs.y;
+                to[16] = -cs.y;
+            }
+            angles = true;
+            __syncwarp();
+        }
+        __nv_bfloat16 *const q_to = p.q_out + static_cast<int64_t>(token) * p.n_q_heads * dim;
+        const int64_t in_page =
+            (static_cast<int64_t>(slot / kPage) * p.n_kv_heads * kPage + slot % kPage) * dim;
+        __nv_bfloat16 *const k_to = p.k_cache + in_page, *const v_to = p.v_cache + in_page;
+#pragma unroll
+        for (int i = 0; i < kRopeMaxIter; ++i) {
+            if (i >= p.iters) break;
+            const int32_t row = row0 + i * rows_at_once;
+            float2 x[8];  // 8 values of each chunk
+            {
+                const uint32_t xa[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, xb[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = unpack_bf16x2(xa[e]);
+                    x[4 + e] = unpack_bf16x2(xb[e]);
+                }
+            }
+            // (every lane of the warp: a row's lanes are its units; what a lane did not load is 0)
+            auto over_row = [&](float s) {
+                if (kDim == 128) {
+                    s += __shfl_xor_sync(0xffffffffu, s, 1);
+                    s += __shfl_xor_sync(0xffffffffu, s, 2);
+                    return s + __shfl_xor_sync(0xffffffffu, s, 4);
+                }
+                if ((units & (units - 1)) == 0) {
+                    for (int o = 1; o < units; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                    return s;
+                }
+                float all = 0.f;
+                for (int j = 0; j < units; ++j) all += __shfl_sync(0xffffffffu, s, (sub * units + j) & 31);
+                return all;
+            };
+            float2 s2 = mul2(x[0], x[0]);
+#pragma unroll
+            for (int e = 1; e < 8; ++e) s2 = fma2(x[e], x[e], s2);
+            const float sum = over_row(s2.x + s2.y);
+            float scaled = 0.f;
+            if (__any_sync(0xffffffffu, !(sum <= FLT_MAX))) {
+                float s = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y0 = x[e].x * kSquareScale, y1 = x[e].y * kSquareScale;
+                    s = fmaf(y0, y0, fmaf(y1, y1, s));
+                }
+                scaled = over_row(s);
+            }
+            if (!has_row || row >= n_rows || (row >= p.n_q_heads && slot < 0)) continue;
+            if (row < n_turned) {
+                const float f = norm_factor(sum, scaled, p.inv_dim, p.eps);
+                const float4 *const w4 =
+                    reinterpret_cast<const float4 *>(weights + ((row < p.n_q_heads ? 0 : units) + u) * kPitch);
+                const float2 ff = make_float2(f, f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float4 wt = w4[e];
+                    x[2 * e] = mul2(mul2(x[2 * e], ff), make_float2(wt.x, wt.y));
+                    x[2 * e + 1] = mul2(mul2(x[2 * e + 1], ff), make_float2(wt.z, wt.w));
+                }
+                if (turned) {
+                    const float *const at = table + u * kTurnPitch;
+                    if constexpr (kInterleaved) {  // pair e is (x[e].x, x[e].y)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float c = at[e], s = at[8 + e], m = x[e].x;
+                            x[e].x = m * c - x[e].y * s;
+                            x[e].y = x[e].y * c + m * s;
+                        }
+                    } else {  // pairs 2 e and 2 e + 1 are (x[e].x, x[4 + e].x) and (x[e].y, x[4 + e].y)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float4 c = reinterpret_cast<const float4 *>(at)[h];
+                            const float4 s = reinterpret_cast<const float4 *>(at)[2 + h];
+                            const float4 z = reinterpret_cast<const float4 *>(at)[4 + h];
+                            auto turn = [](float2 &m, float2 &n, float2 c_, float2 s_, float2 z_) {
+                                const float2 m0 = m;
+                                m = fma2(n, z_, mul2(m, c_));
+                                n = fma2(m0, s_, mul2(n, c_));
+                            };
+                            turn(x[2 * h], x[4 + 2 * h], make_float2(c.x, c.y), make_float2(s.x, s.y),
+                                 make_float2(z.x, z.y));
+                            turn(x[2 * h + 1], x[4 + 2 * h + 1], make_float2(c.z, c.w), make_float2(s.z, s.w),
+                                 make_float2(z.z, z.w));
+                        }
+                    }
+                }
+                a[i] = make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y),
+                                  pack_bf16x2(x[3].x, x[3].y));
+                b[i] = make_uint4(pack_bf16x2(x[4].x, x[4].y), pack_bf16x2(x[5].x, x[5].y), pack_bf16x2(x[6].x, x[6].y),
+                                  pack_bf16x2(x[7].x, x[7].y));
+            }
+            uint4 *const to = reinterpret_cast<uint4 *>(
+                row < p.n_q_heads ? q_to + row * dim
+                                  : (row < n_turned ? k_to + (row - p.n_q_heads) * kPage * dim
+                                                    : v_to + (row - n_turned) * kPage * dim));
+            to[ca] = a[i];
+            if (has_b) to[cb] = b[i];
+        }
+        __syncwarp();  // the angles have been read
+        if (++part == p.tasks_per_token) {
+            part = 0;
+            ++token;
+            angles = false;
+        }
     }
 }
 
@@ -400,11 +504,18 @@ cudaError_t launch_rope_append(RopeParams p, cudaStream_t st) {
         const size_t smem = static_cast<size_t>(kRopeWarps) * (p.rotary_dim / 16) * kUnitPitch * sizeof(float2);
         PdlLaunch l(dim3(static_cast<unsigned>((tasks + kRopeWarps - 1) / kRopeWarps)), dim3(kRopeWarps * 32), smem,
                     st);
-        if (p.norm)
-            return p.interleaved ? cudaLaunchKernelEx(&l.cfg, rope_append_kernel<true, true>, p)
-                                 : cudaLaunchKernelEx(&l.cfg, rope_append_kernel<false, true>, p);
-        return p.interleaved ? cudaLaunchKernelEx(&l.cfg, rope_append_kernel<true, false>, p)
-                             : cudaLaunchKernelEx(&l.cfg, rope_append_kernel<false, false>, p);
+        if (p.norm) {
+            // (angles once a token: as many CTAs as the SMs hold at a time)
+            l.cfg.dynamicSmemBytes = norm_rope_smem(p.head_dim, p.rotary_dim);
+            const unsigned most = static_cast<unsigned>(sms) * kNormCtas;
+            if (l.cfg.gridDim.x > most) l.cfg.gridDim.x = most;
+            const bool d128 = p.head_dim == 128;
+            const auto kernel = p.interleaved ? (d128 ? norm_rope_append_kernel<true, 128> : norm_rope_append_kernel<true, 0>)
+                                              : (d128 ? norm_rope_append_kernel<false, 128> : norm_rope_append_kernel<false, 0>);
+            return cudaLaunchKernelEx(&l.cfg, kernel, p);
+        }
+        return p.interleaved ? cudaLaunchKernelEx(&l.cfg, rope_append_kernel<true>, p)
+                             : cudaLaunchKernelEx(&l.cfg, rope_append_kernel<false>, p);
     }
     if (p.norm) {
         const int64_t warps = (static_cast<int64_t>(p.n_tokens) * n_rows + 7) / 8;
