@@ -14,6 +14,7 @@
 // so that it counts to 2^-17 of itself.
 #include <algorithm>
 #include <cmath>
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -27,6 +28,10 @@ constexpr int kAThreads = 256;
 constexpr int kAWarps = kAThreads / 32;
 constexpr int kAChunk = 64;  // inner sums worked at a time
 constexpr int kAMaxCluster = 8;
+constexpr int32_t kATileRows = 128;  // rows of a tile
+constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make one
+constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space)
+constexpr uint32_t kTSmem = 232448;  // shared memory of a CTA
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -202,7 +207,499 @@ __global__ void __launch_bounds__(kAThreads)
     }
 }
 
-AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies) {
+// ---------------------------------------------------------------- long runs of rows
+// A tile of 128 rows of one adapter, on the tcgen05 tensor cores: the inner sums
+// s = x A^T [128, slices x rank] accumulate in TMEM over blocks of 64 of K, each slice's on
+// columns of its own (rank rounded up to 16).  The epilogue warps turn them, in
+// place, into two bf16 numbers each, the operand A in TMEM of the second product, and
+// add that product, a block of columns at a time, to y.  So s never leaves the SM, and
+// x, y and out cross HBM once.  Where there are fewer tiles than SMs a cluster of CTAs
+// shares a tile: each takes a part of K, the parts are summed row by row through
+// distributed shared memory, and each takes a share of the columns.
+//   warp 0      TMA: x and A tiles into a ring, B tiles into another, y tiles into a
+//               third, from which, with the products added, they are stored
+//   warp 1      allocates TMEM, issues the MMAs
+//   warps 2-9   inner sums, and y + scale s B^T in shared memory: a thread has a row (its
+//               TMEM lane), two warps each 32 rows, half the block's columns each
+// (With y and out moved by the epilogue's threads, through a transposition in shared
+// memory, a block took 3000 cycles: 16384 rows, 4096 x 6144, rank 64 in 176 us.)
+namespace {
+
+constexpr int kTRows = 128;
+constexpr int kTK = 64;
+constexpr int kTThreads = 320;
+constexpr int kTEpilogue = 256;
+constexpr int kTMaxStages = 6;
+constexpr int kTBStages = 3;
+constexpr int kTYStages = 4;
+constexpr uint32_t kTXBytes = kTRows * kTK * 2;
+constexpr uint32_t kTBoxBytes = kTRows * 128;  // 64 columns of y
+enum : int {
+    T_FULL = 0,
+    T_EMPTY = T_FULL + kTMaxStages,
+    T_SUMS = T_EMPTY + kTMaxStages,  // the inner sums are in TMEM
+    T_READY,                         // and turned into an operand
+    T_BFULL,
+    T_BEMPTY = T_BFULL + kTBStages,
+    T_YFULL = T_BEMPTY + kTBStages,
+    T_YDONE = T_YFULL + kTYStages,     // the products are added
+    T_OUTFULL = T_YDONE + kTYStages,   // [2] a block's products are in TMEM
+    T_OUTEMPTY = T_OUTFULL + 2,
+    T_DONE = T_OUTEMPTY + 2,           // every MMA has completed
+    T_COUNT
+};
+constexpr uint32_t kTBarBytes = 320;
+static_assert(T_COUNT * 8 + 8 <= kTBarBytes, "barrier area");
+
+// how a tile lies in shared memory and TMEM
+struct TileShape {
+    int32_t rank16;    // rank rounded up to 16
+    int32_t wide16;    // TMEM columns of all slices' inner sums, rounded up to 32
+    int32_t block_log; // log2 of the columns of y worked at a time: 128, or 64
+    int32_t ctas_log;
+    int32_t stages;    // of the ring of x and A
+    uint32_t a_bytes;  // of a stage: the slices' A tiles
+    uint32_t b_bytes;  // of a B tile: block rows, 128 bytes for each 64 of rank
+    // y's ring, where the ring of x and A was and behind it (behind the sums that the
+    // cluster's other CTAs read)
+    uint32_t y_at;
+    int32_t y_stages;
+    uint32_t b_at, bars_at, smem;  // offsets, and all of it
+    int32_t tmem;      // columns allocated
+};
+__host__ __device__ constexpr uint32_t sums_bytes(int wide16, int rows) {
+    return static_cast<uint32_t>(rows * (wide16 + 4) * 4);
+}
+
+struct TileParams {
+    AdapterParams p;
+    TileShape s;
+    int32_t *err;
+    int32_t block_at[kAMaxSlices + 1];  // first block of columns of each slice; all of them
+    AdapterTile tiles[kMaxTiles];
+};
+static_assert(sizeof(TileParams) + 3 * 128 + 2 * 128 <= 32764, "kernel parameter space");
+
+// block i of the columns: its slice, first column and width
+struct ColumnBlock {
+    int slice, c0, width;
+};
+__device__ __forceinline__ ColumnBlock column_block(const TileParams &tp, int i) {
+    ColumnBlock b;
+    b.slice = (i >= tp.block_at[1]) + (i >= tp.block_at[2]) + (i >= tp.block_at[3]);
+    b.c0 = tp.p.slice_at[b.slice] + ((i - tp.block_at[b.slice]) << tp.s.block_log);
+    b.width = min(1 << tp.s.block_log, tp.p.slice_at[b.slice + 1] - b.c0);
+    return b;
+}
+static_assert(kAMaxSlices == 4, "column_block compares with three of them");
+
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(a)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t from, int32_t x, int32_t y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(from), "r"(x), "r"(y)
+                 : "memory");
+}
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// until the memory of all but this thread's last n groups of stores has been read
+template <int n>
+__device__ __forceinline__ void stores_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(n) : "memory");
+}
+__device__ __forceinline__ void stores_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+}  // namespace
+
+__global__ void __launch_bounds__(kTThreads, 1)
+    adapter_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a,
+                         const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_y,
+                         const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ TileParams tp) {
+    extern __shared__ uint8_t smem_raw[];
+    const AdapterParams &p = tp.p;
+    const TileShape &ts = tp.s;
+    const uint32_t raw_s = smem_u32(smem_raw);
+    const uint32_t sb = (raw_s + 1023u) & ~1023u;
+    uint8_t *const sg = smem_raw + (sb - raw_s);
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // (uniform)
+    auto bar = [&](int i) { return sb + ts.bars_at + 8u * static_cast<uint32_t>(i); };
+    volatile uint32_t *const tmem_base = reinterpret_cast<volatile uint32_t *>(sg + ts.bars_at + T_COUNT * 8);
+    volatile int *const abort_flag = reinterpret_cast<volatile int *>(sg + ts.bars_at + T_COUNT * 8 + 4);
+    const int ctas = 1 << ts.ctas_log, rank = static_cast<int>(cluster_ctarank());
+    const AdapterTile tile = tp.tiles[blockIdx.x >> ts.ctas_log];
+
+    if (warp == 1) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_base)), static_cast<uint32_t>(ts.tmem));
+        tmem_relinquish();
+    }
+    if (warp == 0) {
+        if (lane == 0) {
+            prefetch_tmap(&tm_x);
+            prefetch_tmap(&tm_a);
+            prefetch_tmap(&tm_b);
+            prefetch_tmap(&tm_y);
+            prefetch_tmap(&tm_out);
+            *abort_flag = 0;
+        }
+        for (int i = lane; i < T_COUNT; i += 32) {
+            const bool by_warps = i == T_READY || (i >= T_YDONE && i < T_YDONE + kTYStages) || i == T_OUTEMPTY ||
+                                  i == T_OUTEMPTY + 1;
+            mbar_init(bar(i), by_warps ? 8 : 1);
+        }
+        fence_mbar_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_base, 0);
+    const uint32_t outs = tmem + static_cast<uint32_t>(ts.wide16);  // two blocks of products behind the sums
+    // the set-up above overlaps the kernel before this one on the stream
+    grid_dep_wait();
+    grid_dep_launch();
+
+    // this CTA's blocks of K, and its blocks of columns: rank, rank + ctas, ...
+    const int k_blocks = (p.hidden + kTK - 1) / kTK;
+    const int kb0 = (k_blocks * rank) >> ts.ctas_log, kb1 = (k_blocks * (rank + 1)) >> ts.ctas_log;
+    const int mine = (tp.block_at[kAMaxSlices] - rank + ctas - 1) >> ts.ctas_log;
+    const uint32_t stage_bytes = kTXBytes + ts.a_bytes;
+    const int block = 1 << ts.block_log, boxes = block / 64;
+    const uint32_t y_bytes = static_cast<uint32_t>(boxes) * kTBoxBytes;
+    // (every thread, on every path: the same number of cluster barriers)
+    auto cluster_point = [&]() {
+        if (ctas > 1) {
+            __syncwarp();
+            cluster_sync_all();
+        }
+    };
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- TMA
+        bool ok = true;
+        int q = 0;
+        for (int s = 0, round = 0; kb0 + q < kb1; ++q) {
+            if (round > 0 && !mbar_wait_warp(bar(T_EMPTY + s), (round & 1) ^ 1, tp.err)) {
+                ok = false;
+                break;
+            }
+            if (elect_one()) {
+                const uint32_t dst = sb + static_cast<uint32_t>(s) * stage_bytes;
+                mbar_expect_tx(bar(T_FULL + s), stage_bytes);
+                tma_load_2d(dst, &tm_x, (kb0 + q) * kTK, tile.first, bar(T_FULL + s));
+                tma_load_3d(dst + kTXBytes, &tm_a, (kb0 + q) * kTK, 0, tile.adapter * p.n_slices, bar(T_FULL + s));
+            }
+            __syncwarp();
+            if (++s == ts.stages) {
+                s = 0;
+                ++round;
+            }
+        }
+        const int rank_tiles = (p.rank + 63) / 64;
+        auto load_b = [&](int i) {
+            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const int s = i % kTBStages;
+            if (elect_one()) {
+                mbar_expect_tx(bar(T_BFULL + s), ts.b_bytes);
+                for (int h = 0; h < rank_tiles; ++h)
+                    tma_load_2d(sb + ts.b_at + static_cast<uint32_t>(s) * ts.b_bytes +
+                                    static_cast<uint32_t>(h * block) * 128,
+                                &tm_b, h * 64, tile.adapter * p.cols + cb.c0, bar(T_BFULL + s));
+            }
+            __syncwarp();
+        };
+        auto load_y = [&](int i) {
+            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const int s = i % ts.y_stages;
+            if (lane == 0) {
+                const uint32_t dst = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes;
+                mbar_expect_tx(bar(T_YFULL + s), y_bytes);
+                for (int h = 0; h < boxes; ++h)
+                    tma_load_2d(dst + static_cast<uint32_t>(h) * kTBoxBytes, &tm_y, cb.c0 + h * 64, tile.first,
+                                bar(T_YFULL + s));
+            }
+            __syncwarp();
+        };
+        int nb = 0, ny = 0;
+        for (; ok && nb < min(mine, kTBStages); ++nb) load_b(nb);
+        cluster_point();
+        cluster_point();
+        // every MMA on the ring of x and A has completed: its memory is y's (which the
+        // cluster's other CTAs no longer read)
+        if (ok) ok = mbar_wait_warp(bar(T_SUMS), 0, tp.err);
+        for (; ok && ny < min(mine, ts.y_stages); ++ny) load_y(ny);
+        for (int i = 0; ok && i < mine; ++i) {
+            const int s = i % ts.y_stages;
+            if (!mbar_wait_warp(bar(T_YDONE + s), (i / ts.y_stages) & 1, tp.err)) {
+                ok = false;
+                break;
+            }
+            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            if (lane == 0) {
+                const uint32_t from = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes;
+                if (tile.n == kTRows)
+                    for (int h = 0; h < boxes; ++h)
+                        if (h * 64 + 64 <= cb.width)
+                            tma_store_2d(&tm_out, from + static_cast<uint32_t>(h) * kTBoxBytes, cb.c0 + h * 64, tile.first);
+                stores_commit();
+            }
+            __syncwarp();
+            if (nb < mine) {
+                if (!mbar_wait_warp(bar(T_BEMPTY + nb % kTBStages), ((nb / kTBStages) & 1) ^ 1, tp.err)) {
+                    ok = false;
+                    break;
+                }
+                load_b(nb++);
+            }
+            // the block before this one has been stored from its memory
+            if (i > 0 && ny < mine) {
+                if (lane == 0) stores_wait_read<1>();
+                __syncwarp();
+                load_y(ny++);
+            }
+        }
+        if (!ok) *abort_flag = 1;
+        // nothing lands, or is read, once the CTA has left
+        ring_land(bar(T_FULL), q, ts.stages, lane);
+        ring_land(bar(T_BFULL), nb, kTBStages, lane);
+        ring_land(bar(T_YFULL), ny, ts.y_stages, lane);
+        if (lane == 0) stores_wait();
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- MMAs
+        bool ok = true;
+        {
+            const int width = p.n_slices * ts.rank16;  // N of the first product, in parts of at most 256
+            const int n0 = min(width, 256), n1 = width - n0;
+            const uint32_t idesc = idesc_bf16_f32(kTRows, 16, false, false);
+            const uint32_t idesc0 = idesc + (static_cast<uint32_t>((n0 - 16) >> 3) << 17);
+            const uint32_t idesc1 = idesc + (static_cast<uint32_t>((n1 - 16) >> 3) << 17);
+            const uint64_t dx0 = smem_desc_sw128(sb, 16, 1024), da0 = smem_desc_sw128(sb + kTXBytes, 16, 1024);
+            for (int q = 0, s = 0, round = 0; q < kb1 - kb0; ++q) {
+                if (!mbar_wait_warp(bar(T_FULL + s), round & 1, tp.err)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint64_t at = (static_cast<uint32_t>(s) * stage_bytes) >> 4;
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < kTK / 16; ++kk) {
+                        const uint32_t accumulate = q > 0 || kk > 0 ? 1u : 0u;
+                        umma_bf16(tmem, dx0 + at + kk * 2, da0 + at + kk * 2, idesc0, accumulate);
+                        if (n1 > 0)
+                            umma_bf16(tmem + 256, dx0 + at + kk * 2, da0 + at + 256 * 8 + kk * 2, idesc1, accumulate);
+                    }
+                    umma_commit(bar(T_EMPTY + s));
+                    if (q == kb1 - kb0 - 1) umma_commit(bar(T_SUMS));
+                }
+                __syncwarp();
+                if (++s == ts.stages) {
+                    s = 0;
+                    ++round;
+                }
+            }
+        }
+        cluster_point();
+        cluster_point();
+        if (ok) ok = mbar_wait_warp(bar(T_READY), 0, tp.err);
+        tc_fence_after();
+        const uint32_t idesc = idesc_bf16_f32(kTRows, 64, false, false) +
+                               (static_cast<uint32_t>((block - 64) >> 3) << 17);
+        const uint64_t db0 = smem_desc_sw128(sb + ts.b_at, 16, 1024);
+        for (int i = 0; ok && i < mine; ++i) {
+            const int s = i % kTBStages, buf = i & 1;
+            const int slice = column_block(tp, rank + (i << ts.ctas_log)).slice;
+            if (!mbar_wait_warp(bar(T_BFULL + s), (i / kTBStages) & 1, tp.err) ||
+                (i >= 2 && !mbar_wait_warp(bar(T_OUTEMPTY + buf), ((i >> 1) & 1) ^ 1, tp.err))) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t d = outs + static_cast<uint32_t>(buf * block);
+                const uint64_t db = db0 + ((static_cast<uint32_t>(s) * ts.b_bytes) >> 4);
+                for (int k = 0; k < ts.rank16; k += 16) {
+                    // 16 inner sums: columns c .. c + 15 became halves of 8 columns each of c's group of 32
+                    const int c = slice * ts.rank16 + k;
+                    const uint32_t a = tmem + static_cast<uint32_t>((c & ~31) + ((c & 16) >> 1));
+                    const uint64_t b = db + static_cast<uint64_t>((k >> 6) * block * 8 + ((k & 63) >> 3));
+                    umma_bf16_ts(d, a, b, idesc, k > 0 ? 1u : 0u);
+                    umma_bf16_ts(d, a + 16, b, idesc, 1u);
+                }
+                umma_commit(bar(T_BEMPTY + s));
+                umma_commit(bar(T_OUTFULL + buf));
+            }
+            __syncwarp();
+        }
+        if (!ok) *abort_flag = 1;
+        if (elect_one()) umma_commit(bar(T_DONE));
+        __syncwarp();
+        mbar_wait_warp(bar(T_DONE), 0, tp.err);
+    } else {
+        // ---------------------------------------------------------------- inner sums, output
+        const int wq = warp & 3, half = (warp - 2) >> 2;  // TMEM lane quarter, half of the columns
+        const int row = wq * 32 + lane;                    // this thread's TMEM lane
+        const uint32_t t_lane = static_cast<uint32_t>(wq * 32) << 16;
+        const float scale = p.scales ? __ldg(p.scales + tile.adapter) : 1.f;
+        // (every MMA on the ring has completed by then, and with them its copies: its memory is free)
+        bool ok = mbar_wait_warp(bar(T_SUMS), 0, tp.err);
+        if (!ok) *abort_flag = 1;
+        tc_fence_after();
+        const int pitch = ts.wide16 + 4, own_log = 7 - ts.ctas_log;
+        // [128 / ctas][pitch] the cluster's sums of this CTA's rows, [128][pitch] this CTA's part
+        float *const summed = reinterpret_cast<float *>(sg);
+        float *const part = reinterpret_cast<float *>(sg + sums_bytes(ts.wide16, kTRows >> ts.ctas_log));
+        if (ctas > 1) {
+            for (int c = half * 32; ok && c < ts.wide16; c += 64) {
+                float v[32];
+                tmem_ld32_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
+                float4 *const to = reinterpret_cast<float4 *>(part + row * pitch + c);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+            cluster_point();
+            const int vecs = ts.wide16 / 4;
+            for (int i = tid - 64; i < vecs << own_log; i += kTEpilogue) {
+                const int r = i / vecs, c = (i - r * vecs) * 4;
+                const uint32_t at = smem_u32(part + ((rank << own_log) + r) * pitch + c);
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int o = 0; o < ctas; ++o) {
+                    const float4 v = ld_cluster_f32x4(dsmem_addr(at, static_cast<uint32_t>(o)));
+                    sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+                }
+                *reinterpret_cast<float4 *>(summed + r * pitch + c) = sum;
+            }
+            fence_proxy_async_smem();  // y's copies come where the parts were
+            cluster_point();
+        }
+        for (int c = half * 32; ok && c < ts.wide16; c += 64) {
+            float v[32];
+            if (ctas > 1) {
+                const uint32_t at = dsmem_addr(smem_u32(summed + (row & ((1 << own_log) - 1)) * pitch + c),
+                                               static_cast<uint32_t>(row >> own_log));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float4 w = ld_cluster_f32x4(at + 16u * static_cast<uint32_t>(i));
+                    v[4 * i] = w.x, v[4 * i + 1] = w.y, v[4 * i + 2] = w.z, v[4 * i + 3] = w.w;
+                }
+            } else {
+                tmem_ld32_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
+            }
+            uint32_t r[32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // columns past the rank, and past the last slice, are 0 (but for rows with an infinity)
+                const int at = c + 16 * h, in_slice = at % ts.rank16;
+                const int some = at < p.n_slices * ts.rank16 ? p.rank - in_slice : 0;
+#pragma unroll
+                for (int i = 8 * h; i < 8 * h + 8; ++i) {
+                    const bool in = 2 * (i - 8 * h) < some;  // (the rank is even)
+                    split_bf16(in ? v[2 * i] : 0.f, in ? v[2 * i + 1] : 0.f, r[i], r[16 + i]);
+                }
+            }
+            tmem_st32(tmem + t_lane + static_cast<uint32_t>(c), r);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(T_READY));
+
+        // this warp's columns of a block: 64, a box of y, or 32, half a box
+        const int groups = block / 64;
+        const uint32_t box = block == 128 ? static_cast<uint32_t>(half) * kTBoxBytes : 0u;
+        const int first = block == 128 ? 0 : half * 4;  // 16-byte pieces of the box's 128-byte rows
+        const int col = half * (block / 2);
+        const float2 scale2 = make_float2(scale, scale);
+        for (int i = 0, s = 0, round = 0; i < mine; ++i) {
+            const int buf = i & 1;
+            if (!mbar_wait_warp(bar(T_OUTFULL + buf), (i >> 1) & 1, tp.err) ||
+                !mbar_wait_warp(bar(T_YFULL + s), round & 1, tp.err) || __any_sync(0xffffffffu, *abort_flag)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t y_row = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes + box + static_cast<uint32_t>(row) * 128;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                if (g >= groups) break;
+                float v[32];
+                tmem_ld32_sync(outs + t_lane + static_cast<uint32_t>(buf * block + col + g * 32), v);
+                if (g == groups - 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(T_OUTEMPTY + buf));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    // (128-byte swizzle)
+                    const uint32_t at = y_row + static_cast<uint32_t>(((first + 4 * g + k) ^ (row & 7)) * 16);
+                    uint32_t w[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                 : "r"(at)
+                                 : "memory");
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 sum = fma2(make_float2(v[8 * k + 2 * e], v[8 * k + 2 * e + 1]), scale2,
+                                                make_float2(__uint_as_float(w[e] << 16),
+                                                            __uint_as_float(w[e] & 0xFFFF0000u)));
+                        w[e] = pack_bf16x2(sum.x, sum.y);
+                    }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                                 "r"(w[3])
+                                 : "memory");
+                }
+            }
+            // a box that the tile or the slice ends in is stored by its warps, others by TMA
+            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const int box_col = block == 128 ? col : 0;
+            if (tile.n < kTRows || box_col + 64 > cb.width) {
+                __syncwarp();
+                const int per_row = block == 128 ? 8 : 4;  // pieces of a row that this warp has
+                const int piece = lane & (per_row - 1), rows_at_once = 32 / per_row;
+                for (int r0 = 0; r0 < 32; r0 += rows_at_once) {
+                    const int r = wq * 32 + r0 + lane / per_row;
+                    const int c = box_col + (first + piece) * 8;
+                    const uint32_t at = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes + box +
+                                        static_cast<uint32_t>(r) * 128 +
+                                        static_cast<uint32_t>(((first + piece) ^ (r & 7)) * 16);
+                    if (r < tile.n && c < cb.width) {
+                        uint4 w;
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                     : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                                     : "r"(at)
+                                     : "memory");
+                        *reinterpret_cast<uint4 *>(p.out + static_cast<int64_t>(tile.first + r) * p.out_stride + cb.c0 + c) = w;
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(T_YDONE + s));
+            if (++s == ts.y_stages) {
+                s = 0;
+                ++round;
+            }
+        }
+        if (!ok) *abort_flag = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, static_cast<uint32_t>(ts.tmem));
+    }
+    cluster_point();  // nobody leaves while others read its sums
+}
+
+AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies,
+                         int32_t tile_rows) {
     constexpr int kCopyRows = 32;  // rows of a unit that is only copied
     AdapterPlan plan;
     std::vector<std::pair<int32_t, int32_t>> rows;  // (adapter, row) of those that are gathered
@@ -216,6 +713,11 @@ AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *a
             continue;
         }
         int32_t r = first;
+        while (at - r >= tile_rows) {
+            const int32_t n = std::min(kATileRows, at - r);
+            plan.tiles.push_back({r, id, n});
+            r += n;
+        }
         for (; at - r >= kAUnitRows; r += kAUnitRows) plan.units.push_back({r, id, kAUnitRows, 0});
         for (; r < at; ++r) rows.emplace_back(id, r);
     }
@@ -271,8 +773,90 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     return cudaLaunchKernelEx(&l.cfg, kernel, u);
 }
 
-cudaError_t launch_adapter(const AdapterParams &p, const AdapterPlan &plan, cudaStream_t st) {
-    cudaError_t e = cudaSuccess;
+// how tiles of this call lie for clusters of 2^ctas_log CTAs; false: not on this kernel
+bool tile_shape(const AdapterParams &p, int ctas_log, TileShape *s) {
+    *s = {};
+    s->ctas_log = ctas_log;
+    s->rank16 = (p.rank + 15) / 16 * 16;
+    s->wide16 = (p.n_slices * s->rank16 + 31) / 32 * 32;
+    // (a block of 128 columns needs less of everything else where it fits)
+    s->block_log = s->wide16 <= 256 && s->rank16 <= 64 ? 7 : 6;
+    const int block = 1 << s->block_log;
+    if (s->wide16 + 2 * block > 512) return false;
+    s->tmem = 32;
+    while (s->tmem < s->wide16 + 2 * block) s->tmem *= 2;
+    s->a_bytes = static_cast<uint32_t>(p.n_slices * s->rank16) * 128;
+    s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
+    const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
+    const uint32_t room = (kTSmem - rest) / 1024 * 1024, stage = kTXBytes + s->a_bytes;
+    s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / stage));
+    const uint32_t ring = static_cast<uint32_t>(s->stages) * stage;
+    // behind the inner sums: what the cluster's other CTAs read of them, then y's ring
+    const uint32_t summed = ctas_log ? sums_bytes(s->wide16, kTRows >> ctas_log) : 0;
+    const uint32_t parts = ctas_log ? summed + sums_bytes(s->wide16, kTRows) : 0;
+    const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * kTBoxBytes;
+    s->y_at = (summed + 1023) / 1024 * 1024;
+    if (s->stages < 2 || parts > room || s->y_at + 2 * y_bytes > room) return false;
+    s->y_stages = std::min<int>(kTYStages, static_cast<int>((room - s->y_at) / y_bytes));
+    s->b_at = std::max(ring, std::max((parts + 1023) / 1024 * 1024, s->y_at + static_cast<uint32_t>(s->y_stages) * y_bytes));
+    s->bars_at = s->b_at + kTBStages * s->b_bytes;
+    s->smem = s->bars_at + kTBarBytes + 1024;
+    return s->smem <= kTSmem;
+}
+
+cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_t n_rows, int32_t n_adapters,
+                         int32_t *err, cudaStream_t st) {
+    static std::atomic<uint64_t> smem_set{0};
+    cudaError_t e = ensure_smem_limit(adapter_tiles_kernel, static_cast<int>(kTSmem), smem_set);
+    if (e != cudaSuccess) return e;
+    const auto tp = std::make_unique<TileParams>();
+    tp->p = p;
+    tp->err = err;
+    for (size_t next = 0; next < plan.tiles.size();) {
+        const int n = static_cast<int>(std::min<size_t>(kMaxTiles, plan.tiles.size() - next));
+        std::copy_n(plan.tiles.begin() + static_cast<std::ptrdiff_t>(next), n, tp->tiles);
+        next += static_cast<size_t>(n);
+        const int k_blocks = (p.hidden + kTK - 1) / kTK;
+        int c = 0;
+        while (2 << c <= kAMaxCluster && (2 << c) * n <= device_sm_count() && 2 << c <= k_blocks &&
+               tile_shape(p, c + 1, &tp->s))
+            ++c;
+        if (!tile_shape(p, c, &tp->s)) return cudaErrorInvalidValue;  // (the plan asked before)
+        for (int j = 0, at = 0; j <= kAMaxSlices; ++j) {
+            tp->block_at[j] = at;
+            if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + (1 << tp->s.block_log) - 1) >> tp->s.block_log;
+        }
+        CUtensorMap tm_x, tm_a, tm_b, tm_y, tm_out;
+        const uint64_t rows = static_cast<uint64_t>(n_rows), cols = static_cast<uint64_t>(p.cols);
+        if (!encode_bf16_rows(&tm_x, p.x, static_cast<uint64_t>(p.hidden), rows, static_cast<uint64_t>(p.x_stride), kTK,
+                              kTRows) ||
+            !encode_bf16_3d(&tm_a, p.a, static_cast<uint64_t>(p.hidden), static_cast<uint64_t>(p.rank),
+                            static_cast<uint64_t>(n_adapters) * p.n_slices, kTK, static_cast<uint32_t>(tp->s.rank16),
+                            static_cast<uint32_t>(p.n_slices)) ||
+            !encode_bf16_2d(&tm_b, p.b, static_cast<uint64_t>(p.rank), static_cast<uint64_t>(n_adapters) * cols, 64,
+                            1u << tp->s.block_log) ||
+            !encode_bf16_rows(&tm_y, p.y, cols, rows, static_cast<uint64_t>(p.y_stride), 64, kTRows) ||
+            !encode_bf16_rows(&tm_out, p.out, cols, rows, static_cast<uint64_t>(p.out_stride), 64, kTRows))
+            return cudaErrorUnknown;
+        PdlLaunch l(dim3(static_cast<unsigned>(n) << c), dim3(kTThreads), tp->s.smem, st);
+        cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
+        if (c > 0) {
+            attrs[1].id = cudaLaunchAttributeClusterDimension;
+            attrs[1].val.clusterDim.x = 1u << c;
+            attrs[1].val.clusterDim.y = 1;
+            attrs[1].val.clusterDim.z = 1;
+            l.cfg.attrs = attrs;
+            l.cfg.numAttrs = 2;
+        }
+        e = cudaLaunchKernelEx(&l.cfg, adapter_tiles_kernel, tm_x, tm_a, tm_b, tm_y, tm_out, *tp);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+cudaError_t launch_adapter(const AdapterParams &p, const AdapterPlan &plan, int64_t n_rows, int32_t n_adapters,
+                           int32_t *err, cudaStream_t st) {
+    cudaError_t e = plan.tiles.empty() ? cudaSuccess : launch_tiles(p, plan, n_rows, n_adapters, err, st);
     const bool few = plan.units.size() <= 64 && plan.rows.size() <= 256;
     for (size_t next = 0; e == cudaSuccess && next < plan.units.size();)
         e = few ? launch_units<64, 256>(p, plan, next, st) : launch_units<1024, 3584>(p, plan, next, st);
@@ -334,8 +918,12 @@ extern "C" ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const v
     p.n_slices = n_slices;
     p.cols = static_cast<int32_t>(cols);
     try {
-        const AdapterPlan plan = plan_adapter(n_seqs, h_q_lens, h_adapters, out != y);
-        return launch_adapter(p, plan, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PPAS_OK : PPAS_ERR_CUDA;
+        TileShape shape;
+        const AdapterPlan plan =
+            plan_adapter(n_seqs, h_q_lens, h_adapters, out != y, tile_shape(p, 0, &shape) ? kATileMin : INT32_MAX);
+        return launch_adapter(p, plan, n_rows, n_adapters, d_err_flag, static_cast<cudaStream_t>(stream)) == cudaSuccess
+                   ? PPAS_OK
+                   : PPAS_ERR_CUDA;
     } catch (const std::exception &) {
         return PPAS_ERR_CAPACITY;  // host memory
     }

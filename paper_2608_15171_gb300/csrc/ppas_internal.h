@@ -315,6 +315,13 @@ GateUpPlan plan_gateup(int32_t n_tokens, int32_t inter, int32_t max_pairs);
 // 128-byte swizzle (box_inner * 2 bytes must be 128)
 bool encode_bf16_2d(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint32_t box_inner,
                     uint32_t box_outer);
+// the same with rows `stride` elements apart (a multiple of 8)
+bool encode_bf16_rows(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint64_t stride,
+                      uint32_t box_inner, uint32_t box_outer);
+
+// 3D bf16 [outer, mid, inner], contiguous, 128-byte swizzle as above
+bool encode_bf16_3d(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, uint64_t outer,
+                    uint32_t box_inner, uint32_t box_mid, uint32_t box_outer);
 
 // pairs: CTA pairs (one item at a time each); tm_x, tm_w: boxes of 128 rows;
 // tm_cut: of 128 / p.cut
@@ -407,13 +414,22 @@ struct AdapterParams {
     int32_t hidden, rank, n_slices, cols;
     int32_t slice_at[kAMaxSlices + 1];  // first column of each slice; cols
 };
+// up to 128 rows of one adapter, from row `first` on
+struct AdapterTile {
+    int32_t first;
+    int32_t adapter;
+    int32_t n;
+};
 struct AdapterPlan {
     std::vector<AdapterUnit> units;
     std::vector<int32_t> rows;  // of the listed units
+    std::vector<AdapterTile> tiles;
 };
-// the units of sequences of q_lens rows with these adapters (-1: none); copies:
-// rows without an adapter have to be copied
-AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies);
+// The units and tiles of sequences of q_lens rows with these adapters (-1: none);
+// copies: rows without an adapter have to be copied; tile_rows: rows of an adapter
+// next to one another that make tiles (INT32_MAX: never)
+AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies,
+                         int32_t tile_rows);
 
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its
