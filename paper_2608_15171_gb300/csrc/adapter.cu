@@ -16,6 +16,7 @@
 #include <cmath>
 #include <memory>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "ppas_device.cuh"
@@ -24,9 +25,13 @@
 namespace ppas {
 namespace {
 
-constexpr int kAThreads = 256;
+#ifndef USLOT
+#define USLOT 1
+#endif
+constexpr int kAThreads = 512;
 constexpr int kAWarps = kAThreads / 32;
-constexpr int kAChunk = 64;  // inner sums worked at a time
+constexpr int kAChunk = 96;  // inner sums worked at a time: the loads of 12 x 16 bytes a lane are under way at once
+constexpr int kAAhead = 4;   // of the rank in B, 16 times this are loaded ahead
 constexpr int kAMaxCluster = 8;
 constexpr int32_t kATileRows = 128;  // rows of a tile
 constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make one
@@ -44,6 +49,10 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t a) {
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
     return v;
 }
+// the first half of a cluster barrier, behind what this thread has read
+__device__ __forceinline__ void cluster_arrive() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
 // two values as bf16, and what their rounding left (0 of an infinity)
 __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint32_t &lo) {
     hi = pack_bf16x2(a, b);
@@ -54,6 +63,8 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint3
 template <int kUnits, int kRows>
 struct UnitParams {
     AdapterParams p;
+    int32_t ctas_log;
+    int32_t group_at[kAMaxSlices + 1];  // first group of 32 columns of each slice; all of them
     AdapterUnit units[kUnits];
     int32_t rows[kRows];
 };
@@ -68,14 +79,14 @@ __host__ __device__ constexpr size_t unit_smem(int wide) {
 }  // namespace
 
 template <int kUnits, int kRows>
-__global__ void __launch_bounds__(kAThreads)
+__global__ void __launch_bounds__(kAThreads, 1)
     adapter_units_kernel(const __grid_constant__ UnitParams<kUnits, kRows> u) {
     extern __shared__ __align__(16) float adapter_smem[];
     const AdapterParams &p = u.p;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
-    const uint32_t ctas = cluster_nctarank(), rank = cluster_ctarank();
-    const AdapterUnit &unit = u.units[blockIdx.x / ctas];
+    const int ctas = 1 << u.ctas_log, rank = static_cast<int>(cluster_ctarank());
+    const AdapterUnit unit = u.units[blockIdx.x >> u.ctas_log];
     const int n = unit.n;
     auto row_of = [&](int i) { return static_cast<int64_t>(unit.listed ? u.rows[unit.first + i] : unit.first + i); };
     grid_dep_launch();
@@ -87,37 +98,66 @@ __global__ void __launch_bounds__(kAThreads)
             const int64_t row = row_of(i);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.y + row * p.y_stride);
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * p.out_stride);
-            for (int v = static_cast<int>(rank) * kAThreads + tid; v < vecs; v += static_cast<int>(ctas) * kAThreads)
-                dst[v] = src[v];
+            for (int v = rank * kAThreads + tid; v < vecs; v += kAThreads << u.ctas_log) dst[v] = src[v];
         }
         return;
     }
     const int wide = p.n_slices * p.rank, chunk = min(wide, kAChunk), pitch = unit_pitch(wide);
-    float *const red = adapter_smem;                       // [warp][row][chunk]
+    float *const red = adapter_smem;                         // [warp][row][chunk]
     float *const part = red + kAWarps * kAUnitRows * chunk;  // [row][wide]: this CTA's part of K
-    float *const sum = part + kAUnitRows * wide;           // [row][pitch]
+    float *const sum = part + kAUnitRows * wide;             // [row][pitch]
     const __nv_bfloat16 *const a = p.a + static_cast<int64_t>(unit.adapter) * wide * p.hidden;
     const __nv_bfloat16 *const b = p.b + static_cast<int64_t>(unit.adapter) * p.cols * p.rank;
     const bool has0 = g < n, has1 = g + 8 < n;
     const int64_t row0 = row_of(has0 ? g : 0), row1 = row_of(has1 ? g + 8 : 0);
-    const float scale = p.scales ? __ldg(p.scales + unit.adapter) : 1.f;
     const uint4 zero = make_uint4(0, 0, 0, 0);
 
+    // a group of 32 columns: its slice's inner sums, B and y
+    struct Group {
+        uint2 w[4][kAAhead];  // [column tile][16 of the rank]
+        uint4 y0, y1;
+    };
+    auto column_of = [&](int group, int &slice) {
+        slice = (group >= u.group_at[1]) + (group >= u.group_at[2]) + (group >= u.group_at[3]);
+        return p.slice_at[slice] + (group - u.group_at[slice]) * 32;
+    };
+    auto load_w = [&](int base, int c1, int j, int k) {
+        const int at = base + (g >> 1) * 8 + 2 * j + (g & 1);
+        return k < p.rank && at < c1
+                   ? __ldg(reinterpret_cast<const uint2 *>(b + static_cast<int64_t>(at) * p.rank + k))
+                   : make_uint2(0, 0);
+    };
+    auto fetch = [&](int group, Group &f) {
+        int slice;
+        const int base = column_of(group, slice), c1 = p.slice_at[slice + 1], col = base + 8 * t;
+#pragma unroll
+        for (int q = 0; q < kAAhead; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f.w[j][q] = q * 16 < p.rank ? load_w(base, c1, j, q * 16 + 4 * t) : make_uint2(0, 0);
+        f.y0 = f.y1 = zero;
+        if (col < c1 && has0) f.y0 = *reinterpret_cast<const uint4 *>(p.y + row0 * p.y_stride + col);
+        if (col < c1 && has1) f.y1 = *reinterpret_cast<const uint4 *>(p.y + row1 * p.y_stride + col);
+    };
+    const int n_groups = u.group_at[kAMaxSlices], step = kAWarps << u.ctas_log;
+    int group = rank * kAWarps + warp;
+    Group f;
+
     // ---- s = x A^T over this CTA's blocks of 32 of K
-    const int blocks = (p.hidden + 31) / 32, per = (blocks + static_cast<int>(ctas) - 1) / static_cast<int>(ctas);
-    const int kb1 = min(blocks, (static_cast<int>(rank) + 1) * per);
+    const int blocks = (p.hidden + 31) / 32;
+    const int kb0 = (blocks * rank) >> u.ctas_log, kb1 = (blocks * (rank + 1)) >> u.ctas_log;
     for (int n0 = 0; n0 < wide; n0 += kAChunk) {
         float acc[kAChunk / 8][4] = {};
-        for (int kb = static_cast<int>(rank) * per + warp; kb < kb1; kb += kAWarps) {
+        for (int kb = kb0 + warp; kb < kb1; kb += kAWarps) {
             const int k = kb * 32 + t * 8;
             const bool in = k < p.hidden;
             const uint4 x0 = in && has0 ? __ldg(reinterpret_cast<const uint4 *>(p.x + row0 * p.x_stride + k)) : zero;
             const uint4 x1 = in && has1 ? __ldg(reinterpret_cast<const uint4 *>(p.x + row1 * p.x_stride + k)) : zero;
             uint4 w[kAChunk / 8];
+            const __nv_bfloat16 *const at = a + static_cast<int64_t>(n0 + g) * p.hidden + k;
 #pragma unroll
             for (int j = 0; j < kAChunk / 8; ++j)
                 w[j] = in && n0 + 8 * j < wide
-                           ? __ldg(reinterpret_cast<const uint4 *>(a + static_cast<int64_t>(n0 + 8 * j + g) * p.hidden + k))
+                           ? __ldg(reinterpret_cast<const uint4 *>(at + static_cast<int64_t>(8 * j) * p.hidden))
                            : zero;
             const uint32_t f0[4] = {x0.x, x1.x, x0.y, x1.y}, f1[4] = {x0.z, x1.z, x0.w, x1.w};
 #pragma unroll
@@ -127,12 +167,14 @@ __global__ void __launch_bounds__(kAThreads)
                 mma_16816(acc[j], f1, w[j].z, w[j].w);
             }
         }
+        // (what the second product reads first is on its way while the sums are joined)
+        if (n0 + kAChunk >= wide && group < n_groups) fetch(group, f);
 #pragma unroll
         for (int j = 0; j < kAChunk / 8; ++j) {
             if (n0 + 8 * j >= wide) break;
             float *const to = red + (warp * kAUnitRows + g) * chunk + 8 * j + 2 * t;
             *reinterpret_cast<float2 *>(to) = make_float2(acc[j][0], acc[j][1]);
-            *reinterpret_cast<float2 *>(to + 8 * chunk) = make_float2(acc[j][2], acc[j][3]);
+            if (n > 8) *reinterpret_cast<float2 *>(to + 8 * chunk) = make_float2(acc[j][2], acc[j][3]);
         }
         __syncthreads();
         const int width = min(chunk, wide - n0);
@@ -143,37 +185,50 @@ __global__ void __launch_bounds__(kAThreads)
             for (int w = 0; w < kAWarps; ++w) v += red[(w * kAUnitRows + row) * chunk + c];
             part[row * wide + n0 + c] = v;
         }
-        __syncthreads();
+        if (n0 + kAChunk < wide) __syncthreads();
     }
     cluster_sync_all();
     for (int i = tid; i < kAUnitRows * wide; i += kAThreads) {
         const int row = i / wide, c = i - row * wide;
-        float v = 0.f;
-        if (row < n)
-            for (uint32_t r = 0; r < ctas; ++r) v += ld_cluster_f32(dsmem_addr(smem_u32(part + row * wide + c), r));
+        float v = 0.f, from[kAMaxCluster];
+        if (row < n) {
+            const uint32_t at = smem_u32(part + row * wide + c);
+#pragma unroll
+            for (int r = 0; r < kAMaxCluster; ++r)
+                if (r < ctas) from[r] = ld_cluster_f32(dsmem_addr(at, static_cast<uint32_t>(r)));
+#pragma unroll
+            for (int r = 0; r < kAMaxCluster; ++r)
+                if (r < ctas) v += from[r];
+        }
         sum[row * pitch + c] = v;
     }
-    cluster_sync_all();  // nothing of another CTA's is read from here on
+    __syncthreads();
+    cluster_arrive();  // nothing of another CTA's is read from here on
 
     // ---- out = y + scale s B^T: groups of 32 columns, in each an MMA's column n is
     // column (n / 2) * 8 + 2 j + n % 2 of the group, so that a lane ends with 8 neighbours
-    int group = 0;
-    for (int slice = 0; slice < p.n_slices; ++slice) {
-        const int c0 = p.slice_at[slice], c1 = p.slice_at[slice + 1];
+    const float scale = p.scales ? __ldg(p.scales + unit.adapter) : 1.f;
+    for (; group < n_groups; group += step) {
+        int slice;
+        const int base = column_of(group, slice), c1 = p.slice_at[slice + 1], col = base + 8 * t;
         const float *const s = sum + slice * p.rank;
-        for (int base = c0; base < c1; base += 32, ++group) {
-            if (group % (kAWarps * static_cast<int>(ctas)) != static_cast<int>(rank) * kAWarps + warp) continue;
-            const int col = base + 8 * t;
-            const bool in = col < c1;
-            uint4 y0 = zero, y1 = zero;
-            if (in && has0) y0 = *reinterpret_cast<const uint4 *>(p.y + row0 * p.y_stride + col);
-            if (in && has1) y1 = *reinterpret_cast<const uint4 *>(p.y + row1 * p.y_stride + col);
-            float acc[4][4] = {};
-            for (int q = 0; q < p.rank; q += 16) {
-                const int k = q + 4 * t;
-                const bool k_in = k < p.rank;
+        float acc[4][4] = {};
+#pragma unroll 1
+        for (int q = 0; q < p.rank; q += 16 * kAAhead) {
+            uint2 w[4][kAAhead];
+#pragma unroll
+            for (int e = 0; e < kAAhead; ++e)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j][e] = f.w[j][e];
+                    if (q > 0) w[j][e] = load_w(base, c1, j, q + 16 * e + 4 * t);
+                }
+#pragma unroll
+            for (int e = 0; e < kAAhead; ++e) {
+                const int k = q + 16 * e + 4 * t;
+                if (q + 16 * e >= p.rank) break;
                 float4 s0 = make_float4(0.f, 0.f, 0.f, 0.f), s1 = s0;
-                if (k_in) {
+                if (k < p.rank) {
                     s0 = *reinterpret_cast<const float4 *>(s + g * pitch + k);
                     s1 = *reinterpret_cast<const float4 *>(s + (g + 8) * pitch + k);
                 }
@@ -184,27 +239,27 @@ __global__ void __launch_bounds__(kAThreads)
                 split_bf16(s1.z, s1.w, hi[3], lo[3]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int at = base + (g >> 1) * 8 + 2 * j + (g & 1);
-                    const uint2 w = k_in && at < c1 ? __ldg(reinterpret_cast<const uint2 *>(
-                                                          b + static_cast<int64_t>(at) * p.rank + k))
-                                                    : make_uint2(0, 0);
-                    mma_16816(acc[j], hi, w.x, w.y);
-                    mma_16816(acc[j], lo, w.x, w.y);
+                    mma_16816(acc[j], hi, w[j][e].x, w[j][e].y);
+                    mma_16816(acc[j], lo, w[j][e].x, w[j][e].y);
                 }
             }
-            auto put = [&](uint4 y, int64_t row, int h) {
-                uint32_t v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float lo_ = __uint_as_float(v[j] << 16), hi_ = __uint_as_float(v[j] & 0xFFFF0000u);
-                    v[j] = pack_bf16x2(fmaf(scale, acc[j][2 * h], lo_), fmaf(scale, acc[j][2 * h + 1], hi_));
-                }
-                *reinterpret_cast<uint4 *>(p.out + row * p.out_stride + col) = make_uint4(v[0], v[1], v[2], v[3]);
-            };
-            if (in && has0) put(y0, row0, 0);
-            if (in && has1) put(y1, row1, 1);
         }
+        const uint4 y0 = f.y0, y1 = f.y1;
+        if (group + step < n_groups) fetch(group + step, f);
+        auto put = [&](uint4 y, int64_t row, int h) {
+            uint32_t v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float lo_ = __uint_as_float(v[j] << 16), hi_ = __uint_as_float(v[j] & 0xFFFF0000u);
+                v[j] = pack_bf16x2(fmaf(scale, acc[j][2 * h], lo_), fmaf(scale, acc[j][2 * h + 1], hi_));
+            }
+            *reinterpret_cast<uint4 *>(p.out + row * p.out_stride + col) = make_uint4(v[0], v[1], v[2], v[3]);
+        };
+        if (col < c1 && has0) put(y0, row0, 0);
+        if (col < c1 && has1) put(y1, row1, 1);
     }
+    __syncwarp();
+    cluster_wait();  // nobody leaves while others read its part
 }
 
 // ---------------------------------------------------------------- long runs of rows
@@ -219,16 +274,17 @@ __global__ void __launch_bounds__(kAThreads)
 //   warp 0      TMA: x and A tiles into a ring, B tiles into another, y tiles into a
 //               third, from which, with the products added, they are stored
 //   warp 1      allocates TMEM, issues the MMAs
-//   warps 2-9   inner sums, and y + scale s B^T in shared memory: a thread has a row (its
-//               TMEM lane), two warps each 32 rows, half the block's columns each
+//   warps 2-17  inner sums, and y + scale s B^T in shared memory: a thread has a row (its
+//               TMEM lane); 8 warps have the even blocks of columns, 8 the odd ones, two
+//               of them 32 rows, half the columns each
 // (With y and out moved by the epilogue's threads, through a transposition in shared
 // memory, a block took 3000 cycles: 16384 rows, 4096 x 6144, rank 64 in 176 us.)
 namespace {
 
 constexpr int kTRows = 128;
 constexpr int kTK = 64;
-constexpr int kTThreads = 320;
-constexpr int kTEpilogue = 256;
+constexpr int kTEpilogue = 512;
+constexpr int kTThreads = 64 + kTEpilogue;
 constexpr int kTMaxStages = 6;
 constexpr int kTBStages = 3;
 constexpr int kTYStages = 4;
@@ -254,7 +310,7 @@ static_assert(T_COUNT * 8 + 8 <= kTBarBytes, "barrier area");
 // how a tile lies in shared memory and TMEM
 struct TileShape {
     int32_t rank16;    // rank rounded up to 16
-    int32_t wide16;    // TMEM columns of all slices' inner sums, rounded up to 32
+    int32_t wide16;    // TMEM columns for all slices' inner sums, rounded up to 32
     int32_t block_log; // log2 of the columns of y worked at a time: 128, or 64
     int32_t ctas_log;
     int32_t stages;    // of the ring of x and A
@@ -301,6 +357,16 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
                  : "memory");
     return v;
 }
+__device__ __forceinline__ void tmem_ld16_sync(uint32_t taddr, float (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+          "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t from, int32_t x, int32_t y) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
                      reinterpret_cast<uint64_t>(map)),
@@ -335,6 +401,12 @@ __global__ void __launch_bounds__(kTThreads, 1)
     const int ctas = 1 << ts.ctas_log, rank = static_cast<int>(cluster_ctarank());
     const AdapterTile tile = tp.tiles[blockIdx.x >> ts.ctas_log];
 
+    // the parameters' lines all at once (one after another, as they are used, the first
+    // copies went out 2 us later)
+    if (warp >= 2 && warp < 2 + 8) {
+        const int32_t word = reinterpret_cast<const int32_t *>(&tp)[(warp - 2) * 16];
+        asm volatile("" ::"r"(word));
+    }
     if (warp == 1) {
         tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_base)), static_cast<uint32_t>(ts.tmem));
         tmem_relinquish();
@@ -351,7 +423,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         for (int i = lane; i < T_COUNT; i += 32) {
             const bool by_warps = i == T_READY || (i >= T_YDONE && i < T_YDONE + kTYStages) || i == T_OUTEMPTY ||
                                   i == T_OUTEMPTY + 1;
-            mbar_init(bar(i), by_warps ? 8 : 1);
+            mbar_init(bar(i), i == T_READY ? kTEpilogue / 32 : by_warps ? 8 : 1);
         }
         fence_mbar_init();
     }
@@ -473,38 +545,41 @@ __global__ void __launch_bounds__(kTThreads, 1)
     } else if (warp == 1) {
         // ---------------------------------------------------------------- MMAs
         bool ok = true;
-        {
-            const int width = p.n_slices * ts.rank16;  // N of the first product, in parts of at most 256
-            const int n0 = min(width, 256), n1 = width - n0;
-            const uint32_t idesc = idesc_bf16_f32(kTRows, 16, false, false);
-            const uint32_t idesc0 = idesc + (static_cast<uint32_t>((n0 - 16) >> 3) << 17);
-            const uint32_t idesc1 = idesc + (static_cast<uint32_t>((n1 - 16) >> 3) << 17);
+        const int width = p.n_slices * ts.rank16;  // N of the first product, in parts of at most 256
+        const uint32_t idesc16 = idesc_bf16_f32(kTRows, 16, false, false);
+        // (two loops: what an iteration issues decides how fast blocks of K are taken,
+        // with the test for a second part in it 470 cycles, 350 without)
+        auto inner_sums = [&](auto parts) {
+            constexpr bool kTwo = decltype(parts)::value == 2;
+            const uint32_t idesc0 = idesc16 + (static_cast<uint32_t>(((kTwo ? 256 : width) - 16) >> 3) << 17);
+            const uint32_t idesc1 = idesc16 + (static_cast<uint32_t>((width - 256 - 16) >> 3) << 17);
             const uint64_t dx0 = smem_desc_sw128(sb, 16, 1024), da0 = smem_desc_sw128(sb + kTXBytes, 16, 1024);
-            for (int q = 0, s = 0, round = 0; q < kb1 - kb0; ++q) {
-                if (!mbar_wait_warp(bar(T_FULL + s), round & 1, tp.err)) {
-                    ok = false;
-                    break;
-                }
+            uint32_t accumulate = 0;
+            for (int q = kb1 - kb0, s = 0, parity = 0; q > 0; --q) {
+                if (!mbar_wait_warp(bar(T_FULL + s), parity, tp.err)) return false;
                 tc_fence_after();
                 const uint64_t at = (static_cast<uint32_t>(s) * stage_bytes) >> 4;
+                const uint64_t dx = dx0 + at, da = da0 + at;
                 if (elect_one()) {
 #pragma unroll
                     for (int kk = 0; kk < kTK / 16; ++kk) {
-                        const uint32_t accumulate = q > 0 || kk > 0 ? 1u : 0u;
-                        umma_bf16(tmem, dx0 + at + kk * 2, da0 + at + kk * 2, idesc0, accumulate);
-                        if (n1 > 0)
-                            umma_bf16(tmem + 256, dx0 + at + kk * 2, da0 + at + 256 * 8 + kk * 2, idesc1, accumulate);
+                        umma_bf16(tmem, dx + kk * 2, da + kk * 2, idesc0, kk > 0 ? 1u : accumulate);
+                        if (kTwo) umma_bf16(tmem + 256, dx + kk * 2, da + 256 * 8 + kk * 2, idesc1, kk > 0 ? 1u : accumulate);
                     }
                     umma_commit(bar(T_EMPTY + s));
-                    if (q == kb1 - kb0 - 1) umma_commit(bar(T_SUMS));
                 }
                 __syncwarp();
+                accumulate = 1;
                 if (++s == ts.stages) {
                     s = 0;
-                    ++round;
+                    parity ^= 1;
                 }
             }
-        }
+            if (elect_one()) umma_commit(bar(T_SUMS));
+            __syncwarp();
+            return true;
+        };
+        ok = width > 256 ? inner_sums(std::integral_constant<int, 2>{}) : inner_sums(std::integral_constant<int, 1>{});
         cluster_point();
         cluster_point();
         if (ok) ok = mbar_wait_warp(bar(T_READY), 0, tp.err);
@@ -525,12 +600,11 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 const uint32_t d = outs + static_cast<uint32_t>(buf * block);
                 const uint64_t db = db0 + ((static_cast<uint32_t>(s) * ts.b_bytes) >> 4);
                 for (int k = 0; k < ts.rank16; k += 16) {
-                    // 16 inner sums: columns c .. c + 15 became halves of 8 columns each of c's group of 32
-                    const int c = slice * ts.rank16 + k;
-                    const uint32_t a = tmem + static_cast<uint32_t>((c & ~31) + ((c & 16) >> 1));
+                    // 16 inner sums: of their columns the first 8 hold their values, the others what was left
+                    const uint32_t a = tmem + static_cast<uint32_t>(slice * ts.rank16 + k);
                     const uint64_t b = db + static_cast<uint64_t>((k >> 6) * block * 8 + ((k & 63) >> 3));
                     umma_bf16_ts(d, a, b, idesc, k > 0 ? 1u : 0u);
-                    umma_bf16_ts(d, a + 16, b, idesc, 1u);
+                    umma_bf16_ts(d, a + 8, b, idesc, 1u);
                 }
                 umma_commit(bar(T_BEMPTY + s));
                 umma_commit(bar(T_OUTFULL + buf));
@@ -543,7 +617,9 @@ __global__ void __launch_bounds__(kTThreads, 1)
         mbar_wait_warp(bar(T_DONE), 0, tp.err);
     } else {
         // ---------------------------------------------------------------- inner sums, output
-        const int wq = warp & 3, half = (warp - 2) >> 2;  // TMEM lane quarter, half of the columns
+        // TMEM lane quarter, half of the columns, even or odd blocks
+        const int wq = warp & 3, half = ((warp - 2) >> 2) & 1, set = (warp - 2) >> 3;
+        const int c_first = ((warp - 2) >> 2) * 16, c_step = kTEpilogue / 8;  // inner sums of this warp: 16 columns at a time
         const int row = wq * 32 + lane;                    // this thread's TMEM lane
         const uint32_t t_lane = static_cast<uint32_t>(wq * 32) << 16;
         const float scale = p.scales ? __ldg(p.scales + tile.adapter) : 1.f;
@@ -551,59 +627,57 @@ __global__ void __launch_bounds__(kTThreads, 1)
         bool ok = mbar_wait_warp(bar(T_SUMS), 0, tp.err);
         if (!ok) *abort_flag = 1;
         tc_fence_after();
-        const int pitch = ts.wide16 + 4, own_log = 7 - ts.ctas_log;
+        const int width = p.n_slices * ts.rank16, pitch = ts.wide16 + 4, own_log = 7 - ts.ctas_log;
         // [128 / ctas][pitch] the cluster's sums of this CTA's rows, [128][pitch] this CTA's part
         float *const summed = reinterpret_cast<float *>(sg);
         float *const part = reinterpret_cast<float *>(sg + sums_bytes(ts.wide16, kTRows >> ts.ctas_log));
         if (ctas > 1) {
-            for (int c = half * 32; ok && c < ts.wide16; c += 64) {
-                float v[32];
-                tmem_ld32_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
+            for (int c = c_first; ok && c < width; c += c_step) {
+                float v[16];
+                tmem_ld16_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
                 float4 *const to = reinterpret_cast<float4 *>(part + row * pitch + c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                for (int i = 0; i < 4; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             }
             cluster_point();
-            const int vecs = ts.wide16 / 4;
+            const int vecs = width / 4;
             for (int i = tid - 64; i < vecs << own_log; i += kTEpilogue) {
                 const int r = i / vecs, c = (i - r * vecs) * 4;
                 const uint32_t at = smem_u32(part + ((rank << own_log) + r) * pitch + c);
-                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int o = 0; o < ctas; ++o) {
-                    const float4 v = ld_cluster_f32x4(dsmem_addr(at, static_cast<uint32_t>(o)));
-                    sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-                }
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f), v[kAMaxCluster];
+#pragma unroll
+                for (int o = 0; o < kAMaxCluster; ++o)
+                    if (o < ctas) v[o] = ld_cluster_f32x4(dsmem_addr(at, static_cast<uint32_t>(o)));
+#pragma unroll
+                for (int o = 0; o < kAMaxCluster; ++o)
+                    if (o < ctas) sum.x += v[o].x, sum.y += v[o].y, sum.z += v[o].z, sum.w += v[o].w;
                 *reinterpret_cast<float4 *>(summed + r * pitch + c) = sum;
             }
             fence_proxy_async_smem();  // y's copies come where the parts were
             cluster_point();
         }
-        for (int c = half * 32; ok && c < ts.wide16; c += 64) {
-            float v[32];
+        for (int c = c_first; ok && c < width; c += c_step) {
+            float v[16];
             if (ctas > 1) {
                 const uint32_t at = dsmem_addr(smem_u32(summed + (row & ((1 << own_log) - 1)) * pitch + c),
                                                static_cast<uint32_t>(row >> own_log));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     const float4 w = ld_cluster_f32x4(at + 16u * static_cast<uint32_t>(i));
                     v[4 * i] = w.x, v[4 * i + 1] = w.y, v[4 * i + 2] = w.z, v[4 * i + 3] = w.w;
                 }
             } else {
-                tmem_ld32_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
+                tmem_ld16_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
             }
-            uint32_t r[32];
+            // (columns past the rank are 0, A's rows there are; but for rows with an infinity, so they are made so)
+            const int some = p.rank - c % ts.rank16;
+            uint32_t r[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // columns past the rank, and past the last slice, are 0 (but for rows with an infinity)
-                const int at = c + 16 * h, in_slice = at % ts.rank16;
-                const int some = at < p.n_slices * ts.rank16 ? p.rank - in_slice : 0;
-#pragma unroll
-                for (int i = 8 * h; i < 8 * h + 8; ++i) {
-                    const bool in = 2 * (i - 8 * h) < some;  // (the rank is even)
-                    split_bf16(in ? v[2 * i] : 0.f, in ? v[2 * i + 1] : 0.f, r[i], r[16 + i]);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const bool in = 2 * i < some;  // (the rank is even)
+                split_bf16(in ? v[2 * i] : 0.f, in ? v[2 * i + 1] : 0.f, r[i], r[8 + i]);
             }
-            tmem_st32(tmem + t_lane + static_cast<uint32_t>(c), r);
+            tmem_st16(tmem + t_lane + static_cast<uint32_t>(c), r);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -616,8 +690,8 @@ __global__ void __launch_bounds__(kTThreads, 1)
         const int first = block == 128 ? 0 : half * 4;  // 16-byte pieces of the box's 128-byte rows
         const int col = half * (block / 2);
         const float2 scale2 = make_float2(scale, scale);
-        for (int i = 0, s = 0, round = 0; i < mine; ++i) {
-            const int buf = i & 1;
+        for (int i = set; i < mine; i += 2) {
+            const int buf = i & 1, s = i % ts.y_stages, round = i / ts.y_stages;
             if (!mbar_wait_warp(bar(T_OUTFULL + buf), (i >> 1) & 1, tp.err) ||
                 !mbar_wait_warp(bar(T_YFULL + s), round & 1, tp.err) || __any_sync(0xffffffffu, *abort_flag)) {
                 ok = false;
@@ -682,10 +756,6 @@ __global__ void __launch_bounds__(kTThreads, 1)
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(T_YDONE + s));
-            if (++s == ts.y_stages) {
-                s = 0;
-                ++round;
-            }
         }
         if (!ok) *abort_flag = 1;
     }
@@ -713,11 +783,9 @@ AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *a
             continue;
         }
         int32_t r = first;
-        while (at - r >= tile_rows) {
-            const int32_t n = std::min(kATileRows, at - r);
-            plan.tiles.push_back({r, id, n});
-            r += n;
-        }
+        for (const bool tiles = at - r >= tile_rows; tiles && r < at; r += kATileRows)
+            plan.tiles.push_back({r, id, std::min(kATileRows, at - r)});
+        r = std::min(r, at);
         for (; at - r >= kAUnitRows; r += kAUnitRows) plan.units.push_back({r, id, kAUnitRows, 0});
         for (; r < at; ++r) rows.emplace_back(id, r);
     }
@@ -757,9 +825,16 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
         }
         u.units[n] = unit;
     }
-    // as many CTAs a unit as the SMs hold twice, 128 values of K each at least
-    int c = 1;
-    while (c < kAMaxCluster && 2 * c * n <= 2 * device_sm_count() && p.hidden >= 2 * c * 128) c *= 2;
+    for (int j = 0, at = 0; j <= kAMaxSlices; ++j) {
+        u.group_at[j] = at;
+        if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + 31) / 32;
+    }
+    // as many CTAs a unit as there are SMs for, 128 values of K each at least
+    u.ctas_log = 0;
+    while (2 << u.ctas_log <= kAMaxCluster && (2 << u.ctas_log) * n <= device_sm_count() * USLOT &&
+           p.hidden >= (2 << u.ctas_log) * 128)
+        ++u.ctas_log;
+    const int c = 1 << u.ctas_log;
     PdlLaunch l(dim3(static_cast<unsigned>(n * c)), dim3(kAThreads), unit_smem(wide), st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
