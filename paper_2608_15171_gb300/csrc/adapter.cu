@@ -69,11 +69,12 @@ struct UnitParams {
     int32_t rows[kRows];
 };
 
+// floats of a warp's sums of 16 rows and up to kAChunk columns
+__host__ __device__ constexpr int unit_red(int wide) { return kAUnitRows * (wide < kAChunk ? wide : kAChunk); }
 __host__ __device__ constexpr int unit_pitch(int wide) { return wide + 4; }
-__host__ __device__ constexpr size_t unit_smem(int wide) {
-    const int chunk = wide < kAChunk ? wide : kAChunk;
-    return 4 * (static_cast<size_t>(kAWarps) * kAUnitRows * chunk + kAUnitRows * wide +
-                kAUnitRows * unit_pitch(wide));
+__host__ __device__ constexpr size_t unit_smem(int wide, int steps) {
+    return 4 * (static_cast<size_t>(kAWarps) * unit_red(wide) + kAUnitRows * wide + kAUnitRows * unit_pitch(wide)) +
+           static_cast<size_t>(steps) * 32 * 32;
 }
 
 }  // namespace
@@ -102,49 +103,34 @@ __global__ void __launch_bounds__(kAThreads, 1)
         }
         return;
     }
-    const int wide = p.n_slices * p.rank, chunk = min(wide, kAChunk), pitch = unit_pitch(wide);
-    float *const red = adapter_smem;                         // [warp][row][chunk]
-    float *const part = red + kAWarps * kAUnitRows * chunk;  // [row][wide]: this CTA's part of K
-    float *const sum = part + kAUnitRows * wide;             // [row][pitch]
+    const int wide = p.n_slices * p.rank, pitch = unit_pitch(wide), rank16 = (p.rank + 15) / 16;
+    float *const red = adapter_smem;                          // [warp][row][columns]
+    float *const part = red + kAWarps * unit_red(wide);       // [row][wide]: this CTA's part of K
+    float *const sum = part + kAUnitRows * wide;              // [row][pitch]
+    uint4 *const frag = reinterpret_cast<uint4 *>(sum + kAUnitRows * pitch);  // [slice][16 of the rank][lane][2]
     const __nv_bfloat16 *const a = p.a + static_cast<int64_t>(unit.adapter) * wide * p.hidden;
     const __nv_bfloat16 *const b = p.b + static_cast<int64_t>(unit.adapter) * p.cols * p.rank;
     const bool has0 = g < n, has1 = g + 8 < n;
     const int64_t row0 = row_of(has0 ? g : 0), row1 = row_of(has1 ? g + 8 : 0);
     const uint4 zero = make_uint4(0, 0, 0, 0);
 
-    // a group of 32 columns: its slice's inner sums, B and y
-    struct Group {
-        uint2 w[4][kAAhead];  // [column tile][16 of the rank]
-        uint4 y0, y1;
-    };
-    auto column_of = [&](int group, int &slice) {
-        slice = (group >= u.group_at[1]) + (group >= u.group_at[2]) + (group >= u.group_at[3]);
-        return p.slice_at[slice] + (group - u.group_at[slice]) * 32;
-    };
-    auto load_w = [&](int base, int c1, int j, int k) {
-        const int at = base + (g >> 1) * 8 + 2 * j + (g & 1);
-        return k < p.rank && at < c1
-                   ? __ldg(reinterpret_cast<const uint2 *>(b + static_cast<int64_t>(at) * p.rank + k))
-                   : make_uint2(0, 0);
-    };
-    auto fetch = [&](int group, Group &f) {
-        int slice;
-        const int base = column_of(group, slice), c1 = p.slice_at[slice + 1], col = base + 8 * t;
-#pragma unroll
-        for (int q = 0; q < kAAhead; ++q)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f.w[j][q] = q * 16 < p.rank ? load_w(base, c1, j, q * 16 + 4 * t) : make_uint2(0, 0);
-        f.y0 = f.y1 = zero;
-        if (col < c1 && has0) f.y0 = *reinterpret_cast<const uint4 *>(p.y + row0 * p.y_stride + col);
-        if (col < c1 && has1) f.y1 = *reinterpret_cast<const uint4 *>(p.y + row1 * p.y_stride + col);
-    };
-    const int n_groups = u.group_at[kAMaxSlices], step = kAWarps << u.ctas_log;
-    int group = rank * kAWarps + warp;
-    Group f;
-
     // ---- s = x A^T over this CTA's blocks of 32 of K
     const int blocks = (p.hidden + 31) / 32;
     const int kb0 = (blocks * rank) >> u.ctas_log, kb1 = (blocks * (rank + 1)) >> u.ctas_log;
+    // where a warp's place holds the sums of all columns they are joined once, else kAChunk of them at a time
+    const bool once = n * wide <= unit_red(wide);
+    const int red_pitch = once ? wide : min(wide, kAChunk);
+    auto join = [&](int c0, int width) {
+        __syncthreads();
+        for (int i = tid; i < n * width; i += kAThreads) {
+            const int row = i / width, c = i - row * width;
+            const float *const from = red + row * red_pitch + (once ? c0 : 0) + c;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kAWarps; ++w) v += from[w * unit_red(wide)];
+            part[row * wide + c0 + c] = v;
+        }
+    };
     for (int n0 = 0; n0 < wide; n0 += kAChunk) {
         float acc[kAChunk / 8][4] = {};
         for (int kb = kb0 + warp; kb < kb1; kb += kAWarps) {
@@ -153,12 +139,12 @@ __global__ void __launch_bounds__(kAThreads, 1)
             const uint4 x0 = in && has0 ? __ldg(reinterpret_cast<const uint4 *>(p.x + row0 * p.x_stride + k)) : zero;
             const uint4 x1 = in && has1 ? __ldg(reinterpret_cast<const uint4 *>(p.x + row1 * p.x_stride + k)) : zero;
             uint4 w[kAChunk / 8];
-            const __nv_bfloat16 *const at = a + static_cast<int64_t>(n0 + g) * p.hidden + k;
+            const __nv_bfloat16 *at = a + static_cast<int64_t>(n0 + g) * p.hidden + k;
 #pragma unroll
-            for (int j = 0; j < kAChunk / 8; ++j)
-                w[j] = in && n0 + 8 * j < wide
-                           ? __ldg(reinterpret_cast<const uint4 *>(at + static_cast<int64_t>(8 * j) * p.hidden))
-                           : zero;
+            for (int j = 0; j < kAChunk / 8; ++j) {
+                w[j] = in && n0 + 8 * j < wide ? __ldg(reinterpret_cast<const uint4 *>(at)) : zero;
+                at += 8 * p.hidden;
+            }
             const uint32_t f0[4] = {x0.x, x1.x, x0.y, x1.y}, f1[4] = {x0.z, x1.z, x0.w, x1.w};
 #pragma unroll
             for (int j = 0; j < kAChunk / 8; ++j) {
@@ -167,26 +153,55 @@ __global__ void __launch_bounds__(kAThreads, 1)
                 mma_16816(acc[j], f1, w[j].z, w[j].w);
             }
         }
-        // (what the second product reads first is on its way while the sums are joined)
-        if (n0 + kAChunk >= wide && group < n_groups) fetch(group, f);
+        float *const to = red + warp * unit_red(wide) + g * red_pitch + (once ? n0 : 0) + 2 * t;
 #pragma unroll
         for (int j = 0; j < kAChunk / 8; ++j) {
             if (n0 + 8 * j >= wide) break;
-            float *const to = red + (warp * kAUnitRows + g) * chunk + 8 * j + 2 * t;
-            *reinterpret_cast<float2 *>(to) = make_float2(acc[j][0], acc[j][1]);
-            if (n > 8) *reinterpret_cast<float2 *>(to + 8 * chunk) = make_float2(acc[j][2], acc[j][3]);
+            if (has0) *reinterpret_cast<float2 *>(to + 8 * j) = make_float2(acc[j][0], acc[j][1]);
+            if (has1) *reinterpret_cast<float2 *>(to + 8 * red_pitch + 8 * j) = make_float2(acc[j][2], acc[j][3]);
         }
-        __syncthreads();
-        const int width = min(chunk, wide - n0);
-        for (int i = tid; i < n * width; i += kAThreads) {
-            const int row = i / width, c = i - row * width;
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < kAWarps; ++w) v += red[(w * kAUnitRows + row) * chunk + c];
-            part[row * wide + n0 + c] = v;
+        if (!once) {
+            join(n0, min(kAChunk, wide - n0));
+            __syncthreads();
         }
-        if (n0 + kAChunk < wide) __syncthreads();
     }
+    // ---- out = y + scale s B^T: groups of 32 columns, in each an MMA's column n is
+    // column (n / 2) * 8 + 2 j + n % 2 of the group, so that a lane ends with 8 neighbours
+    struct Group {
+        int slice, col;  // this lane's columns: col .. col + 7
+        bool in;
+        const __nv_bfloat16 *b;  // its first row of B, the column tiles' 2 rows apart
+        int rows;                // of B from there to the slice's end
+        uint2 w[4][kAAhead];     // [column tile][16 of the rank]
+        uint4 y0, y1;
+    };
+    auto load_w = [&](const Group &f, int j, int k) {
+        return 2 * j < f.rows && k + 4 * t < p.rank ? __ldg(reinterpret_cast<const uint2 *>(f.b + 2 * j * p.rank + k))
+                                                    : make_uint2(0, 0);
+    };
+    auto fetch = [&](int group, Group &f) {
+        f.slice = (group >= u.group_at[1]) + (group >= u.group_at[2]) + (group >= u.group_at[3]);
+        const int base = p.slice_at[f.slice] + (group - u.group_at[f.slice]) * 32, c1 = p.slice_at[f.slice + 1];
+        const int first = base + (g >> 1) * 8 + (g & 1);
+        f.col = base + 8 * t;
+        f.in = f.col < c1;
+        f.rows = c1 - first;
+        f.b = b + static_cast<int64_t>(first) * p.rank + 4 * t;
+#pragma unroll
+        for (int q = 0; q < kAAhead; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f.w[j][q] = load_w(f, j, 16 * q);
+        f.y0 = f.y1 = zero;
+        if (f.in && has0) f.y0 = *reinterpret_cast<const uint4 *>(p.y + row0 * p.y_stride + f.col);
+        if (f.in && has1) f.y1 = *reinterpret_cast<const uint4 *>(p.y + row1 * p.y_stride + f.col);
+    };
+    const int n_groups = u.group_at[kAMaxSlices], step = kAWarps << u.ctas_log;
+    int group = rank * kAWarps + warp;
+    Group f;
+    f.slice = 0;
+    // (what the second product reads first is on its way while the sums are joined)
+    if (group < n_groups) fetch(group, f);
+    if (once) join(0, wide);
     cluster_sync_all();
     for (int i = tid; i < kAUnitRows * wide; i += kAThreads) {
         const int row = i / wide, c = i - row * wide;
@@ -204,47 +219,51 @@ __global__ void __launch_bounds__(kAThreads, 1)
     }
     __syncthreads();
     cluster_arrive();  // nothing of another CTA's is read from here on
-
-    // ---- out = y + scale s B^T: groups of 32 columns, in each an MMA's column n is
-    // column (n / 2) * 8 + 2 j + n % 2 of the group, so that a lane ends with 8 neighbours
+    // as the second product's operand, once for all groups: per lane the values and what their rounding left
+    for (int i = tid; i < p.n_slices * rank16 * 32; i += kAThreads) {
+        const int s = i >> 5, l = i & 31, k = s % rank16 * 16 + 4 * (l & 3);
+        float4 s0 = make_float4(0.f, 0.f, 0.f, 0.f), s1 = s0;
+        if (k < p.rank) {
+            const float *const from = sum + (l >> 2) * pitch + s / rank16 * p.rank + k;
+            s0 = *reinterpret_cast<const float4 *>(from);
+            s1 = *reinterpret_cast<const float4 *>(from + 8 * pitch);
+        }
+        uint4 hi, lo;
+        split_bf16(s0.x, s0.y, hi.x, lo.x);
+        split_bf16(s1.x, s1.y, hi.y, lo.y);
+        split_bf16(s0.z, s0.w, hi.z, lo.z);
+        split_bf16(s1.z, s1.w, hi.w, lo.w);
+        frag[2 * i] = hi;
+        frag[2 * i + 1] = lo;
+    }
     const float scale = p.scales ? __ldg(p.scales + unit.adapter) : 1.f;
+    __syncthreads();
     for (; group < n_groups; group += step) {
-        int slice;
-        const int base = column_of(group, slice), c1 = p.slice_at[slice + 1], col = base + 8 * t;
-        const float *const s = sum + slice * p.rank;
         float acc[4][4] = {};
+        const uint4 *const s = frag + 2 * (f.slice * rank16 * 32 + lane);
 #pragma unroll 1
-        for (int q = 0; q < p.rank; q += 16 * kAAhead) {
-            uint2 w[4][kAAhead];
+        for (int q0 = 0; q0 < rank16; q0 += kAAhead) {
+            if (q0 > 0) {
 #pragma unroll
-            for (int e = 0; e < kAAhead; ++e)
+                for (int e = 0; e < kAAhead; ++e)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    w[j][e] = f.w[j][e];
-                    if (q > 0) w[j][e] = load_w(base, c1, j, q + 16 * e + 4 * t);
-                }
+                    for (int j = 0; j < 4; ++j) f.w[j][e] = load_w(f, j, 16 * (q0 + e));
+            }
 #pragma unroll
             for (int e = 0; e < kAAhead; ++e) {
-                const int k = q + 16 * e + 4 * t;
-                if (q + 16 * e >= p.rank) break;
-                float4 s0 = make_float4(0.f, 0.f, 0.f, 0.f), s1 = s0;
-                if (k < p.rank) {
-                    s0 = *reinterpret_cast<const float4 *>(s + g * pitch + k);
-                    s1 = *reinterpret_cast<const float4 *>(s + (g + 8) * pitch + k);
-                }
-                uint32_t hi[4], lo[4];
-                split_bf16(s0.x, s0.y, hi[0], lo[0]);
-                split_bf16(s1.x, s1.y, hi[1], lo[1]);
-                split_bf16(s0.z, s0.w, hi[2], lo[2]);
-                split_bf16(s1.z, s1.w, hi[3], lo[3]);
+                if (q0 + e >= rank16) break;
+                const uint4 h = s[(q0 + e) * 64], l = s[(q0 + e) * 64 + 1];
+                const uint32_t hi[4] = {h.x, h.y, h.z, h.w}, lo[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    mma_16816(acc[j], hi, w[j][e].x, w[j][e].y);
-                    mma_16816(acc[j], lo, w[j][e].x, w[j][e].y);
+                    mma_16816(acc[j], hi, f.w[j][e].x, f.w[j][e].y);
+                    mma_16816(acc[j], lo, f.w[j][e].x, f.w[j][e].y);
                 }
             }
         }
         const uint4 y0 = f.y0, y1 = f.y1;
+        const int col = f.col;
+        const bool in = f.in;
         if (group + step < n_groups) fetch(group + step, f);
         auto put = [&](uint4 y, int64_t row, int h) {
             uint32_t v[4] = {y.x, y.y, y.z, y.w};
@@ -255,8 +274,8 @@ __global__ void __launch_bounds__(kAThreads, 1)
             }
             *reinterpret_cast<uint4 *>(p.out + row * p.out_stride + col) = make_uint4(v[0], v[1], v[2], v[3]);
         };
-        if (col < c1 && has0) put(y0, row0, 0);
-        if (col < c1 && has1) put(y1, row1, 1);
+        if (in && has0) put(y0, row0, 0);
+        if (in && has1) put(y1, row1, 1);
     }
     __syncwarp();
     cluster_wait();  // nobody leaves while others read its part
@@ -810,7 +829,8 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     const auto kernel = adapter_units_kernel<kUnits, kRows>;
     const int wide = p.n_slices * p.rank;
     const cudaError_t e =
-        ensure_smem_limit(kernel, static_cast<int>(unit_smem(kAMaxSlices * kAMaxRank)), smem_set);
+        ensure_smem_limit(
+        kernel, static_cast<int>(unit_smem(kAMaxSlices * kAMaxRank, kAMaxSlices * kAMaxRank / 16)), smem_set);
     if (e != cudaSuccess) return e;
     UnitParams<kUnits, kRows> u;
     u.p = p;
@@ -835,7 +855,8 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
            p.hidden >= (2 << u.ctas_log) * 128)
         ++u.ctas_log;
     const int c = 1 << u.ctas_log;
-    PdlLaunch l(dim3(static_cast<unsigned>(n * c)), dim3(kAThreads), unit_smem(wide), st);
+    PdlLaunch l(dim3(static_cast<unsigned>(n * c)), dim3(kAThreads),
+                unit_smem(wide, p.n_slices * ((p.rank + 15) / 16)), st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
         attrs[1].id = cudaLaunchAttributeClusterDimension;
