@@ -25,16 +25,17 @@
 namespace ppas {
 namespace {
 
-#ifndef USLOT
-#define USLOT 1
-#endif
 constexpr int kAThreads = 512;
 constexpr int kAWarps = kAThreads / 32;
 constexpr int kAChunk = 96;  // inner sums worked at a time: the loads of 12 x 16 bytes a lane are under way at once
 constexpr int kAAhead = 4;   // of the rank in B, 16 times this are loaded ahead
 constexpr int kAMaxCluster = 8;
 constexpr int32_t kATileRows = 128;  // rows of a tile
-constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make one
+constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make tiles,
+// and of all such runs together (below, units of 16 rows are done first: 512 rows, 2048 x
+// 2560, rank 16 7.1 us, tiles 10.0; 4096 x 6144, rank 64 21.7, 22.3; past it 1024 rows 16.9,
+// 15.3 and 37.6, 24.9)
+constexpr int32_t kATileTotal = 513;
 constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space)
 constexpr uint32_t kTSmem = 232448;  // shared memory of a CTA
 
@@ -63,7 +64,8 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint3
 template <int kUnits, int kRows>
 struct UnitParams {
     AdapterParams p;
-    int32_t ctas_log;
+    int32_t ctas;          // of a cluster
+    int32_t beside_tiles;  // launched behind a call's tiles, to run beside them
     int32_t group_at[kAMaxSlices + 1];  // first group of 32 columns of each slice; all of them
     AdapterUnit units[kUnits];
     int32_t rows[kRows];
@@ -86,12 +88,16 @@ __global__ void __launch_bounds__(kAThreads, 1)
     const AdapterParams &p = u.p;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
-    const int ctas = 1 << u.ctas_log, rank = static_cast<int>(cluster_ctarank());
-    const AdapterUnit unit = u.units[blockIdx.x >> u.ctas_log];
+    const int ctas = u.ctas, rank = static_cast<int>(cluster_ctarank());
+    const AdapterUnit unit = u.units[blockIdx.x / static_cast<uint32_t>(ctas)];
     const int n = unit.n;
     auto row_of = [&](int i) { return static_cast<int64_t>(unit.listed ? u.rows[unit.first + i] : unit.first + i); };
     grid_dep_launch();
-    grid_dep_wait();
+    // Beside tiles: their kernel lets this one start only after its own wait, so all that
+    // came before the call has completed; the two write different rows and read nothing
+    // that the other writes.  The wait comes at the end then, so that what follows this
+    // kernel follows the tiles too.
+    if (!u.beside_tiles) grid_dep_wait();
 
     if (unit.adapter < 0) {  // (every CTA of the cluster)
         const int vecs = p.cols / 8;
@@ -99,8 +105,9 @@ __global__ void __launch_bounds__(kAThreads, 1)
             const int64_t row = row_of(i);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.y + row * p.y_stride);
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * p.out_stride);
-            for (int v = rank * kAThreads + tid; v < vecs; v += kAThreads << u.ctas_log) dst[v] = src[v];
+            for (int v = rank * kAThreads + tid; v < vecs; v += kAThreads * ctas) dst[v] = src[v];
         }
+        if (u.beside_tiles) grid_dep_wait();
         return;
     }
     const int wide = p.n_slices * p.rank, pitch = unit_pitch(wide), rank16 = (p.rank + 15) / 16;
@@ -116,7 +123,7 @@ __global__ void __launch_bounds__(kAThreads, 1)
 
     // ---- s = x A^T over this CTA's blocks of 32 of K
     const int blocks = (p.hidden + 31) / 32;
-    const int kb0 = (blocks * rank) >> u.ctas_log, kb1 = (blocks * (rank + 1)) >> u.ctas_log;
+    const int kb0 = blocks * rank / ctas, kb1 = blocks * (rank + 1) / ctas;
     // where a warp's place holds the sums of all columns they are joined once, else kAChunk of them at a time
     const bool once = n * wide <= unit_red(wide);
     const int red_pitch = once ? wide : min(wide, kAChunk);
@@ -195,7 +202,7 @@ __global__ void __launch_bounds__(kAThreads, 1)
         if (f.in && has0) f.y0 = *reinterpret_cast<const uint4 *>(p.y + row0 * p.y_stride + f.col);
         if (f.in && has1) f.y1 = *reinterpret_cast<const uint4 *>(p.y + row1 * p.y_stride + f.col);
     };
-    const int n_groups = u.group_at[kAMaxSlices], step = kAWarps << u.ctas_log;
+    const int n_groups = u.group_at[kAMaxSlices], step = kAWarps * ctas;
     int group = rank * kAWarps + warp;
     Group f;
     f.slice = 0;
@@ -279,6 +286,7 @@ __global__ void __launch_bounds__(kAThreads, 1)
     }
     __syncwarp();
     cluster_wait();  // nobody leaves while others read its part
+    if (u.beside_tiles) grid_dep_wait();
 }
 
 // ---------------------------------------------------------------- long runs of rows
@@ -331,14 +339,16 @@ struct TileShape {
     int32_t rank16;    // rank rounded up to 16
     int32_t wide16;    // TMEM columns for all slices' inner sums, rounded up to 32
     int32_t block_log; // log2 of the columns of y worked at a time: 128, or 64
-    int32_t ctas_log;
+    int32_t ctas;      // of a cluster
+    int32_t own_rows;  // of the sums that each of them joins
     int32_t stages;    // of the ring of x and A
     uint32_t a_bytes;  // of a stage: the slices' A tiles
     uint32_t b_bytes;  // of a B tile: block rows, 128 bytes for each 64 of rank
-    // y's ring, where the ring of x and A was and behind it (behind the sums that the
-    // cluster's other CTAs read)
-    uint32_t y_at;
-    int32_t y_stages;
+    // y's ring lies where the ring of x and A was, and in a cluster, from stage y_free on,
+    // where the parts of the sums are until they are an operand; the sums that other
+    // CTAs read come behind
+    int32_t y_stages, y_free;
+    uint32_t part_at, summed_at;
     uint32_t b_at, bars_at, smem;  // offsets, and all of it
     int32_t tmem;      // columns allocated
 };
@@ -417,8 +427,8 @@ __global__ void __launch_bounds__(kTThreads, 1)
     auto bar = [&](int i) { return sb + ts.bars_at + 8u * static_cast<uint32_t>(i); };
     volatile uint32_t *const tmem_base = reinterpret_cast<volatile uint32_t *>(sg + ts.bars_at + T_COUNT * 8);
     volatile int *const abort_flag = reinterpret_cast<volatile int *>(sg + ts.bars_at + T_COUNT * 8 + 4);
-    const int ctas = 1 << ts.ctas_log, rank = static_cast<int>(cluster_ctarank());
-    const AdapterTile tile = tp.tiles[blockIdx.x >> ts.ctas_log];
+    const int ctas = ts.ctas, rank = static_cast<int>(cluster_ctarank());
+    const AdapterTile tile = tp.tiles[blockIdx.x / static_cast<uint32_t>(ctas)];
 
     // the parameters' lines all at once (one after another, as they are used, the first
     // copies went out 2 us later)
@@ -457,8 +467,8 @@ __global__ void __launch_bounds__(kTThreads, 1)
 
     // this CTA's blocks of K, and its blocks of columns: rank, rank + ctas, ...
     const int k_blocks = (p.hidden + kTK - 1) / kTK;
-    const int kb0 = (k_blocks * rank) >> ts.ctas_log, kb1 = (k_blocks * (rank + 1)) >> ts.ctas_log;
-    const int mine = (tp.block_at[kAMaxSlices] - rank + ctas - 1) >> ts.ctas_log;
+    const int kb0 = k_blocks * rank / ctas, kb1 = k_blocks * (rank + 1) / ctas;
+    const int mine = (tp.block_at[kAMaxSlices] - rank + ctas - 1) / ctas;
     const uint32_t stage_bytes = kTXBytes + ts.a_bytes;
     const int block = 1 << ts.block_log, boxes = block / 64;
     const uint32_t y_bytes = static_cast<uint32_t>(boxes) * kTBoxBytes;
@@ -493,7 +503,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         }
         const int rank_tiles = (p.rank + 63) / 64;
         auto load_b = [&](int i) {
-            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const ColumnBlock cb = column_block(tp, rank + i * ctas);
             const int s = i % kTBStages;
             if (elect_one()) {
                 mbar_expect_tx(bar(T_BFULL + s), ts.b_bytes);
@@ -505,10 +515,10 @@ __global__ void __launch_bounds__(kTThreads, 1)
             __syncwarp();
         };
         auto load_y = [&](int i) {
-            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const ColumnBlock cb = column_block(tp, rank + i * ctas);
             const int s = i % ts.y_stages;
             if (lane == 0) {
-                const uint32_t dst = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes;
+                const uint32_t dst = sb + static_cast<uint32_t>(s) * y_bytes;
                 mbar_expect_tx(bar(T_YFULL + s), y_bytes);
                 for (int h = 0; h < boxes; ++h)
                     tma_load_2d(dst + static_cast<uint32_t>(h) * kTBoxBytes, &tm_y, cb.c0 + h * 64, tile.first,
@@ -520,9 +530,10 @@ __global__ void __launch_bounds__(kTThreads, 1)
         for (; ok && nb < min(mine, kTBStages); ++nb) load_b(nb);
         cluster_point();
         cluster_point();
-        // every MMA on the ring of x and A has completed: its memory is y's (which the
-        // cluster's other CTAs no longer read)
+        // every MMA on the ring of x and A has completed: its memory is y's
         if (ok) ok = mbar_wait_warp(bar(T_SUMS), 0, tp.err);
+        for (; ok && ny < min(mine, ts.y_free); ++ny) load_y(ny);
+        if (ok && ny < min(mine, ts.y_stages)) ok = mbar_wait_warp(bar(T_READY), 0, tp.err);
         for (; ok && ny < min(mine, ts.y_stages); ++ny) load_y(ny);
         for (int i = 0; ok && i < mine; ++i) {
             const int s = i % ts.y_stages;
@@ -530,9 +541,9 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 ok = false;
                 break;
             }
-            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const ColumnBlock cb = column_block(tp, rank + i * ctas);
             if (lane == 0) {
-                const uint32_t from = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes;
+                const uint32_t from = sb + static_cast<uint32_t>(s) * y_bytes;
                 if (tile.n == kTRows)
                     for (int h = 0; h < boxes; ++h)
                         if (h * 64 + 64 <= cb.width)
@@ -608,7 +619,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         const uint64_t db0 = smem_desc_sw128(sb + ts.b_at, 16, 1024);
         for (int i = 0; ok && i < mine; ++i) {
             const int s = i % kTBStages, buf = i & 1;
-            const int slice = column_block(tp, rank + (i << ts.ctas_log)).slice;
+            const int slice = column_block(tp, rank + i * ctas).slice;
             if (!mbar_wait_warp(bar(T_BFULL + s), (i / kTBStages) & 1, tp.err) ||
                 (i >= 2 && !mbar_wait_warp(bar(T_OUTEMPTY + buf), ((i >> 1) & 1) ^ 1, tp.err))) {
                 ok = false;
@@ -646,10 +657,11 @@ __global__ void __launch_bounds__(kTThreads, 1)
         bool ok = mbar_wait_warp(bar(T_SUMS), 0, tp.err);
         if (!ok) *abort_flag = 1;
         tc_fence_after();
-        const int width = p.n_slices * ts.rank16, pitch = ts.wide16 + 4, own_log = 7 - ts.ctas_log;
-        // [128 / ctas][pitch] the cluster's sums of this CTA's rows, [128][pitch] this CTA's part
-        float *const summed = reinterpret_cast<float *>(sg);
-        float *const part = reinterpret_cast<float *>(sg + sums_bytes(ts.wide16, kTRows >> ts.ctas_log));
+        const int width = p.n_slices * ts.rank16, pitch = ts.wide16 + 4;
+        // [own_rows][pitch] the cluster's sums of this CTA's rows, [128][pitch] this CTA's
+        // part, later all rows' sums
+        float *const summed = reinterpret_cast<float *>(sg + ts.summed_at);
+        float *const part = reinterpret_cast<float *>(sg + ts.part_at);
         if (ctas > 1) {
             for (int c = c_first; ok && c < width; c += c_step) {
                 float v[16];
@@ -659,10 +671,12 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 for (int i = 0; i < 4; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             }
             cluster_point();
-            const int vecs = width / 4;
-            for (int i = tid - 64; i < vecs << own_log; i += kTEpilogue) {
+            // the parts of this CTA's rows, summed; then every CTA's sums (both ways along the
+            // rows: with each thread reading its own row of the others, 192 sums took 8 us, not 3.5)
+            const int vecs = width / 4, own0 = rank * ts.own_rows, own = min(ts.own_rows, kTRows - own0);
+            for (int i = tid - 64; i < vecs * own; i += kTEpilogue) {
                 const int r = i / vecs, c = (i - r * vecs) * 4;
-                const uint32_t at = smem_u32(part + ((rank << own_log) + r) * pitch + c);
+                const uint32_t at = smem_u32(part + (own0 + r) * pitch + c);
                 float4 sum = make_float4(0.f, 0.f, 0.f, 0.f), v[kAMaxCluster];
 #pragma unroll
                 for (int o = 0; o < kAMaxCluster; ++o)
@@ -672,17 +686,31 @@ __global__ void __launch_bounds__(kTThreads, 1)
                     if (o < ctas) sum.x += v[o].x, sum.y += v[o].y, sum.z += v[o].z, sum.w += v[o].w;
                 *reinterpret_cast<float4 *>(summed + r * pitch + c) = sum;
             }
-            fence_proxy_async_smem();  // y's copies come where the parts were
             cluster_point();
+            for (int i0 = tid - 64; i0 < vecs * kTRows; i0 += 4 * kTEpilogue) {
+                float4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int i = i0 + k * kTEpilogue, r = i / vecs, c = (i - r * vecs) * 4, o = r / ts.own_rows;
+                    if (i < vecs * kTRows)
+                        v[k] = ld_cluster_f32x4(dsmem_addr(smem_u32(summed + (r - o * ts.own_rows) * pitch + c),
+                                                           static_cast<uint32_t>(o)));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int i = i0 + k * kTEpilogue, r = i / vecs, c = (i - r * vecs) * 4;
+                    if (i < vecs * kTRows) *reinterpret_cast<float4 *>(part + r * pitch + c) = v[k];
+                }
+            }
+            nbar_sync(1, kTEpilogue);
         }
         for (int c = c_first; ok && c < width; c += c_step) {
             float v[16];
             if (ctas > 1) {
-                const uint32_t at = dsmem_addr(smem_u32(summed + (row & ((1 << own_log) - 1)) * pitch + c),
-                                               static_cast<uint32_t>(row >> own_log));
+                const float4 *const from = reinterpret_cast<const float4 *>(part + row * pitch + c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float4 w = ld_cluster_f32x4(at + 16u * static_cast<uint32_t>(i));
+                    const float4 w = from[i];
                     v[4 * i] = w.x, v[4 * i + 1] = w.y, v[4 * i + 2] = w.z, v[4 * i + 3] = w.w;
                 }
             } else {
@@ -700,6 +728,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         }
         tmem_wait_st();
         tc_fence_before();
+        fence_proxy_async_smem();  // y's copies may come where the parts were
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(T_READY));
 
@@ -717,7 +746,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 break;
             }
             tc_fence_after();
-            const uint32_t y_row = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes + box + static_cast<uint32_t>(row) * 128;
+            const uint32_t y_row = sb + static_cast<uint32_t>(s) * y_bytes + box + static_cast<uint32_t>(row) * 128;
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 if (g >= groups) break;
@@ -750,7 +779,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 }
             }
             // a box that the tile or the slice ends in is stored by its warps, others by TMA
-            const ColumnBlock cb = column_block(tp, rank + (i << ts.ctas_log));
+            const ColumnBlock cb = column_block(tp, rank + i * ctas);
             const int box_col = block == 128 ? col : 0;
             if (tile.n < kTRows || box_col + 64 > cb.width) {
                 __syncwarp();
@@ -759,7 +788,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 for (int r0 = 0; r0 < 32; r0 += rows_at_once) {
                     const int r = wq * 32 + r0 + lane / per_row;
                     const int c = box_col + (first + piece) * 8;
-                    const uint32_t at = sb + ts.y_at + static_cast<uint32_t>(s) * y_bytes + box +
+                    const uint32_t at = sb + static_cast<uint32_t>(s) * y_bytes + box +
                                         static_cast<uint32_t>(r) * 128 +
                                         static_cast<uint32_t>(((first + piece) ^ (r & 7)) * 16);
                     if (r < tile.n && c < cb.width) {
@@ -788,10 +817,18 @@ __global__ void __launch_bounds__(kTThreads, 1)
 }
 
 AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies,
-                         int32_t tile_rows) {
+                         int32_t tile_rows, int32_t tile_total) {
     constexpr int kCopyRows = 32;  // rows of a unit that is only copied
     AdapterPlan plan;
     std::vector<std::pair<int32_t, int32_t>> rows;  // (adapter, row) of those that are gathered
+    int64_t in_tiles = 0;
+    for (int32_t s = 0; s < n_seqs;) {
+        const int32_t id = adapters[s];
+        int64_t n = 0;
+        while (s < n_seqs && adapters[s] == id) n += q_lens[s++];
+        if (id >= 0 && n >= tile_rows) in_tiles += n;
+    }
+    if (in_tiles < tile_total) tile_rows = INT32_MAX;
     int32_t at = 0;
     for (int32_t s = 0; s < n_seqs;) {
         const int32_t id = adapters[s], first = at;
@@ -823,14 +860,47 @@ AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *a
 
 namespace {
 
+// Clusters of 2 .. kAMaxCluster CTAs of a kernel (of a whole SM each) that the current
+// device holds at a time; cached per device.
+template <auto kernel>
+cudaError_t clusters_at_a_time(int threads, int smem, int32_t (&clusters)[kAMaxCluster + 1]) {
+    static std::atomic<int32_t> known[64][kAMaxCluster + 1] = {};  // + 1; 0: not asked
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    for (int c = 2; c <= kAMaxCluster; ++c) {
+        int32_t n = dev >= 0 && dev < 64 ? known[dev][c].load(std::memory_order_acquire) : 0;
+        if (n == 0) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(static_cast<unsigned>(c));
+            cfg.blockDim = dim3(static_cast<unsigned>(threads));
+            cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+            cudaLaunchAttribute a = {};
+            a.id = cudaLaunchAttributeClusterDimension;
+            a.val.clusterDim.x = static_cast<unsigned>(c);
+            a.val.clusterDim.y = a.val.clusterDim.z = 1;
+            cfg.attrs = &a;
+            cfg.numAttrs = 1;
+            int most = 0;
+            e = cudaOccupancyMaxActiveClusters(&most, kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            n = most + 1;
+            if (dev >= 0 && dev < 64) known[dev][c].store(n, std::memory_order_release);
+        }
+        clusters[c] = n - 1;
+    }
+    return cudaSuccess;
+}
+
+constexpr int kUnitSmem = static_cast<int>(unit_smem(kAMaxSlices * kAMaxRank, kAMaxSlices * kAMaxRank / 16));
+static_assert(kUnitSmem <= static_cast<int>(kTSmem), "shared memory of a CTA");
+
 template <int kUnits, int kRows>
-cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t &next, cudaStream_t st) {
+cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t &next, bool beside_tiles, cudaStream_t st) {
     static std::atomic<uint64_t> smem_set{0};
     const auto kernel = adapter_units_kernel<kUnits, kRows>;
     const int wide = p.n_slices * p.rank;
-    const cudaError_t e =
-        ensure_smem_limit(
-        kernel, static_cast<int>(unit_smem(kAMaxSlices * kAMaxRank, kAMaxSlices * kAMaxRank / 16)), smem_set);
+    cudaError_t e = ensure_smem_limit(kernel, kUnitSmem, smem_set);
     if (e != cudaSuccess) return e;
     UnitParams<kUnits, kRows> u;
     u.p = p;
@@ -849,12 +919,14 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
         u.group_at[j] = at;
         if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + 31) / 32;
     }
-    // as many CTAs a unit as there are SMs for, 128 values of K each at least
-    u.ctas_log = 0;
-    while (2 << u.ctas_log <= kAMaxCluster && (2 << u.ctas_log) * n <= device_sm_count() * USLOT &&
-           p.hidden >= (2 << u.ctas_log) * 128)
-        ++u.ctas_log;
-    const int c = 1 << u.ctas_log;
+    // as many CTAs a unit as run at a time, 128 values of K each at least
+    int32_t clusters[kAMaxCluster + 1] = {};
+    e = clusters_at_a_time<adapter_units_kernel<kUnits, kRows>>(kAThreads, kUnitSmem, clusters);
+    if (e != cudaSuccess) return e;
+    int c = kAMaxCluster;
+    while (c > 1 && (n > clusters[c] || p.hidden < c * 128)) --c;
+    u.ctas = c;
+    u.beside_tiles = beside_tiles ? 1 : 0;
     PdlLaunch l(dim3(static_cast<unsigned>(n * c)), dim3(kAThreads),
                 unit_smem(wide, p.n_slices * ((p.rank + 15) / 16)), st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
@@ -869,41 +941,50 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     return cudaLaunchKernelEx(&l.cfg, kernel, u);
 }
 
-// how tiles of this call lie for clusters of 2^ctas_log CTAs; false: not on this kernel
-bool tile_shape(const AdapterParams &p, int ctas_log, TileShape *s) {
+// how tiles of this call lie for clusters of `ctas` CTAs; false: not on this kernel
+bool tile_shape(const AdapterParams &p, int ctas, TileShape *s) {
     *s = {};
-    s->ctas_log = ctas_log;
+    s->ctas = ctas;
+    s->own_rows = (kTRows + ctas - 1) / ctas;
     s->rank16 = (p.rank + 15) / 16 * 16;
     s->wide16 = (p.n_slices * s->rank16 + 31) / 32 * 32;
-    // (a block of 128 columns needs less of everything else where it fits)
-    s->block_log = s->wide16 <= 256 && s->rank16 <= 64 ? 7 : 6;
-    const int block = 1 << s->block_log;
-    if (s->wide16 + 2 * block > 512) return false;
-    s->tmem = 32;
-    while (s->tmem < s->wide16 + 2 * block) s->tmem *= 2;
     s->a_bytes = static_cast<uint32_t>(p.n_slices * s->rank16) * 128;
-    s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
-    const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
-    const uint32_t room = (kTSmem - rest) / 1024 * 1024, stage = kTXBytes + s->a_bytes;
-    s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / stage));
-    const uint32_t ring = static_cast<uint32_t>(s->stages) * stage;
-    // behind the inner sums: what the cluster's other CTAs read of them, then y's ring
-    const uint32_t summed = ctas_log ? sums_bytes(s->wide16, kTRows >> ctas_log) : 0;
-    const uint32_t parts = ctas_log ? summed + sums_bytes(s->wide16, kTRows) : 0;
-    const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * kTBoxBytes;
-    s->y_at = (summed + 1023) / 1024 * 1024;
-    if (s->stages < 2 || parts > room || s->y_at + 2 * y_bytes > room) return false;
-    s->y_stages = std::min<int>(kTYStages, static_cast<int>((room - s->y_at) / y_bytes));
-    s->b_at = std::max(ring, std::max((parts + 1023) / 1024 * 1024, s->y_at + static_cast<uint32_t>(s->y_stages) * y_bytes));
-    s->bars_at = s->b_at + kTBStages * s->b_bytes;
-    s->smem = s->bars_at + kTBarBytes + 1024;
-    return s->smem <= kTSmem;
+    const uint32_t stage = kTXBytes + s->a_bytes;
+    // blocks of 128 columns where they fit, else of 64
+    for (s->block_log = 7; s->block_log >= 6; --s->block_log) {
+        const int block = 1 << s->block_log;
+        if (s->wide16 + 2 * block > 512) continue;
+        s->tmem = 32;
+        while (s->tmem < s->wide16 + 2 * block) s->tmem *= 2;
+        s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
+        const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
+        const uint32_t room = (kTSmem - rest) / 1024 * 1024;
+        s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / stage));
+        const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * kTBoxBytes;
+        const uint32_t summed = ctas > 1 ? sums_bytes(s->wide16, s->own_rows) : 0;
+        const uint32_t part = ctas > 1 ? sums_bytes(s->wide16, kTRows) : 0;
+        if (s->stages < 2 || summed + part > room || summed + 2 * y_bytes > room) continue;
+        s->y_stages = std::min<int>(kTYStages, static_cast<int>((room - summed) / y_bytes));
+        s->b_at = std::max(static_cast<uint32_t>(s->stages) * stage,
+                           std::max(static_cast<uint32_t>(s->y_stages) * y_bytes, part) + summed);
+        s->b_at = (s->b_at + 1023) / 1024 * 1024;
+        s->summed_at = s->b_at - summed;
+        s->part_at = s->summed_at - part;
+        s->y_free = std::min<int>(s->y_stages, static_cast<int>(s->part_at / y_bytes));
+        s->bars_at = s->b_at + kTBStages * s->b_bytes;
+        s->smem = s->bars_at + kTBarBytes + 1024;
+        if (s->smem <= kTSmem) return true;
+    }
+    return false;
 }
 
 cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_t n_rows, int32_t n_adapters,
                          int32_t *err, cudaStream_t st) {
     static std::atomic<uint64_t> smem_set{0};
     cudaError_t e = ensure_smem_limit(adapter_tiles_kernel, static_cast<int>(kTSmem), smem_set);
+    if (e != cudaSuccess) return e;
+    int32_t clusters[kAMaxCluster + 1] = {};
+    e = clusters_at_a_time<adapter_tiles_kernel>(kTThreads, static_cast<int>(kTSmem), clusters);
     if (e != cudaSuccess) return e;
     const auto tp = std::make_unique<TileParams>();
     tp->p = p;
@@ -913,10 +994,10 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
         std::copy_n(plan.tiles.begin() + static_cast<std::ptrdiff_t>(next), n, tp->tiles);
         next += static_cast<size_t>(n);
         const int k_blocks = (p.hidden + kTK - 1) / kTK;
-        int c = 0;
-        while (2 << c <= kAMaxCluster && (2 << c) * n <= device_sm_count() && 2 << c <= k_blocks &&
-               tile_shape(p, c + 1, &tp->s))
-            ++c;
+        // as many CTAs a tile as run at a time (2k step of 17 tiles, hidden 11008: 4 CTAs 19.8
+        // us; 8, whose clusters take two rounds, 26.0)
+        int c = kAMaxCluster;
+        while (c > 1 && (n > clusters[c] || c > k_blocks || !tile_shape(p, c, &tp->s))) --c;
         if (!tile_shape(p, c, &tp->s)) return cudaErrorInvalidValue;  // (the plan asked before)
         for (int j = 0, at = 0; j <= kAMaxSlices; ++j) {
             tp->block_at[j] = at;
@@ -934,11 +1015,11 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
             !encode_bf16_rows(&tm_y, p.y, cols, rows, static_cast<uint64_t>(p.y_stride), 64, kTRows) ||
             !encode_bf16_rows(&tm_out, p.out, cols, rows, static_cast<uint64_t>(p.out_stride), 64, kTRows))
             return cudaErrorUnknown;
-        PdlLaunch l(dim3(static_cast<unsigned>(n) << c), dim3(kTThreads), tp->s.smem, st);
+        PdlLaunch l(dim3(static_cast<unsigned>(n) * static_cast<unsigned>(c)), dim3(kTThreads), tp->s.smem, st);
         cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
-        if (c > 0) {
+        if (c > 1) {
             attrs[1].id = cudaLaunchAttributeClusterDimension;
-            attrs[1].val.clusterDim.x = 1u << c;
+            attrs[1].val.clusterDim.x = static_cast<unsigned>(c);
             attrs[1].val.clusterDim.y = 1;
             attrs[1].val.clusterDim.z = 1;
             l.cfg.attrs = attrs;
@@ -955,7 +1036,8 @@ cudaError_t launch_adapter(const AdapterParams &p, const AdapterPlan &plan, int6
     cudaError_t e = plan.tiles.empty() ? cudaSuccess : launch_tiles(p, plan, n_rows, n_adapters, err, st);
     const bool few = plan.units.size() <= 64 && plan.rows.size() <= 256;
     for (size_t next = 0; e == cudaSuccess && next < plan.units.size();)
-        e = few ? launch_units<64, 256>(p, plan, next, st) : launch_units<1024, 3584>(p, plan, next, st);
+        e = few ? launch_units<64, 256>(p, plan, next, !plan.tiles.empty(), st)
+                : launch_units<1024, 3584>(p, plan, next, !plan.tiles.empty() && next == 0, st);
     return e;
 }
 
@@ -1016,7 +1098,8 @@ extern "C" ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const v
     try {
         TileShape shape;
         const AdapterPlan plan =
-            plan_adapter(n_seqs, h_q_lens, h_adapters, out != y, tile_shape(p, 0, &shape) ? kATileMin : INT32_MAX);
+            plan_adapter(n_seqs, h_q_lens, h_adapters, out != y,
+                                              tile_shape(p, 1, &shape) ? kATileMin : INT32_MAX, kATileTotal);
         return launch_adapter(p, plan, n_rows, n_adapters, d_err_flag, static_cast<cudaStream_t>(stream)) == cudaSuccess
                    ? PPAS_OK
                    : PPAS_ERR_CUDA;
