@@ -816,11 +816,14 @@ __global__ void __launch_bounds__(kTThreads, 1)
     cluster_point();  // nobody leaves while others read its sums
 }
 
-AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies,
-                         int32_t tile_rows, int32_t tile_total) {
+void plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies, int32_t tile_rows,
+                  int32_t tile_total, AdapterPlan &plan) {
     constexpr int kCopyRows = 32;  // rows of a unit that is only copied
-    AdapterPlan plan;
-    std::vector<std::pair<int32_t, int32_t>> rows;  // (adapter, row) of those that are gathered
+    plan.units.clear();
+    plan.rows.clear();
+    plan.tiles.clear();
+    auto &rows = plan.gathered;
+    rows.clear();
     int64_t in_tiles = 0;
     for (int32_t s = 0; s < n_seqs;) {
         const int32_t id = adapters[s];
@@ -855,7 +858,6 @@ AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *a
         for (; i < e; ++i)
             if (!run) plan.rows.push_back(rows[i].second);
     }
-    return plan;
 }
 
 namespace {
@@ -925,6 +927,9 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     if (e != cudaSuccess) return e;
     int c = kAMaxCluster;
     while (c > 1 && (n > clusters[c] || p.hidden < c * 128)) --c;
+    // (beside tiles, on the SMs that their clusters leave: 2k step of 17 tiles and 9 units,
+    // clusters of 4 18.3 us, of 8, which find no room, 24.2, of 2 19.8)
+    if (beside_tiles) c = std::min(c, 4);
     u.ctas = c;
     u.beside_tiles = beside_tiles ? 1 : 0;
     PdlLaunch l(dim3(static_cast<unsigned>(n * c)), dim3(kAThreads),
@@ -1097,9 +1102,9 @@ extern "C" ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const v
     p.cols = static_cast<int32_t>(cols);
     try {
         TileShape shape;
-        const AdapterPlan plan =
-            plan_adapter(n_seqs, h_q_lens, h_adapters, out != y,
-                                              tile_shape(p, 1, &shape) ? kATileMin : INT32_MAX, kATileTotal);
+        thread_local AdapterPlan plan;  // (for its memory alone)
+        plan_adapter(n_seqs, h_q_lens, h_adapters, out != y, tile_shape(p, 1, &shape) ? kATileMin : INT32_MAX,
+                     kATileTotal, plan);
         return launch_adapter(p, plan, n_rows, n_adapters, d_err_flag, static_cast<cudaStream_t>(stream)) == cudaSuccess
                    ? PPAS_OK
                    : PPAS_ERR_CUDA;

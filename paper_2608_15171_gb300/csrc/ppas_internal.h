@@ -9,6 +9,7 @@
 
 #include <atomic>
 #include <memory>
+#include <utility>
 #include <vector>
 
 #include "ppas.h"
@@ -424,13 +425,14 @@ struct AdapterPlan {
     std::vector<AdapterUnit> units;
     std::vector<int32_t> rows;  // of the listed units
     std::vector<AdapterTile> tiles;
+    std::vector<std::pair<int32_t, int32_t>> gathered;  // (adapter, row) of those that are not next to others of theirs
 };
 // The units and tiles of sequences of q_lens rows with these adapters (-1: none);
 // copies: rows without an adapter have to be copied; tile_rows: rows of an adapter
 // next to one another that make tiles (INT32_MAX: never), where all such runs have
 // tile_total rows at least
-AdapterPlan plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies,
-                         int32_t tile_rows, int32_t tile_total);
+void plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies, int32_t tile_rows,
+                  int32_t tile_total, AdapterPlan &plan);
 
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its
