@@ -513,7 +513,7 @@ ppas_status ppas_norm_rope_append(const void *q, const void *k, const void *v, i
  * Pointers are 16-byte aligned, strides multiples of 8 and at least the row's
  * width, else PPAS_ERR_INVALID_ARG.  Supported: hidden, rank and each slice's
  * columns multiples of 8, rank up to 128 (smaller ones of some adapters padded
- * with zeros), up to 4 slices, 2^24 rows, hidden and cols up to 2^24,
+ * with zeros), up to 4 slices, 2^24 rows, hidden and cols up to 2^24, strides to 2^36,
  * n_adapters * n_slices * rank and n_adapters * cols below 2^31; otherwise
  * PPAS_ERR_UNSUPPORTED.  n_seqs == 0 is a no-op.  A row's result depends on its
  * own x, y and adapter alone, but for the order of its sums over k, which follows

@@ -29,15 +29,12 @@ constexpr int kAThreads = 512;
 constexpr int kAWarps = kAThreads / 32;
 constexpr int kAChunk = 96;  // inner sums worked at a time: the loads of 12 x 16 bytes a lane are under way at once
 constexpr int kAAhead = 4;   // of the rank in B, 16 times this are loaded ahead
-constexpr int kAMaxCluster = 8;
-constexpr int32_t kATileRows = 128;  // rows of a tile
 constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make tiles,
 // and of all such runs together (below, units of 16 rows are done first: 512 rows, 2048 x
 // 2560, rank 16 7.1 us, tiles 10.0; 4096 x 6144, rank 64 21.7, 22.3; past it 1024 rows 16.9,
 // 15.3 and 37.6, 24.9)
 constexpr int32_t kATileTotal = 513;
 constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space)
-constexpr uint32_t kTSmem = 232448;  // shared memory of a CTA
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -308,15 +305,8 @@ __global__ void __launch_bounds__(kAThreads, 1)
 // memory, a block took 3000 cycles: 16384 rows, 4096 x 6144, rank 64 in 176 us.)
 namespace {
 
-constexpr int kTRows = 128;
-constexpr int kTK = 64;
 constexpr int kTEpilogue = 512;
 constexpr int kTThreads = 64 + kTEpilogue;
-constexpr int kTMaxStages = 6;
-constexpr int kTBStages = 3;
-constexpr int kTYStages = 4;
-constexpr uint32_t kTXBytes = kTRows * kTK * 2;
-constexpr uint32_t kTBoxBytes = kTRows * 128;  // 64 columns of y
 enum : int {
     T_FULL = 0,
     T_EMPTY = T_FULL + kTMaxStages,
@@ -331,30 +321,7 @@ enum : int {
     T_DONE = T_OUTEMPTY + 2,           // every MMA has completed
     T_COUNT
 };
-constexpr uint32_t kTBarBytes = 320;
 static_assert(T_COUNT * 8 + 8 <= kTBarBytes, "barrier area");
-
-// how a tile lies in shared memory and TMEM
-struct TileShape {
-    int32_t rank16;    // rank rounded up to 16
-    int32_t wide16;    // TMEM columns for all slices' inner sums, rounded up to 32
-    int32_t block_log; // log2 of the columns of y worked at a time: 128, or 64
-    int32_t ctas;      // of a cluster
-    int32_t own_rows;  // of the sums that each of them joins
-    int32_t stages;    // of the ring of x and A
-    uint32_t a_bytes;  // of a stage: the slices' A tiles
-    uint32_t b_bytes;  // of a B tile: block rows, 128 bytes for each 64 of rank
-    // y's ring lies where the ring of x and A was, and in a cluster, from stage y_free on,
-    // where the parts of the sums are until they are an operand; the sums that other
-    // CTAs read come behind
-    int32_t y_stages, y_free;
-    uint32_t part_at, summed_at;
-    uint32_t b_at, bars_at, smem;  // offsets, and all of it
-    int32_t tmem;      // columns allocated
-};
-__host__ __device__ constexpr uint32_t sums_bytes(int wide16, int rows) {
-    return static_cast<uint32_t>(rows * (wide16 + 4) * 4);
-}
 
 struct TileParams {
     AdapterParams p;
@@ -816,6 +783,43 @@ __global__ void __launch_bounds__(kTThreads, 1)
     cluster_point();  // nobody leaves while others read its sums
 }
 
+// how tiles of this call lie for clusters of `ctas` CTAs; false: not on this kernel
+bool tile_shape(const AdapterParams &p, int ctas, TileShape *s) {
+    *s = {};
+    s->ctas = ctas;
+    s->own_rows = (kTRows + ctas - 1) / ctas;
+    s->rank16 = (p.rank + 15) / 16 * 16;
+    s->wide16 = (p.n_slices * s->rank16 + 31) / 32 * 32;
+    s->a_bytes = static_cast<uint32_t>(p.n_slices * s->rank16) * 128;
+    const uint32_t stage = kTXBytes + s->a_bytes;
+    // blocks of 128 columns where they fit, else of 64
+    for (s->block_log = 7; s->block_log >= 6; --s->block_log) {
+        const int block = 1 << s->block_log;
+        if (s->wide16 + 2 * block > 512) continue;
+        s->tmem = 32;
+        while (s->tmem < s->wide16 + 2 * block) s->tmem *= 2;
+        s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
+        const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
+        const uint32_t room = (kTSmem - rest) / 1024 * 1024;
+        s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / stage));
+        const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * kTBoxBytes;
+        const uint32_t summed = ctas > 1 ? sums_bytes(s->wide16, s->own_rows) : 0;
+        const uint32_t part = ctas > 1 ? sums_bytes(s->wide16, kTRows) : 0;
+        if (s->stages < 2 || summed + part > room || summed + 2 * y_bytes > room) continue;
+        s->y_stages = std::min<int>(kTYStages, static_cast<int>((room - summed) / y_bytes));
+        s->b_at = std::max(static_cast<uint32_t>(s->stages) * stage,
+                           std::max(static_cast<uint32_t>(s->y_stages) * y_bytes, part) + summed);
+        s->b_at = (s->b_at + 1023) / 1024 * 1024;
+        s->summed_at = s->b_at - summed;
+        s->part_at = s->summed_at - part;
+        s->y_free = std::min<int>(s->y_stages, static_cast<int>(s->part_at / y_bytes));
+        s->bars_at = s->b_at + kTBStages * s->b_bytes;
+        s->smem = s->bars_at + kTBarBytes + 1024;
+        if (s->smem <= kTSmem) return true;
+    }
+    return false;
+}
+
 void plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies, int32_t tile_rows,
                   int32_t tile_total, AdapterPlan &plan) {
     constexpr int kCopyRows = 32;  // rows of a unit that is only copied
@@ -842,8 +846,8 @@ void plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters
             continue;
         }
         int32_t r = first;
-        for (const bool tiles = at - r >= tile_rows; tiles && r < at; r += kATileRows)
-            plan.tiles.push_back({r, id, std::min(kATileRows, at - r)});
+        for (const bool tiles = at - r >= tile_rows; tiles && r < at; r += kTRows)
+            plan.tiles.push_back({r, id, std::min(kTRows, at - r)});
         r = std::min(r, at);
         for (; at - r >= kAUnitRows; r += kAUnitRows) plan.units.push_back({r, id, kAUnitRows, 0});
         for (; r < at; ++r) rows.emplace_back(id, r);
@@ -946,43 +950,6 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     return cudaLaunchKernelEx(&l.cfg, kernel, u);
 }
 
-// how tiles of this call lie for clusters of `ctas` CTAs; false: not on this kernel
-bool tile_shape(const AdapterParams &p, int ctas, TileShape *s) {
-    *s = {};
-    s->ctas = ctas;
-    s->own_rows = (kTRows + ctas - 1) / ctas;
-    s->rank16 = (p.rank + 15) / 16 * 16;
-    s->wide16 = (p.n_slices * s->rank16 + 31) / 32 * 32;
-    s->a_bytes = static_cast<uint32_t>(p.n_slices * s->rank16) * 128;
-    const uint32_t stage = kTXBytes + s->a_bytes;
-    // blocks of 128 columns where they fit, else of 64
-    for (s->block_log = 7; s->block_log >= 6; --s->block_log) {
-        const int block = 1 << s->block_log;
-        if (s->wide16 + 2 * block > 512) continue;
-        s->tmem = 32;
-        while (s->tmem < s->wide16 + 2 * block) s->tmem *= 2;
-        s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
-        const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
-        const uint32_t room = (kTSmem - rest) / 1024 * 1024;
-        s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / stage));
-        const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * kTBoxBytes;
-        const uint32_t summed = ctas > 1 ? sums_bytes(s->wide16, s->own_rows) : 0;
-        const uint32_t part = ctas > 1 ? sums_bytes(s->wide16, kTRows) : 0;
-        if (s->stages < 2 || summed + part > room || summed + 2 * y_bytes > room) continue;
-        s->y_stages = std::min<int>(kTYStages, static_cast<int>((room - summed) / y_bytes));
-        s->b_at = std::max(static_cast<uint32_t>(s->stages) * stage,
-                           std::max(static_cast<uint32_t>(s->y_stages) * y_bytes, part) + summed);
-        s->b_at = (s->b_at + 1023) / 1024 * 1024;
-        s->summed_at = s->b_at - summed;
-        s->part_at = s->summed_at - part;
-        s->y_free = std::min<int>(s->y_stages, static_cast<int>(s->part_at / y_bytes));
-        s->bars_at = s->b_at + kTBStages * s->b_bytes;
-        s->smem = s->bars_at + kTBarBytes + 1024;
-        if (s->smem <= kTSmem) return true;
-    }
-    return false;
-}
-
 cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_t n_rows, int32_t n_adapters,
                          int32_t *err, cudaStream_t st) {
     static std::atomic<uint64_t> smem_set{0};
@@ -1081,6 +1048,8 @@ extern "C" ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const v
         n_adapters * cols > INT32_MAX)
         return PPAS_ERR_UNSUPPORTED;
     if (n_rows == 0) return PPAS_OK;
+    constexpr int64_t kStrides = int64_t{1} << 36;  // (a tensor map's are below 2^40 bytes)
+    if (x_stride > kStrides || y_stride > kStrides || out_stride > kStrides) return PPAS_ERR_UNSUPPORTED;
     if (x_stride < hidden || y_stride < cols || out_stride < cols || x_stride % 8 || y_stride % 8 || out_stride % 8)
         return PPAS_ERR_INVALID_ARG;
     if (!x || !y || !out || !a || !b || !on16(x) || !on16(y) || !on16(out) || !on16(a) || !on16(b) ||

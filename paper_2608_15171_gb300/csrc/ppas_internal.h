@@ -434,6 +434,42 @@ struct AdapterPlan {
 void plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters, bool copies, int32_t tile_rows,
                   int32_t tile_total, AdapterPlan &plan);
 
+constexpr int kAMaxCluster = 8;  // CTAs of a cluster
+
+// Tiles: 128 rows of an adapter, on the tensor cores.
+constexpr int kTRows = 128;
+constexpr int kTK = 64;           // of K at a time
+constexpr int kTMaxStages = 6;    // of the ring of x and A tiles
+constexpr int kTBStages = 3;
+constexpr int kTYStages = 4;
+constexpr uint32_t kTSmem = 232448;  // shared memory of a CTA
+constexpr uint32_t kTXBytes = kTRows * kTK * 2;
+constexpr uint32_t kTBoxBytes = kTRows * 128;  // 64 columns of y
+constexpr uint32_t kTBarBytes = 320;
+// how a tile lies in shared memory and TMEM
+struct TileShape {
+    int32_t rank16;    // rank rounded up to 16
+    int32_t wide16;    // TMEM columns for all slices' inner sums, rounded up to 32
+    int32_t block_log; // log2 of the columns of y worked at a time: 128, or 64
+    int32_t ctas;      // of a cluster
+    int32_t own_rows;  // of the sums that each of them joins
+    int32_t stages;    // of the ring of x and A
+    uint32_t a_bytes;  // of a stage: the slices' A tiles
+    uint32_t b_bytes;  // of a B tile: block rows, 128 bytes for each 64 of rank
+    // y's ring lies where the ring of x and A was, and in a cluster, from stage y_free on,
+    // where the parts of the sums are until they are an operand; the sums that other
+    // CTAs read come behind
+    int32_t y_stages, y_free;
+    uint32_t part_at, summed_at;
+    uint32_t b_at, bars_at, smem;  // offsets, and all of it
+    int32_t tmem;      // columns allocated
+};
+__host__ __device__ constexpr uint32_t sums_bytes(int wide16, int rows) {
+    return static_cast<uint32_t>(rows * (wide16 + 4) * 4);
+}
+// the shape for clusters of `ctas` CTAs; false: this call's rows are not done in tiles
+bool tile_shape(const AdapterParams &p, int ctas, TileShape *s);
+
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its
 // own global accesses after it with grid_dep_wait()

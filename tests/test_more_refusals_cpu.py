@@ -44,7 +44,7 @@ def test_adapter_refusals(ppas):  # noqa: F811
            dict(out=16), dict(adapters=[0]), dict(d_err_flag=3)]
     _refused(ppas.ppas_adapter_add, ok, bad, ppas.PPAS_ERR_INVALID_ARG, ppas.PpasError)
     bad = [dict(hidden=252, x_stride=256), dict(rank=12), dict(rank=136), dict(slice_cols=[128, 60]),
-           dict(slice_cols=[8] * 5), dict(q_lens=[1 << 24, 1]), dict(n_adapters=1 << 27),
+           dict(slice_cols=[8] * 5), dict(x_stride=1 << 37), dict(q_lens=[1 << 24, 1]), dict(n_adapters=1 << 27),
            dict(slice_cols=[1 << 24, 8], y_stride=1 << 25, out_stride=1 << 25)]
     _refused(ppas.ppas_adapter_add, ok, bad, ppas.PPAS_ERR_UNSUPPORTED, ppas.PpasError)
     ppas.ppas_adapter_add(**{**ok, "q_lens": [], "adapters": [], "x": 0})  # no-op
