@@ -29,9 +29,15 @@ namespace {
 
 constexpr int kLThreads = 256;
 constexpr int kLWarps = kLThreads / 32;
-constexpr int kLLoads = 4;       // 16-byte loads of a round, a thread
-constexpr int kLStages = 3;      // rounds that are under way
-constexpr int kLAnSm = 4;        // CTAs an SM holds
+// 16-byte loads of a round, a thread (32 logits), and rounds under way: 3 CTAs an SM of
+// fp32, 4 of bf16 (fp32, 4 loads and 3 rounds: 1 x 152000 8.8 us, 7.8 so; 256 x 152000 32.7
+// and 31.9; bf16, 8 and 2: 1024 x 128000 50.4, 46.4 so)
+template <class T>
+constexpr int kLLoads = sizeof(T) == 4 ? 8 : 4;
+template <class T>
+constexpr int kLStages = sizeof(T) == 4 ? 2 : 3;
+template <class T>
+constexpr int kLAnSm = sizeof(T) == 4 ? 3 : 4;  // CTAs an SM holds
 constexpr int kLGroups = kLThreads / 2;
 constexpr int kLList = 640;     // places of a list
 constexpr uint32_t kLFew = 64;   // lists that are ranked as they are
@@ -85,13 +91,6 @@ struct LPart {
     float top, s, t;
 };
 struct LShared {
-    union {
-        uint4 ring[kLStages][kLLoads][kLThreads];  // each thread's own logits under way
-        struct {
-            uint64_t kept[kLList];                  // of the list the places at or above the last bound
-            uint64_t all[kLMaxCluster * kLMaxTop];  // first CTA: every CTA's alternatives
-        };
-    };
     uint64_t list[kLList];    // places at or above the bound
     uint64_t best[kLMaxTop];  // this CTA's alternatives, in order; 0: none
     LPart parts[kLMaxCluster];
@@ -104,6 +103,18 @@ struct LShared {
     float bound;
     uint64_t bound_place;
     uint32_t n_list, n_kept;
+};
+
+// Each thread's own logits under way; the memory has other uses once they are through.
+template <class T>
+struct LRing {
+    union {
+        uint4 ring[kLStages<T>][kLLoads<T>][kLThreads];
+        struct {
+            uint64_t kept[kLList];
+            uint64_t all[kLMaxCluster * kLMaxTop];
+        };
+    };
 };
 
 __device__ __forceinline__ uint64_t block_max(LShared &sh, uint64_t v) {
@@ -320,7 +331,9 @@ __device__ __forceinline__ void copies_wait() {
 template <class T, bool kTop>
 __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_constant__ LogprobParams p) {
     extern __shared__ __align__(16) uint8_t logprob_smem[];
-    LShared &sh = *reinterpret_cast<LShared *>(logprob_smem);
+    LRing<T> &ring = *reinterpret_cast<LRing<T> *>(logprob_smem);
+    LShared &sh = *reinterpret_cast<LShared *>(logprob_smem + sizeof(LRing<T>));
+    constexpr int kLoads = kLLoads<T>, kStages = kLStages<T>;
     constexpr int kPer = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ctas = cluster_nctarank(), rank = ctas > 1 ? cluster_ctarank() : 0;
@@ -342,38 +355,38 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     const uint4 *const src4 = reinterpret_cast<const uint4 *>(src - pad);
     // A thread's copies go to its own places of the ring, from which it alone reads:
     // its own waits are all that it takes.
-    constexpr int kRound = kLThreads * kLLoads;
+    constexpr int kRound = kLThreads * kLoads;
     const int rounds = (vecs + kRound - 1) / kRound;
     auto fetch = [&](int round, int stage) {
         const int v0 = round * kRound;
         if (v0 >= whole0 && v0 + kRound <= whole1) {
             const uint4 *from = src4 + v0 + tid;
-            const uint32_t to = smem_u32(&sh.ring[stage][0][tid]);
+            const uint32_t to = smem_u32(&ring.ring[stage][0][tid]);
 #pragma unroll
-            for (int k = 0; k < kLLoads; ++k) copy16_async(to + k * kLThreads * 16, from + k * kLThreads);
+            for (int k = 0; k < kLoads; ++k) copy16_async(to + k * kLThreads * 16, from + k * kLThreads);
         } else if (round < rounds) {
 #pragma unroll 1
-            for (int k = 0; k < kLLoads; ++k) {
+            for (int k = 0; k < kLoads; ++k) {
                 const int v = v0 + k * kLThreads + tid;
-                if (v >= whole0 && v < whole1) copy16_async(smem_u32(&sh.ring[stage][k][tid]), src4 + v);
-                else sh.ring[stage][k][tid] = edge_vector(src, v * kPer - pad, n);
+                if (v >= whole0 && v < whole1) copy16_async(smem_u32(&ring.ring[stage][k][tid]), src4 + v);
+                else ring.ring[stage][k][tid] = edge_vector(src, v * kPer - pad, n);
             }
         }
         copies_commit();
     };
 #pragma unroll
-    for (int i = 0; i < kLStages - 1; ++i) fetch(i, i);
+    for (int i = 0; i < kStages - 1; ++i) fetch(i, i);
     float top = -INFINITY, c = -1e30f, s = 0.f, t = 0.f, bound = INFINITY;
     bool bad = false;
-    for (int round = 0, stage = 0; round < rounds; ++round, stage = stage + 1 == kLStages ? 0 : stage + 1) {
-        fetch(round + kLStages - 1, stage == 0 ? kLStages - 1 : stage - 1);
-        copies_wait<kLStages - 1>();
-        uint4 q[kLLoads];
+    for (int round = 0, stage = 0; round < rounds; ++round, stage = stage + 1 == kStages ? 0 : stage + 1) {
+        fetch(round + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        copies_wait<kStages - 1>();
+        uint4 q[kLoads];
 #pragma unroll
-        for (int k = 0; k < kLLoads; ++k) q[k] = sh.ring[stage][k][tid];
-        uint32_t most[kLLoads], all = 0;
+        for (int k = 0; k < kLoads; ++k) q[k] = ring.ring[stage][k][tid];
+        uint32_t most[kLoads], all = 0;
 #pragma unroll
-        for (int k = 0; k < kLLoads; ++k) {
+        for (int k = 0; k < kLoads; ++k) {
             most[k] = max_bits<T>(q[k]);
             all = k ? max_bits<T>(all, most[k]) : most[k];
         }
@@ -389,7 +402,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         }
         float2 s2 = make_float2(0.f, 0.f), t2 = s2;
 #pragma unroll
-        for (int k = 0; k < kLLoads; ++k) {
+        for (int k = 0; k < kLoads; ++k) {
             float x[kPer];
             widen<T>(floored<T>(q[k]), x);
 #pragma unroll
@@ -408,7 +421,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             // few of them at a time keep the whole warp, and 256 x 152000 takes 36.5 us)
             uint32_t hits = __ballot_sync(0xffffffffu, here >= bound && here > -INFINITY);
             if (hits) {
-                constexpr int kValues = kLLoads * kPer;
+                constexpr int kValues = kLoads * kPer;
                 __syncwarp();
                 do {
                     const int from = (tid & ~31) + __ffs(hits) - 1;
@@ -417,10 +430,10 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
                     for (int j0 = 0; j0 < kValues; j0 += 32) {
                         const int j = j0 + lane, k = j / kPer, e = j % kPer;
                         if (j < kValues) {
-                            const float x = value_of(reinterpret_cast<const T *>(&sh.ring[stage][k][from])[e]);
+                            const float x = value_of(reinterpret_cast<const T *>(&ring.ring[stage][k][from])[e]);
                             if (x >= bound && x > -INFINITY) {
                                 const uint32_t at = atomicAdd(&sh.n_list, 1u);
-                                const int index = i0 + ((round * kLLoads + k) * kLThreads + from) * kPer + e - pad;
+                                const int index = i0 + ((round * kLoads + k) * kLThreads + from) * kPer + e - pad;
                                 if (at < kLList) sh.list[at] = place_of(x + 0.f, static_cast<uint32_t>(index));
                             }
                         }
@@ -474,10 +487,10 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             if (m > kLFew) {  // without those that only an earlier bound let in
                 for (uint32_t i = tid; i < m; i += kLThreads) {
                     const uint64_t v = sh.list[i];
-                    if (place_logit(v) >= bound) sh.kept[atomicAdd(&sh.n_kept, 1u)] = v;
+                    if (place_logit(v) >= bound) ring.kept[atomicAdd(&sh.n_kept, 1u)] = v;
                 }
                 __syncthreads();
-                from = sh.kept;
+                from = ring.kept;
                 left = sh.n_kept;
             }
             rank_places(from, static_cast<int>(left), sh.best, p.n_top);
@@ -498,7 +511,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         dsmem_st_f32(to + 8, any ? t : 0.f);
     }
     if (kTop && ctas > 1 && tid < p.n_top)
-        st_cluster_u64(dsmem_addr(smem_u32(&sh.all[rank * p.n_top + tid]), 0), sh.best[tid]);
+        st_cluster_u64(dsmem_addr(smem_u32(&ring.all[rank * p.n_top + tid]), 0), sh.best[tid]);
     if (ctas > 1) cluster_sync_all();
     else __syncthreads();
     if (rank != 0) return;
@@ -521,15 +534,15 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             // the n-th largest of all is at least the least of every CTA's (n / CTAs)-th
             const int at = (p.n_top + static_cast<int>(ctas) - 1) / static_cast<int>(ctas) - 1;
             const uint32_t least = __reduce_min_sync(
-                0xffffffffu, static_cast<uint32_t>(sh.all[min(lane, static_cast<int>(ctas) - 1) * p.n_top + at] >> 32));
+                0xffffffffu, static_cast<uint32_t>(ring.all[min(lane, static_cast<int>(ctas) - 1) * p.n_top + at] >> 32));
             if (tid == 0) sh.n_kept = 0;
             __syncthreads();
             for (int i = tid; i < static_cast<int>(ctas) * p.n_top; i += kLThreads) {
-                const uint64_t v = sh.all[i];
-                if (v != 0 && static_cast<uint32_t>(v >> 32) >= least) sh.kept[atomicAdd(&sh.n_kept, 1u)] = v;
+                const uint64_t v = ring.all[i];
+                if (v != 0 && static_cast<uint32_t>(v >> 32) >= least) ring.kept[atomicAdd(&sh.n_kept, 1u)] = v;
             }
             __syncthreads();
-            rank_places(sh.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
+            rank_places(ring.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
         }
         const uint64_t mine = tid < p.n_top ? found[tid] : 0;
         if (tid < p.n_top) {
@@ -549,59 +562,63 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
 }
 
 static_assert(kLMaxCluster * kLMaxTop <= kLList, "the first CTA ranks them in `kept`");
-static_assert(kLAnSm * (sizeof(LShared) + 1024) <= 233472, "shared memory of an SM");
+template <class T>
+constexpr int kLSmem = static_cast<int>(sizeof(LRing<T>) + sizeof(LShared));
+static_assert(kLAnSm<float> * (kLSmem<float> + 1024) <= 233472 &&
+                  kLAnSm<__nv_bfloat16> * (kLSmem<__nv_bfloat16> + 1024) <= 233472,
+              "shared memory of an SM");
 
-// A kernel's shared memory limit, and whether this device holds a cluster of
-// kLMaxCluster of its CTAs (more than the portable 8); once per device.
+// How many clusters of 2, 4, 8 and 16 CTAs (16 are more than the portable 8) of a kernel
+// this device holds at a time; once per device.
 template <class T, bool kTop>
-cudaError_t prepare_logprobs(bool *wide) {
+cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
+    static std::atomic<uint64_t> limit_set{0};
+    static std::atomic<int32_t> known[64][5] = {};  // + 1; 0: not asked
     const auto kernel = token_logprobs_kernel<T, kTop>;
-    static std::atomic<uint64_t> limit_set{0}, yes{0}, no{0};
-    *wide = false;
-    cudaError_t e = ensure_smem_limit(kernel, sizeof(LShared), limit_set);
+    cudaError_t e = ensure_smem_limit(kernel, kLSmem<T>, limit_set);
     int dev = 0;
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t{1} << dev : 0;
-    if (!bit || (no.load(std::memory_order_acquire) & bit)) return cudaSuccess;
-    if (!(yes.load(std::memory_order_acquire) & bit)) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(kLMaxCluster);
-        cfg.blockDim = dim3(kLThreads);
-        cfg.dynamicSmemBytes = sizeof(LShared);
-        cudaLaunchAttribute a = {};
-        a.id = cudaLaunchAttributeClusterDimension;
-        a.val.clusterDim.x = kLMaxCluster;
-        a.val.clusterDim.y = a.val.clusterDim.z = 1;
-        cfg.attrs = &a;
-        cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            no.fetch_or(bit, std::memory_order_release);
-            return cudaSuccess;
+    for (int i = 1; i < 5; ++i) {
+        int32_t n = dev >= 0 && dev < 64 ? known[dev][i].load(std::memory_order_acquire) : 0;
+        if (n == 0) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << i);
+            cfg.blockDim = dim3(kLThreads);
+            cfg.dynamicSmemBytes = kLSmem<T>;
+            cudaLaunchAttribute a = {};
+            a.id = cudaLaunchAttributeClusterDimension;
+            a.val.clusterDim.x = 1u << i;
+            a.val.clusterDim.y = a.val.clusterDim.z = 1;
+            cfg.attrs = &a;
+            cfg.numAttrs = 1;
+            int most = 0;
+            if ((i == 4 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+                cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                most = 0;  // (none: a row has fewer CTAs)
+            }
+            n = most + 1;
+            if (dev >= 0 && dev < 64) known[dev][i].store(n, std::memory_order_release);
         }
-        yes.fetch_or(bit, std::memory_order_release);
+        clusters[i] = n - 1;
     }
-    *wide = true;
     return cudaSuccess;
 }
 
 template <class T, bool kTop>
 cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
-    // As many CTAs a row as the SMs hold at a time, 4096 logits each at least
-    // (64 x 32003 bf16: 8 CTAs 6.4 us, 4 7.3; 1 x 152000: 16 CTAs 9.5, 8 11.0; 256 x
-    // 152000: 2 CTAs 33.6, 1 41.7; 4, in two rounds, 44.6).
-    bool wide = false;
-    const cudaError_t e = prepare_logprobs<T, kTop>(&wide);
+    // As many CTAs a row as run at a time, 4096 logits each at least, 16 only where each
+    // has an SM (64 x 32003 bf16: 8 CTAs 7.1 us, 2 7.7; 1 x 152000: 16 CTAs 7.8, 8 11.0; 32 x
+    // 128000 bf16: 8 CTAs 8.5, 16 11.6; 256 x 152000: 2 CTAs 31.9, 1 43.5, 4 40.5).
+    int32_t clusters[5] = {};
+    const cudaError_t e = prepare_logprobs<T, kTop>(clusters);
     if (e != cudaSuccess) return e;
-    const int64_t slots = kLAnSm * static_cast<int64_t>(device_sm_count());
-    const int32_t most = wide ? kLMaxCluster : kPortableLCluster;
-    int32_t c = 1;
-    while (c < most && 2 * c * static_cast<int64_t>(n_rows) <= slots && p.vocab >= 2 * c * 4096) c *= 2;
+    int i = 16 * static_cast<int64_t>(n_rows) <= device_sm_count() ? 4 : 3;
+    while (i > 0 && (n_rows > clusters[i] || p.vocab < 4096 << i)) --i;
+    const int32_t c = 1 << i;
     p.chunk = ((p.vocab + c - 1) / c + 15) / 16 * 16;
-    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), sizeof(LShared), st);
+    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), kLSmem<T>, st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
         attrs[1].id = cudaLaunchAttributeClusterDimension;

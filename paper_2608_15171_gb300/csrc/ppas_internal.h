@@ -379,7 +379,6 @@ cudaError_t launch_sample(SampleParams p, int32_t n_rows, bool bf16, cudaStream_
 // ------------------------------------------------------------------ log probabilities
 constexpr int kLMaxTop = 32;      // alternatives of a row
 constexpr int kLMaxCluster = 16;  // CTAs of a row
-constexpr int kPortableLCluster = 8;
 struct LogprobParams {
     const void *logits;  // fp32 or bf16, row r at logits + r * row_stride
     int64_t row_stride;
