@@ -97,12 +97,21 @@ __global__ void __launch_bounds__(kAThreads, 1)
     if (!u.beside_tiles) grid_dep_wait();
 
     if (unit.adapter < 0) {  // (every CTA of the cluster)
+        // a warp a row, 8 x 16 bytes a lane under way
         const int vecs = p.cols / 8;
-        for (int i = 0; i < n; ++i) {
+        for (int i = rank * kAWarps + warp; i < n; i += kAWarps * ctas) {
             const int64_t row = row_of(i);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.y + row * p.y_stride);
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * p.out_stride);
-            for (int v = rank * kAThreads + tid; v < vecs; v += kAThreads * ctas) dst[v] = src[v];
+            for (int v0 = lane; v0 < vecs; v0 += 8 * 32) {
+                uint4 w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (v0 + k * 32 < vecs) w[k] = src[v0 + k * 32];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (v0 + k * 32 < vecs) dst[v0 + k * 32] = w[k];
+            }
         }
         if (u.beside_tiles) grid_dep_wait();
         return;
