@@ -38,9 +38,9 @@ template <class T>
 constexpr int kLStages = sizeof(T) == 4 ? 2 : 3;
 template <class T>
 constexpr int kLAnSm = sizeof(T) == 4 ? 3 : 4;  // CTAs an SM holds
-constexpr int kLGroups = kLThreads / 2;
-constexpr int kLList = 640;     // places of a list
-constexpr uint32_t kLFew = 64;   // lists that are ranked as they are
+constexpr int kLGroups = kLThreads / 4;
+constexpr int kLList = 640;     // places of the lists, kLOfWarp of each warp
+constexpr int kLOfWarp = kLList / kLWarps;
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLLimit = 0x1p22f;  // |x L| from here on: the whole numbers c have no room left
 constexpr float kLFloor = -1e30f;   // logits below count as this: 2^(x L - c) is 0, and 0 times x L - c too
@@ -91,7 +91,8 @@ struct LPart {
     float top, s, t;
 };
 struct LShared {
-    uint64_t list[kLList];    // places at or above the bound
+    uint64_t list[kLList];    // each warp's places at or above the bound
+    uint32_t n_list[kLWarps];
     uint64_t best[kLMaxTop];  // this CTA's alternatives, in order; 0: none
     LPart parts[kLMaxCluster];
     union {
@@ -102,7 +103,7 @@ struct LShared {
     float s[kLWarps], t[kLWarps], top[kLWarps];
     float bound;
     uint64_t bound_place;
-    uint32_t n_list, n_kept;
+    uint32_t n_kept;
 };
 
 // Each thread's own logits under way; the memory has other uses once they are through.
@@ -137,28 +138,27 @@ __device__ __forceinline__ void st_cluster_u64(uint32_t a, uint64_t v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 
-// The n-th largest of the groups' maxima (or a little less), given every thread's:
-// a warp takes the largest key out n times.
+// The n-th largest of the groups' maxima (or a little less), given every thread's: four
+// threads count how many are above a group's.
 __device__ __forceinline__ float bound_of(LShared &sh, float top, int n) {
     constexpr uint32_t kIndex = kLGroups - 1;  // a key's low bits tell equal maxima apart
     const int tid = threadIdx.x;
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    if ((tid & 1) == 0) sh.group[tid >> 1] = (ascending(top) & ~kIndex) | static_cast<uint32_t>(tid >> 1);
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t mine = (ascending(top) & ~kIndex) | static_cast<uint32_t>(tid >> 2);
+    if ((tid & 3) == 0) sh.group[tid >> 2] = mine;
     __syncthreads();
-    if (tid < 32) {
-        const uint4 g = reinterpret_cast<const uint4 *>(sh.group)[tid];
-        uint32_t a = max(g.x, g.y), b = min(g.x, g.y), c = max(g.z, g.w), d = min(g.z, g.w), u;
-        u = max(a, c), c = min(a, c), a = u;
-        u = max(b, d), d = min(b, d), b = u;
-        u = max(b, c), c = min(b, c), b = u;
-        uint32_t m = 0;
-        for (int i = 0; i < n; ++i) {
-            m = __reduce_max_sync(0xffffffffu, a);
-            if (a == m) a = b, b = c, c = d, d = 0;
-        }
-        m &= ~kIndex;
-        if (tid == 0) sh.bound = m <= ascending(-INFINITY) ? -INFINITY : of_ascending(m);
+    const uint4 *g4 = reinterpret_cast<const uint4 *>(sh.group) + (tid & 3) * (kLGroups / 16);
+    int above = 0;
+#pragma unroll
+    for (int j = 0; j < kLGroups / 16; ++j) {
+        const uint4 g = g4[j];
+        above += (g.x > mine) + (g.y > mine) + (g.z > mine) + (g.w > mine);
     }
+    above += __shfl_xor_sync(0xffffffffu, above, 1);
+    above += __shfl_xor_sync(0xffffffffu, above, 2);
+    if (above == n - 1 && (tid & 3) == 0)
+        sh.bound = (mine & ~kIndex) <= ascending(-INFINITY) ? -INFINITY : of_ascending(mine & ~kIndex);
     __syncthreads();
     return sh.bound;
 }
@@ -193,11 +193,13 @@ __device__ __noinline__ void slow_top(LShared &sh, const T *src, int n, int i0, 
         const uint64_t v = place_of(logit_of(src[i]), static_cast<uint32_t>(i0 + i));
         best = v > best ? v : best;
     }
-    const uint64_t other = __shfl_xor_sync(0xffffffffu, best, 1);
-    best = other > best ? other : best;
+    for (int o = 1; o < 4; o <<= 1) {
+        const uint64_t other = __shfl_xor_sync(0xffffffffu, best, o);
+        best = other > best ? other : best;
+    }
     __syncthreads();
-    if ((tid & 1) == 0) sh.group_place[tid >> 1] = best;
-    if (tid == 0) sh.n_list = 0;
+    if ((tid & 3) == 0) sh.group_place[tid >> 2] = best;
+    if (tid == 0) sh.n_kept = 0;
     __syncthreads();
     if (tid < kLGroups) {
         const uint64_t mine = sh.group_place[tid];
@@ -211,12 +213,12 @@ __device__ __noinline__ void slow_top(LShared &sh, const T *src, int n, int i0, 
     for (int i = tid; i < n; i += kLThreads) {
         const uint64_t v = place_of(logit_of(src[i]), static_cast<uint32_t>(i0 + i));
         if (v >= bound && place_logit(v) > -INFINITY) {
-            const uint32_t at = atomicAdd(&sh.n_list, 1u);
+            const uint32_t at = atomicAdd(&sh.n_kept, 1u);
             if (at < kLList) sh.list[at] = v;
         }
     }
     __syncthreads();
-    const uint32_t m = sh.n_list;
+    const uint32_t m = sh.n_kept;
     if (m <= kLList) {
         rank_places(sh.list, static_cast<int>(m), sh.best, n_top);
         return;
@@ -338,13 +340,11 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ctas = cluster_nctarank(), rank = ctas > 1 ? cluster_ctarank() : 0;
     const int64_t r = blockIdx.x / ctas;
-    if (tid == 0) sh.n_list = sh.n_kept = 0;
+    if (tid == 0) sh.n_kept = 0;
     grid_dep_launch();
     grid_dep_wait();
     const T *const row = static_cast<const T *>(p.logits) + r * p.row_stride;
     const bool joins = rank == 0 && tid == 0;
-    const int32_t given = joins && p.tokens ? __ldg(p.tokens + r) : -1;
-    const float x_given = given >= 0 && given < p.vocab ? logit_of(row[given]) : 0.f;
 
     // ---- this CTA's part of the row, from the 16-byte boundary at or before its first logit
     const int i0 = min(static_cast<int>(rank) * p.chunk, p.vocab), n = min(p.chunk, p.vocab - i0);
@@ -376,14 +376,19 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     };
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) fetch(i, i);
+    const int32_t given = joins && p.tokens ? __ldg(p.tokens + r) : -1;
     float top = -INFINITY, c = -1e30f, s = 0.f, t = 0.f, bound = INFINITY;
     bool bad = false;
+    uint32_t n_list = 0;  // of this warp
+    T x_given = {};
     for (int round = 0, stage = 0; round < rounds; ++round, stage = stage + 1 == kStages ? 0 : stage + 1) {
         fetch(round + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
         copies_wait<kStages - 1>();
         uint4 q[kLoads];
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) q[k] = ring.ring[stage][k][tid];
+        // (by now the given token is known, and its logit has until the end to come)
+        if (round == 0 && given >= 0 && given < p.vocab) x_given = row[given];
         uint32_t most[kLoads], all = 0;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
@@ -422,27 +427,25 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             uint32_t hits = __ballot_sync(0xffffffffu, here >= bound && here > -INFINITY);
             if (hits) {
                 constexpr int kValues = kLoads * kPer;
+                static_assert(kValues == 32, "a lane looks at one of them");
+                const int k = lane / kPer, e = lane % kPer;
                 __syncwarp();
                 do {
                     const int from = (tid & ~31) + __ffs(hits) - 1;
                     hits &= hits - 1;
-#pragma unroll
-                    for (int j0 = 0; j0 < kValues; j0 += 32) {
-                        const int j = j0 + lane, k = j / kPer, e = j % kPer;
-                        if (j < kValues) {
-                            const float x = value_of(reinterpret_cast<const T *>(&ring.ring[stage][k][from])[e]);
-                            if (x >= bound && x > -INFINITY) {
-                                const uint32_t at = atomicAdd(&sh.n_list, 1u);
-                                const int index = i0 + ((round * kLoads + k) * kLThreads + from) * kPer + e - pad;
-                                if (at < kLList) sh.list[at] = place_of(x + 0.f, static_cast<uint32_t>(index));
-                            }
-                        }
-                    }
+                    const float x = value_of(reinterpret_cast<const T *>(&ring.ring[stage][k][from])[e]);
+                    const bool in = x >= bound && x > -INFINITY;
+                    const uint32_t those = __ballot_sync(0xffffffffu, in);
+                    const uint32_t at = n_list + __popc(those & ((1u << lane) - 1));
+                    const int index = i0 + ((round * kLoads + k) * kLThreads + from) * kPer + e - pad;
+                    if (in && at < kLOfWarp) sh.list[warp * kLOfWarp + at] = place_of(x + 0.f, static_cast<uint32_t>(index));
+                    n_list += __popc(those);
                 } while (hits);
                 __syncwarp();
             }
         }
     }
+    if (kTop && lane == 0) sh.n_list[warp] = n_list;
     __syncthreads();  // (the ring's memory has other uses from here on)
     // the first CTA's ring may take the others' finds once every CTA is here (the other
     // half of this barrier is before the first store to it)
@@ -476,24 +479,27 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     }
     // ---- its alternatives
     if (kTop) {
-        const uint32_t m = sh.n_list;
+        bool full = part_bad;
+#pragma unroll
+        for (int w = 0; w < kLWarps; ++w) full = full || sh.n_list[w] > kLOfWarp;
         if (!any) {
             if (tid < p.n_top) sh.best[tid] = 0;
-        } else if (m > kLList || part_bad) {
+        } else if (full) {
             slow_top(sh, src, n, i0, p.n_top);
         } else {
-            const uint64_t *from = sh.list;
-            uint32_t left = m;
-            if (m > kLFew) {  // without those that only an earlier bound let in
-                for (uint32_t i = tid; i < m; i += kLThreads) {
-                    const uint64_t v = sh.list[i];
-                    if (place_logit(v) >= bound) ring.kept[atomicAdd(&sh.n_kept, 1u)] = v;
-                }
-                __syncthreads();
-                from = ring.kept;
-                left = sh.n_kept;
+            // without those that only an earlier bound let in
+            for (uint32_t i0_ = 0; i0_ < n_list; i0_ += 32) {
+                const uint32_t i = i0_ + static_cast<uint32_t>(lane);
+                const uint64_t v = i < n_list ? sh.list[warp * kLOfWarp + i] : 0;
+                const bool in = i < n_list && place_logit(v) >= bound;
+                const uint32_t those = __ballot_sync(0xffffffffu, in);
+                uint32_t at = 0;
+                if (lane == 0) at = atomicAdd(&sh.n_kept, static_cast<uint32_t>(__popc(those)));
+                at = __shfl_sync(0xffffffffu, at, 0) + __popc(those & ((1u << lane) - 1));
+                if (in) ring.kept[at] = v;
             }
-            rank_places(from, static_cast<int>(left), sh.best, p.n_top);
+            __syncthreads();
+            rank_places(ring.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
         }
     }
     __syncthreads();
@@ -515,17 +521,22 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     if (ctas > 1) cluster_sync_all();
     else __syncthreads();
     if (rank != 0) return;
-    float m = -INFINITY;
-    for (uint32_t i = 0; i < ctas; ++i) m = fmaxf(m, sh.parts[i].top);
-    s = t = 0.f;
+    float m = sh.parts[0].top;
+    if (ctas == 1) {
+        s = sh.parts[0].s;
+        t = sh.parts[0].t;
+    } else {
+        for (uint32_t i = 1; i < ctas; ++i) m = fmaxf(m, sh.parts[i].top);
+        s = t = 0.f;
+        if (m > -INFINITY)
+            for (uint32_t i = 0; i < ctas; ++i) {
+                const LPart part = sh.parts[i];
+                const float d = part.top - m, f = expf(d);
+                s = fmaf(part.s, f, s);
+                t += f > 0.f ? f * fmaf(d, part.s, part.t) : 0.f;
+            }
+    }
     const bool row_any = m > -INFINITY;
-    if (row_any)
-        for (uint32_t i = 0; i < ctas; ++i) {
-            const LPart part = sh.parts[i];
-            const float d = part.top - m, f = expf(d);
-            s = fmaf(part.s, f, s);
-            t += f > 0.f ? f * fmaf(d, part.s, part.t) : 0.f;
-        }
     s = fmaxf(s, 1.f);  // (the maximum's own, but for roundings)
     const float ln_s = logf(s);
     if (kTop) {
@@ -555,7 +566,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         if (p.logprobs) {
             float lp = 0.f;
             if (given >= p.vocab) report_error(p.err, PPAS_DEVERR_BAD_INDEX);
-            if (given >= 0) lp = row_any && given < p.vocab ? x_given - m - ln_s : -INFINITY;
+            if (given >= 0) lp = row_any && given < p.vocab ? logit_of(x_given) - m - ln_s : -INFINITY;
             p.logprobs[r] = lp;
         }
     }
