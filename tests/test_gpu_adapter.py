@@ -175,3 +175,161 @@ def test_other_stream_and_graph(ppas):
         c.out.fill_(0.0)
         graph.replay()
         c.check()
+
+
+# ---- runs of more than 512 rows, which are done in tiles of 128 (short runs beside them in units)
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 64, 72, 104, 128])
+@pytest.mark.parametrize("slices", [[256], [136, 40], [320, 64, 64], [8, 8, 16, 24]])
+def test_tiles_ranks_and_slices(ppas, rank, slices):
+    for lens, ids in (([1, 150, 470], [1, 0, 1]), ([513], [0])):
+        c = Call(lens, ids, 320, slices, rank, seed=rank)
+        ppas.ppas_adapter_add(**c.args())
+        c.check()
+
+
+@pytest.mark.parametrize("hidden", [8, 56, 64, 72, 136, 200, 264, 1000, 4096])
+@pytest.mark.parametrize("cols", [8, 72, 264, 1032])
+def test_tiles_hidden_sizes(ppas, hidden, cols):
+    """From one block of K, and a cluster of one CTA, to clusters of eight."""
+    c = Call([2, 140, 513], [0, 1, 0], hidden, [cols], 16, seed=hidden + cols, gap=8)
+    ppas.ppas_adapter_add(**c.args())
+    c.check()
+
+
+@pytest.mark.parametrize("tiles", [5, 9, 15, 16, 23, 24, 28, 36, 37, 50, 76, 77, 100, 153])
+def test_tiles_counts(ppas, tiles):
+    """Clusters of every size, to single CTAs in more than one round."""
+    rows = [128 * (tiles - 3) - 5, 48, 101]  # 3 + (tiles - 3) tiles of three runs
+    c = Call([1] + rows, [0, 1, 2, 0], 520, [136, 64], 16, seed=tiles)
+    ppas.ppas_adapter_add(**c.args())
+    c.check()
+
+
+def test_tiles_wide_inner_sums(ppas):
+    """384 inner sums, of 256 and 128 in two products; rows of the last tile few."""
+    for rows in (514, 900, 10000):
+        c = Call([rows], [1], 512, [128, 64, 40], 128, seed=rows)
+        ppas.ppas_adapter_add(**c.args())
+        c.check()
+
+
+def test_tiles_strides_in_place_and_no_scales(ppas):
+    for lens, ids in (([600, 130, 1], [1, -1, 0]), ([1, 512, 200], [0, 0, 1])):
+        c = Call(lens, ids, 256, [128, 72], 16, seed=5, gap=24, scales=False)
+        host = c.host()
+        c.full[:c.T, :c.cols] = c.y
+        c.y = c.out
+        ppas.ppas_adapter_add(**c.args(y=c.out, y_stride=c.out.stride(0)))
+        c.check(host)
+
+
+def test_tiles_rows_do_not_meet(ppas):
+    """NaN and infinities of one row, and of the adapters before and behind, stay away from the others."""
+    for rank in (8, 16, 40):
+        for slices in ([200], [72, 136]):
+            c = Call([700, 2, 100], [1, 2, 1], 328, slices, rank, n_adapters=4, seed=7)
+            clean = Call([700, 2, 100], [1, 2, 1], 328, slices, rank, n_adapters=4, seed=7)
+            c.x[3] = float("nan")
+            c.x[690, 5] = float("inf")
+            c.y[128, 9] = float("nan")
+            for k in (0, 3):
+                c.a[k], c.b[k] = float("nan"), float("nan")
+            for v in (c, clean):
+                ppas.ppas_adapter_add(**v.args())
+            torch.cuda.synchronize()
+            same = torch.ones_like(c.out, dtype=torch.bool)
+            same[3] = same[690] = False
+            same[128, 9] = False
+            assert torch.equal(c.out[same], clean.out[same])
+            assert bool(c.out[3].isnan().all()) and bool(c.out[128, 9].isnan())
+
+
+def test_tiles_past_32_bit_offsets(ppas):
+    """Rows of x and out further than 2^31 elements apart, and weights behind 2^31."""
+    t, stride = 600, 1 << 23
+    c = Call([t], [0], 128, [64], 16, seed=12)
+    x = torch.zeros((t, stride), dtype=torch.bfloat16, device="cuda")
+    x[:, :128] = c.x
+    n = 1 << 14
+    a = torch.zeros((n, 16, 16384), dtype=torch.bfloat16, device="cuda")
+    b = torch.zeros((n, 64, 16), dtype=torch.bfloat16, device="cuda")
+    out = torch.empty((t, stride), dtype=torch.bfloat16, device="cuda")
+    a = a.view(n * 128, 16, 128)
+    c.lens, c.ids = np.array([t], np.int32), np.array([n - 1], np.int32)
+    a[n - 1], b[n - 1] = c.a[0], c.b[0]
+    scales = torch.ones(n, device="cuda")
+    scales[n - 1] = c.scales[0]
+    ppas.ppas_adapter_add(**c.args(x=x, x_stride=stride, out=out, out_stride=stride, a=a, b=b, d_scales=scales,
+                                   n_adapters=n))
+    c.out.copy_(out[:, :64])
+    c.ids = np.array([0], np.int32)
+    c.check()
+    # the last adapter's weights lie behind 2^31 elements
+    big = torch.zeros((n, 16, 16384), dtype=torch.bfloat16, device="cuda")
+    x2 = _normal((t, 16384), 3)
+    d = Call([t], [0], 16384, [64], 16, seed=13)
+    d.x = x2
+    big[n - 1], b[n - 1] = d.a[0], d.b[0]
+    scales[n - 1] = d.scales[0]
+    ppas.ppas_adapter_add(**d.args(a=big, b=b, d_scales=scales, n_adapters=n, adapters=[n - 1]))
+    d.check()
+
+
+def test_calls_behind_one_another(ppas):
+    """Each call reads what the one before wrote, tiles and units in all of them, and a graph of them."""
+    lens, ids = [1, 600, 1, 1, 300, 20], [1, 0, -1, 0, 2, 1]
+    layers = [Call(lens, ids, 256, [256], 16, n_adapters=3, seed=20 + i) for i in range(6)]
+
+    def chain(wait):
+        x = layers[0].x
+        for c in layers:
+            ppas.ppas_adapter_add(**c.args(x=x, x_stride=x.stride(0)))
+            if wait:
+                torch.cuda.synchronize()
+            x = c.out
+    chain(True)
+    want = [c.full.clone() for c in layers]
+    for _ in range(5):
+        for c in layers:
+            c.out.fill_(float("nan"))
+        chain(False)
+        torch.cuda.synchronize()
+        assert all(torch.equal(c.full, w) for c, w in zip(layers, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(False)
+    for _ in range(5):
+        for c in layers:
+            c.out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(c.full, w) for c, w in zip(layers, want))
+
+
+def test_two_streams_at_once(ppas):
+    """Calls of two streams, and of two captured graphs, share nothing."""
+    a = Call([1, 700, 1, 30], [0, 1, 1, 0], 512, [192, 64], 16, seed=30)
+    b = Call([900, 1, 1], [1, 0, 1], 512, [192, 64], 16, seed=31)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for c, s in zip((a, b), streams):
+            ppas.ppas_adapter_add(**c.args(stream=s))
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+    graphs = []
+    for c in (a, b):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ppas.ppas_adapter_add(**c.args())
+        c.out.fill_(0.0)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
