@@ -6,7 +6,7 @@
  * plain host or device pointers and sizes; nothing here mentions a framework
  * type.  The library keeps no global state apart from per-device caches
  * (driver entry points, the SM count, the kernels' shared-memory limits, how
- * many decode thread-block clusters the device holds co-resident, one
+ * many thread-block clusters of the kernels the device holds co-resident, one
  * side stream with two events for steps too large for one launch, all created
  * on first use and thread-safe)
  * and the fixed scratch array of ppas_attention_step_noalloc; the only

@@ -7,11 +7,18 @@
 // One pass over the row.  A thread sums 2^(x L - c), L = log2 e, against a whole
 // number c of its own, raised when its logits outgrow it: a new c scales the
 // sums by a power of two, exactly, and x L - c is rounded once.  (M need not be known,
-// and a row is read from HBM once.)  The n-th largest of the maxima of 128
+// and a row is read from HBM once, by asynchronous copies into each thread's own
+// places: no thread waits for another's.)  The n-th largest of the maxima of 64
 // groups of threads is at most the n-th largest logit; what reaches it, a few times
 // n of all logits, goes to a list, whose first n are found by comparing all pairs.
 // That bound is raised as rounds of the pass double.  A cluster of CTAs shares a
 // row where rows are few, and its first CTA joins what they found.
+//
+// Many rows are bound by HBM: 4096 x 128000 bf16 in 153.7 us, 6.8 TB/s, the copy's rate,
+// with the issue slots 70 % busy (about 9 instructions a logit); 256 x 152000 with 20
+// alternatives 27.9 us (5.6 TB/s, 26 without alternatives: one wave of CTAs that
+// start and end together).  Few rows are a chain of copy, bound, list, ranks and two cluster
+// barriers: 1 x 152000 7.9 us, 4.8 without alternatives.
 //
 // Rows that this does not suit (a maximum of 2^22 / L and more, infinite ones
 // among them, or more logits at the bound than the list holds, as where all are equal)
@@ -29,15 +36,17 @@ namespace {
 
 constexpr int kLThreads = 256;
 constexpr int kLWarps = kLThreads / 32;
-// 16-byte loads of a round, a thread (32 logits), and rounds under way: 3 CTAs an SM of
-// fp32, 4 of bf16 (fp32, 4 loads and 3 rounds: 1 x 152000 8.8 us, 7.8 so; 256 x 152000 32.7
-// and 31.9; bf16, 8 and 2: 1024 x 128000 50.4, 46.4 so)
+// 16-byte loads of a round, a thread (32 logits), rounds under way, and the CTAs that an SM
+// then holds: of fp32 3 (bf16 4), and where there are fewer, kFew, 2 (3) with a round
+// more under way.  (256 x 152000: 28.0 us, 29.5 with the shorter ring; 128: 18.8 and 21.2; 400
+// 47.3 and 40.4; 32 x 128000 bf16 7.8 and 8.9, 1024 x 128000 48.5 and 44.6.  Rounds of 16
+// logits of fp32: 1 x 152000 8.8 us for 7.8; of 64 of bf16: 1024 x 128000 50.4 for 46.4.)
 template <class T>
 constexpr int kLLoads = sizeof(T) == 4 ? 8 : 4;
-template <class T>
-constexpr int kLStages = sizeof(T) == 4 ? 2 : 3;
-template <class T>
-constexpr int kLAnSm = sizeof(T) == 4 ? 3 : 4;  // CTAs an SM holds
+template <class T, bool kFew>
+constexpr int kLStages = (sizeof(T) == 4 ? 2 : 3) + (kFew ? 1 : 0);
+template <class T, bool kFew>
+constexpr int kLAnSm = (sizeof(T) == 4 ? 3 : 4) - (kFew ? 1 : 0);
 constexpr int kLGroups = kLThreads / 4;
 constexpr int kLList = 640;     // places of the lists, kLOfWarp of each warp
 constexpr int kLOfWarp = kLList / kLWarps;
@@ -107,10 +116,10 @@ struct LShared {
 };
 
 // Each thread's own logits under way; the memory has other uses once they are through.
-template <class T>
+template <class T, bool kFew>
 struct LRing {
     union {
-        uint4 ring[kLStages<T>][kLLoads<T>][kLThreads];
+        uint4 ring[kLStages<T, kFew>][kLLoads<T>][kLThreads];
         struct {
             uint64_t kept[kLList];
             uint64_t all[kLMaxCluster * kLMaxTop];
@@ -330,12 +339,13 @@ __device__ __forceinline__ void copies_wait() {
 
 }  // namespace
 
-template <class T, bool kTop>
+template <class T, bool kTop, bool kFew>
 __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_constant__ LogprobParams p) {
     extern __shared__ __align__(16) uint8_t logprob_smem[];
-    LRing<T> &ring = *reinterpret_cast<LRing<T> *>(logprob_smem);
-    LShared &sh = *reinterpret_cast<LShared *>(logprob_smem + sizeof(LRing<T>));
-    constexpr int kLoads = kLLoads<T>, kStages = kLStages<T>;
+    using Ring = LRing<T, kFew>;
+    Ring &ring = *reinterpret_cast<Ring *>(logprob_smem);
+    LShared &sh = *reinterpret_cast<LShared *>(logprob_smem + sizeof(Ring));
+    constexpr int kLoads = kLLoads<T>, kStages = kLStages<T, kFew>;
     constexpr int kPer = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ctas = cluster_nctarank(), rank = ctas > 1 ? cluster_ctarank() : 0;
@@ -422,8 +432,8 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         t += t2.x + t2.y;
         if (kTop) {
             // the logits at or above the bound go to the list: the warp looks through the
-            // values of one of its lanes after another (a lane by itself through its own: a
-            // few of them at a time keep the whole warp, and 256 x 152000 takes 36.5 us)
+            // values of one of its lanes after another (a lane by itself through its own, a
+            // few of them at a time keeping the whole warp: 256 x 152000 36.5 us, 32.5 so)
             uint32_t hits = __ballot_sync(0xffffffffu, here >= bound && here > -INFINITY);
             if (hits) {
                 constexpr int kValues = kLoads * kPer;
@@ -573,20 +583,21 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
 }
 
 static_assert(kLMaxCluster * kLMaxTop <= kLList, "the first CTA ranks them in `kept`");
-template <class T>
-constexpr int kLSmem = static_cast<int>(sizeof(LRing<T>) + sizeof(LShared));
-static_assert(kLAnSm<float> * (kLSmem<float> + 1024) <= 233472 &&
-                  kLAnSm<__nv_bfloat16> * (kLSmem<__nv_bfloat16> + 1024) <= 233472,
+template <class T, bool kFew>
+constexpr int kLSmem = static_cast<int>(sizeof(LRing<T, kFew>) + sizeof(LShared));
+template <class T, bool kFew>
+constexpr bool kLFits = kLAnSm<T, kFew> * (kLSmem<T, kFew> + 1024) <= 233472;
+static_assert(kLFits<float, false> && kLFits<float, true> && kLFits<__nv_bfloat16, false> && kLFits<__nv_bfloat16, true>,
               "shared memory of an SM");
 
 // How many clusters of 2, 4, 8 and 16 CTAs (16 are more than the portable 8) of a kernel
 // this device holds at a time; once per device.
-template <class T, bool kTop>
+template <class T, bool kTop, bool kFew>
 cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
     static std::atomic<uint64_t> limit_set{0};
     static std::atomic<int32_t> known[64][5] = {};  // + 1; 0: not asked
-    const auto kernel = token_logprobs_kernel<T, kTop>;
-    cudaError_t e = ensure_smem_limit(kernel, kLSmem<T>, limit_set);
+    const auto kernel = token_logprobs_kernel<T, kTop, kFew>;
+    cudaError_t e = ensure_smem_limit(kernel, kLSmem<T, kFew>, limit_set);
     int dev = 0;
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -596,7 +607,7 @@ cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(1u << i);
             cfg.blockDim = dim3(kLThreads);
-            cfg.dynamicSmemBytes = kLSmem<T>;
+            cfg.dynamicSmemBytes = kLSmem<T, kFew>;
             cudaLaunchAttribute a = {};
             a.id = cudaLaunchAttributeClusterDimension;
             a.val.clusterDim.x = 1u << i;
@@ -617,19 +628,20 @@ cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
     return cudaSuccess;
 }
 
-template <class T, bool kTop>
+template <class T, bool kTop, bool kFew>
 cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
     // As many CTAs a row as run at a time, 4096 logits each at least, 16 only where each
-    // has an SM (64 x 32003 bf16: 8 CTAs 7.1 us, 2 7.7; 1 x 152000: 16 CTAs 7.8, 8 11.0; 32 x
-    // 128000 bf16: 8 CTAs 8.5, 16 11.6; 256 x 152000: 2 CTAs 31.9, 1 43.5, 4 40.5).
+    // has an SM (1 x 152000: 16 CTAs 7.8 us, 8 11.0; 12 x 128000 bf16: 8 CTAs 6.5, 16 7.5; 64 x
+    // 32003 bf16: 4096 logits at least 7.1, 8192 7.7, 2048 8.0; 64 x 152000: 8 CTAs 17.4, 16, in
+    // two rounds, 27.7).
     int32_t clusters[5] = {};
-    const cudaError_t e = prepare_logprobs<T, kTop>(clusters);
+    const cudaError_t e = prepare_logprobs<T, kTop, kFew>(clusters);
     if (e != cudaSuccess) return e;
     int i = 16 * static_cast<int64_t>(n_rows) <= device_sm_count() ? 4 : 3;
     while (i > 0 && (n_rows > clusters[i] || p.vocab < 4096 << i)) --i;
     const int32_t c = 1 << i;
     p.chunk = ((p.vocab + c - 1) / c + 15) / 16 * 16;
-    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), kLSmem<T>, st);
+    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), kLSmem<T, kFew>, st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
         attrs[1].id = cudaLaunchAttributeClusterDimension;
@@ -639,7 +651,13 @@ cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
         l.cfg.attrs = attrs;
         l.cfg.numAttrs = 2;
     }
-    return cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, kTop>, p);
+    return cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, kTop, kFew>, p);
+}
+
+template <class T, bool kTop>
+cudaError_t launch_logprobs(const LogprobParams &p, int32_t n_rows, cudaStream_t st) {
+    const bool few = n_rows <= kLAnSm<T, true> * static_cast<int64_t>(device_sm_count());
+    return few ? launch_logprobs<T, kTop, true>(p, n_rows, st) : launch_logprobs<T, kTop, false>(p, n_rows, st);
 }
 
 cudaError_t launch_token_logprobs(const LogprobParams &p, int32_t n_rows, bool bf16, cudaStream_t st) {

@@ -25,7 +25,7 @@
 // dim, r = 1 / sqrt(mean x^2 + eps), all in fp32 and rounded once behind the
 // rotation.  A row is in the registers of one warp, so its sum of squares takes a
 // few shuffles and no memory: the bytes are those of the rotation alone.  16384 tokens
-// of 32/8 heads in 68.4 us (5.9 TB/s), 2056 of 16/2 in 7.0.
+// of 32/8 heads in 68.4 us (5.9 TB/s), 2056 of 16/2 in 7.1.
 #include <float.h>
 #include <math.h>
 
