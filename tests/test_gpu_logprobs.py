@@ -184,3 +184,42 @@ def test_other_stream_and_graph(ppas):
     graph.replay()
     b = _call(ppas, x, [1] * 20, 5)
     assert np.array_equal(lp.double().cpu().numpy(), b["lp"]) and np.array_equal(tok.cpu().numpy(), b["tok"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_past_32_bit_offsets(ppas, dtype):
+    v, stride = 3000, (1 << 30) + 5
+    x = torch.empty(3 * stride, dtype=dtype, device="cuda").as_strided((3, v), (stride, 1))
+    x.copy_(_logits(3, v, seed=11, dtype=dtype))
+    _check(ppas, x, [7, 2999, 0], 9)
+
+
+def test_long_lists_of_few_lanes(ppas):
+    """More logits at the bound than a warp's list holds: all of them in one lane's, or one warp's, places."""
+    v = 30000
+    for first, step, count in ((64, 1024 * 8, 40), (0, 1, 400), (2048, 4, 300), (5, 32, 200)):
+        for dtype in (torch.float32, torch.bfloat16):
+            x = _logits(2, v, seed=12, spread=0.5, dtype=dtype)
+            at = (first + step * torch.arange(count, device="cuda")) % v
+            x[:, at] = (20 + torch.randn(2, count, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))).to(dtype)
+            _check(ppas, x, [int(at[0]), int(at[-1])], 32)
+
+
+def test_two_streams_at_once(ppas):
+    xs = [_logits(40, 20000, seed=13), _logits(300, 9000, seed=14)]
+    streams = [torch.cuda.Stream() for _ in xs]
+    alone = [_call(ppas, x, [3] * x.shape[0], 10) for x in xs]
+    outs = []
+    for x in xs:
+        n = x.shape[0]
+        outs.append((torch.full((n,), 3, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda"),
+                     torch.empty(n, device="cuda"), torch.empty((n, 10), dtype=torch.int32, device="cuda"),
+                     torch.empty((n, 10), device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, o, s in zip(xs, outs, streams):
+            ppas.ppas_token_logprobs(x, False, x.stride(0), x.shape[0], x.shape[1], o[0], o[1], o[2], 10, o[3], o[4], None, s)
+    torch.cuda.synchronize()
+    for a, o in zip(alone, outs):
+        for k, t in zip(("lp", "ent", "tok", "top"), o[1:]):
+            assert np.array_equal(a[k], t.double().cpu().numpy())

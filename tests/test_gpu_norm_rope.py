@@ -201,3 +201,58 @@ def test_other_stream_and_graph(ppas):
     s.kc.fill_(7.0)
     graph.replay()
     s.check()
+
+
+def test_past_32_bit_offsets(ppas):
+    """Tokens' rows, and pages of the cache, further than 2^31 elements from the first."""
+    T, hq, hk, D = 40, 4, 2, 128
+    s = Step(T, hq, hk, D, 128, False, seed=10)
+    stride = 1 << 26  # 40 * 2^26 > 2^31
+    far = torch.empty((T, stride), dtype=torch.bfloat16, device="cuda")
+    far[:, :hq * D] = s.q.reshape(T, hq * D)
+    far[:, 1024:1024 + hk * D] = s.k.reshape(T, hk * D)
+    far[:, 2048:2048 + hk * D] = s.v.reshape(T, hk * D)
+    blocks = (1 << 31) // (hk * 16 * D) + 100
+    kc = torch.zeros((blocks, hk, 16, D), dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    slots = np.arange(T) + (blocks - 3) * 16
+    want = Step(T, hq, hk, D, 128, False, seed=10)
+    want.slots = np.arange(T, dtype=np.int32)
+    want.d_slots = torch.from_numpy(want.slots).cuda()
+    ppas.ppas_norm_rope_append(**want.args())
+    ppas.ppas_norm_rope_append(**s.args(q=far, k=far[:, 1024:], v=far[:, 2048:], q_stride=stride, k_stride=stride,
+                                        v_stride=stride, d_slot_mapping=torch.from_numpy(slots.astype(np.int32)).cuda(),
+                                        k_cache=kc, v_cache=vc, num_blocks=blocks))
+    torch.cuda.synchronize()
+    assert int(s.err.item()) == 0 and torch.equal(s.out[:T], want.out[:T])
+    assert torch.equal(kc[-3:, :, :].transpose(1, 2).reshape(-1, hk, D)[:T], want.kc.transpose(1, 2).reshape(-1, hk, D)[:T])
+    assert torch.equal(vc[-3:, :, :].transpose(1, 2).reshape(-1, hk, D)[:T], want.vc.transpose(1, 2).reshape(-1, hk, D)[:T])
+
+
+def test_cache_read_by_the_attention_step(ppas):
+    """The next kernel of the stream reads what was appended, call after call without a wait."""
+    hq, hk, D, T = 16, 2, 128, 64
+    s = Step(T, hq, hk, D, 128, False, seed=11)
+    s.slots = np.arange(T, dtype=np.int32)
+    s.d_slots = torch.from_numpy(s.slots).cuda()
+    s.kc.zero_()
+    s.vc.zero_()
+    table = torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    out = torch.empty((T, hq, D), dtype=torch.float32, device="cuda")
+
+    def step(wait):
+        ppas.ppas_norm_rope_append(**s.args())
+        if wait:
+            torch.cuda.synchronize()
+        size = ppas.ppas_attention_workspace_size([T], [T], hq, hk)
+        ws = torch.empty(max(size, 256), dtype=torch.uint8, device="cuda")
+        ppas.ppas_attention_step(s.out, s.kc, s.vc, s.blocks, table, 4, [T], [T], hq, hk, D, D ** -0.5, out, True, ws, size,
+                                 s.err)
+        torch.cuda.synchronize()
+        return out.clone()
+    want = step(True)
+    for i in range(10):
+        s.kc.fill_(float(i))
+        s.vc.fill_(float(i))
+        s.out.fill_(1.0)
+        assert torch.equal(step(False), want)
