@@ -16,9 +16,9 @@
 //
 // Many rows are bound by HBM: 4096 x 128000 bf16 in 153.7 us, 6.8 TB/s, the copy's rate,
 // with the issue slots 70 % busy (about 9 instructions a logit); 256 x 152000 with 20
-// alternatives 27.9 us (5.6 TB/s, 26 without alternatives: one wave of CTAs that
+// alternatives 28.0 us (5.6 TB/s, 26.5 without alternatives: one wave of CTAs that
 // start and end together).  Few rows are a chain of copy, bound, list, ranks and two cluster
-// barriers: 1 x 152000 7.9 us, 4.8 without alternatives.
+// barriers: 1 x 152000 7.8 us, 4.6 without alternatives.
 //
 // Rows that this does not suit (a maximum of 2^22 / L and more, infinite ones
 // among them, or more logits at the bound than the list holds, as where all are equal)
@@ -110,6 +110,7 @@ struct LShared {
     };
     uint64_t place[kLWarps];
     float s[kLWarps], t[kLWarps], top[kLWarps];
+    uint32_t bad[kLWarps];
     float bound;
     uint64_t bound_place;
     uint32_t n_kept;
@@ -172,24 +173,25 @@ __device__ __forceinline__ float bound_of(LShared &sh, float top, int n) {
     return sh.bound;
 }
 
-// best[0 .. n) of the m places in `from` (a 0 is none), in order (0 where there are
-// fewer): a place's rank is the number of larger ones, counted by several lanes.
-__device__ __forceinline__ void rank_places(const uint64_t *from, int m, uint64_t *best, int n) {
-    if (static_cast<int>(threadIdx.x) < n) best[threadIdx.x] = 0;
-    __syncthreads();
+// emit(i, place) for the first n of the m places in `from` in their order, and emit(i, 0)
+// for what they do not have: a place's rank is the number of larger ones, counted by several
+// lanes.  By whichever thread: no barrier.
+template <class Emit>
+__device__ __forceinline__ void rank_places(const uint64_t *from, int m, int n, Emit &&emit) {
+    const int tid = threadIdx.x;
+    if (tid >= m && tid < n) emit(tid, 0);
     int lanes = 32;
     while (lanes > 1 && m * lanes > kLThreads) lanes >>= 1;
-    const int l = threadIdx.x & (lanes - 1);
+    const int l = tid & (lanes - 1);
     for (int base = 0; base < m; base += kLThreads / lanes) {
-        const int i = base + static_cast<int>(threadIdx.x) / lanes;
+        const int i = base + tid / lanes;
         const uint64_t mine = i < m ? from[i] : 0;
         int before = 0;
 #pragma unroll 4
         for (int j = l; j < m; j += lanes) before += from[j] > mine;
         for (int o = lanes >> 1; o; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-        if (l == 0 && before < n && mine != 0) best[before] = mine;
+        if (l == 0 && i < m && before < n) emit(before, mine);
     }
-    __syncthreads();
 }
 
 // A part's alternatives where the list overflowed: by places instead of logits,
@@ -229,7 +231,8 @@ __device__ __noinline__ void slow_top(LShared &sh, const T *src, int n, int i0, 
     __syncthreads();
     const uint32_t m = sh.n_kept;
     if (m <= kLList) {
-        rank_places(sh.list, static_cast<int>(m), sh.best, n_top);
+        rank_places(sh.list, static_cast<int>(m), n_top, [&](int i, uint64_t v) { sh.best[i] = v; });
+        __syncthreads();
         return;
     }
     uint64_t before = ~uint64_t{0};
@@ -455,88 +458,105 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             }
         }
     }
-    if (kTop && lane == 0) sh.n_list[warp] = n_list;
-    __syncthreads();  // (the ring's memory has other uses from here on)
+    // ---- each warp's maximum and sums relative to it, behind one barrier (from which on
+    // the ring's memory has other uses)
+    {
+        float most = top;
+        for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        const bool some = most > -INFINITY;
+        if (some) {
+            const float z = fmaf(most, kLog2E, -c), f = ex2(-z);  // (a thread without logits: z = 1e30, f = 0)
+            t = kLn2 * (t - z * s) * f;
+            s *= f;
+        }
+        for (int o = 16; o; o >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+            t += __shfl_xor_sync(0xffffffffu, t, o);
+        }
+        bad = __any_sync(0xffffffffu, bad) || (some && !(fabsf(most) * kLog2E < kLLimit));
+        if (lane == 0) {
+            sh.top[warp] = most;
+            sh.s[warp] = s;
+            sh.t[warp] = t;
+            sh.bad[warp] = bad;
+            sh.n_list[warp] = n_list;
+        }
+    }
+    __syncthreads();
     // the first CTA's ring may take the others' finds once every CTA is here (the other
     // half of this barrier is before the first store to it)
-    cluster_arrive();
+    if (ctas > 1) cluster_arrive();
 
-    // ---- the part's maximum and sums
-    float part_top = top;
-    for (int o = 16; o; o >>= 1) part_top = fmaxf(part_top, __shfl_xor_sync(0xffffffffu, part_top, o));
-    if (lane == 0) sh.top[warp] = part_top;
-    __syncthreads();
-    for (int w = 0; w < kLWarps; ++w) part_top = fmaxf(part_top, sh.top[w]);
+    // ---- the part's, by every warp for itself
+    const int w8 = lane % kLWarps;
+    float part_top = sh.top[w8];
+    for (int o = 1; o < kLWarps; o <<= 1) part_top = fmaxf(part_top, __shfl_xor_sync(0xffffffffu, part_top, o));
     part_top = fminf(part_top, kLLargest<T>);
     const bool any = part_top > -INFINITY;
-    const bool part_bad = __syncthreads_or(bad || (any && !(fabsf(part_top) * kLog2E < kLLimit))) != 0;
+    const bool part_bad = __any_sync(0xffffffffu, sh.bad[w8] != 0);
+    const bool full = __any_sync(0xffffffffu, sh.n_list[w8] > kLOfWarp);
     if (any && part_bad) {
         const float2 v = slow_sums(src, n, part_top);
         s = v.x;
         t = v.y;
-    } else if (any) {
-        const float z = fmaf(part_top, kLog2E, -c), f = ex2(-z);  // (a thread without logits: z = 1e30, f = 0)
-        t = kLn2 * (t - z * s) * f;
-        s *= f;
+        for (int o = 16; o; o >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+            t += __shfl_xor_sync(0xffffffffu, t, o);
+        }
+        __syncthreads();
+        if (lane == 0) {
+            sh.s[warp] = s;
+            sh.t[warp] = t;
+        }
+        __syncthreads();
+        s = sh.s[w8];
+        t = sh.t[w8];
+    } else {
+        const float d = sh.top[w8] - part_top, f = any ? expf(d) : 0.f;
+        s = f > 0.f ? sh.s[w8] * f : 0.f;
+        t = f > 0.f ? fmaf(d, sh.s[w8], sh.t[w8]) * f : 0.f;
     }
-    for (int o = 16; o; o >>= 1) {
+    for (int o = 1; o < kLWarps; o <<= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
         t += __shfl_xor_sync(0xffffffffu, t, o);
     }
-    if (lane == 0) {
-        sh.s[warp] = s;
-        sh.t[warp] = t;
+    // ---- its alternatives: in `kept`, or in their order in `best`
+    const bool in_best = kTop && any && (part_bad || full);
+    if (in_best) {
+        slow_top(sh, src, n, i0, p.n_top);
+    } else if (kTop) {
+        // without those that only an earlier bound let in
+        for (uint32_t j = 0; j < n_list; j += 32) {
+            const uint32_t i = j + static_cast<uint32_t>(lane);
+            const uint64_t v = i < n_list ? sh.list[warp * kLOfWarp + i] : 0;
+            const bool in = i < n_list && place_logit(v) >= bound;
+            const uint32_t those = __ballot_sync(0xffffffffu, in);
+            uint32_t at = 0;
+            if (lane == 0) at = atomicAdd(&sh.n_kept, static_cast<uint32_t>(__popc(those)));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(those & ((1u << lane) - 1));
+            if (in) ring.kept[at] = v;
+        }
+        __syncthreads();
     }
-    // ---- its alternatives
-    if (kTop) {
-        bool full = part_bad;
-#pragma unroll
-        for (int w = 0; w < kLWarps; ++w) full = full || sh.n_list[w] > kLOfWarp;
-        if (!any) {
-            if (tid < p.n_top) sh.best[tid] = 0;
-        } else if (full) {
-            slow_top(sh, src, n, i0, p.n_top);
-        } else {
-            // without those that only an earlier bound let in
-            for (uint32_t i0_ = 0; i0_ < n_list; i0_ += 32) {
-                const uint32_t i = i0_ + static_cast<uint32_t>(lane);
-                const uint64_t v = i < n_list ? sh.list[warp * kLOfWarp + i] : 0;
-                const bool in = i < n_list && place_logit(v) >= bound;
-                const uint32_t those = __ballot_sync(0xffffffffu, in);
-                uint32_t at = 0;
-                if (lane == 0) at = atomicAdd(&sh.n_kept, static_cast<uint32_t>(__popc(those)));
-                at = __shfl_sync(0xffffffffu, at, 0) + __popc(those & ((1u << lane) - 1));
-                if (in) ring.kept[at] = v;
-            }
+    float m = part_top;
+    if (ctas > 1) {
+        // ---- the first CTA joins the parts
+        if (kTop && !in_best) {
+            rank_places(ring.kept, static_cast<int>(sh.n_kept), p.n_top, [&](int i, uint64_t v) { sh.best[i] = v; });
             __syncthreads();
-            rank_places(ring.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
         }
-    }
-    __syncthreads();
-    // ---- the first CTA joins the parts
-    cluster_wait();
-    if (tid == 0) {
-        s = t = 0.f;
-        for (int w = 0; w < kLWarps; ++w) {
-            s += sh.s[w];
-            t += sh.t[w];
+        cluster_wait();
+        if (tid == 0) {
+            const uint32_t to = dsmem_addr(smem_u32(&sh.parts[rank]), 0);
+            dsmem_st_f32(to, part_top);
+            dsmem_st_f32(to + 4, any ? s : 0.f);
+            dsmem_st_f32(to + 8, any ? t : 0.f);
         }
-        const uint32_t to = dsmem_addr(smem_u32(&sh.parts[rank]), 0);
-        dsmem_st_f32(to, part_top);
-        dsmem_st_f32(to + 4, any ? s : 0.f);
-        dsmem_st_f32(to + 8, any ? t : 0.f);
-    }
-    if (kTop && ctas > 1 && tid < p.n_top)
-        st_cluster_u64(dsmem_addr(smem_u32(&ring.all[rank * p.n_top + tid]), 0), sh.best[tid]);
-    if (ctas > 1) cluster_sync_all();
-    else __syncthreads();
-    if (rank != 0) return;
-    float m = sh.parts[0].top;
-    if (ctas == 1) {
-        s = sh.parts[0].s;
-        t = sh.parts[0].t;
-    } else {
-        for (uint32_t i = 1; i < ctas; ++i) m = fmaxf(m, sh.parts[i].top);
+        if (kTop && tid < p.n_top)
+            st_cluster_u64(dsmem_addr(smem_u32(&ring.all[rank * p.n_top + tid]), 0), sh.best[tid]);
+        cluster_sync_all();
+        if (rank != 0) return;
+        for (uint32_t i = 0; i < ctas; ++i) m = fmaxf(m, sh.parts[i].top);
         s = t = 0.f;
         if (m > -INFINITY)
             for (uint32_t i = 0; i < ctas; ++i) {
@@ -545,13 +565,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
                 s = fmaf(part.s, f, s);
                 t += f > 0.f ? f * fmaf(d, part.s, part.t) : 0.f;
             }
-    }
-    const bool row_any = m > -INFINITY;
-    s = fmaxf(s, 1.f);  // (the maximum's own, but for roundings)
-    const float ln_s = logf(s);
-    if (kTop) {
-        const uint64_t *found = sh.best;
-        if (ctas > 1) {
+        if (kTop) {
             // the n-th largest of all is at least the least of every CTA's (n / CTAs)-th
             const int at = (p.n_top + static_cast<int>(ctas) - 1) / static_cast<int>(ctas) - 1;
             const uint32_t least = __reduce_min_sync(
@@ -563,12 +577,20 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
                 if (v != 0 && static_cast<uint32_t>(v >> 32) >= least) ring.kept[atomicAdd(&sh.n_kept, 1u)] = v;
             }
             __syncthreads();
-            rank_places(ring.kept, static_cast<int>(sh.n_kept), sh.best, p.n_top);
         }
-        const uint64_t mine = tid < p.n_top ? found[tid] : 0;
-        if (tid < p.n_top) {
-            p.top_tokens[r * p.n_top + tid] = mine ? place_index(mine) : -1;
-            p.top_logprobs[r * p.n_top + tid] = mine ? place_logit(mine) - m - ln_s : -INFINITY;
+    }
+    const bool row_any = m > -INFINITY;
+    s = fmaxf(s, 1.f);  // (the maximum's own, but for roundings)
+    const float ln_s = logf(s);
+    if (kTop) {
+        auto put = [&](int i, uint64_t v) {
+            p.top_tokens[r * p.n_top + i] = v ? place_index(v) : -1;
+            p.top_logprobs[r * p.n_top + i] = v ? place_logit(v) - m - ln_s : -INFINITY;
+        };
+        if (in_best && ctas == 1) {
+            if (tid < p.n_top) put(tid, sh.best[tid]);
+        } else {
+            rank_places(ring.kept, static_cast<int>(sh.n_kept), p.n_top, put);
         }
     }
     if (tid == 0) {
