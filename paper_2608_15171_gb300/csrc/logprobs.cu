@@ -14,11 +14,11 @@
 // That bound is raised as rounds of the pass double.  A cluster of CTAs shares a
 // row where rows are few, and its first CTA joins what they found.
 //
-// Many rows are bound by HBM: 4096 x 128000 bf16 in 153.7 us, 6.8 TB/s, the copy's rate,
+// Many rows are bound by HBM: 4096 x 128000 bf16 in 152.0 us, 6.9 TB/s, the copy's rate,
 // with the issue slots 70 % busy (about 9 instructions a logit); 256 x 152000 with 20
-// alternatives 28.0 us (5.6 TB/s, 26.5 without alternatives: one wave of CTAs that
+// alternatives 27.8 us (5.6 TB/s, 26.5 without alternatives: one wave of CTAs that
 // start and end together).  Few rows are a chain of copy, bound, list, ranks and two cluster
-// barriers: 1 x 152000 7.8 us, 4.6 without alternatives.
+// barriers: 1 x 152000 7.4 us, 4.2 without alternatives.
 //
 // Rows that this does not suit (a maximum of 2^22 / L and more, infinite ones
 // among them, or more logits at the bound than the list holds, as where all are equal)
@@ -370,6 +370,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     // its own waits are all that it takes.
     constexpr int kRound = kLThreads * kLoads;
     const int rounds = (vecs + kRound - 1) / kRound;
+    constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf, bf16 twice
     auto fetch = [&](int round, int stage) {
         const int v0 = round * kRound;
         if (v0 >= whole0 && v0 + kRound <= whole1) {
@@ -377,11 +378,27 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             const uint32_t to = smem_u32(&ring.ring[stage][0][tid]);
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) copy16_async(to + k * kLThreads * 16, from + k * kLThreads);
+        } else if (sizeof(T) == 4 && round < rounds) {
+            // (a part's last round, all at once; of bf16 one 16 bytes after another, which the
+            // kernel's other rounds lose least to: 3292 x 5323 fp32 22.6 us, 25.4 so; 4096 x
+            // 128000 bf16 152.0, 169.1 all at once)
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                const int v = v0 + k * kLThreads + tid;
+                if (v >= whole0 && v < whole1) copy16_async(smem_u32(&ring.ring[stage][k][tid]), src4 + v);
+                else if (v >= vecs) ring.ring[stage][k][tid] = make_uint4(kNone, kNone, kNone, kNone);
+            }
+            // the part's first 16 bytes and its last, where they are not whole
+            if (whole0 && v0 + tid == 0) ring.ring[stage][0][tid] = edge_vector(src, -pad, n);
+            if (const int k = (whole1 - v0 - tid) / kLThreads;
+                whole1 < vecs && whole1 >= max(v0, whole0) && k < kLoads && (whole1 - tid) % kLThreads == 0)
+                ring.ring[stage][k][tid] = edge_vector(src, whole1 * kPer - pad, n);
         } else if (round < rounds) {
 #pragma unroll 1
             for (int k = 0; k < kLoads; ++k) {
                 const int v = v0 + k * kLThreads + tid;
                 if (v >= whole0 && v < whole1) copy16_async(smem_u32(&ring.ring[stage][k][tid]), src4 + v);
+                else if (v >= vecs) ring.ring[stage][k][tid] = make_uint4(kNone, kNone, kNone, kNone);
                 else ring.ring[stage][k][tid] = edge_vector(src, v * kPer - pad, n);
             }
         }
