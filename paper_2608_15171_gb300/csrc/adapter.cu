@@ -17,6 +17,7 @@
 // 38.8 (4.7 TB/s).
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <memory>
 #include <new>
 #include <type_traits>
@@ -30,7 +31,8 @@ namespace {
 
 constexpr int kAThreads = 512;
 constexpr int kAWarps = kAThreads / 32;
-constexpr int kAChunk = 96;  // inner sums worked at a time: the loads of 12 x 16 bytes a lane are under way at once
+constexpr int kAUnitCluster = 16;  // CTAs of a unit's cluster (more than the portable 8)
+constexpr int kAChunk = 96;  // inner sums of a warp at most: its loads of 12 x 16 bytes a lane are under way at once
 constexpr int kAAhead = 4;   // of the rank in B, 16 times this are loaded ahead
 constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make tiles,
 // and of all such runs together (below, units of 16 rows are done first: 512 rows, 2048 x
@@ -45,10 +47,19 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t a) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(a)
+                 : "memory");
     return v;
+}
+__device__ __forceinline__ void add_to(float4 &v, float4 w) {
+    v.x += w.x;
+    v.y += w.y;
+    v.z += w.z;
+    v.w += w.w;
 }
 // the first half of a cluster barrier, behind what this thread has read
 __device__ __forceinline__ void cluster_arrive() {
@@ -71,11 +82,20 @@ struct UnitParams {
     int32_t rows[kRows];
 };
 
-// floats of a warp's sums of 16 rows and up to kAChunk columns
-__host__ __device__ constexpr int unit_red(int wide) { return kAUnitRows * (wide < kAChunk ? wide : kAChunk); }
+// The inner sums are parted among 2^unit_parts_log(wide) of the warps, up to kAChunk each,
+// and K among as many warps as that leaves: log2, and a part's width.
+__host__ __device__ constexpr int unit_parts_log(int wide) {
+    int l = 0;
+    while (wide > kAChunk << l) ++l;
+    return l;
+}
+__host__ __device__ constexpr int unit_part(int wide) {
+    return ((wide + (1 << unit_parts_log(wide)) - 1 >> unit_parts_log(wide)) + 7) / 8 * 8;
+}
+static_assert(1 << unit_parts_log(kAMaxSlices * kAMaxRank) <= kAWarps, "a warp has one part");
 __host__ __device__ constexpr int unit_pitch(int wide) { return wide + 4; }
-__host__ __device__ constexpr size_t unit_smem(int wide, int steps) {
-    return 4 * (static_cast<size_t>(kAWarps) * unit_red(wide) + kAUnitRows * wide + kAUnitRows * unit_pitch(wide)) +
+__host__ __device__ constexpr size_t unit_smem(int wide, int part, int steps) {
+    return 4 * (static_cast<size_t>(kAWarps) * kAUnitRows * part + kAUnitRows * wide + kAUnitRows * unit_pitch(wide)) +
            static_cast<size_t>(steps) * 32 * 32;
 }
 
@@ -120,8 +140,9 @@ __global__ void __launch_bounds__(kAThreads, 1)
         return;
     }
     const int wide = p.n_slices * p.rank, pitch = unit_pitch(wide), rank16 = (p.rank + 15) / 16;
-    float *const red = adapter_smem;                          // [warp][row][columns]
-    float *const part = red + kAWarps * unit_red(wide);       // [row][wide]: this CTA's part of K
+    const int parts_log = unit_parts_log(wide), width = unit_part(wide);
+    float *const red = adapter_smem;                          // [warp][row][width]
+    float *const part = red + kAWarps * kAUnitRows * width;   // [row][wide]: this CTA's part of K
     float *const sum = part + kAUnitRows * wide;              // [row][pitch]
     uint4 *const frag = reinterpret_cast<uint4 *>(sum + kAUnitRows * pitch);  // [slice][16 of the rank][lane][2]
     const __nv_bfloat16 *const a = p.a + static_cast<int64_t>(unit.adapter) * wide * p.hidden;
@@ -133,23 +154,10 @@ __global__ void __launch_bounds__(kAThreads, 1)
     // ---- s = x A^T over this CTA's blocks of 32 of K
     const int blocks = (p.hidden + 31) / 32;
     const int kb0 = blocks * rank / ctas, kb1 = blocks * (rank + 1) / ctas;
-    // where a warp's place holds the sums of all columns they are joined once, else kAChunk of them at a time
-    const bool once = n * wide <= unit_red(wide);
-    const int red_pitch = once ? wide : min(wide, kAChunk);
-    auto join = [&](int c0, int width) {
-        __syncthreads();
-        for (int i = tid; i < n * width; i += kAThreads) {
-            const int row = i / width, c = i - row * width;
-            const float *const from = red + row * red_pitch + (once ? c0 : 0) + c;
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < kAWarps; ++w) v += from[w * unit_red(wide)];
-            part[row * wide + c0 + c] = v;
-        }
-    };
-    for (int n0 = 0; n0 < wide; n0 += kAChunk) {
+    {
+        const int n0 = (warp & ((1 << parts_log) - 1)) * width, n1 = min(n0 + width, wide);
         float acc[kAChunk / 8][4] = {};
-        for (int kb = kb0 + warp; kb < kb1; kb += kAWarps) {
+        for (int kb = kb0 + (warp >> parts_log); kb < kb1; kb += kAWarps >> parts_log) {
             const int k = kb * 32 + t * 8;
             const bool in = k < p.hidden;
             const uint4 x0 = in && has0 ? __ldg(reinterpret_cast<const uint4 *>(p.x + row0 * p.x_stride + k)) : zero;
@@ -158,27 +166,23 @@ __global__ void __launch_bounds__(kAThreads, 1)
             const __nv_bfloat16 *at = a + static_cast<int64_t>(n0 + g) * p.hidden + k;
 #pragma unroll
             for (int j = 0; j < kAChunk / 8; ++j) {
-                w[j] = in && n0 + 8 * j < wide ? __ldg(reinterpret_cast<const uint4 *>(at)) : zero;
+                w[j] = in && n0 + 8 * j < n1 ? __ldg(reinterpret_cast<const uint4 *>(at)) : zero;
                 at += 8 * p.hidden;
             }
             const uint32_t f0[4] = {x0.x, x1.x, x0.y, x1.y}, f1[4] = {x0.z, x1.z, x0.w, x1.w};
 #pragma unroll
             for (int j = 0; j < kAChunk / 8; ++j) {
-                if (n0 + 8 * j >= wide) break;
+                if (n0 + 8 * j >= n1) break;
                 mma_16816(acc[j], f0, w[j].x, w[j].y);
                 mma_16816(acc[j], f1, w[j].z, w[j].w);
             }
         }
-        float *const to = red + warp * unit_red(wide) + g * red_pitch + (once ? n0 : 0) + 2 * t;
+        float *const to = red + (warp * kAUnitRows + g) * width + 2 * t;
 #pragma unroll
         for (int j = 0; j < kAChunk / 8; ++j) {
-            if (n0 + 8 * j >= wide) break;
+            if (n0 + 8 * j >= n1) break;
             if (has0) *reinterpret_cast<float2 *>(to + 8 * j) = make_float2(acc[j][0], acc[j][1]);
-            if (has1) *reinterpret_cast<float2 *>(to + 8 * red_pitch + 8 * j) = make_float2(acc[j][2], acc[j][3]);
-        }
-        if (!once) {
-            join(n0, min(kAChunk, wide - n0));
-            __syncthreads();
+            if (has1) *reinterpret_cast<float2 *>(to + 8 * width + 8 * j) = make_float2(acc[j][2], acc[j][3]);
         }
     }
     // ---- out = y + scale s B^T: groups of 32 columns, in each an MMA's column n is
@@ -217,21 +221,35 @@ __global__ void __launch_bounds__(kAThreads, 1)
     f.slice = 0;
     // (what the second product reads first is on its way while the sums are joined)
     if (group < n_groups) fetch(group, f);
-    if (once) join(0, wide);
+    __syncthreads();
+    const int vecs = wide / 4;
+    for (int i = tid; i < n * vecs; i += kAThreads) {
+        const int row = i / vecs, c = (i - row * vecs) * 4, from_warp = c / width;
+        const float *const from = red + (from_warp * kAUnitRows + row) * width + c - from_warp * width;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < kAWarps >> parts_log; ++w)
+            add_to(v, *reinterpret_cast<const float4 *>(from + (w << parts_log) * kAUnitRows * width));
+        *reinterpret_cast<float4 *>(part + row * wide + c) = v;
+    }
     cluster_sync_all();
-    for (int i = tid; i < kAUnitRows * wide; i += kAThreads) {
-        const int row = i / wide, c = i - row * wide;
-        float v = 0.f, from[kAMaxCluster];
+    for (int i = tid; i < kAUnitRows * vecs; i += kAThreads) {
+        const int row = i / vecs, c = (i - row * vecs) * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row < n) {
             const uint32_t at = smem_u32(part + row * wide + c);
 #pragma unroll
-            for (int r = 0; r < kAMaxCluster; ++r)
-                if (r < ctas) from[r] = ld_cluster_f32(dsmem_addr(at, static_cast<uint32_t>(r)));
+            for (int r0 = 0; r0 < kAUnitCluster; r0 += 8) {
+                if (r0 >= ctas) break;
+                float4 from[8];
 #pragma unroll
-            for (int r = 0; r < kAMaxCluster; ++r)
-                if (r < ctas) v += from[r];
+                for (int r = 0; r < 8; ++r)
+                    if (r0 + r < ctas) from[r] = ld_cluster_f32x4(dsmem_addr(at, static_cast<uint32_t>(r0 + r)));
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r0 + r < ctas) add_to(v, from[r]);
+            }
         }
-        sum[row * pitch + c] = v;
+        *reinterpret_cast<float4 *>(sum + row * pitch + c) = v;
     }
     __syncthreads();
     cluster_arrive();  // nothing of another CTA's is read from here on
@@ -299,7 +317,7 @@ __global__ void __launch_bounds__(kAThreads, 1)
 }
 
 // ---------------------------------------------------------------- long runs of rows
-// A tile of 128 rows of one adapter, on the tcgen05 tensor cores: the inner sums
+// A tile of 128 rows (or 64, of the products' 128) of one adapter, on the tcgen05 tensor cores: the inner sums
 // s = x A^T [128, slices x rank] accumulate in TMEM over blocks of 64 of K, each slice's on
 // columns of its own (rank rounded up to 16).  The epilogue warps turn them, in
 // place, into two bf16 numbers each, the operand A in TMEM of the second product, and
@@ -360,14 +378,6 @@ __device__ __forceinline__ ColumnBlock column_block(const TileParams &tp, int i)
 }
 static_assert(kAMaxSlices == 4, "column_block compares with three of them");
 
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(a)
-                 : "memory");
-    return v;
-}
 __device__ __forceinline__ void tmem_ld16_sync(uint32_t taddr, float (&v)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -451,9 +461,9 @@ __global__ void __launch_bounds__(kTThreads, 1)
     const int k_blocks = (p.hidden + kTK - 1) / kTK;
     const int kb0 = k_blocks * rank / ctas, kb1 = k_blocks * (rank + 1) / ctas;
     const int mine = (tp.block_at[kAMaxSlices] - rank + ctas - 1) / ctas;
-    const uint32_t stage_bytes = kTXBytes + ts.a_bytes;
+    const uint32_t sub_bytes = ts.x_bytes + ts.a_bytes, stage_bytes = static_cast<uint32_t>(ts.subs) * sub_bytes;
     const int block = 1 << ts.block_log, boxes = block / 64;
-    const uint32_t y_bytes = static_cast<uint32_t>(boxes) * kTBoxBytes;
+    const uint32_t y_bytes = static_cast<uint32_t>(boxes) * ts.x_bytes;
     // (every thread, on every path: the same number of cluster barriers)
     auto cluster_point = [&]() {
         if (ctas > 1) {
@@ -466,16 +476,19 @@ __global__ void __launch_bounds__(kTThreads, 1)
         // ---------------------------------------------------------------- TMA
         bool ok = true;
         int q = 0;
-        for (int s = 0, round = 0; kb0 + q < kb1; ++q) {
+        for (int s = 0, round = 0, kb = kb0; kb < kb1; kb += ts.subs, ++q) {
             if (round > 0 && !mbar_wait_warp(bar(T_EMPTY + s), (round & 1) ^ 1, tp.err)) {
                 ok = false;
                 break;
             }
             if (elect_one()) {
-                const uint32_t dst = sb + static_cast<uint32_t>(s) * stage_bytes;
-                mbar_expect_tx(bar(T_FULL + s), stage_bytes);
-                tma_load_2d(dst, &tm_x, (kb0 + q) * kTK, tile.first, bar(T_FULL + s));
-                tma_load_3d(dst + kTXBytes, &tm_a, (kb0 + q) * kTK, 0, tile.adapter * p.n_slices, bar(T_FULL + s));
+                uint32_t dst = sb + static_cast<uint32_t>(s) * stage_bytes;
+                const int subs = min(ts.subs, kb1 - kb);
+                mbar_expect_tx(bar(T_FULL + s), static_cast<uint32_t>(subs) * sub_bytes);
+                for (int j = 0; j < subs; ++j, dst += sub_bytes) {
+                    tma_load_2d(dst, &tm_x, (kb + j) * kTK, tile.first, bar(T_FULL + s));
+                    tma_load_3d(dst + ts.x_bytes, &tm_a, (kb + j) * kTK, 0, tile.adapter * p.n_slices, bar(T_FULL + s));
+                }
             }
             __syncwarp();
             if (++s == ts.stages) {
@@ -503,7 +516,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 const uint32_t dst = sb + static_cast<uint32_t>(s) * y_bytes;
                 mbar_expect_tx(bar(T_YFULL + s), y_bytes);
                 for (int h = 0; h < boxes; ++h)
-                    tma_load_2d(dst + static_cast<uint32_t>(h) * kTBoxBytes, &tm_y, cb.c0 + h * 64, tile.first,
+                    tma_load_2d(dst + static_cast<uint32_t>(h) * ts.x_bytes, &tm_y, cb.c0 + h * 64, tile.first,
                                 bar(T_YFULL + s));
             }
             __syncwarp();
@@ -526,10 +539,10 @@ __global__ void __launch_bounds__(kTThreads, 1)
             const ColumnBlock cb = column_block(tp, rank + i * ctas);
             if (lane == 0) {
                 const uint32_t from = sb + static_cast<uint32_t>(s) * y_bytes;
-                if (tile.n == kTRows)
+                if (tile.n == ts.rows)
                     for (int h = 0; h < boxes; ++h)
                         if (h * 64 + 64 <= cb.width)
-                            tma_store_2d(&tm_out, from + static_cast<uint32_t>(h) * kTBoxBytes, cb.c0 + h * 64, tile.first);
+                            tma_store_2d(&tm_out, from + static_cast<uint32_t>(h) * ts.x_bytes, cb.c0 + h * 64, tile.first);
                 stores_commit();
             }
             __syncwarp();
@@ -565,23 +578,28 @@ __global__ void __launch_bounds__(kTThreads, 1)
             constexpr bool kTwo = decltype(parts)::value == 2;
             const uint32_t idesc0 = idesc16 + (static_cast<uint32_t>(((kTwo ? 256 : width) - 16) >> 3) << 17);
             const uint32_t idesc1 = idesc16 + (static_cast<uint32_t>((width - 256 - 16) >> 3) << 17);
-            const uint64_t dx0 = smem_desc_sw128(sb, 16, 1024), da0 = smem_desc_sw128(sb + kTXBytes, 16, 1024);
+            const uint64_t dx0 = smem_desc_sw128(sb, 16, 1024), da0 = smem_desc_sw128(sb + ts.x_bytes, 16, 1024);
             uint32_t accumulate = 0;
-            for (int q = kb1 - kb0, s = 0, parity = 0; q > 0; --q) {
+            for (int q = kb1 - kb0, s = 0, parity = 0; q > 0; q -= ts.subs) {
                 if (!mbar_wait_warp(bar(T_FULL + s), parity, tp.err)) return false;
                 tc_fence_after();
                 const uint64_t at = (static_cast<uint32_t>(s) * stage_bytes) >> 4;
-                const uint64_t dx = dx0 + at, da = da0 + at;
                 if (elect_one()) {
+                    uint64_t dx = dx0 + at, da = da0 + at;
+#pragma unroll 1
+                    for (int j = min(ts.subs, q); j > 0; --j, dx += sub_bytes >> 4, da += sub_bytes >> 4) {
 #pragma unroll
-                    for (int kk = 0; kk < kTK / 16; ++kk) {
-                        umma_bf16(tmem, dx + kk * 2, da + kk * 2, idesc0, kk > 0 ? 1u : accumulate);
-                        if (kTwo) umma_bf16(tmem + 256, dx + kk * 2, da + 256 * 8 + kk * 2, idesc1, kk > 0 ? 1u : accumulate);
+                        for (int kk = 0; kk < kTK / 16; ++kk) {
+                            const uint32_t more = kk > 0 ? 1u : accumulate;
+                            umma_bf16(tmem, dx + kk * 2, da + kk * 2, idesc0, more);
+                            if (kTwo) umma_bf16(tmem + 256, dx + kk * 2, da + 256 * 8 + kk * 2, idesc1, more);
+                        }
+                        accumulate = 1;
                     }
                     umma_commit(bar(T_EMPTY + s));
                 }
                 __syncwarp();
-                accumulate = 1;
+                accumulate = 1;  // (whichever thread is elected)
                 if (++s == ts.stages) {
                     s = 0;
                     parity ^= 1;
@@ -633,6 +651,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         const int wq = warp & 3, half = ((warp - 2) >> 2) & 1, set = (warp - 2) >> 3;
         const int c_first = ((warp - 2) >> 2) * 16, c_step = kTEpilogue / 8;  // inner sums of this warp: 16 columns at a time
         const int row = wq * 32 + lane;                    // this thread's TMEM lane
+        const bool works = wq * 32 < ts.rows;              // (others only take part in the barriers)
         const uint32_t t_lane = static_cast<uint32_t>(wq * 32) << 16;
         const float scale = p.scales ? __ldg(p.scales + tile.adapter) : 1.f;
         // (every MMA on the ring has completed by then, and with them its copies: its memory is free)
@@ -645,7 +664,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         float *const summed = reinterpret_cast<float *>(sg + ts.summed_at);
         float *const part = reinterpret_cast<float *>(sg + ts.part_at);
         if (ctas > 1) {
-            for (int c = c_first; ok && c < width; c += c_step) {
+            for (int c = c_first; ok && works && c < width; c += c_step) {
                 float v[16];
                 tmem_ld16_sync(tmem + t_lane + static_cast<uint32_t>(c), v);
                 float4 *const to = reinterpret_cast<float4 *>(part + row * pitch + c);
@@ -655,7 +674,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
             cluster_point();
             // the parts of this CTA's rows, summed; then every CTA's sums (both ways along the
             // rows: with each thread reading its own row of the others, 192 sums took 8 us, not 3.5)
-            const int vecs = width / 4, own0 = rank * ts.own_rows, own = min(ts.own_rows, kTRows - own0);
+            const int vecs = width / 4, own0 = rank * ts.own_rows, own = min(ts.own_rows, ts.rows - own0);
             for (int i = tid - 64; i < vecs * own; i += kTEpilogue) {
                 const int r = i / vecs, c = (i - r * vecs) * 4;
                 const uint32_t at = smem_u32(part + (own0 + r) * pitch + c);
@@ -665,28 +684,28 @@ __global__ void __launch_bounds__(kTThreads, 1)
                     if (o < ctas) v[o] = ld_cluster_f32x4(dsmem_addr(at, static_cast<uint32_t>(o)));
 #pragma unroll
                 for (int o = 0; o < kAMaxCluster; ++o)
-                    if (o < ctas) sum.x += v[o].x, sum.y += v[o].y, sum.z += v[o].z, sum.w += v[o].w;
+                    if (o < ctas) add_to(sum, v[o]);
                 *reinterpret_cast<float4 *>(summed + r * pitch + c) = sum;
             }
             cluster_point();
-            for (int i0 = tid - 64; i0 < vecs * kTRows; i0 += 4 * kTEpilogue) {
+            for (int i0 = tid - 64; i0 < vecs * ts.rows; i0 += 4 * kTEpilogue) {
                 float4 v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int i = i0 + k * kTEpilogue, r = i / vecs, c = (i - r * vecs) * 4, o = r / ts.own_rows;
-                    if (i < vecs * kTRows)
+                    if (i < vecs * ts.rows)
                         v[k] = ld_cluster_f32x4(dsmem_addr(smem_u32(summed + (r - o * ts.own_rows) * pitch + c),
                                                            static_cast<uint32_t>(o)));
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int i = i0 + k * kTEpilogue, r = i / vecs, c = (i - r * vecs) * 4;
-                    if (i < vecs * kTRows) *reinterpret_cast<float4 *>(part + r * pitch + c) = v[k];
+                    if (i < vecs * ts.rows) *reinterpret_cast<float4 *>(part + r * pitch + c) = v[k];
                 }
             }
             nbar_sync(1, kTEpilogue);
         }
-        for (int c = c_first; ok && c < width; c += c_step) {
+        for (int c = c_first; ok && works && c < width; c += c_step) {
             float v[16];
             if (ctas > 1) {
                 const float4 *const from = reinterpret_cast<const float4 *>(part + row * pitch + c);
@@ -716,7 +735,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
 
         // this warp's columns of a block: 64, a box of y, or 32, half a box
         const int groups = block / 64;
-        const uint32_t box = block == 128 ? static_cast<uint32_t>(half) * kTBoxBytes : 0u;
+        const uint32_t box = block == 128 ? static_cast<uint32_t>(half) * ts.x_bytes : 0u;
         const int first = block == 128 ? 0 : half * 4;  // 16-byte pieces of the box's 128-byte rows
         const int col = half * (block / 2);
         const float2 scale2 = make_float2(scale, scale);
@@ -732,6 +751,10 @@ __global__ void __launch_bounds__(kTThreads, 1)
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 if (g >= groups) break;
+                if (!works) {
+                    if (g == groups - 1 && lane == 0) mbar_arrive(bar(T_OUTEMPTY + buf));
+                    continue;
+                }
                 float v[32];
                 tmem_ld32_sync(outs + t_lane + static_cast<uint32_t>(buf * block + col + g * 32), v);
                 if (g == groups - 1) {
@@ -763,7 +786,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
             // a box that the tile or the slice ends in is stored by its warps, others by TMA
             const ColumnBlock cb = column_block(tp, rank + i * ctas);
             const int box_col = block == 128 ? col : 0;
-            if (tile.n < kTRows || box_col + 64 > cb.width) {
+            if (works && (tile.n < ts.rows || box_col + 64 > cb.width)) {
                 __syncwarp();
                 const int per_row = block == 128 ? 8 : 4;  // pieces of a row that this warp has
                 const int piece = lane & (per_row - 1), rows_at_once = 32 / per_row;
@@ -799,14 +822,16 @@ __global__ void __launch_bounds__(kTThreads, 1)
 }
 
 // how tiles of this call lie for clusters of `ctas` CTAs; false: not on this kernel
-bool tile_shape(const AdapterParams &p, int ctas, TileShape *s) {
+bool tile_shape(const AdapterParams &p, int ctas, TileShape *s, int rows) {
     *s = {};
     s->ctas = ctas;
-    s->own_rows = (kTRows + ctas - 1) / ctas;
+    s->rows = rows;
+    s->own_rows = (rows + ctas - 1) / ctas;
+    s->x_bytes = static_cast<uint32_t>(rows) * 128;
     s->rank16 = (p.rank + 15) / 16 * 16;
     s->wide16 = (p.n_slices * s->rank16 + 31) / 32 * 32;
     s->a_bytes = static_cast<uint32_t>(p.n_slices * s->rank16) * 128;
-    const uint32_t stage = kTXBytes + s->a_bytes;
+    const uint32_t stage = s->x_bytes + s->a_bytes;
     // blocks of 128 columns where they fit, else of 64
     for (s->block_log = 7; s->block_log >= 6; --s->block_log) {
         const int block = 1 << s->block_log;
@@ -816,13 +841,15 @@ bool tile_shape(const AdapterParams &p, int ctas, TileShape *s) {
         s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
         const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
         const uint32_t room = (kTSmem - rest) / 1024 * 1024;
-        s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / stage));
-        const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * kTBoxBytes;
+        // (two of them in a stage where three such fit: 2048 rows, 4096 x 6144, rank 16 20.4 us, 19.9)
+        s->subs = room / (2 * stage) >= 3 ? 2 : 1;
+        s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / (s->subs * stage)));
+        const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * s->x_bytes;
         const uint32_t summed = ctas > 1 ? sums_bytes(s->wide16, s->own_rows) : 0;
-        const uint32_t part = ctas > 1 ? sums_bytes(s->wide16, kTRows) : 0;
+        const uint32_t part = ctas > 1 ? sums_bytes(s->wide16, rows) : 0;
         if (s->stages < 2 || summed + part > room || summed + 2 * y_bytes > room) continue;
         s->y_stages = std::min<int>(kTYStages, static_cast<int>((room - summed) / y_bytes));
-        s->b_at = std::max(static_cast<uint32_t>(s->stages) * stage,
+        s->b_at = std::max(static_cast<uint32_t>(s->stages * s->subs) * stage,
                            std::max(static_cast<uint32_t>(s->y_stages) * y_bytes, part) + summed);
         s->b_at = (s->b_at + 1023) / 1024 * 1024;
         s->summed_at = s->b_at - summed;
@@ -881,15 +908,15 @@ void plan_adapter(int32_t n_seqs, const int32_t *q_lens, const int32_t *adapters
 
 namespace {
 
-// Clusters of 2 .. kAMaxCluster CTAs of a kernel (of a whole SM each) that the current
-// device holds at a time; cached per device.
-template <auto kernel>
-cudaError_t clusters_at_a_time(int threads, int smem, int32_t (&clusters)[kAMaxCluster + 1]) {
-    static std::atomic<int32_t> known[64][kAMaxCluster + 1] = {};  // + 1; 0: not asked
+// Clusters of 2 .. kMost CTAs of a kernel (of a whole SM each) that the current device
+// holds at a time; cached per device.
+template <auto kernel, int kMost>
+cudaError_t clusters_at_a_time(int threads, int smem, int32_t (&clusters)[kMost + 1]) {
+    static std::atomic<int32_t> known[64][kMost + 1] = {};  // + 1; 0: not asked
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    for (int c = 2; c <= kAMaxCluster; ++c) {
+    for (int c = 2; c <= kMost; ++c) {
         int32_t n = dev >= 0 && dev < 64 ? known[dev][c].load(std::memory_order_acquire) : 0;
         if (n == 0) {
             cudaLaunchConfig_t cfg = {};
@@ -903,8 +930,13 @@ cudaError_t clusters_at_a_time(int threads, int smem, int32_t (&clusters)[kAMaxC
             cfg.attrs = &a;
             cfg.numAttrs = 1;
             int most = 0;
-            e = cudaOccupancyMaxActiveClusters(&most, kernel, &cfg);
-            if (e != cudaSuccess) return e;
+            e = c == 9 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
+            if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&most, kernel, &cfg);
+            if (e != cudaSuccess && c <= 8) return e;
+            if (e != cudaSuccess) {
+                cudaGetLastError();
+                most = 0;  // (none of that size)
+            }
             n = most + 1;
             if (dev >= 0 && dev < 64) known[dev][c].store(n, std::memory_order_release);
         }
@@ -913,7 +945,7 @@ cudaError_t clusters_at_a_time(int threads, int smem, int32_t (&clusters)[kAMaxC
     return cudaSuccess;
 }
 
-constexpr int kUnitSmem = static_cast<int>(unit_smem(kAMaxSlices * kAMaxRank, kAMaxSlices * kAMaxRank / 16));
+constexpr int kUnitSmem = static_cast<int>(unit_smem(kAMaxSlices * kAMaxRank, kAChunk, kAMaxSlices * kAMaxRank / 16));
 static_assert(kUnitSmem <= static_cast<int>(kTSmem), "shared memory of a CTA");
 
 template <int kUnits, int kRows>
@@ -925,7 +957,7 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     if (e != cudaSuccess) return e;
     UnitParams<kUnits, kRows> u;
     u.p = p;
-    int n = 0, listed = 0;
+    int n = 0, listed = 0, rows = 0;
     for (; next < plan.units.size() && n < kUnits; ++next, ++n) {
         AdapterUnit unit = plan.units[next];
         if (unit.listed) {
@@ -934,25 +966,38 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
             unit.first = listed;
             listed += unit.n;
         }
+        if (unit.adapter >= 0) rows = std::max(rows, unit.n);
         u.units[n] = unit;
     }
     for (int j = 0, at = 0; j <= kAMaxSlices; ++j) {
         u.group_at[j] = at;
         if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + 31) / 32;
     }
-    // as many CTAs a unit as run at a time, 128 values of K each at least
-    int32_t clusters[kAMaxCluster + 1] = {};
-    e = clusters_at_a_time<adapter_units_kernel<kUnits, kRows>>(kAThreads, kUnitSmem, clusters);
+    int32_t clusters[kAUnitCluster + 1] = {};
+    e = clusters_at_a_time<adapter_units_kernel<kUnits, kRows>, kAUnitCluster>(kAThreads, kUnitSmem, clusters);
     if (e != cudaSuccess) return e;
+    // As many CTAs a unit as run at a time, up to 8, 128 values of K each at least; and 16
+    // where a warp then has fewer blocks one after another, of few enough sums that every CTA
+    // reads all others' (a row, 4096 x 6144: rank 16 4.5 us, of 8 5.3, rank 64 6.7 and 9.4; 8
+    // rows, 2048 x 2560, rank 64, of 16 10.6, 8.0).
     int c = kAMaxCluster;
     while (c > 1 && (n > clusters[c] || p.hidden < c * 128)) --c;
+    auto blocks = [&](int ctas) {
+        auto parts = [](int all, int of) { return (all + of - 1) / of; };
+        return parts(parts((p.hidden + 31) / 32, ctas) << unit_parts_log(wide), kAWarps) +
+               parts(u.group_at[kAMaxSlices], ctas * kAWarps);
+    };
+    constexpr int kFewSums = 768;
+    if (n <= clusters[kAUnitCluster] && p.hidden >= kAUnitCluster * 128 && rows * wide <= kFewSums &&
+        blocks(kAUnitCluster) < blocks(c))
+        c = kAUnitCluster;
     // (beside tiles, on the SMs that their clusters leave: 2k step of 17 tiles and 9 units,
     // clusters of 4 18.3 us, of 8, which find no room, 24.2, of 2 19.8)
     if (beside_tiles) c = std::min(c, 4);
     u.ctas = c;
     u.beside_tiles = beside_tiles ? 1 : 0;
     PdlLaunch l(dim3(static_cast<unsigned>(n * c)), dim3(kAThreads),
-                unit_smem(wide, p.n_slices * ((p.rank + 15) / 16)), st);
+                unit_smem(wide, unit_part(wide), p.n_slices * ((p.rank + 15) / 16)), st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
         attrs[1].id = cudaLaunchAttributeClusterDimension;
@@ -971,36 +1016,62 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
     cudaError_t e = ensure_smem_limit(adapter_tiles_kernel, static_cast<int>(kTSmem), smem_set);
     if (e != cudaSuccess) return e;
     int32_t clusters[kAMaxCluster + 1] = {};
-    e = clusters_at_a_time<adapter_tiles_kernel>(kTThreads, static_cast<int>(kTSmem), clusters);
+    e = clusters_at_a_time<adapter_tiles_kernel, kAMaxCluster>(kTThreads, static_cast<int>(kTSmem), clusters);
     if (e != cudaSuccess) return e;
     const auto tp = std::make_unique<TileParams>();
     tp->p = p;
     tp->err = err;
-    for (size_t next = 0; next < plan.tiles.size();) {
-        const int n = static_cast<int>(std::min<size_t>(kMaxTiles, plan.tiles.size() - next));
-        std::copy_n(plan.tiles.begin() + static_cast<std::ptrdiff_t>(next), n, tp->tiles);
-        next += static_cast<size_t>(n);
-        const int k_blocks = (p.hidden + kTK - 1) / kTK;
-        // as many CTAs a tile as run at a time (2k step of 17 tiles, hidden 11008: 4 CTAs 19.8
-        // us; 8, whose clusters take two rounds, 26.0)
+    // As many CTAs a tile as run at a time (2k step of 17 tiles, hidden 11008: 4 CTAs 19.8 us;
+    // 8, whose clusters take two rounds, 26.0).
+    clusters[1] = device_sm_count();
+    const int k_blocks = (p.hidden + kTK - 1) / kTK;
+    auto ctas_of = [&](int64_t n, int rows) {
         int c = kAMaxCluster;
-        while (c > 1 && (n > clusters[c] || c > k_blocks || !tile_shape(p, c, &tp->s))) --c;
-        if (!tile_shape(p, c, &tp->s)) return cudaErrorInvalidValue;  // (the plan asked before)
+        while (c > 1 && (n > clusters[c] || c > k_blocks || !tile_shape(p, c, &tp->s, rows))) --c;
+        return c;
+    };
+    // Tiles of 64 rows where all of them run at a time and a CTA has a tenth less to do, by
+    // what it moves (a block of columns takes no less, its epilogue's warps being half
+    // idle) and the joining of the parts, a sum as much as 5 values moved: 768 rows, 4096
+    // x 6144, rank 64 18.8 us, of 128 rows 23.3; 1024 rows of rank 16 16.5 and 15.4.
+    auto work = [&](int rows) {
+        int64_t n = 0;
+        for (const AdapterTile &tile : plan.tiles) n += (tile.n + rows - 1) / rows;
+        const int c = ctas_of(n, rows);
+        if (n > clusters[c] || !tile_shape(p, c, &tp->s, rows)) return std::numeric_limits<double>::infinity();
+        return (static_cast<double>(p.hidden) * (rows + tp->s.wide16) +
+                static_cast<double>(p.cols) * (2 * kTRows + tp->s.rank16)) / c +
+               (c > 1 ? 5.0 * rows * tp->s.wide16 : 0.0);
+    };
+    const int rows_of_tile = work(kTRows / 2) < 0.9 * work(kTRows) ? kTRows / 2 : kTRows;
+    std::vector<AdapterTile> parts;
+    if (rows_of_tile < kTRows)
+        for (const AdapterTile &tile : plan.tiles)
+            for (int32_t r = 0; r < tile.n; r += rows_of_tile)
+                parts.push_back({tile.first + r, tile.adapter, std::min(rows_of_tile, tile.n - r)});
+    const std::vector<AdapterTile> &tiles = rows_of_tile < kTRows ? parts : plan.tiles;
+    for (size_t next = 0; next < tiles.size();) {
+        const int n = static_cast<int>(std::min<size_t>(kMaxTiles, tiles.size() - next));
+        std::copy_n(tiles.begin() + static_cast<std::ptrdiff_t>(next), n, tp->tiles);
+        next += static_cast<size_t>(n);
+        const int c = ctas_of(n, rows_of_tile);
+        if (!tile_shape(p, c, &tp->s, rows_of_tile)) return cudaErrorInvalidValue;  // (the plan asked before)
         for (int j = 0, at = 0; j <= kAMaxSlices; ++j) {
             tp->block_at[j] = at;
             if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + (1 << tp->s.block_log) - 1) >> tp->s.block_log;
         }
         CUtensorMap tm_x, tm_a, tm_b, tm_y, tm_out;
+        const uint32_t box_rows = static_cast<uint32_t>(rows_of_tile);
         const uint64_t rows = static_cast<uint64_t>(n_rows), cols = static_cast<uint64_t>(p.cols);
         if (!encode_bf16_rows(&tm_x, p.x, static_cast<uint64_t>(p.hidden), rows, static_cast<uint64_t>(p.x_stride), kTK,
-                              kTRows) ||
+                              box_rows) ||
             !encode_bf16_3d(&tm_a, p.a, static_cast<uint64_t>(p.hidden), static_cast<uint64_t>(p.rank),
                             static_cast<uint64_t>(n_adapters) * p.n_slices, kTK, static_cast<uint32_t>(tp->s.rank16),
                             static_cast<uint32_t>(p.n_slices)) ||
             !encode_bf16_2d(&tm_b, p.b, static_cast<uint64_t>(p.rank), static_cast<uint64_t>(n_adapters) * cols, 64,
                             1u << tp->s.block_log) ||
-            !encode_bf16_rows(&tm_y, p.y, cols, rows, static_cast<uint64_t>(p.y_stride), 64, kTRows) ||
-            !encode_bf16_rows(&tm_out, p.out, cols, rows, static_cast<uint64_t>(p.out_stride), 64, kTRows))
+            !encode_bf16_rows(&tm_y, p.y, cols, rows, static_cast<uint64_t>(p.y_stride), 64, box_rows) ||
+            !encode_bf16_rows(&tm_out, p.out, cols, rows, static_cast<uint64_t>(p.out_stride), 64, box_rows))
             return cudaErrorUnknown;
         PdlLaunch l(dim3(static_cast<unsigned>(n) * static_cast<unsigned>(c)), dim3(kTThreads), tp->s.smem, st);
         cudaLaunchAttribute attrs[2] = {l.attr[0], {}};

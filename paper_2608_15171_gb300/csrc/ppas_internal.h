@@ -442,8 +442,6 @@ constexpr int kTMaxStages = 6;    // of the ring of x and A tiles
 constexpr int kTBStages = 3;
 constexpr int kTYStages = 4;
 constexpr uint32_t kTSmem = 232448;  // shared memory of a CTA
-constexpr uint32_t kTXBytes = kTRows * kTK * 2;
-constexpr uint32_t kTBoxBytes = kTRows * 128;  // 64 columns of y
 constexpr uint32_t kTBarBytes = 320;
 // how a tile lies in shared memory and TMEM
 struct TileShape {
@@ -451,9 +449,12 @@ struct TileShape {
     int32_t wide16;    // TMEM columns for all slices' inner sums, rounded up to 32
     int32_t block_log; // log2 of the columns of y worked at a time: 128, or 64
     int32_t ctas;      // of a cluster
+    int32_t rows;      // of a tile: kTRows, or fewer, a multiple of 32
     int32_t own_rows;  // of the sums that each of them joins
     int32_t stages;    // of the ring of x and A
-    uint32_t a_bytes;  // of a stage: the slices' A tiles
+    int32_t subs;      // blocks of K of a stage
+    uint32_t x_bytes;  // of each: x, as 64 columns of y
+    uint32_t a_bytes;  // and the slices' A tiles
     uint32_t b_bytes;  // of a B tile: block rows, 128 bytes for each 64 of rank
     // y's ring lies where the ring of x and A was, and in a cluster, from stage y_free on,
     // where the parts of the sums are until they are an operand; the sums that other
@@ -467,7 +468,7 @@ __host__ __device__ constexpr uint32_t sums_bytes(int wide16, int rows) {
     return static_cast<uint32_t>(rows * (wide16 + 4) * 4);
 }
 // the shape for clusters of `ctas` CTAs; false: this call's rows are not done in tiles
-bool tile_shape(const AdapterParams &p, int ctas, TileShape *s);
+bool tile_shape(const AdapterParams &p, int ctas, TileShape *s, int rows = kTRows);
 
 // launch configuration with programmatic stream serialization: the kernel
 // may launch before its predecessor in the stream completes and orders its

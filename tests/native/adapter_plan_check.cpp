@@ -49,23 +49,26 @@ static std::string shapes() {
     int refused = 0;
     for (int slices = 1; slices <= kAMaxSlices; ++slices)
         for (int rank = 8; rank <= kAMaxRank; rank += 8)
-            for (int ctas = 1; ctas <= kAMaxCluster; ++ctas) {
+            for (int ctas = 1, rows = kTRows; ctas <= kAMaxCluster; rows = rows > 32 ? rows / 2 : (++ctas, kTRows)) {
                 AdapterParams p = {};
                 p.rank = rank;
                 p.n_slices = slices;
                 TileShape s;
-                if (!tile_shape(p, ctas, &s)) {
+                if (!tile_shape(p, ctas, &s, rows)) {
                     if (ctas == 1 && (slices < 4 || rank <= 96)) return "refused alone";
                     ++refused;
                     continue;
                 }
-                const uint32_t block = 1u << s.block_log, y = block / 64 * kTBoxBytes, stage = kTXBytes + s.a_bytes;
-                const uint32_t sums = s.wide16 + 4, part = kTRows * sums * 4, summed = s.own_rows * sums * 4;
+                const uint32_t block = 1u << s.block_log, y = block / 64 * rows * 128, stage = s.subs * (rows * 128 + s.a_bytes);
+                const uint32_t sums = s.wide16 + 4, part = rows * sums * 4, summed = s.own_rows * sums * 4;
                 if (s.rank16 < rank || s.rank16 % 16 || s.wide16 < slices * s.rank16 || s.wide16 % 32) return "widths";
-                if (s.own_rows * ctas < kTRows || (s.own_rows - 1) * ctas >= kTRows) return "rows of the sums";
+                if (s.rows != rows || s.own_rows * ctas < rows || (s.own_rows - 1) * ctas >= rows) return "rows of the sums";
                 if (s.tmem < s.wide16 + 2 * static_cast<int>(block) || s.tmem > 512 || (s.tmem & (s.tmem - 1))) return "tmem";
                 if (s.stages < 2 || s.stages > kTMaxStages || s.y_stages < 2 || s.y_stages > kTYStages) return "stages";
                 if (stage % 1024 || y % 1024 || s.b_bytes % 1024 || s.b_at % 1024 || s.bars_at % 8) return "alignment";
+                if (s.x_bytes != static_cast<uint32_t>(rows * 128)) return "x";
+                // the products read 128 rows of x's place, whatever they hold
+                if (s.subs < 1 || s.stages * stage - (rows * 128 + s.a_bytes) + kTRows * 128 > s.bars_at) return "x past its end";
                 if (s.a_bytes != static_cast<uint32_t>(slices * s.rank16 * 128)) return "A";
                 if (s.b_bytes != block * ((rank + 63) / 64) * 128) return "B";
                 // the rings and the sums end before B, B before the barriers, all of it within the CTA's memory

@@ -333,3 +333,32 @@ def test_two_streams_at_once(ppas):
     torch.cuda.synchronize()
     a.check()
     b.check()
+
+
+# tiles of 64 rows: few enough rows that all of them run at a time, inner sums that make up for it
+@pytest.mark.parametrize("rank", [8, 16, 40, 64, 128])
+@pytest.mark.parametrize("hidden,slices", [(2048, [1024, 256, 256]), (1000, [264, 72]), (520, [200])])
+def test_half_tiles(ppas, rank, hidden, slices):
+    for lens, ids in (([300, 100, 77, 129, 1], [0, 1, 0, 2, -1]), ([64, 65, 63, 200, 191], [0, 1, 2, 0, 3]), ([768], [0])):
+        c = Call(lens, ids, hidden, slices, rank, seed=rank)
+        ppas.ppas_adapter_add(**c.args())
+        c.check()
+
+
+def test_half_tiles_in_place_and_strides(ppas):
+    c = Call([400, 333, 48], [0, 1, 0], 2048, [1024, 264, 256], 64, gap=24, seed=5, scales=False)
+    h = c.host()
+    c.out.copy_(c.y)
+    ppas.ppas_adapter_add(**c.args(y=c.out, y_stride=c.out.stride(0)))
+    c.check(h)
+
+
+# few rows of wide inner sums or many columns: a row's cluster has 16 CTAs
+@pytest.mark.parametrize("hidden,slices,rank", [(4096, [64, 8, 24], 64), (4104, [2048, 2048, 2056], 16), (11008, [264], 40),
+                                                (2048, [4096, 1000], 128), (2056, [8] * 4, 128)])
+@pytest.mark.parametrize("ids", [[0], [-1], [0, 0], [0, 1, 0, 2], [0] * 4, [4, -1, 2, 3, 1], list(range(7)), list(range(12)),
+                                 [0] * 9])
+def test_long_rows_few_at_a_time(ppas, hidden, slices, rank, ids):
+    c = Call([1] * len(ids), ids, hidden, slices, rank, seed=len(ids))
+    ppas.ppas_adapter_add(**c.args())
+    c.check()
