@@ -404,6 +404,7 @@ __device__ __forceinline__ void stores_wait() { asm volatile("cp.async.bulk.wait
 
 }  // namespace
 
+template <int kRows>
 __global__ void __launch_bounds__(kTThreads, 1)
     adapter_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a,
                          const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_y,
@@ -411,6 +412,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     const AdapterParams &p = tp.p;
     const TileShape &ts = tp.s;
+    constexpr uint32_t kXBytes = kRows * 128;
     const uint32_t raw_s = smem_u32(smem_raw);
     const uint32_t sb = (raw_s + 1023u) & ~1023u;
     uint8_t *const sg = smem_raw + (sb - raw_s);
@@ -461,9 +463,9 @@ __global__ void __launch_bounds__(kTThreads, 1)
     const int k_blocks = (p.hidden + kTK - 1) / kTK;
     const int kb0 = k_blocks * rank / ctas, kb1 = k_blocks * (rank + 1) / ctas;
     const int mine = (tp.block_at[kAMaxSlices] - rank + ctas - 1) / ctas;
-    const uint32_t sub_bytes = ts.x_bytes + ts.a_bytes, stage_bytes = static_cast<uint32_t>(ts.subs) * sub_bytes;
+    const uint32_t sub_bytes = kXBytes + ts.a_bytes, stage_bytes = static_cast<uint32_t>(ts.subs) * sub_bytes;
     const int block = 1 << ts.block_log, boxes = block / 64;
-    const uint32_t y_bytes = static_cast<uint32_t>(boxes) * ts.x_bytes;
+    const uint32_t y_bytes = static_cast<uint32_t>(boxes) * kXBytes;
     // (every thread, on every path: the same number of cluster barriers)
     auto cluster_point = [&]() {
         if (ctas > 1) {
@@ -487,7 +489,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 mbar_expect_tx(bar(T_FULL + s), static_cast<uint32_t>(subs) * sub_bytes);
                 for (int j = 0; j < subs; ++j, dst += sub_bytes) {
                     tma_load_2d(dst, &tm_x, (kb + j) * kTK, tile.first, bar(T_FULL + s));
-                    tma_load_3d(dst + ts.x_bytes, &tm_a, (kb + j) * kTK, 0, tile.adapter * p.n_slices, bar(T_FULL + s));
+                    tma_load_3d(dst + kXBytes, &tm_a, (kb + j) * kTK, 0, tile.adapter * p.n_slices, bar(T_FULL + s));
                 }
             }
             __syncwarp();
@@ -516,7 +518,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 const uint32_t dst = sb + static_cast<uint32_t>(s) * y_bytes;
                 mbar_expect_tx(bar(T_YFULL + s), y_bytes);
                 for (int h = 0; h < boxes; ++h)
-                    tma_load_2d(dst + static_cast<uint32_t>(h) * ts.x_bytes, &tm_y, cb.c0 + h * 64, tile.first,
+                    tma_load_2d(dst + static_cast<uint32_t>(h) * kXBytes, &tm_y, cb.c0 + h * 64, tile.first,
                                 bar(T_YFULL + s));
             }
             __syncwarp();
@@ -539,10 +541,10 @@ __global__ void __launch_bounds__(kTThreads, 1)
             const ColumnBlock cb = column_block(tp, rank + i * ctas);
             if (lane == 0) {
                 const uint32_t from = sb + static_cast<uint32_t>(s) * y_bytes;
-                if (tile.n == ts.rows)
+                if (tile.n == kRows)
                     for (int h = 0; h < boxes; ++h)
                         if (h * 64 + 64 <= cb.width)
-                            tma_store_2d(&tm_out, from + static_cast<uint32_t>(h) * ts.x_bytes, cb.c0 + h * 64, tile.first);
+                            tma_store_2d(&tm_out, from + static_cast<uint32_t>(h) * kXBytes, cb.c0 + h * 64, tile.first);
                 stores_commit();
             }
             __syncwarp();
@@ -578,23 +580,25 @@ __global__ void __launch_bounds__(kTThreads, 1)
             constexpr bool kTwo = decltype(parts)::value == 2;
             const uint32_t idesc0 = idesc16 + (static_cast<uint32_t>(((kTwo ? 256 : width) - 16) >> 3) << 17);
             const uint32_t idesc1 = idesc16 + (static_cast<uint32_t>((width - 256 - 16) >> 3) << 17);
-            const uint64_t dx0 = smem_desc_sw128(sb, 16, 1024), da0 = smem_desc_sw128(sb + ts.x_bytes, 16, 1024);
+            const uint64_t dx0 = smem_desc_sw128(sb, 16, 1024), da0 = smem_desc_sw128(sb + kXBytes, 16, 1024);
             uint32_t accumulate = 0;
             for (int q = kb1 - kb0, s = 0, parity = 0; q > 0; q -= ts.subs) {
                 if (!mbar_wait_warp(bar(T_FULL + s), parity, tp.err)) return false;
                 tc_fence_after();
                 const uint64_t at = (static_cast<uint32_t>(s) * stage_bytes) >> 4;
                 if (elect_one()) {
-                    uint64_t dx = dx0 + at, da = da0 + at;
-#pragma unroll 1
-                    for (int j = min(ts.subs, q); j > 0; --j, dx += sub_bytes >> 4, da += sub_bytes >> 4) {
+                    auto block_of_k = [&](uint64_t dx, uint64_t da) {
 #pragma unroll
                         for (int kk = 0; kk < kTK / 16; ++kk) {
                             const uint32_t more = kk > 0 ? 1u : accumulate;
                             umma_bf16(tmem, dx + kk * 2, da + kk * 2, idesc0, more);
                             if (kTwo) umma_bf16(tmem + 256, dx + kk * 2, da + 256 * 8 + kk * 2, idesc1, more);
                         }
+                    };
+                    block_of_k(dx0 + at, da0 + at);
+                    if (!kTwo && ts.subs == 2 && q > 1) {
                         accumulate = 1;
+                        block_of_k(dx0 + at + (sub_bytes >> 4), da0 + at + (sub_bytes >> 4));
                     }
                     umma_commit(bar(T_EMPTY + s));
                 }
@@ -651,7 +655,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
         const int wq = warp & 3, half = ((warp - 2) >> 2) & 1, set = (warp - 2) >> 3;
         const int c_first = ((warp - 2) >> 2) * 16, c_step = kTEpilogue / 8;  // inner sums of this warp: 16 columns at a time
         const int row = wq * 32 + lane;                    // this thread's TMEM lane
-        const bool works = wq * 32 < ts.rows;              // (others only take part in the barriers)
+        const bool works = kRows == kTRows || wq * 32 < kRows;  // (others only take part in the barriers)
         const uint32_t t_lane = static_cast<uint32_t>(wq * 32) << 16;
         const float scale = p.scales ? __ldg(p.scales + tile.adapter) : 1.f;
         // (every MMA on the ring has completed by then, and with them its copies: its memory is free)
@@ -674,7 +678,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
             cluster_point();
             // the parts of this CTA's rows, summed; then every CTA's sums (both ways along the
             // rows: with each thread reading its own row of the others, 192 sums took 8 us, not 3.5)
-            const int vecs = width / 4, own0 = rank * ts.own_rows, own = min(ts.own_rows, ts.rows - own0);
+            const int vecs = width / 4, own0 = rank * ts.own_rows, own = min(ts.own_rows, kRows - own0);
             for (int i = tid - 64; i < vecs * own; i += kTEpilogue) {
                 const int r = i / vecs, c = (i - r * vecs) * 4;
                 const uint32_t at = smem_u32(part + (own0 + r) * pitch + c);
@@ -688,19 +692,19 @@ __global__ void __launch_bounds__(kTThreads, 1)
                 *reinterpret_cast<float4 *>(summed + r * pitch + c) = sum;
             }
             cluster_point();
-            for (int i0 = tid - 64; i0 < vecs * ts.rows; i0 += 4 * kTEpilogue) {
+            for (int i0 = tid - 64; i0 < vecs * kRows; i0 += 4 * kTEpilogue) {
                 float4 v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int i = i0 + k * kTEpilogue, r = i / vecs, c = (i - r * vecs) * 4, o = r / ts.own_rows;
-                    if (i < vecs * ts.rows)
+                    if (i < vecs * kRows)
                         v[k] = ld_cluster_f32x4(dsmem_addr(smem_u32(summed + (r - o * ts.own_rows) * pitch + c),
                                                            static_cast<uint32_t>(o)));
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int i = i0 + k * kTEpilogue, r = i / vecs, c = (i - r * vecs) * 4;
-                    if (i < vecs * ts.rows) *reinterpret_cast<float4 *>(part + r * pitch + c) = v[k];
+                    if (i < vecs * kRows) *reinterpret_cast<float4 *>(part + r * pitch + c) = v[k];
                 }
             }
             nbar_sync(1, kTEpilogue);
@@ -735,7 +739,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
 
         // this warp's columns of a block: 64, a box of y, or 32, half a box
         const int groups = block / 64;
-        const uint32_t box = block == 128 ? static_cast<uint32_t>(half) * ts.x_bytes : 0u;
+        const uint32_t box = block == 128 ? static_cast<uint32_t>(half) * kXBytes : 0u;
         const int first = block == 128 ? 0 : half * 4;  // 16-byte pieces of the box's 128-byte rows
         const int col = half * (block / 2);
         const float2 scale2 = make_float2(scale, scale);
@@ -786,7 +790,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
             // a box that the tile or the slice ends in is stored by its warps, others by TMA
             const ColumnBlock cb = column_block(tp, rank + i * ctas);
             const int box_col = block == 128 ? col : 0;
-            if (works && (tile.n < ts.rows || box_col + 64 > cb.width)) {
+            if (works && (tile.n < kRows || box_col + 64 > cb.width)) {
                 __syncwarp();
                 const int per_row = block == 128 ? 8 : 4;  // pieces of a row that this warp has
                 const int piece = lane & (per_row - 1), rows_at_once = 32 / per_row;
@@ -842,7 +846,7 @@ bool tile_shape(const AdapterParams &p, int ctas, TileShape *s, int rows) {
         const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
         const uint32_t room = (kTSmem - rest) / 1024 * 1024;
         // (two of them in a stage where three such fit: 2048 rows, 4096 x 6144, rank 16 20.4 us, 19.9)
-        s->subs = room / (2 * stage) >= 3 ? 2 : 1;
+        s->subs = s->a_bytes <= 256 * 128 && room / (2 * stage) >= 3 ? 2 : 1;
         s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / (s->subs * stage)));
         const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * s->x_bytes;
         const uint32_t summed = ctas > 1 ? sums_bytes(s->wide16, s->own_rows) : 0;
@@ -1012,11 +1016,13 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
 
 cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_t n_rows, int32_t n_adapters,
                          int32_t *err, cudaStream_t st) {
-    static std::atomic<uint64_t> smem_set{0};
-    cudaError_t e = ensure_smem_limit(adapter_tiles_kernel, static_cast<int>(kTSmem), smem_set);
+    static std::atomic<uint64_t> smem_set{0}, smem_set_half{0};
+    cudaError_t e = ensure_smem_limit(adapter_tiles_kernel<kTRows>, static_cast<int>(kTSmem), smem_set);
+    if (e == cudaSuccess)
+        e = ensure_smem_limit(adapter_tiles_kernel<kTRows / 2>, static_cast<int>(kTSmem), smem_set_half);
     if (e != cudaSuccess) return e;
     int32_t clusters[kAMaxCluster + 1] = {};
-    e = clusters_at_a_time<adapter_tiles_kernel, kAMaxCluster>(kTThreads, static_cast<int>(kTSmem), clusters);
+    e = clusters_at_a_time<adapter_tiles_kernel<kTRows>, kAMaxCluster>(kTThreads, static_cast<int>(kTSmem), clusters);
     if (e != cudaSuccess) return e;
     const auto tp = std::make_unique<TileParams>();
     tp->p = p;
@@ -1083,7 +1089,8 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
             l.cfg.attrs = attrs;
             l.cfg.numAttrs = 2;
         }
-        e = cudaLaunchKernelEx(&l.cfg, adapter_tiles_kernel, tm_x, tm_a, tm_b, tm_y, tm_out, *tp);
+        const auto kernel = rows_of_tile == kTRows ? adapter_tiles_kernel<kTRows> : adapter_tiles_kernel<kTRows / 2>;
+        e = cudaLaunchKernelEx(&l.cfg, kernel, tm_x, tm_a, tm_b, tm_y, tm_out, *tp);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
