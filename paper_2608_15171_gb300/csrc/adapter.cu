@@ -11,10 +11,12 @@
 // order as long as both operands agree: a lane takes 8 neighbouring values of K with
 // one 16-byte load for two MMAs, so the operands go from global memory to registers.)
 // s enters the second product as two bf16 numbers, a value and what its rounding left,
-// so that it counts to 2^-17 of itself.  A row: 2048 x 2560 of rank 16 4.5 us, a chain of
-// loads, a cluster barrier, loads and stores; 64 rows of 32 adapters, 4096 x 6144, rank 32 13.5
-// (2.8 TB/s of weights, in clusters of 4 on 128 SMs); 128 rows of 72 adapters of rank 64
-// 38.8 (4.7 TB/s).
+// so that it counts to 2^-17 of itself.  A row: 2048 x 2560 of rank 16 4.3 us, a chain of
+// loads, a cluster barrier, loads and stores; 64 rows of 32 adapters, 4096 x 6144, rank 32 13.0
+// (2.9 TB/s of weights, in clusters of 3 and 4); 128 rows of 72 adapters of rank 64 38.0
+// (4.8 TB/s).  (B copied to shared memory while the inner sums are made, by bulk copies: 4.9
+// and 15.3 us, 48.5.  One warp's inner sums 96 after another, not parted among warps: 512 rows
+// of one adapter of rank 64 20.8 us, 17.6 so.)
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -36,8 +38,8 @@ constexpr int kAChunk = 96;  // inner sums of a warp at most: its loads of 12 x 
 constexpr int kAAhead = 4;   // of the rank in B, 16 times this are loaded ahead
 constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make tiles,
 // and of all such runs together (below, units of 16 rows are done first: 512 rows, 2048 x
-// 2560, rank 16 7.1 us, tiles 10.0; 4096 x 6144, rank 64 21.7, 22.3; past it 1024 rows 16.9,
-// 15.3 and 37.6, 24.9)
+// 2560, rank 16 6.5 us, tiles 9.5; 4096 x 6144, rank 16 8.6, 12.6, rank 64 17.7, 17.9; past
+// it 768 rows 15.1, 13.2 and 30.9, 18.7)
 constexpr int32_t kATileTotal = 513;
 constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space)
 
