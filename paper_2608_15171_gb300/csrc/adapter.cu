@@ -13,7 +13,7 @@
 // s enters the second product as two bf16 numbers, a value and what its rounding left,
 // so that it counts to 2^-17 of itself.  A row: 2048 x 2560 of rank 16 4.3 us, a chain of
 // loads, a cluster barrier, loads and stores; 64 rows of 32 adapters, 4096 x 6144, rank 32 13.0
-// (2.9 TB/s of weights, in clusters of 3 and 4); 128 rows of 72 adapters of rank 64 38.0
+// (2.9 TB/s of weights, in clusters of 4); 128 rows of 72 adapters of rank 64 38.0
 // (4.8 TB/s).  (B copied to shared memory while the inner sums are made, by bulk copies: 4.9
 // and 15.3 us, 48.5.  One warp's inner sums 96 after another, not parted among warps: 512 rows
 // of one adapter of rank 64 20.8 us, 17.6 so.)
@@ -333,8 +333,8 @@ __global__ void __launch_bounds__(kAThreads, 1)
 //   warps 2-17  inner sums, and y + scale s B^T in shared memory: a thread has a row (its
 //               TMEM lane); 8 warps have the even blocks of columns, 8 the odd ones, two
 //               of them 32 rows, half the columns each
-// 16384 rows, 4096 x 6144, rank 64: 98.3 us (544 MB: 5.5 TB/s, 0.81 of the copy's rate; the
-// tensor pipe is 22 % busy); 2048 x 2560, rank 16 42.9 us (5.5 TB/s).  HBM is what bounds
+// 16384 rows, 4096 x 6144, rank 64: 99.2 us (544 MB: 5.5 TB/s, 0.81 of the copy's rate; the
+// tensor pipe is 22 % busy); 2048 x 2560, rank 16 42.6 us (5.5 TB/s).  HBM is what bounds
 // it, but for the turn from the first product to the second, in which a CTA, alone on
 // its SM, neither reads nor writes.  (With y and out moved by the epilogue's threads,
 // through a transposition in shared memory, a block took 3000 cycles and the call 176 us.)
