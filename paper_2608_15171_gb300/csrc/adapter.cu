@@ -41,7 +41,8 @@ constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another t
 // 2560, rank 16 6.5 us, tiles 9.5; 4096 x 6144, rank 16 8.6, 12.6, rank 64 17.7, 17.9; past
 // it 768 rows 15.1, 13.2 and 30.9, 18.7)
 constexpr int32_t kATileTotal = 513;
-constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space)
+constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space),
+constexpr int kFewTiles = 160;       // or 2 KB of it (2k step 18.0 us, 18.2 with all of it)
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -359,20 +360,23 @@ enum : int {
 };
 static_assert(T_COUNT * 8 + 8 <= kTBarBytes, "barrier area");
 
-struct TileParams {
+struct TileCall {
     AdapterParams p;
     TileShape s;
     int32_t *err;
     int32_t block_at[kAMaxSlices + 1];  // first block of columns of each slice; all of them
-    AdapterTile tiles[kMaxTiles];
 };
-static_assert(sizeof(TileParams) + 3 * 128 + 2 * 128 <= 32764, "kernel parameter space");
+template <int kTiles>
+struct TileParams : TileCall {
+    AdapterTile tiles[kTiles];
+};
+static_assert(sizeof(TileParams<kMaxTiles>) + 3 * 128 + 2 * 128 <= 32764, "kernel parameter space");
 
 // block i of the columns: its slice, first column and width
 struct ColumnBlock {
     int slice, c0, width;
 };
-__device__ __forceinline__ ColumnBlock column_block(const TileParams &tp, int i) {
+__device__ __forceinline__ ColumnBlock column_block(const TileCall &tp, int i) {
     ColumnBlock b;
     b.slice = (i >= tp.block_at[1]) + (i >= tp.block_at[2]) + (i >= tp.block_at[3]);
     b.c0 = tp.p.slice_at[b.slice] + ((i - tp.block_at[b.slice]) << tp.s.block_log);
@@ -407,11 +411,11 @@ __device__ __forceinline__ void stores_wait() { asm volatile("cp.async.bulk.wait
 
 }  // namespace
 
-template <int kRows>
+template <int kRows, int kTiles>
 __global__ void __launch_bounds__(kTThreads, 1)
     adapter_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a,
                          const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_y,
-                         const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ TileParams tp) {
+                         const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ TileParams<kTiles> tp) {
     extern __shared__ uint8_t smem_raw[];
     const AdapterParams &p = tp.p;
     const TileShape &ts = tp.s;
@@ -1020,24 +1024,26 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
 
 cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_t n_rows, int32_t n_adapters,
                          int32_t *err, cudaStream_t st) {
-    static std::atomic<uint64_t> smem_set{0}, smem_set_half{0};
-    cudaError_t e = ensure_smem_limit(adapter_tiles_kernel<kTRows>, static_cast<int>(kTSmem), smem_set);
-    if (e == cudaSuccess)
-        e = ensure_smem_limit(adapter_tiles_kernel<kTRows / 2>, static_cast<int>(kTSmem), smem_set_half);
+    static std::atomic<uint64_t> smem_set[3] = {};
+    constexpr auto kMany = adapter_tiles_kernel<kTRows, kMaxTiles>;
+    constexpr auto kFew = adapter_tiles_kernel<kTRows, kFewTiles>, kHalf = adapter_tiles_kernel<kTRows / 2, kFewTiles>;
+    cudaError_t e = ensure_smem_limit(kMany, static_cast<int>(kTSmem), smem_set[0]);
+    if (e == cudaSuccess) e = ensure_smem_limit(kFew, static_cast<int>(kTSmem), smem_set[1]);
+    if (e == cudaSuccess) e = ensure_smem_limit(kHalf, static_cast<int>(kTSmem), smem_set[2]);
     if (e != cudaSuccess) return e;
     int32_t clusters[kAMaxCluster + 1] = {};
-    e = clusters_at_a_time<adapter_tiles_kernel<kTRows>, kAMaxCluster>(kTThreads, static_cast<int>(kTSmem), clusters);
+    e = clusters_at_a_time<kFew, kAMaxCluster>(kTThreads, static_cast<int>(kTSmem), clusters);
     if (e != cudaSuccess) return e;
-    const auto tp = std::make_unique<TileParams>();
-    tp->p = p;
-    tp->err = err;
+    TileCall call;
+    call.p = p;
+    call.err = err;
     // As many CTAs a tile as run at a time (2k step of 17 tiles, hidden 11008: 4 CTAs 19.8 us;
     // 8, whose clusters take two rounds, 26.0).
     clusters[1] = device_sm_count();
     const int k_blocks = (p.hidden + kTK - 1) / kTK;
     auto ctas_of = [&](int64_t n, int rows) {
         int c = kAMaxCluster;
-        while (c > 1 && (n > clusters[c] || c > k_blocks || !tile_shape(p, c, &tp->s, rows))) --c;
+        while (c > 1 && (n > clusters[c] || c > k_blocks || !tile_shape(p, c, &call.s, rows))) --c;
         return c;
     };
     // Tiles of 64 rows where all of them run at a time and a CTA has a tenth less to do, by
@@ -1048,10 +1054,11 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
         int64_t n = 0;
         for (const AdapterTile &tile : plan.tiles) n += (tile.n + rows - 1) / rows;
         const int c = ctas_of(n, rows);
-        if (n > clusters[c] || !tile_shape(p, c, &tp->s, rows)) return std::numeric_limits<double>::infinity();
-        return (static_cast<double>(p.hidden) * (rows + tp->s.wide16) +
-                static_cast<double>(p.cols) * (2 * kTRows + tp->s.rank16)) / c +
-               (c > 1 ? 5.0 * rows * tp->s.wide16 : 0.0);
+        if (n > std::min(clusters[c], kFewTiles) || !tile_shape(p, c, &call.s, rows))
+            return std::numeric_limits<double>::infinity();
+        return (static_cast<double>(p.hidden) * (rows + call.s.wide16) +
+                static_cast<double>(p.cols) * (2 * kTRows + call.s.rank16)) / c +
+               (c > 1 ? 5.0 * rows * call.s.wide16 : 0.0);
     };
     const int rows_of_tile = work(kTRows / 2) < 0.9 * work(kTRows) ? kTRows / 2 : kTRows;
     std::vector<AdapterTile> parts;
@@ -1062,13 +1069,13 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
     const std::vector<AdapterTile> &tiles = rows_of_tile < kTRows ? parts : plan.tiles;
     for (size_t next = 0; next < tiles.size();) {
         const int n = static_cast<int>(std::min<size_t>(kMaxTiles, tiles.size() - next));
-        std::copy_n(tiles.begin() + static_cast<std::ptrdiff_t>(next), n, tp->tiles);
+        const AdapterTile *const those = tiles.data() + next;
         next += static_cast<size_t>(n);
         const int c = ctas_of(n, rows_of_tile);
-        if (!tile_shape(p, c, &tp->s, rows_of_tile)) return cudaErrorInvalidValue;  // (the plan asked before)
+        if (!tile_shape(p, c, &call.s, rows_of_tile)) return cudaErrorInvalidValue;  // (the plan asked before)
         for (int j = 0, at = 0; j <= kAMaxSlices; ++j) {
-            tp->block_at[j] = at;
-            if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + (1 << tp->s.block_log) - 1) >> tp->s.block_log;
+            call.block_at[j] = at;
+            if (j < kAMaxSlices) at += (p.slice_at[j + 1] - p.slice_at[j] + (1 << call.s.block_log) - 1) >> call.s.block_log;
         }
         CUtensorMap tm_x, tm_a, tm_b, tm_y, tm_out;
         const uint32_t box_rows = static_cast<uint32_t>(rows_of_tile);
@@ -1076,14 +1083,14 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
         if (!encode_bf16_rows(&tm_x, p.x, static_cast<uint64_t>(p.hidden), rows, static_cast<uint64_t>(p.x_stride), kTK,
                               box_rows) ||
             !encode_bf16_3d(&tm_a, p.a, static_cast<uint64_t>(p.hidden), static_cast<uint64_t>(p.rank),
-                            static_cast<uint64_t>(n_adapters) * p.n_slices, kTK, static_cast<uint32_t>(tp->s.rank16),
+                            static_cast<uint64_t>(n_adapters) * p.n_slices, kTK, static_cast<uint32_t>(call.s.rank16),
                             static_cast<uint32_t>(p.n_slices)) ||
             !encode_bf16_2d(&tm_b, p.b, static_cast<uint64_t>(p.rank), static_cast<uint64_t>(n_adapters) * cols, 64,
-                            1u << tp->s.block_log) ||
+                            1u << call.s.block_log) ||
             !encode_bf16_rows(&tm_y, p.y, cols, rows, static_cast<uint64_t>(p.y_stride), 64, box_rows) ||
             !encode_bf16_rows(&tm_out, p.out, cols, rows, static_cast<uint64_t>(p.out_stride), 64, box_rows))
             return cudaErrorUnknown;
-        PdlLaunch l(dim3(static_cast<unsigned>(n) * static_cast<unsigned>(c)), dim3(kTThreads), tp->s.smem, st);
+        PdlLaunch l(dim3(static_cast<unsigned>(n) * static_cast<unsigned>(c)), dim3(kTThreads), call.s.smem, st);
         cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
         if (c > 1) {
             attrs[1].id = cudaLaunchAttributeClusterDimension;
@@ -1093,8 +1100,18 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
             l.cfg.attrs = attrs;
             l.cfg.numAttrs = 2;
         }
-        const auto kernel = rows_of_tile == kTRows ? adapter_tiles_kernel<kTRows> : adapter_tiles_kernel<kTRows / 2>;
-        e = cudaLaunchKernelEx(&l.cfg, kernel, tm_x, tm_a, tm_b, tm_y, tm_out, *tp);
+        auto launch = [&](auto kernel, auto &tp) {
+            static_cast<TileCall &>(tp) = call;
+            std::copy_n(those, n, tp.tiles);
+            return cudaLaunchKernelEx(&l.cfg, kernel, tm_x, tm_a, tm_b, tm_y, tm_out, tp);
+        };
+        if (n <= kFewTiles) {
+            TileParams<kFewTiles> tp;
+            e = rows_of_tile == kTRows ? launch(kFew, tp) : launch(kHalf, tp);
+        } else {
+            const auto tp = std::make_unique<TileParams<kMaxTiles>>();
+            e = rows_of_tile == kTRows ? launch(kMany, *tp) : cudaErrorInvalidValue;  // (64 rows: all run at a time)
+        }
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
