@@ -25,6 +25,7 @@
 // are read again, slowly and for sure.
 #include <float.h>
 #include <math.h>
+#include <stddef.h>
 
 #include <atomic>
 
@@ -34,8 +35,7 @@
 namespace ppas {
 namespace {
 
-constexpr int kLThreads = 256;
-constexpr int kLWarps = kLThreads / 32;
+constexpr int kLThreads = 256;  // of a CTA; where rows are many and short, 128 or 64
 // 16-byte loads of a round, a thread (32 logits), rounds under way, and the CTAs that an SM
 // then holds: of fp32 3 (bf16 4), and where there are fewer, kFew, 2 (3) with a round
 // more under way.  (256 x 152000: 28.0 us, 29.5 with the shorter ring; 128: 18.8 and 21.2; 400
@@ -47,9 +47,12 @@ template <class T, bool kFew>
 constexpr int kLStages = (sizeof(T) == 4 ? 2 : 3) + (kFew ? 1 : 0);
 template <class T, bool kFew>
 constexpr int kLAnSm = (sizeof(T) == 4 ? 3 : 4) - (kFew ? 1 : 0);
-constexpr int kLGroups = kLThreads / 4;
-constexpr int kLList = 640;     // places of the lists, kLOfWarp of each warp
-constexpr int kLOfWarp = kLList / kLWarps;
+constexpr int kLGroups = 64;
+// places of the lists, and of each of the N / 32 warps
+template <int N>
+constexpr int kLList = N == kLThreads ? 640 : 512;
+template <int N>
+constexpr int kLOfWarp = kLList<N> / (N / 32);
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLLimit = 0x1p22f;  // |x L| from here on: the whole numbers c have no room left
 constexpr float kLFloor = -1e30f;   // logits below count as this: 2^(x L - c) is 0, and 0 times x L - c too
@@ -99,13 +102,15 @@ __device__ __forceinline__ bool raises(int round, int rounds) {
 struct LPart {
     float top, s, t;
 };
+template <int N>
 struct LShared {
-    uint64_t list[kLList];    // each warp's places at or above the bound
+    static constexpr int kLWarps = N / 32;
+    uint64_t list[kLList<N>];    // each warp's places at or above the bound
     uint32_t n_list[kLWarps];
     uint64_t best[kLMaxTop];  // this CTA's alternatives, in order; 0: none
     LPart parts[kLMaxCluster];
     union {
-        uint32_t group[kLGroups];
+        alignas(16) uint32_t group[kLGroups];  // (read four at a time)
         uint64_t group_place[kLGroups];
     };
     uint64_t place[kLWarps];
@@ -117,18 +122,19 @@ struct LShared {
 };
 
 // Each thread's own logits under way; the memory has other uses once they are through.
-template <class T, bool kFew>
+template <class T, bool kFew, int N>
 struct LRing {
     union {
-        uint4 ring[kLStages<T, kFew>][kLLoads<T>][kLThreads];
+        uint4 ring[kLStages<T, kFew>][kLLoads<T>][N];
         struct {
-            uint64_t kept[kLList];
+            uint64_t kept[kLList<N>];
             uint64_t all[kLMaxCluster * kLMaxTop];
         };
     };
 };
 
-__device__ __forceinline__ uint64_t block_max(LShared &sh, uint64_t v) {
+template <int N>
+__device__ __forceinline__ uint64_t block_max(LShared<N> &sh, uint64_t v) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int o = 16; o; o >>= 1) {
         const uint64_t u = __shfl_xor_sync(0xffffffffu, v, o);
@@ -137,7 +143,7 @@ __device__ __forceinline__ uint64_t block_max(LShared &sh, uint64_t v) {
     __syncthreads();
     if (lane == 0) sh.place[warp] = v;
     __syncthreads();
-    for (int w = 0; w < kLWarps; ++w) v = sh.place[w] > v ? sh.place[w] : v;
+    for (int w = 0; w < N / 32; ++w) v = sh.place[w] > v ? sh.place[w] : v;
     return v;
 }
 
@@ -148,26 +154,28 @@ __device__ __forceinline__ void st_cluster_u64(uint32_t a, uint64_t v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 
-// The n-th largest of the groups' maxima (or a little less), given every thread's: four
-// threads count how many are above a group's.
-__device__ __forceinline__ float bound_of(LShared &sh, float top, int n) {
+// The n-th largest of the groups' maxima (or a little less), given every thread's: a group's
+// threads count how many are above it.
+template <int N>
+__device__ __forceinline__ float bound_of(LShared<N> &sh, float top, int n) {
     constexpr uint32_t kIndex = kLGroups - 1;  // a key's low bits tell equal maxima apart
+    constexpr int kOf = N / kLGroups, kVecs = kLGroups / 4 / kOf;
     const int tid = threadIdx.x;
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t mine = (ascending(top) & ~kIndex) | static_cast<uint32_t>(tid >> 2);
-    if ((tid & 3) == 0) sh.group[tid >> 2] = mine;
+#pragma unroll
+    for (int o = 1; o < kOf; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const uint32_t mine = (ascending(top) & ~kIndex) | static_cast<uint32_t>(tid / kOf);
+    if (tid % kOf == 0) sh.group[tid / kOf] = mine;
     __syncthreads();
-    const uint4 *g4 = reinterpret_cast<const uint4 *>(sh.group) + (tid & 3) * (kLGroups / 16);
+    const uint4 *g4 = reinterpret_cast<const uint4 *>(sh.group) + tid % kOf * kVecs;
     int above = 0;
 #pragma unroll
-    for (int j = 0; j < kLGroups / 16; ++j) {
+    for (int j = 0; j < kVecs; ++j) {
         const uint4 g = g4[j];
         above += (g.x > mine) + (g.y > mine) + (g.z > mine) + (g.w > mine);
     }
-    above += __shfl_xor_sync(0xffffffffu, above, 1);
-    above += __shfl_xor_sync(0xffffffffu, above, 2);
-    if (above == n - 1 && (tid & 3) == 0)
+#pragma unroll
+    for (int o = 1; o < kOf; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+    if (above == n - 1 && tid % kOf == 0)
         sh.bound = (mine & ~kIndex) <= ascending(-INFINITY) ? -INFINITY : of_ascending(mine & ~kIndex);
     __syncthreads();
     return sh.bound;
@@ -176,14 +184,14 @@ __device__ __forceinline__ float bound_of(LShared &sh, float top, int n) {
 // emit(i, place) for the first n of the m places in `from` in their order, and emit(i, 0)
 // for what they do not have: a place's rank is the number of larger ones, counted by several
 // lanes.  By whichever thread: no barrier.
-template <class Emit>
+template <int N, class Emit>
 __device__ __forceinline__ void rank_places(const uint64_t *from, int m, int n, Emit &&emit) {
     const int tid = threadIdx.x;
     if (tid >= m && tid < n) emit(tid, 0);
     int lanes = 32;
-    while (lanes > 1 && m * lanes > kLThreads) lanes >>= 1;
+    while (lanes > 1 && m * lanes > N) lanes >>= 1;
     const int l = tid & (lanes - 1);
-    for (int base = 0; base < m; base += kLThreads / lanes) {
+    for (int base = 0; base < m; base += N / lanes) {
         const int i = base + tid / lanes;
         const uint64_t mine = i < m ? from[i] : 0;
         int before = 0;
@@ -196,20 +204,20 @@ __device__ __forceinline__ void rank_places(const uint64_t *from, int m, int n, 
 
 // A part's alternatives where the list overflowed: by places instead of logits,
 // which tells equal logits apart; and where even those are too many, one by one.
-template <class T>
-__device__ __noinline__ void slow_top(LShared &sh, const T *src, int n, int i0, int n_top) {
+template <class T, int N>
+__device__ __noinline__ void slow_top(LShared<N> &sh, const T *src, int n, int i0, int n_top) {
     const int tid = threadIdx.x;
     uint64_t best = 0;
-    for (int i = tid; i < n; i += kLThreads) {
+    for (int i = tid; i < n; i += N) {
         const uint64_t v = place_of(logit_of(src[i]), static_cast<uint32_t>(i0 + i));
         best = v > best ? v : best;
     }
-    for (int o = 1; o < 4; o <<= 1) {
+    for (int o = 1; o < N / kLGroups; o <<= 1) {
         const uint64_t other = __shfl_xor_sync(0xffffffffu, best, o);
         best = other > best ? other : best;
     }
     __syncthreads();
-    if ((tid & 3) == 0) sh.group_place[tid >> 2] = best;
+    if (tid % (N / kLGroups) == 0) sh.group_place[tid / (N / kLGroups)] = best;
     if (tid == 0) sh.n_kept = 0;
     __syncthreads();
     if (tid < kLGroups) {
@@ -221,24 +229,24 @@ __device__ __noinline__ void slow_top(LShared &sh, const T *src, int n, int i0, 
     }
     __syncthreads();
     const uint64_t bound = sh.bound_place;
-    for (int i = tid; i < n; i += kLThreads) {
+    for (int i = tid; i < n; i += N) {
         const uint64_t v = place_of(logit_of(src[i]), static_cast<uint32_t>(i0 + i));
         if (v >= bound && place_logit(v) > -INFINITY) {
             const uint32_t at = atomicAdd(&sh.n_kept, 1u);
-            if (at < kLList) sh.list[at] = v;
+            if (at < kLList<N>) sh.list[at] = v;
         }
     }
     __syncthreads();
     const uint32_t m = sh.n_kept;
-    if (m <= kLList) {
-        rank_places(sh.list, static_cast<int>(m), n_top, [&](int i, uint64_t v) { sh.best[i] = v; });
+    if (m <= kLList<N>) {
+        rank_places<N>(sh.list, static_cast<int>(m), n_top, [&](int i, uint64_t v) { sh.best[i] = v; });
         __syncthreads();
         return;
     }
     uint64_t before = ~uint64_t{0};
     for (int j = 0; j < n_top; ++j) {
         best = 0;
-        for (int i = tid; i < n; i += kLThreads) {
+        for (int i = tid; i < n; i += N) {
             const uint64_t v = place_of(logit_of(src[i]), static_cast<uint32_t>(i0 + i));
             if (v < before && v > best) best = v;
         }
@@ -250,13 +258,13 @@ __device__ __noinline__ void slow_top(LShared &sh, const T *src, int n, int i0, 
 }
 
 // a part's sums, the maximum known
-template <class T>
+template <class T, int N>
 __device__ __noinline__ float2 slow_sums(const T *src, int n, float top) {
     float s = 0.f, t = 0.f;
     // (32 at a time: fewer roundings lie behind one another)
-    for (int a = threadIdx.x; a < n; a += 32 * kLThreads) {
+    for (int a = threadIdx.x; a < n; a += 32 * N) {
         float s1 = 0.f, t1 = 0.f;
-        for (int i = a; i < n && i < a + 32 * kLThreads; i += kLThreads) {
+        for (int i = a; i < n && i < a + 32 * N; i += N) {
             const float z = logit_of(src[i]) - top, e = expf(z);
             s1 += e;
             t1 += e > 0.f ? z * e : 0.f;
@@ -342,12 +350,13 @@ __device__ __forceinline__ void copies_wait() {
 
 }  // namespace
 
-template <class T, bool kTop, bool kFew>
-__global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_constant__ LogprobParams p) {
+template <class T, bool kTop, bool kFew, int N>
+__global__ void __launch_bounds__(N) token_logprobs_kernel(const __grid_constant__ LogprobParams p) {
     extern __shared__ __align__(16) uint8_t logprob_smem[];
-    using Ring = LRing<T, kFew>;
+    using Ring = LRing<T, kFew, N>;
+    using Shared = LShared<N>;
     Ring &ring = *reinterpret_cast<Ring *>(logprob_smem);
-    LShared &sh = *reinterpret_cast<LShared *>(logprob_smem + sizeof(Ring));
+    Shared &sh = *reinterpret_cast<Shared *>(logprob_smem + sizeof(Ring));
     constexpr int kLoads = kLLoads<T>, kStages = kLStages<T, kFew>;
     constexpr int kPer = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -368,7 +377,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     const uint4 *const src4 = reinterpret_cast<const uint4 *>(src - pad);
     // A thread's copies go to its own places of the ring, from which it alone reads:
     // its own waits are all that it takes.
-    constexpr int kRound = kLThreads * kLoads;
+    constexpr int kRound = N * kLoads;
     const int rounds = (vecs + kRound - 1) / kRound;
     constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf, bf16 twice
     auto fetch = [&](int round, int stage) {
@@ -377,26 +386,26 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
             const uint4 *from = src4 + v0 + tid;
             const uint32_t to = smem_u32(&ring.ring[stage][0][tid]);
 #pragma unroll
-            for (int k = 0; k < kLoads; ++k) copy16_async(to + k * kLThreads * 16, from + k * kLThreads);
+            for (int k = 0; k < kLoads; ++k) copy16_async(to + k * N * 16, from + k * N);
         } else if (sizeof(T) == 4 && round < rounds) {
             // (a part's last round, all at once; of bf16 one 16 bytes after another, which the
             // kernel's other rounds lose least to: 3292 x 5323 fp32 22.6 us, 25.4 so; 4096 x
             // 128000 bf16 152.0, 169.1 all at once)
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
-                const int v = v0 + k * kLThreads + tid;
+                const int v = v0 + k * N + tid;
                 if (v >= whole0 && v < whole1) copy16_async(smem_u32(&ring.ring[stage][k][tid]), src4 + v);
                 else if (v >= vecs) ring.ring[stage][k][tid] = make_uint4(kNone, kNone, kNone, kNone);
             }
             // the part's first 16 bytes and its last, where they are not whole
             if (whole0 && v0 + tid == 0) ring.ring[stage][0][tid] = edge_vector(src, -pad, n);
-            if (const int k = (whole1 - v0 - tid) / kLThreads;
-                whole1 < vecs && whole1 >= max(v0, whole0) && k < kLoads && (whole1 - tid) % kLThreads == 0)
+            if (const int k = (whole1 - v0 - tid) / N;
+                whole1 < vecs && whole1 >= max(v0, whole0) && k < kLoads && (whole1 - tid) % N == 0)
                 ring.ring[stage][k][tid] = edge_vector(src, whole1 * kPer - pad, n);
         } else if (round < rounds) {
 #pragma unroll 1
             for (int k = 0; k < kLoads; ++k) {
-                const int v = v0 + k * kLThreads + tid;
+                const int v = v0 + k * N + tid;
                 if (v >= whole0 && v < whole1) copy16_async(smem_u32(&ring.ring[stage][k][tid]), src4 + v);
                 else if (v >= vecs) ring.ring[stage][k][tid] = make_uint4(kNone, kNone, kNone, kNone);
                 else ring.ring[stage][k][tid] = edge_vector(src, v * kPer - pad, n);
@@ -467,8 +476,8 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
                     const bool in = x >= bound && x > -INFINITY;
                     const uint32_t those = __ballot_sync(0xffffffffu, in);
                     const uint32_t at = n_list + __popc(those & ((1u << lane) - 1));
-                    const int index = i0 + ((round * kLoads + k) * kLThreads + from) * kPer + e - pad;
-                    if (in && at < kLOfWarp) sh.list[warp * kLOfWarp + at] = place_of(x + 0.f, static_cast<uint32_t>(index));
+                    const int index = i0 + ((round * kLoads + k) * N + from) * kPer + e - pad;
+                    if (in && at < kLOfWarp<N>) sh.list[warp * kLOfWarp<N> + at] = place_of(x + 0.f, static_cast<uint32_t>(index));
                     n_list += __popc(those);
                 } while (hits);
                 __syncwarp();
@@ -505,15 +514,15 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     if (ctas > 1) cluster_arrive();
 
     // ---- the part's, by every warp for itself
-    const int w8 = lane % kLWarps;
+    const int w8 = lane % Shared::kLWarps;
     float part_top = sh.top[w8];
-    for (int o = 1; o < kLWarps; o <<= 1) part_top = fmaxf(part_top, __shfl_xor_sync(0xffffffffu, part_top, o));
+    for (int o = 1; o < Shared::kLWarps; o <<= 1) part_top = fmaxf(part_top, __shfl_xor_sync(0xffffffffu, part_top, o));
     part_top = fminf(part_top, kLLargest<T>);
     const bool any = part_top > -INFINITY;
     const bool part_bad = __any_sync(0xffffffffu, sh.bad[w8] != 0);
-    const bool full = __any_sync(0xffffffffu, sh.n_list[w8] > kLOfWarp);
+    const bool full = __any_sync(0xffffffffu, sh.n_list[w8] > kLOfWarp<N>);
     if (any && part_bad) {
-        const float2 v = slow_sums(src, n, part_top);
+        const float2 v = slow_sums<T, N>(src, n, part_top);
         s = v.x;
         t = v.y;
         for (int o = 16; o; o >>= 1) {
@@ -533,7 +542,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         s = f > 0.f ? sh.s[w8] * f : 0.f;
         t = f > 0.f ? fmaf(d, sh.s[w8], sh.t[w8]) * f : 0.f;
     }
-    for (int o = 1; o < kLWarps; o <<= 1) {
+    for (int o = 1; o < Shared::kLWarps; o <<= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
         t += __shfl_xor_sync(0xffffffffu, t, o);
     }
@@ -545,7 +554,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         // without those that only an earlier bound let in
         for (uint32_t j = 0; j < n_list; j += 32) {
             const uint32_t i = j + static_cast<uint32_t>(lane);
-            const uint64_t v = i < n_list ? sh.list[warp * kLOfWarp + i] : 0;
+            const uint64_t v = i < n_list ? sh.list[warp * kLOfWarp<N> + i] : 0;
             const bool in = i < n_list && place_logit(v) >= bound;
             const uint32_t those = __ballot_sync(0xffffffffu, in);
             uint32_t at = 0;
@@ -559,7 +568,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     if (ctas > 1) {
         // ---- the first CTA joins the parts
         if (kTop && !in_best) {
-            rank_places(ring.kept, static_cast<int>(sh.n_kept), p.n_top, [&](int i, uint64_t v) { sh.best[i] = v; });
+            rank_places<N>(ring.kept, static_cast<int>(sh.n_kept), p.n_top, [&](int i, uint64_t v) { sh.best[i] = v; });
             __syncthreads();
         }
         cluster_wait();
@@ -589,7 +598,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
                 0xffffffffu, static_cast<uint32_t>(ring.all[min(lane, static_cast<int>(ctas) - 1) * p.n_top + at] >> 32));
             if (tid == 0) sh.n_kept = 0;
             __syncthreads();
-            for (int i = tid; i < static_cast<int>(ctas) * p.n_top; i += kLThreads) {
+            for (int i = tid; i < static_cast<int>(ctas) * p.n_top; i += N) {
                 const uint64_t v = ring.all[i];
                 if (v != 0 && static_cast<uint32_t>(v >> 32) >= least) ring.kept[atomicAdd(&sh.n_kept, 1u)] = v;
             }
@@ -607,7 +616,7 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
         if (in_best && ctas == 1) {
             if (tid < p.n_top) put(tid, sh.best[tid]);
         } else {
-            rank_places(ring.kept, static_cast<int>(sh.n_kept), p.n_top, put);
+            rank_places<N>(ring.kept, static_cast<int>(sh.n_kept), p.n_top, put);
         }
     }
     if (tid == 0) {
@@ -621,13 +630,18 @@ __global__ void __launch_bounds__(kLThreads) token_logprobs_kernel(const __grid_
     }
 }
 
-static_assert(kLMaxCluster * kLMaxTop <= kLList, "the first CTA ranks them in `kept`");
+static_assert(kLMaxCluster * kLMaxTop <= kLList<kLThreads>, "the first CTA ranks them in `kept`");
+template <class T, bool kFew, int N>
+constexpr int kLSmem = static_cast<int>(sizeof(LRing<T, kFew, N>) + sizeof(LShared<N>));
 template <class T, bool kFew>
-constexpr int kLSmem = static_cast<int>(sizeof(LRing<T, kFew>) + sizeof(LShared));
-template <class T, bool kFew>
-constexpr bool kLFits = kLAnSm<T, kFew> * (kLSmem<T, kFew> + 1024) <= 233472;
+constexpr bool kLFits = kLAnSm<T, kFew> * (kLSmem<T, kFew, kLThreads> + 1024) <= 233472;
 static_assert(kLFits<float, false> && kLFits<float, true> && kLFits<__nv_bfloat16, false> && kLFits<__nv_bfloat16, true>,
               "shared memory of an SM");
+static_assert(kLMaxTop <= 64, "an alternative a thread");
+template <int N>
+constexpr bool kLAligned = offsetof(LShared<N>, group) % 16 == 0 && sizeof(LRing<float, false, N>) % 16 == 0 &&
+                           sizeof(LRing<__nv_bfloat16, false, N>) % 16 == 0;
+static_assert(kLAligned<64> && kLAligned<128> && kLAligned<kLThreads>, "groups are read 16 bytes at a time");
 
 // How many clusters of 2, 4, 8 and 16 CTAs (16 are more than the portable 8) of a kernel
 // this device holds at a time; once per device.
@@ -635,8 +649,8 @@ template <class T, bool kTop, bool kFew>
 cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
     static std::atomic<uint64_t> limit_set{0};
     static std::atomic<int32_t> known[64][5] = {};  // + 1; 0: not asked
-    const auto kernel = token_logprobs_kernel<T, kTop, kFew>;
-    cudaError_t e = ensure_smem_limit(kernel, kLSmem<T, kFew>, limit_set);
+    const auto kernel = token_logprobs_kernel<T, kTop, kFew, kLThreads>;
+    cudaError_t e = ensure_smem_limit(kernel, kLSmem<T, kFew, kLThreads>, limit_set);
     int dev = 0;
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -646,7 +660,7 @@ cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(1u << i);
             cfg.blockDim = dim3(kLThreads);
-            cfg.dynamicSmemBytes = kLSmem<T, kFew>;
+            cfg.dynamicSmemBytes = kLSmem<T, kFew, kLThreads>;
             cudaLaunchAttribute a = {};
             a.id = cudaLaunchAttributeClusterDimension;
             a.val.clusterDim.x = 1u << i;
@@ -680,7 +694,7 @@ cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
     while (i > 0 && (n_rows > clusters[i] || p.vocab < 4096 << i)) --i;
     const int32_t c = 1 << i;
     p.chunk = ((p.vocab + c - 1) / c + 15) / 16 * 16;
-    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), kLSmem<T, kFew>, st);
+    PdlLaunch l(dim3(static_cast<unsigned>(n_rows) * c), dim3(kLThreads), kLSmem<T, kFew, kLThreads>, st);
     cudaLaunchAttribute attrs[2] = {l.attr[0], {}};
     if (c > 1) {
         attrs[1].id = cudaLaunchAttributeClusterDimension;
@@ -690,13 +704,35 @@ cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
         l.cfg.attrs = attrs;
         l.cfg.numAttrs = 2;
     }
-    return cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, kTop, kFew>, p);
+    return cudaLaunchKernelEx(&l.cfg, token_logprobs_kernel<T, kTop, kFew, kLThreads>, p);
+}
+
+template <class T, bool kTop, int N>
+cudaError_t launch_narrow(LogprobParams p, int32_t n_rows, cudaStream_t st) {
+    static std::atomic<uint64_t> limit_set{0};
+    const auto kernel = token_logprobs_kernel<T, kTop, false, N>;
+    constexpr int kSmem = kLSmem<T, false, N>;
+    const cudaError_t e = ensure_smem_limit(kernel, kSmem, limit_set);
+    if (e != cudaSuccess) return e;
+    p.chunk = (p.vocab + 15) / 16 * 16;
+    PdlLaunch l(dim3(static_cast<unsigned>(n_rows)), dim3(N), kSmem, st);
+    return cudaLaunchKernelEx(&l.cfg, kernel, p);
 }
 
 template <class T, bool kTop>
 cudaError_t launch_logprobs(const LogprobParams &p, int32_t n_rows, cudaStream_t st) {
-    const bool few = n_rows <= kLAnSm<T, true> * static_cast<int64_t>(device_sm_count());
-    return few ? launch_logprobs<T, kTop, true>(p, n_rows, st) : launch_logprobs<T, kTop, false>(p, n_rows, st);
+    const int64_t sms = device_sm_count(), wide = kLAnSm<T, false> * sms;
+    // A row's barriers, list and ranks hide behind other rows' loads, so where there are more
+    // than CTAs of 256 threads hold at a time, and short ones, smaller CTAs take them (fp32, 3292 x
+    // 5323, 1 alternative: 64 threads 20.3 us, 256 34.8; 4096 x 8000, 5: 27.7, 128 33.6, 256 42.8;
+    // bf16 1024 x 16000, 20: 24.1, 128 15.4, 256 15.7; 2503 x 42728, 5: 128 44.3, 256 48.6; 300 x
+    // 1000, 5: 64 4.1, 256 5.0; 700 x 64000, 20: 128 32.3, 256 26.4).
+    if (n_rows > sms && (p.vocab <= 2048 || (n_rows > 2 * wide && p.vocab <= 8192)))
+        return launch_narrow<T, kTop, 64>(p, n_rows, st);
+    if (n_rows > wide && (p.vocab <= 16384 || (n_rows > 2 * wide && p.vocab <= 65536)))
+        return launch_narrow<T, kTop, 128>(p, n_rows, st);
+    return n_rows <= kLAnSm<T, true> * sms ? launch_logprobs<T, kTop, true>(p, n_rows, st)
+                                           : launch_logprobs<T, kTop, false>(p, n_rows, st);
 }
 
 cudaError_t launch_token_logprobs(const LogprobParams &p, int32_t n_rows, bool bf16, cudaStream_t st) {

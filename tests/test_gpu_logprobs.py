@@ -223,3 +223,39 @@ def test_two_streams_at_once(ppas):
     for a, o in zip(alone, outs):
         for k, t in zip(("lp", "ent", "tok", "top"), o[1:]):
             assert np.array_equal(a[k], t.double().cpu().numpy())
+
+
+# rows that are many and short: CTAs of 64 and of 128 threads
+@pytest.mark.parametrize("n,v", [(153, 1), (160, 7), (200, 33), (310, 2047), (153, 2048), (700, 2049), (1300, 2050), (1300, 8192),
+                                 (700, 8193), (700, 16384), (1300, 20011)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n_top", [0, 1, 32])
+def test_many_short_rows(ppas, n, v, dtype, n_top):
+    shift = n_top % 5
+    x = _logits(n, v + 3 * shift, seed=n + v, dtype=dtype)[:, shift:shift + v]
+    given = np.random.default_rng(v).integers(-1, v, n)
+    _check(ppas, x, given, n_top)
+
+
+@pytest.mark.parametrize("n,v", [(180, 900), (1300, 5000), (700, 9000), (1300, 17000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_short_rows_of_every_kind(ppas, n, v, dtype):
+    x = _logits(n, v, seed=v, dtype=torch.float32)
+    kinds = 12
+    at = torch.arange(n, device="cuda") % kinds
+    ramp = torch.linspace(-40, 40, v, device="cuda")
+    x[at == 1] = -float("inf")
+    x[at == 2] = 1.5
+    x[at == 3] = ramp
+    x[at == 4] = ramp.flip(0)
+    x[at == 5] = (x[at == 5] * 2).round()          # many equal ones
+    x[at == 6] = x[at == 6] * 1e37
+    x[at == 7] = torch.where(x[at == 7] > 0, x[at == 7], -float("inf"))
+    x[at == 8] = torch.where(x[at == 8] > 0, x[at == 8], float("nan"))
+    x[at == 9, v // 2] = float("inf")
+    x[at == 10, :-1] = -float("inf")               # a sure token
+    x[at == 11] = x[at == 11] * 1e-3 - 1e30
+    x = x.to(dtype)
+    given = np.random.default_rng(v).integers(-1, v, n)
+    _check(ppas, x, given, 20)
+    _check(ppas, x, given, 0)
