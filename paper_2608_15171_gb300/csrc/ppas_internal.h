@@ -357,6 +357,7 @@ struct RopeParams {
     int32_t norm;
     const float *q_weight, *k_weight;
     float eps, inv_dim;
+    float sum_least, sum_most;  // sums of squares that are taken as they are
 };
 cudaError_t launch_rope_append(RopeParams p, cudaStream_t st);
 

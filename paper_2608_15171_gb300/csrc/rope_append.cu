@@ -102,13 +102,27 @@ __device__ __forceinline__ float2 unpack_bf16x2(uint32_t v) {
 
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return fma2(a, b, make_float2(-0.f, -0.f)); }
 
-// Heads whose squares pass the fp32 range (values from 1.8e19 on) are summed again
-// times this; the largest bf16 numbers then stay below 2^59, 512 squares of them in range.
-constexpr float kSquareScale = 0x1p-70f;
+// Heads whose squares leave the fp32 range are summed again times a power of two, eps
+// with them: by kSquareDown where they pass it (the largest bf16 numbers then stay below 2^59,
+// 512 squares of them in range), and by kSquareUp where they are lost below it and
+// eps is as small (below 2^-110 all values are less than 2^-55; the least bf16 number's square is then
+// 2^-126, the least eps 2^-9).  Elsewhere what a sum has lost, 512 2^-150 at the most, is less than 2^-31 of it,
+// or than 2^-40 of eps.
+constexpr float kSquareDown = 0x1p-70f, kSquareUp = 0x1p70f;
+constexpr float kEpsSmall = 0x1p-100f, kEpsLarge = 0x1p100f;  // eps that is lost itself, or passes the range with a sum
+constexpr float kSumSmall = 0x1p-110f;
 
-// 1 / sqrt(mean + eps) of a head's sum of squares, or of the scaled one
-__device__ __forceinline__ float norm_factor(float sum, float scaled, float inv_dim, float eps) {
-    return sum <= FLT_MAX ? rsqrtf(fmaf(sum, inv_dim, eps)) : rsqrtf(scaled * inv_dim) * kSquareScale;
+__device__ __forceinline__ bool in_range(const RopeParams &p, float sum) {
+    return sum >= p.sum_least && sum <= p.sum_most;  // (not NaN)
+}
+// what a sum that is not in range is taken again with, of the values times this
+__device__ __forceinline__ float square_scale(float sum) { return sum < 1.f ? kSquareUp : kSquareDown; }
+// 1 / sqrt(mean + eps) of a head's sum of squares, or of the one of the values times `scale`
+__device__ __forceinline__ float norm_factor(const RopeParams &p, float sum) {
+    return rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+}
+__device__ __forceinline__ float norm_factor(const RopeParams &p, float sum, float scale) {
+    return rsqrtf(fmaf(sum, p.inv_dim, p.eps * scale * scale)) * scale;
 }
 
 // where a token's keys and values go; -1: nowhere
@@ -342,19 +356,21 @@ __global__ void __launch_bounds__(kRopeWarps * 32, kDim ? kNormCtas : 2)
 #pragma unroll
             for (int e = 1; e < 8; ++e) s2 = fma2(x[e], x[e], s2);
             const float sum = over_row(s2.x + s2.y);
-            float scaled = 0.f;
-            if (__any_sync(0xffffffffu, !(sum <= FLT_MAX))) {
+            const bool in = in_range(p, sum);
+            float again = 0.f;
+            if (__any_sync(0xffffffffu, !in)) {
+                const float scale = square_scale(sum);
                 float s = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float y0 = x[e].x * kSquareScale, y1 = x[e].y * kSquareScale;
+                    const float y0 = x[e].x * scale, y1 = x[e].y * scale;
                     s = fmaf(y0, y0, fmaf(y1, y1, s));
                 }
-                scaled = over_row(s);
+                again = norm_factor(p, over_row(s), scale);
             }
             if (!has_row || row >= n_rows || (row >= p.n_q_heads && slot < 0)) continue;
             if (row < n_turned) {
-                const float f = norm_factor(sum, scaled, p.inv_dim, p.eps);
+                const float f = in ? norm_factor(p, sum) : again;
                 const float4 *const w4 =
                     reinterpret_cast<const float4 *>(weights + ((row < p.n_q_heads ? 0 : units) + u) * kPitch);
                 const float2 ff = make_float2(f, f);
@@ -470,7 +486,8 @@ __global__ void __launch_bounds__(256) norm_rope_append_any_kernel(const __grid_
             return s;
         };
         const float sum = row_sum(1.f);
-        const float f = norm_factor(sum, sum <= FLT_MAX ? 0.f : row_sum(kSquareScale), p.inv_dim, p.eps);
+        const float scale = square_scale(sum);
+        const float f = in_range(p, sum) ? norm_factor(p, sum) : norm_factor(p, row_sum(scale), scale);
         const float *const weight = r.is_q ? p.q_weight : p.k_weight;
         const int32_t position = __ldg(p.positions + token);
         auto normed = [&](int e) { return __bfloat162float(r.src[e]) * f * (weight ? __ldg(weight + e) : 1.f); };
@@ -622,6 +639,8 @@ ppas_status rope_call(const void *q, const void *k, const void *v, int64_t q_str
     p.k_weight = d_k_weight;
     p.eps = eps;
     p.inv_dim = 1.f / static_cast<float>(head_dim);
+    p.sum_least = eps < kEpsSmall ? kSumSmall : 0.f;
+    p.sum_most = eps > kEpsLarge ? kEpsLarge : FLT_MAX;  // (eps plus a mean that large is rounded to eps)
     return launch_rope_append(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PPAS_OK : PPAS_ERR_CUDA;
 }
 
