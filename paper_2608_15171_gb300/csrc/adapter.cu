@@ -68,11 +68,11 @@ __device__ __forceinline__ void add_to(float4 &v, float4 w) {
 __device__ __forceinline__ void cluster_arrive() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
-// two values as bf16, and what their rounding left (0 of an infinity)
+// two values as bf16, and what their rounding left.  (Finite: a value past the largest bf16 number, an
+// infinity too, is that number and what is left.)
 __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint32_t &lo) {
-    hi = pack_bf16x2(a, b);
-    const float ha = __uint_as_float(hi << 16), hb = __uint_as_float(hi & 0xFFFF0000u);
-    lo = pack_bf16x2(fabsf(ha) < INFINITY ? a - ha : 0.f, fabsf(hb) < INFINITY ? b - hb : 0.f);
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(b), "f"(a));
+    lo = pack_bf16x2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xFFFF0000u));
 }
 
 template <int kUnits, int kRows>
