@@ -153,7 +153,8 @@ class Batch:
 
     def run(self, on_logits=None, max_steps: int = 100000):
         """All requests to their ends; ``on_logits(request, place, row of logits)`` sees
-        the logits behind every generated token."""
+        the logits behind every generated token.  RuntimeError if some have not ended
+        after ``max_steps`` iterations."""
         sch = ppas.Scheduler(self.blocks, wl.page_permutation(self.blocks, self.seed), cap_rows=len(self.requests),
                              cap_blocks_per_seq=max(wl.blocks_for(len(r.prompt) + r.length) for r in self.requests),
                              cap_tokens=self.mbt_hi)
@@ -189,6 +190,9 @@ class Batch:
             sch.close()
         if int(self.err.item()) != 0:
             raise RuntimeError(f"device error flag {int(self.err.item())}")
+        unfinished = [i for i, r in enumerate(self.requests) if len(r.tokens) < r.length]
+        if unfinished:
+            raise RuntimeError(f"requests {unfinished} are unfinished")
         return self.requests
 
     def _score_prompts(self, st, hidden, ends) -> None:

@@ -1,0 +1,33 @@
+"""What a batch of differently fine-tuned requests refuses, and that it does not return
+unfinished ones (CPU only: a model without layers, no iteration is run)."""
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_15171_gb300 import workloads as wl
+from test_boundary_cpu import ppas  # noqa: F401
+
+
+@pytest.fixture(scope="module")
+def tuned(ppas):  # noqa: F811
+    from paper_2608_15171_gb300 import tuned as t
+    return t
+
+
+def _model():
+    return SimpleNamespace(geo=wl.QWEN25_3B, layers=0, vocab=100, n_adapters=2, embed=torch.zeros(100, 8))
+
+
+def test_unfinished_requests_are_an_error(tuned):
+    batch = tuned.Batch(_model(), [tuned.Request(np.arange(5), 3)])
+    with pytest.raises(RuntimeError, match="unfinished"):
+        batch.run(max_steps=0)
+
+
+def test_an_empty_plan_with_requests_left_is_an_error(tuned, monkeypatch):
+    monkeypatch.setattr(tuned.ppas.Scheduler, "plan", lambda self, *a: SimpleNamespace(n_rows=0))
+    batch = tuned.Batch(_model(), [tuned.Request(np.arange(5), 3), tuned.Request(np.arange(2), 1)])
+    with pytest.raises(RuntimeError, match="unfinished"):
+        batch.run()
