@@ -76,7 +76,8 @@ class Request:
 
 
 class Batch:
-    """Runs requests to their ends, every planned iteration over all layers."""
+    """Runs requests to their ends, every planned iteration over all layers.  A request holds what
+    was drawn for it, so it may be in one batch, once, and a batch runs once."""
 
     def __init__(self, model: TunedDecoder, requests, rules: answers.Rules = answers.Rules(), n_top: int = 5,
                  score_prompts: bool = False, mbt_hi: int = 16384, mbt_lo: int = 2048, seed: int = 0):
@@ -86,6 +87,7 @@ class Batch:
         for r in self.requests:
             if len(r.prompt) < 1 or r.length < 1 or not -1 <= r.adapter < model.n_adapters:
                 raise ValueError("a prompt, a token to generate and an adapter of the model, or -1")
+        self._check_fresh()
         self.blocks = sum(wl.blocks_for(len(r.prompt) + r.length) for r in self.requests) + 1
         shape = (self.blocks, geo.n_kv_heads, wl.PAGE_TOKENS, geo.head_dim)
         self.k = [torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(model.layers)]
@@ -95,6 +97,11 @@ class Batch:
         self.generator = torch.Generator(device=dev)
         self.generator.manual_seed(seed)
         self.device, self.seed = dev, seed
+
+    def _check_fresh(self) -> None:
+        if len({id(r) for r in self.requests}) < len(self.requests) or \
+                any(r.tokens or r.logprobs or r.entropy or r.alternatives or r.prompt_logprobs for r in self.requests):
+            raise ValueError("a request may run once")
 
     def _adapt(self, x, y, q_lens, ids, adapters) -> None:
         """y += the requests' adapters of x, in place."""
@@ -155,6 +162,7 @@ class Batch:
         """All requests to their ends; ``on_logits(request, place, row of logits)`` sees
         the logits behind every generated token.  RuntimeError if some have not ended
         after ``max_steps`` iterations."""
+        self._check_fresh()
         sch = ppas.Scheduler(self.blocks, wl.page_permutation(self.blocks, self.seed), cap_rows=len(self.requests),
                              cap_blocks_per_seq=max(wl.blocks_for(len(r.prompt) + r.length) for r in self.requests),
                              cap_tokens=self.mbt_hi)

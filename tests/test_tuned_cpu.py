@@ -31,3 +31,17 @@ def test_an_empty_plan_with_requests_left_is_an_error(tuned, monkeypatch):
     batch = tuned.Batch(_model(), [tuned.Request(np.arange(5), 3), tuned.Request(np.arange(2), 1)])
     with pytest.raises(RuntimeError, match="unfinished"):
         batch.run()
+
+
+def test_requests_that_have_run_or_come_twice_are_refused(tuned):
+    """Tokens are appended to a request as they are drawn: each may be in one batch, once."""
+    fresh, ran, scored = (tuned.Request(np.arange(5), 3) for _ in range(3))
+    ran.tokens.append(1)
+    scored.prompt_logprobs.append(-1.0)
+    for requests in ([fresh, ran], [scored], [fresh, fresh]):
+        with pytest.raises(ValueError):
+            tuned.Batch(_model(), requests)
+    batch = tuned.Batch(_model(), [fresh])
+    fresh.tokens.append(1)
+    with pytest.raises(ValueError):
+        batch.run(max_steps=0)
