@@ -45,3 +45,11 @@ def test_requests_that_have_run_or_come_twice_are_refused(tuned):
     fresh.tokens.append(1)
     with pytest.raises(ValueError):
         batch.run(max_steps=0)
+
+
+def test_tokens_outside_the_vocabulary_are_refused(tuned):
+    """Before they index the embedding on the device."""
+    for prompt in ([5, 100], [-1, 3], [2 ** 31, 0], [0.5, 1.0], [[1, 2], [3, 4]]):
+        with pytest.raises(ValueError):
+            tuned.Batch(_model(), [tuned.Request(np.array(prompt), 2)])
+    tuned.Batch(_model(), [tuned.Request(np.array([0, 99], dtype), 2) for dtype in (np.int32, np.int64, np.uint8)])
