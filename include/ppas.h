@@ -547,8 +547,11 @@ ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const void *y, int
  * finite value of the logits' type; alternatives that a row does not have are
  * token -1, log probability -inf.  A row with no other logit has entropy 0 and
  * log probabilities -inf.  vocab at most 262144, else PPAS_ERR_UNSUPPORTED.
- * n_rows == 0 is a no-op.  A row's answers do not depend on the other rows.  One
- * launch, with programmatic stream serialization; no workspace.
+ * n_rows == 0 is a no-op.  A row's tokens depend on its own logits alone; so do its
+ * log probabilities and entropy, but for the order of their sums, which follows
+ * n_rows (they may differ in their last bits between batches of other sizes);
+ * equal calls give equal bits.  One launch, with programmatic stream
+ * serialization; no workspace.
  * ------------------------------------------------------------------------- */
 ppas_status ppas_token_logprobs(const void *logits, int32_t logits_are_bf16, int64_t row_stride, int32_t n_rows,
                                 int32_t vocab, const int32_t *d_tokens, float *d_logprobs, float *d_entropy,
