@@ -517,8 +517,10 @@ ppas_status ppas_norm_rope_append(const void *q, const void *k, const void *v, i
  * n_adapters * n_slices * rank and n_adapters * cols below 2^31; otherwise
  * PPAS_ERR_UNSUPPORTED.  n_seqs == 0 is a no-op.  A row's result depends on its
  * own x, y and adapter alone, but for the order of its sums over k, which follows
- * the step's size; equal calls give equal bits.  No workspace; launches with
- * programmatic stream serialization.
+ * the step's size; equal calls give equal bits.  An infinity or NaN in x or y stays in
+ * its row, in A in the rows of its adapter, in a row of B in that column of them
+ * (where an infinity may give a NaN, the inner sums being two numbers).  No workspace;
+ * launches with programmatic stream serialization.
  * ------------------------------------------------------------------------- */
 ppas_status ppas_adapter_add(const void *x, int64_t x_stride, const void *y, int64_t y_stride, void *out,
                              int64_t out_stride, int32_t n_seqs, const int32_t *h_q_lens, const int32_t *h_adapters,
