@@ -12,11 +12,11 @@
 // one 16-byte load for two MMAs, so the operands go from global memory to registers.)
 // s enters the second product as two bf16 numbers, a value and what its rounding left,
 // so that it counts to 2^-17 of itself.  A row: 2048 x 2560 of rank 16 4.3 us, a chain of
-// loads, a cluster barrier, loads and stores; 64 rows of 32 adapters, 4096 x 6144, rank 32 13.0
-// (2.9 TB/s of weights, in clusters of 4); 128 rows of 72 adapters of rank 64 38.0
-// (4.8 TB/s).  (B copied to shared memory while the inner sums are made, by bulk copies: 4.9
+// loads, a cluster barrier, loads and stores; 64 rows of 31 adapters, 4096 x 6144, rank 32 12.9
+// (36.6 MB of weights: 2.8 TB/s, in clusters of 4); 128 rows of 76 adapters of rank 64 38.1
+// (179 MB: 4.7 TB/s).  (B copied to shared memory while the inner sums are made, by bulk copies: 4.9
 // and 15.3 us, 48.5.  One warp's inner sums 96 after another, not parted among warps: 512 rows
-// of one adapter of rank 64 20.8 us, 17.6 so.)
+// of one adapter of rank 64 20.8 us, 18.1 so.)
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -38,8 +38,8 @@ constexpr int kAChunk = 96;  // inner sums of a warp at most: its loads of 12 x 
 constexpr int kAAhead = 4;   // of the rank in B, 16 times this are loaded ahead
 constexpr int32_t kATileMin = 48;    // rows of an adapter next to one another that make tiles,
 // and of all such runs together (below, units of 16 rows are done first: 512 rows, 2048 x
-// 2560, rank 16 6.5 us, tiles 9.5; 4096 x 6144, rank 16 8.6, 12.6, rank 64 17.7, 17.9; past
-// it 768 rows 15.1, 13.2 and 30.9, 18.7)
+// 2560, rank 16 6.7 us, tiles 9.3; 4096 x 6144, rank 16 8.6, 12.2, rank 64 18.1, 17.8, rank 128 29.9,
+// 29.6; past it 768 rows 8.5, 9.5 and 15.7, 13.0 and 32.8, 18.5)
 constexpr int32_t kATileTotal = 513;
 constexpr int kMaxTiles = 2600;      // of a launch (bounded by the 32 KB parameter space),
 constexpr int kFewTiles = 160;       // or 2 KB of it (2k step 18.0 us, 18.2 with all of it)
@@ -335,8 +335,8 @@ __global__ void __launch_bounds__(kAThreads, 1)
 //   warps 2-17  inner sums, and y + scale s B^T in shared memory: a thread has a row (its
 //               TMEM lane); 8 warps have the even blocks of columns, 8 the odd ones, two
 //               of them 32 rows, half the columns each
-// 16384 rows, 4096 x 6144, rank 64: 99.2 us (544 MB: 5.5 TB/s, 0.81 of the copy's rate; the
-// tensor pipe is 22 % busy); 2048 x 2560, rank 16 42.6 us (5.5 TB/s).  HBM is what bounds
+// 16384 rows, 4096 x 6144, rank 64: 98.9 us (544 MB: 5.5 TB/s, 0.81 of the copy's rate; the
+// tensor pipe is 22 % busy); 2048 x 2560, rank 16 42.9 us (5.5 TB/s).  HBM is what bounds
 // it, but for the turn from the first product to the second, in which a CTA, alone on
 // its SM, neither reads nor writes.  (With y and out moved by the epilogue's threads,
 // through a transposition in shared memory, a block took 3000 cycles and the call 176 us.)
@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(kTThreads, 1)
             cluster_point();
             // the parts of this CTA's rows, summed; then every CTA's sums (both ways along the
             // rows: with each thread reading its own row of the others, 192 sums took 8 us, not 3.5;
-            // with every CTA summing all rows, one barrier less, the 2k step of rank 16 18.4 for 17.4)
+            // with every CTA summing all rows, one barrier less, the tiles of the 2k step 18.4 for 17.4)
             const int vecs = width / 4, own0 = rank * ts.own_rows, own = min(ts.own_rows, kRows - own0);
             for (int i = tid - 64; i < vecs * own; i += kTEpilogue) {
                 const int r = i / vecs, c = (i - r * vecs) * 4;
@@ -853,7 +853,7 @@ bool tile_shape(const AdapterParams &p, int ctas, TileShape *s, int rows) {
         s->b_bytes = static_cast<uint32_t>(block * ((p.rank + 63) / 64)) * 128;
         const uint32_t rest = kTBStages * s->b_bytes + kTBarBytes + 1024;  // 1024: to the first boundary of that size
         const uint32_t room = (kTSmem - rest) / 1024 * 1024;
-        // (two of them in a stage where three such fit: 2048 rows, 4096 x 6144, rank 16 20.4 us, 19.9)
+        // (two of them in a stage where three such fit: 2048 rows, 4096 x 6144, rank 16 19.6 us, one 19.9)
         s->subs = s->a_bytes <= 256 * 128 && room / (2 * stage) >= 3 ? 2 : 1;
         s->stages = std::min<int>(kTMaxStages, static_cast<int>(room / (s->subs * stage)));
         const uint32_t y_bytes = static_cast<uint32_t>(block / 64) * s->x_bytes;
@@ -990,8 +990,8 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     if (e != cudaSuccess) return e;
     // As many CTAs a unit as run at a time, up to 8, 128 values of K each at least; and 16
     // where a warp then has fewer blocks one after another, of few enough sums that every CTA
-    // reads all others' (a row, 4096 x 6144: rank 16 4.5 us, of 8 5.3, rank 64 6.7 and 9.4; 8
-    // rows, 2048 x 2560, rank 64, of 16 10.6, 8.0).
+    // reads all others' (a row, 4096 x 6144: rank 16 4.5 us, of 8 5.5, rank 64 6.8 and 9.7; 8
+    // rows, 2048 x 2560, rank 64, of 16 10.6, 8.2).
     int c = kAMaxCluster;
     while (c > 1 && (n > clusters[c] || p.hidden < c * 128)) --c;
     auto blocks = [&](int ctas) {
@@ -1003,8 +1003,8 @@ cudaError_t launch_units(const AdapterParams &p, const AdapterPlan &plan, size_t
     if (n <= clusters[kAUnitCluster] && p.hidden >= kAUnitCluster * 128 && rows * wide <= kFewSums &&
         blocks(kAUnitCluster) < blocks(c))
         c = kAUnitCluster;
-    // (beside tiles, on the SMs that their clusters leave: 2k step of 17 tiles and 9 units,
-    // clusters of 4 18.3 us, of 8, which find no room, 24.2, of 2 19.8)
+    // (beside tiles, on the SMs that their clusters leave: 2k step of 17 tiles and 7 units,
+    // clusters of 4 18.0 us, of 8, which find no room, 23.7, of 2 20.7)
     if (beside_tiles) c = std::min(c, 4);
     u.ctas = c;
     u.beside_tiles = beside_tiles ? 1 : 0;
@@ -1037,8 +1037,8 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
     TileCall call;
     call.p = p;
     call.err = err;
-    // As many CTAs a tile as run at a time (2k step of 17 tiles, hidden 11008: 4 CTAs 19.8 us;
-    // 8, whose clusters take two rounds, 26.0).
+    // As many CTAs a tile as run at a time (the 17 tiles of a 2k step, hidden 11008: 6 CTAs 17.4 us;
+    // 4 19.5; 8, whose clusters take two rounds, 26.5).
     clusters[1] = device_sm_count();
     const int k_blocks = (p.hidden + kTK - 1) / kTK;
     auto ctas_of = [&](int64_t n, int rows) {
@@ -1049,7 +1049,7 @@ cudaError_t launch_tiles(const AdapterParams &p, const AdapterPlan &plan, int64_
     // Tiles of 64 rows where all of them run at a time and a CTA has a tenth less to do, by
     // what it moves (a block of columns takes no less, its epilogue's warps being half
     // idle) and the joining of the parts, a sum as much as 5 values moved: 768 rows, 4096
-    // x 6144, rank 64 18.8 us, of 128 rows 23.3; 1024 rows of rank 16 16.5 and 15.4.
+    // x 6144, rank 64 18.4 us, of 128 rows 22.7; 1024 rows of rank 16 16.0 and 15.0.
     auto work = [&](int rows) {
         int64_t n = 0;
         for (const AdapterTile &tile : plan.tiles) n += (tile.n + rows - 1) / rows;

@@ -18,11 +18,18 @@
 // with the issue slots 70 % busy (about 9 instructions a logit); 256 x 152000 with 20
 // alternatives 27.8 us (5.6 TB/s, 26.5 without alternatives: one wave of CTAs that
 // start and end together).  Few rows are a chain of copy, bound, list, ranks and two cluster
-// barriers: 1 x 152000 7.4 us, 4.2 without alternatives.
+// barriers: 1 x 152000 7.4 us, 4.3 without alternatives.
 //
-// Rows that this does not suit (a maximum of 2^22 / L and more, infinite ones
-// among them, or more logits at the bound than the list holds, as where all are equal)
-// are read again, slowly and for sure.
+// A CTA's part of a row that this does not suit is read again, a logit at a time, once for the
+// sums and twice or more for the alternatives:
+//  - where c has to follow a maximum (of a thread's 32 logits of a round) of 2^22 / L (2.9e6) and more in
+//    size, or all logits of a warp are so: +inf, a finite mask between -6.9e29 and -2.9e6 that has all 32
+//    of a thread's first ones (of half of a row's logits, at random, none has, of 99 % many), the
+//    types' lowest values where they have all of a warp's (-inf never);
+//  - where more logits reach the bound than a warp's list holds: all equal, or fewer
+//    alternatives in front of the mask than are asked for.
+// 256 x 152000 with 20 alternatives 426 us (99 % masked by -1e9, or +inf in every row; 27.8 by
+// -inf), one row 20 to 33; 1024 x 128000 bf16 with 5 680.
 #include <float.h>
 #include <math.h>
 #include <stddef.h>
@@ -38,9 +45,9 @@ namespace {
 constexpr int kLThreads = 256;  // of a CTA; where rows are many and short, 128 or 64
 // 16-byte loads of a round, a thread (32 logits), rounds under way, and the CTAs that an SM
 // then holds: of fp32 3 (bf16 4), and where there are fewer, kFew, 2 (3) with a round
-// more under way.  (256 x 152000: 28.0 us, 29.5 with the shorter ring; 128: 18.8 and 21.2; 400
-// 47.3 and 40.4; 32 x 128000 bf16 7.8 and 8.9, 1024 x 128000 48.5 and 44.6.  Rounds of 16
-// logits of fp32: 1 x 152000 8.8 us for 7.8; of 64 of bf16: 1024 x 128000 50.4 for 46.4.)
+// more under way.  (256 x 152000: 27.7 us, 29.0 with the shorter ring; 128: 19.0 and 20.7; 400
+// 48.8 and 39.6; 32 x 128000 bf16 7.7 and 9.0, 1024 x 128000 48.2 and 43.7.  Rounds of 16
+// logits of fp32: 1 x 152000 13 % longer; of 64 of bf16: 1024 x 128000 9 %.)
 template <class T>
 constexpr int kLLoads = sizeof(T) == 4 ? 8 : 4;
 template <class T, bool kFew>
@@ -389,8 +396,8 @@ __global__ void __launch_bounds__(N) token_logprobs_kernel(const __grid_constant
             for (int k = 0; k < kLoads; ++k) copy16_async(to + k * N * 16, from + k * N);
         } else if (sizeof(T) == 4 && round < rounds) {
             // (a part's last round, all at once; of bf16 one 16 bytes after another, which the
-            // kernel's other rounds lose least to: 3292 x 5323 fp32 22.6 us, 25.4 so; 4096 x
-            // 128000 bf16 152.0, 169.1 all at once)
+            // kernel's other rounds lose least to: 3292 x 5323 fp32 takes 12 % longer so; 4096 x
+            // 128000 bf16 11 % longer all at once)
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
                 const int v = v0 + k * N + tid;
@@ -462,7 +469,7 @@ __global__ void __launch_bounds__(N) token_logprobs_kernel(const __grid_constant
         if (kTop) {
             // the logits at or above the bound go to the list: the warp looks through the
             // values of one of its lanes after another (a lane by itself through its own, a
-            // few of them at a time keeping the whole warp: 256 x 152000 36.5 us, 32.5 so)
+            // few of them at a time keeping the whole warp: 256 x 152000 12 % longer)
             uint32_t hits = __ballot_sync(0xffffffffu, here >= bound && here > -INFINITY);
             if (hits) {
                 constexpr int kValues = kLoads * kPer;
@@ -684,9 +691,9 @@ cudaError_t prepare_logprobs(int32_t (&clusters)[5]) {
 template <class T, bool kTop, bool kFew>
 cudaError_t launch_logprobs(LogprobParams p, int32_t n_rows, cudaStream_t st) {
     // As many CTAs a row as run at a time, 4096 logits each at least, 16 only where each
-    // has an SM (1 x 152000: 16 CTAs 7.8 us, 8 11.0; 12 x 128000 bf16: 8 CTAs 6.5, 16 7.5; 64 x
-    // 32003 bf16: 4096 logits at least 7.1, 8192 7.7, 2048 8.0; 64 x 152000: 8 CTAs 17.4, 16, in
-    // two rounds, 27.7).
+    // has an SM (1 x 152000: 16 CTAs 7.4 us, 8 8.0, 4 9.7; 12 x 128000 bf16: 8 CTAs 6.8, 16 7.5, 4 7.4;
+    // 64 x 32003 bf16: 4 CTAs 6.7, 8, of fewer logits and in two rounds, 11.3, 2 8.0, 1 6.3; 64 x 152000:
+    // 4 CTAs 14.4, 8, in two rounds, 20.2, 2 17.2).
     int32_t clusters[5] = {};
     const cudaError_t e = prepare_logprobs<T, kTop, kFew>(clusters);
     if (e != cudaSuccess) return e;
@@ -724,9 +731,9 @@ cudaError_t launch_logprobs(const LogprobParams &p, int32_t n_rows, cudaStream_t
     const int64_t sms = device_sm_count(), wide = kLAnSm<T, false> * sms;
     // A row's barriers, list and ranks hide behind other rows' loads, so where there are more
     // than CTAs of 256 threads hold at a time, and short ones, smaller CTAs take them (fp32, 3292 x
-    // 5323, 1 alternative: 64 threads 20.3 us, 256 34.8; 4096 x 8000, 5: 27.7, 128 33.6, 256 42.8;
+    // 5323, 1 alternative: 64 threads 20.3 us, 256 35.0; 4096 x 8000, 5: 27.6, 128 33.5, 256 42.8;
     // bf16 1024 x 16000, 20: 24.1, 128 15.4, 256 15.7; 2503 x 42728, 5: 128 44.3, 256 48.6; 300 x
-    // 1000, 5: 64 4.1, 256 5.0; 700 x 64000, 20: 128 32.3, 256 26.4).
+    // 1000, 5: 64 4.1, 256 5.0; 700 x 64000, 20: 128 32.3, 256 26.7).
     if (n_rows > sms && (p.vocab <= 2048 || (n_rows > 2 * wide && p.vocab <= 8192)))
         return launch_narrow<T, kTop, 64>(p, n_rows, st);
     if (n_rows > wide && (p.vocab <= 16384 || (n_rows > 2 * wide && p.vocab <= 65536)))

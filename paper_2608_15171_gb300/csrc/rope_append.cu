@@ -25,7 +25,7 @@
 // dim, r = 1 / sqrt(mean x^2 + eps), all in fp32 and rounded once behind the
 // rotation.  A row is in the registers of one warp, so its sum of squares takes a
 // few shuffles and no memory: the bytes are those of the rotation alone.  16384 tokens
-// of 32/8 heads in 68.4 us (5.9 TB/s), 2056 of 16/2 in 7.1.
+// of 32/8 heads in 68.6 us (5.9 TB/s), 2056 of 16/2 in 7.2.
 #include <float.h>
 #include <math.h>
 
@@ -36,8 +36,8 @@ namespace ppas {
 namespace {
 
 constexpr int kRopeWarps = 8;
-// CTAs an SM holds of the kernel with norms (of 80 registers; 16384 tokens of 32/8
-// heads: 68.4 us, with 4 of 64 73.2, with 2 74.5)
+// CTAs an SM holds of the kernel with norms for heads of 128 (of 80 registers; 16384 tokens of
+// 32/8 heads: 68.6 us, with 4 of 64 73.2, with 2 74.5)
 constexpr int kNormCtas = 3;
 constexpr int kRopeMaxIter = 4;      // 32-lane passes over head rows a warp makes, loads of all in flight
 constexpr int kRopeMaxDim = 512;     // head_dim: 16 values a lane
@@ -522,7 +522,8 @@ cudaError_t launch_rope_append(RopeParams p, cudaStream_t st) {
         PdlLaunch l(dim3(static_cast<unsigned>((tasks + kRopeWarps - 1) / kRopeWarps)), dim3(kRopeWarps * 32), smem,
                     st);
         if (p.norm) {
-            // (angles once a token: as many CTAs as the SMs hold at a time)
+            // (angles once a token: as many CTAs as the SMs hold at a time of the kernel for heads of 128;
+            // of the one for other sizes, of 103 and 110 registers, they hold 2, and a third start behind those)
             l.cfg.dynamicSmemBytes = norm_rope_smem(p.head_dim, p.rotary_dim);
             const unsigned most = static_cast<unsigned>(sms) * kNormCtas;
             if (l.cfg.gridDim.x > most) l.cfg.gridDim.x = most;
