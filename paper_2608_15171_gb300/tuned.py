@@ -34,7 +34,8 @@ from . import workloads as wl
 
 
 class TunedDecoder(answers.Decoder):
-    """The decoder of ``answers`` with norms of query and key heads and ``n_adapters`` adapters of ``rank``."""
+    """The decoder of ``answers`` with norms of query and key heads (which models of this
+    geometry do not have; others do) and ``n_adapters`` adapters of ``rank``."""
 
     EPS = 1e-6
 
