@@ -89,7 +89,7 @@ class Batch:
             if len(r.prompt) < 1 or r.length < 1 or not -1 <= r.adapter < model.n_adapters:
                 raise ValueError("a prompt, a token to generate and an adapter of the model, or -1")
             p = np.asarray(r.prompt)
-            if p.ndim != 1 or p.dtype.kind not in "iu" or p.min() < 0 or p.max() >= model.vocab:
+            if p.ndim != 1 or not np.all((p >= 0) & (p < model.vocab) & (p.astype(np.int64) == p)):
                 raise ValueError("a prompt of tokens of the vocabulary")
         self._check_fresh()
         self.blocks = sum(wl.blocks_for(len(r.prompt) + r.length) for r in self.requests) + 1

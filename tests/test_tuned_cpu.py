@@ -52,4 +52,8 @@ def test_tokens_outside_the_vocabulary_are_refused(tuned):
     for prompt in ([5, 100], [-1, 3], [2 ** 31, 0], [0.5, 1.0], [[1, 2], [3, 4]]):
         with pytest.raises(ValueError):
             tuned.Batch(_model(), [tuned.Request(np.array(prompt), 2)])
-    tuned.Batch(_model(), [tuned.Request(np.array([0, 99], dtype), 2) for dtype in (np.int32, np.int64, np.uint8)])
+    with np.errstate(invalid="ignore"), pytest.raises(ValueError):
+        tuned.Batch(_model(), [tuned.Request(np.array([0.0, np.nan]), 2)])
+    # whole numbers of any type are tokens
+    tuned.Batch(_model(), [tuned.Request(np.array([0, 99], dtype), 2) for dtype in (np.int32, np.int64, np.uint8, float)])
+    tuned.Batch(_model(), [tuned.Request([0, 99], 2), tuned.Request(torch.tensor([5]), 2)])
